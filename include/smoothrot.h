@@ -257,6 +257,100 @@ int smoothrot_kv_dequant(const uint8_t* q, const float* step, const float* zero,
                          int64_t C, void* Y_f16, int64_t ldy, void* stream);
 
 /*
+ * Paged key-value cache and the attention over it: the part of a decoder layer between the fused
+ * QKV projection and the head-mixing quantizer in front of the output projection
+ * (smoothrot_quant_act_heads), with 4-bit keys and values as in the paper's W4A4KV4 setting or fp16 ones.
+ * (The paper fixes the quantizer of the cache; pages, position rotation and attention are the
+ * models' own, LLaMA's and Mistral's, in their usual formulas.)
+ *
+ * Cache.  `bits` 16: k_cache and v_cache are fp16 [pages][n_kv_heads][page_size][head_dim].
+ * `bits` 4: bytes [pages][n_kv_heads][page_size][head_dim / 2], unsigned codes, value 2i in bits 0-3 and
+ * 2i+1 in bits 4-7 as in smoothrot_kv_quant, and k_params, v_params fp32
+ * [pages][groups][page_size][2] hold the step and the zero point of each group of 128 values of a
+ * token's row of n_kv_heads * head_dim values (groups = n_kv_heads * head_dim / 128; with heads of
+ * 64 two heads share a group, so n_kv_heads must be even).  A value is (code - zero) * step.  k_params and v_params are
+ * ignored with `bits` 16.  All 16-byte aligned.  page_size is a power of two up to 1024, head_dim is
+ * 64 or 128 (else SMOOTHROT_UNSUPPORTED_K).  A slot is page * page_size + offset.
+ *
+ * Values that only the device sees (slots, positions, pages, lengths) are checked by the kernels: what is out of range is
+ * left out as each call says, nothing is read or written outside the buffers, and smoothrot_device_status reports
+ * a code from 32 on.
+ */
+
+/*
+ * Appends T tokens.  Row t of Q [T x ldq], K [T x ldk], V [T x ldv] (fp16, e.g. the three slices of the
+ * fused projection's output row) holds the token's n_heads query heads, n_kv_heads key heads and
+ * value heads.  Queries and keys are rotated by the token's position p = positions[t]:
+ *     a' = a cos(p, i) - b sin(p, i),  b' = b cos(p, i) + a sin(p, i)          (fp32, each product rounded)
+ * for the pairs (a, b) = (x[i], x[i + head_dim/2]), or (x[2i], x[2i+1]) with `interleaved` = 1;
+ * rotary [rotary_rows x head_dim] fp32 holds head_dim/2 cosines and then head_dim/2 sines per position.
+ * With `walsh` = 1 every query and key head is then multiplied by H_head_dim / sqrt(head_dim) (Walsh): products of
+ * queries and keys stay what they are, and key outliers are spread before they are coded.
+ * The results: Q_out [T x ldqo] fp16; K_out [T x ldko] fp16 if not NULL; keys and values at slots[t] of the
+ * cache, 4-bit codes with smoothrot_kv_quant's formulas (the keys' from the fp32 values after the rotation) at
+ * clip ratio `clip`.  A negative slot: rotated, not cached.  A token whose position is outside
+ * [0, rotary_rows) or whose slot is beyond the cache: nothing of it is written, status code 32.
+ * Two tokens of one call must not share a slot.  n_heads may be 0 (keys and values alone; Q, Q_out ignored).
+ * Q_out may be Q and K_out may be K (same leading dimension).
+ */
+int smoothrot_kv_append(const void* Q_f16, int64_t ldq, const void* K_f16, int64_t ldk,
+                        const void* V_f16, int64_t ldv, int64_t T, int64_t n_heads,
+                        int64_t n_kv_heads, int64_t head_dim, const int32_t* positions,
+                        const float* rotary, int64_t rotary_rows, int interleaved, int walsh,
+                        void* Q_out_f16, int64_t ldqo, void* K_out_f16, int64_t ldko,
+                        const int64_t* slots, int bits, int64_t pages, int64_t page_size,
+                        void* k_cache, void* v_cache, float* k_params, float* v_params,
+                        float clip, void* stream);
+
+/*
+ * Reads T rows of the cache back: K_out [T x ldk], V_out [T x ldv] fp16, row t from slots[t], 4-bit
+ * codes as smoothrot_kv_dequant turns them into values.  For a later chunk of a prompt, whose
+ * queries attend to the cached prefix through smoothrot_attn_prefill.  A negative slot gives a row of zeros, one
+ * beyond the cache zeros and status code 33.  T * n_kv_heads * head_dim / 128 must stay below 2^31.
+ */
+int smoothrot_kv_gather(const int64_t* slots, int64_t T, int64_t n_kv_heads, int64_t head_dim,
+                        int bits, int64_t pages, int64_t page_size, const void* k_cache,
+                        const void* v_cache, const float* k_params, const float* v_params,
+                        void* K_out_f16, int64_t ldk, void* V_out_f16, int64_t ldv, void* stream);
+
+/*
+ * Attention of one new token of each of B sequences over the cache.  For sequence b and query head h,
+ * over the tokens j < lengths[b] of key head h / (n_heads / n_kv_heads):
+ *     y = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * q.k_j - max)
+ * with fp32 scores, statistics and sums; y = 0 for an empty sequence.  Token j of sequence b lies in page
+ * block_table[b * max_pages + j / page_size] at offset j % page_size.  Q [B x ldq] and Y [B x ldy] fp16
+ * rows of n_heads * head_dim values; n_heads a multiple of n_kv_heads; B <= 8192.
+ * A length outside [0, max_pages * page_size] is clamped and a token on a page outside [0, pages) left out, both
+ * with status code 34.  The order of all sums is fixed by the shapes and lengths: a call repeated gives the same bits.
+ * `workspace`: smoothrot_attn_decode_workspace_bytes(...) bytes, 16-byte aligned, contents on entry do not matter; calls
+ * that may overlap on the GPU need one each.
+ */
+size_t smoothrot_attn_decode_workspace_bytes(int64_t B, int64_t n_heads, int64_t n_kv_heads,
+                                             int64_t head_dim);
+int smoothrot_attn_decode(const void* Q_f16, int64_t ldq, int64_t B, int64_t n_heads,
+                          int64_t n_kv_heads, int64_t head_dim, int bits, int64_t pages,
+                          int64_t page_size, const void* k_cache, const void* v_cache,
+                          const float* k_params, const float* v_params,
+                          const int32_t* block_table, int64_t max_pages, const int32_t* lengths,
+                          float scale, void* Y_f16, int64_t ldy, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * Attention over B packed sequences: sequence b has the queries cu_q[b] .. cu_q[b+1]-1 and the keys and values
+ * cu_k[b] .. cu_k[b+1]-1 (int32, device, B + 1 entries, not decreasing).  The same formula as above over the
+ * keys of the query's sequence, with `causal` = 1 over those with j <= i + keys - queries (i, j from the
+ * sequence's start): the sequences' ends are aligned, a prefix of earlier keys is visible to all, and a
+ * query that sees no key gives y = 0.  What a query does not see has no part in its output, whatever its values.
+ * Q [total_q x ldq], K [total_k x ldk], V [total_k x ldv], Y [total_q x ldy] fp16 rows of heads.
+ * Rows that belong to no sequence are not written; a sequence that leaves the buffers is left out, status code 35.
+ */
+int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, const void* K_f16,
+                           int64_t ldk, const void* V_f16, int64_t ldv, int64_t total_k,
+                           int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
+                           const int32_t* cu_q, const int32_t* cu_k, int64_t B, int causal,
+                           float scale, void* Y_f16, int64_t ldy, void* stream);
+
+/*
  * The whole online layer for a handful of tokens in one kernel: the online activation path
  * followed by smoothrot_linear (Fig. 2: ["hadamard" ->] "quantize" -> the quantized projection; Eq. 2
  * on Eq. 1's integer codes), for decode steps, where two launches cost more than the work.  Every
@@ -339,8 +433,9 @@ int smoothrot_base_matrix(int order, int8_t* out_host);
 /*
  * Host, synchronous.  Kernels never spin without bound: a wait that runs out
  * records a non-zero code in a device-side status word and the kernel
- * returns.  This call copies that word for the current device into
- * *status_host (0 = no timeout so far) and clears it when `clear` is non-zero.
+ * returns; the cache and attention calls record a code from 32 on for a slot, position, page or
+ * length out of range.  This call copies that word for the current device into
+ * *status_host (0 = none so far) and clears it when `clear` is non-zero.
  */
 int smoothrot_device_status(int* status_host, int clear);
 

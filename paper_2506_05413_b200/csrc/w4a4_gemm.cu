@@ -41,6 +41,9 @@
 
 // defined with the row transform kernels: their timeout word
 extern "C" int smoothrot_rotate_status_word(int* value, int clear);
+extern "C" int smoothrot_cache_status_word(int* value, int clear);
+extern "C" int smoothrot_decode_status_word(int* value, int clear);
+extern "C" int smoothrot_prefill_status_word(int* value, int clear);
 // defined with the row transform kernels: the limit of their bounded waits
 extern "C" int smoothrot_rotate_set_wait_limit_ns(uint64_t ns);
 
@@ -1998,11 +2001,14 @@ int smoothrot_debug_gemm_i32(const uint8_t* Xq, int64_t M, const uint8_t* Wq, in
 
 int smoothrot_device_status(int* status_host, int clear) {
   if (status_host == nullptr) return SMOOTHROT_INVALID_ARG;
-  int v = 0, rot = 0;
+  int v = 0, rot = 0, cache = 0, dec = 0, pre = 0;
   if (cudaMemcpyFromSymbol(&v, smoothrot::gemm::g_device_status, sizeof(int)) != cudaSuccess)
     return SMOOTHROT_CUDA_ERROR;
   if (smoothrot_rotate_status_word(&rot, clear) != SMOOTHROT_OK) return SMOOTHROT_CUDA_ERROR;
-  *status_host = v != 0 ? v : rot;
+  if (smoothrot_cache_status_word(&cache, clear) != SMOOTHROT_OK) return SMOOTHROT_CUDA_ERROR;
+  if (smoothrot_decode_status_word(&dec, clear) != SMOOTHROT_OK) return SMOOTHROT_CUDA_ERROR;
+  if (smoothrot_prefill_status_word(&pre, clear) != SMOOTHROT_OK) return SMOOTHROT_CUDA_ERROR;
+  *status_host = v != 0 ? v : (rot != 0 ? rot : (cache != 0 ? cache : (dec != 0 ? dec : pre)));
   if (clear && v != 0) {
     const int zero = 0;
     if (cudaMemcpyToSymbol(smoothrot::gemm::g_device_status, &zero, sizeof(int)) != cudaSuccess)
