@@ -1,75 +1,621 @@
 // Attention over packed prompts of different lengths: queries [total_q] and keys [total_k] of all sequences one after
 // another, grouped heads, causal (aligned at the sequences' ends) or not.
 //
-//   y_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i.k_j - m_i),  j <= i + keys - queries where causal
+//   y_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = 2^(c q_i.k_j - m_i),  c = scale log2(e),  j <= i + keys - queries where causal
 //
-// One warp per query row and head, one pass over the visible keys with a running maximum and sum.
+// in one pass over the keys with a running reference m_i.  Both products run on the fifth-generation tensor
+// cores with their accumulators in tensor memory:
+//
+//   S = Q K^T    A = 128 query rows (shared memory), B = 128 keys, D = 128 fp32 columns of tensor memory
+//   O += P V     A = P, the weights as fp16 in tensor memory (over S, which is done with), B = V as it
+//                lies in memory (rows of keys: the MN-major form), D = head_dim fp32 columns
+//
+// A CTA owns two tiles of 128 query rows of one key head.  The rows of a tile are the heads of the
+// group for one token after another, so that grouped heads share every key and value that is
+// loaded, and a short prompt fills a tile.  While one tile's weights are computed, the tensor core works for the other.
+//
+// A thread of the softmax warps owns one row: its 128 scores come into registers with tcgen05.ld,
+// so maximum and sum need no exchange.  The reference m is raised only when the row's maximum
+// exceeds it by more than 8 (weights up to 2^8 are as good in fp16): then the row of O is
+// multiplied down in tensor memory, which happens in the first few blocks and hardly ever after.  Sums, scores, O and m are
+// fp32; a weight is rounded once to fp16, the type of the values that it multiplies.
+//
+// Roles: warps 0-3 and 4-7 the softmax of the two tiles, warp 8 issues the products, warp 9 the TMA
+// loads (keys and values through one ring of 128-row stages), warps 10-11 clean the value rows that not every row
+// of the CTA sees: a product of a zero weight with NaN or infinity is NaN, so rows past the sequence's end are
+// zeroed, and values that are not finite taken out of causally masked blocks and put back, row by row, at the end.
+// Every mbarrier wait is bounded; on expiry the CTA records a code and winds down.
+#include <cuda.h>
+
 #include "common.cuh"
+#include "rowquant.cuh"
 
 namespace smoothrot {
 namespace prefill {
 
-__device__ int g_prefill_status = 0;
 constexpr int kRange = 35;
-constexpr int kWarps = 4;
+enum Site { kSiteLoad = 36, kSiteMma = 37, kSiteSoftmax = 38, kSiteGuard = 39, kSiteOutput = 40 };
+constexpr unsigned long long kWaitLimitNs = 2000000000ull;
+constexpr unsigned long long kDrainNs = 50000ull;
+
+__device__ int g_prefill_status = 0;
+__device__ unsigned long long g_prefill_wait_limit_ns = kWaitLimitNs;
+
+constexpr int kTile = 128;         // query rows of a tile, and keys of a block
+constexpr int kThreads = 384;
+constexpr int kSoftmaxThreads = 256;
+constexpr int kGuardThreads = 64;
+
+template <int D>
+struct Cfg {
+  static constexpr int kAtoms = D / 64;                       // 128-byte wide slices of a row
+  static constexpr int kAtomBytes = kTile * 128;
+  static constexpr int kTileBytes = kAtoms * kAtomBytes;      // 128 rows of fp16
+  static constexpr int kStages = D == 128 ? 5 : 10;           // of the ring that keys and values share
+  static constexpr int kBarriers = 2 * kStages + 2 /*S*/ + 2 /*P*/ + 2 /*O*/ + 1 /*Q*/ + 8 /*guard*/;
+  static constexpr int kBarOffset = (2 + kStages) * kTileBytes;
+  static constexpr int kMiscOffset = kBarOffset + 8 * kBarriers;
+  static constexpr int kSmemBytes = 1024 /*alignment slack*/ + kMiscOffset + 128;
+  static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
+};
 
 struct Args {
-  const __half *q, *k, *v;
-  int64_t ldq, ldk, ldv, ldy;
+  const __half *q, *v;
+  int64_t ldq, ldv, ldy;
   __half* y;
   int64_t total_q, total_k;
   const int32_t *cu_q, *cu_k;
-  int batch, n_heads, group, causal;
-  float scale;
+  int batch, group, causal;
+  int heads_per_chunk;       // heads of a group that a CTA handles: all, up to 128
+  int chunks;                // of a group
+  int tokens;                // per tile: 128 / heads_per_chunk
+  int units;                 // kv heads * chunks
+  float c;                   // |scale| log2(e), 1 where scale is 0
+  int sign;                  // of scale: queries are multiplied by it
 };
 
-template <int D>
-__global__ void __launch_bounds__(32 * kWarps)
-attn_prefill_kernel(Args a) {
-  constexpr int R = D / 32;
-  const int lane = threadIdx.x & 31;
-  const int h = blockIdx.y, kv = h / a.group;
-  for (int64_t i = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5); i < a.total_q; i += int64_t(gridDim.x) * kWarps) {
-    int lo = 0, hi = a.batch;                 // the sequence b with cu_q[b] <= i < cu_q[b + 1]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (a.cu_q[mid] <= i) lo = mid; else hi = mid;
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// Bounded wait on a phase; false if it ran out or another role of the CTA gave up.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int site) {
+  if (mbar_try(bar, parity)) return true;
+  const unsigned long long t0 = now_ns();
+  for (uint32_t spin = 1;; ++spin) {
+    if (mbar_try(bar, parity)) return true;
+    if ((spin & 63u) == 0u) {
+      if (*abort_flag != 0) return false;
+      if (now_ns() - t0 > g_prefill_wait_limit_ns) {
+        *abort_flag = 1;
+        atomicCAS(&g_prefill_status, 0, site);
+        return false;
+      }
     }
-    const int64_t q0 = a.cu_q[lo], q1 = a.cu_q[lo + 1], k0 = a.cu_k[lo], k1 = a.cu_k[lo + 1];
-    if (i < q0 || i >= q1) continue;          // a row of no sequence
-    if (q1 > a.total_q || k0 < 0 || k1 < k0 || k1 > a.total_k) {
-      if (lane == 0) atomicCAS(&g_prefill_status, 0, kRange);
-      continue;
-    }
-    int64_t seen = k1 - k0;
-    if (a.causal) {
-      const int64_t most = i - q0 + 1 + (k1 - k0) - (q1 - q0);
-      seen = seen < most ? seen : most;
-    }
-    float q[R], o[R], m = -INFINITY, l = 0.0f;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      q[r] = __half2float(a.q[i * a.ldq + int64_t(h) * D + r * 32 + lane]) * a.scale;
-      o[r] = 0.0f;
-    }
-    for (int64_t j = k0; j < k0 + seen; ++j) {
-      float s = 0.0f;
-#pragma unroll
-      for (int r = 0; r < R; ++r) s += q[r] * __half2float(a.k[j * a.ldk + int64_t(kv) * D + r * 32 + lane]);
-#pragma unroll
-      for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-      const float top = fmaxf(m, s);
-      const float base = top == -INFINITY ? 0.0f : top;
-      const float keep = expf(m - base), p = expf(s - base);
-#pragma unroll
-      for (int r = 0; r < R; ++r) o[r] = o[r] * keep + p * __half2float(a.v[j * a.ldv + int64_t(kv) * D + r * 32 + lane]);
-      l = l * keep + p;
-      m = top;
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      a.y[i * a.ldy + int64_t(h) * D + r * 32 + lane] = __float2half_rn(seen <= 0 ? 0.0f : o[r] / l);
   }
+}
+
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// K-major operand, 128-byte swizzle: rows of 128 bytes, groups of 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_k_major(uint32_t addr) {
+  const uint32_t lo = ((addr & 0x3FFFFu) >> 4) | (1u << 16);
+  const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+  return (uint64_t(hi) << 32) | lo;
+}
+// MN-major operand, 128-byte swizzle: 64 values of N per 128-byte row, one row per k, groups of 8 k
+// 1024 bytes apart, the next 64 values of N one slice of 128 rows further.
+__device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr) {
+  const uint32_t lo = ((addr & 0x3FFFFu) >> 4) | ((uint32_t(kTile) * 128u >> 4) << 16);
+  const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+  return (uint64_t(hi) << 32) | lo;
+}
+// fp16 x fp16 -> fp32, M = 128; bit 16: B is MN-major.
+__host__ __device__ constexpr uint32_t idesc(int n, bool b_mn) {
+  return (1u << 4) | (uint32_t(b_mn) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(kTile >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t taddr, float* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+        "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]),
+        "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
+        "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_store32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// 128 rows of one head: `kAtoms` boxes of 64 values x 128 rows.
+template <int D>
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
+#pragma unroll
+  for (int a = 0; a < Cfg<D>::kAtoms; ++a)
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst + a * Cfg<D>::kAtomBytes), "l"(map), "r"(bar), "r"(head * D + a * 64), "r"(row)
+        : "memory");
+}
+
+// What a CTA works on: two tiles of `tokens` tokens each from token `first` on of one sequence.
+struct Work {
+  int q0, nq, k0, nk;        // the sequence's rows
+  int first;
+  __device__ __forceinline__ int limit(int token, int causal) const {   // keys that a token sees: 0 .. limit - 1
+    const int most = causal ? min(nk, token + 1 + nk - nq) : nk;
+    return max(most, 0);
+  }
+  // blocks of keys that some row of tile t sees
+  __device__ __forceinline__ int blocks(int t, int tokens, int causal) const {
+    const int a = first + t * tokens;
+    if (a >= nq) return 0;
+    return (limit(min(nq, a + tokens) - 1, causal) + kTile - 1) / kTile;
+  }
+};
+
+__device__ __forceinline__ int sequence_tiles(const Args& a, int b, Work* w) {
+  w->q0 = a.cu_q[b];
+  w->nq = a.cu_q[b + 1] - w->q0;
+  w->k0 = a.cu_k[b];
+  w->nk = a.cu_k[b + 1] - w->k0;
+  if (w->nq <= 0) return 0;
+  if (w->q0 < 0 || w->nq > a.total_q - w->q0 || w->k0 < 0 || w->nk < 0 || w->nk > a.total_k - w->k0) {
+    atomicCAS(&g_prefill_status, 0, kRange);
+    return 0;
+  }
+  return (w->nq + 2 * a.tokens - 1) / (2 * a.tokens);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+  using C = Cfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t base = smem_u32(smem);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  // ---- which sequence and which of its tiles: the sequences' tile counts, added up by the whole CTA ----
+  __shared__ int s_sums[kThreads / 32];
+  __shared__ int s_found, s_local;
+  const int unit = int(blockIdx.x) % a.units;
+  const int want = int(blockIdx.x) / a.units;
+  if (tid == 0) s_found = -1;
+  __syncthreads();
+  {
+    const int per = (a.batch + kThreads - 1) / kThreads;
+    const int b0 = min(a.batch, tid * per), b1 = min(a.batch, b0 + per);
+    Work w;
+    int mine = 0;
+    for (int b = b0; b < b1; ++b) mine += sequence_tiles(a, b, &w);
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    if (lane == 31) s_sums[warp] = incl;
+    __syncthreads();
+    for (int i = 0; i < warp; ++i) incl += s_sums[i];
+    int at = incl - mine;
+    if (want >= at && want < incl) {
+      for (int b = b0; b < b1; ++b) {
+        const int n = sequence_tiles(a, b, &w);
+        if (want < at + n) {
+          s_found = b;
+          s_local = n - 1 - (want - at);            // the longest rows of a sequence first
+          break;
+        }
+        at += n;
+      }
+    }
+  }
+  __syncthreads();
+  if (s_found < 0) return;                          // more CTAs than tiles: the grid is an upper bound
+  Work w;
+  sequence_tiles(a, s_found, &w);
+  w.first = s_local * 2 * a.tokens;
+  const int kv = unit / a.chunks, chunk = unit % a.chunks;
+  const int heads = min(a.heads_per_chunk, a.group - chunk * a.heads_per_chunk);
+  const int head0 = kv * a.group + chunk * a.heads_per_chunk;
+  const int n0 = w.blocks(0, a.tokens, a.causal), n1 = w.blocks(1, a.tokens, a.causal);
+  const int n = max(n0, n1);
+  // from this key on some row of the CTA does not see everything
+  const int ragged = w.limit(w.first, a.causal);
+
+  // ---- barriers, tensor memory ----
+  const uint32_t bars = base + C::kBarOffset;
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * C::kStages, bar_s = bar_empty + 8 * C::kStages, bar_p = bar_s + 16,
+                 bar_o = bar_p + 16, bar_q = bar_o + 16, bar_guard = bar_q + 8, bar_go = bar_guard + 32;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kMiscOffset);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 8);
+  volatile int* not_finite = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 16);
+  if (tid == 0) {
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(bar_full + 8 * i, 1);
+      mbar_init(bar_empty + 8 * i, 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(bar_s + 8 * t, 1);
+      mbar_init(bar_p + 8 * t, 4);
+      mbar_init(bar_o + 8 * t, 1);
+    }
+    mbar_init(bar_q, 8);
+    for (int g = 0; g < 4; ++g) {
+      mbar_init(bar_guard + 8 * g, 2);
+      mbar_init(bar_go + 8 * g, 1);
+    }
+    *abort_flag = 0;
+    *not_finite = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const uint32_t q_smem = base, ring = base + 2 * C::kTileBytes;
+
+  if (warp < 8) {
+    // ================= softmax of tile t: one thread per row =================
+    const int t = warp >> 2;
+    const int row = tid & 127;
+    const int token = w.first + t * a.tokens + row / heads;
+    const int head = head0 + row % heads;
+    const bool live = row < a.tokens * heads && token < w.nq;
+    const int limit = live ? w.limit(token, a.causal) : 0;
+    const int nt = t == 0 ? n0 : n1;
+    {
+      // the row's queries into shared memory, K-major with the 128-byte swizzle.  Consecutive threads take consecutive
+      // 16-byte pieces of a row.
+      constexpr int kPieces = D / 8;
+      const uint32_t flip = a.sign < 0 ? 0x80008000u : 0u;
+      for (int i = row; i < kTile * kPieces; i += kTile) {
+        const int r = i / kPieces, piece = i % kPieces;
+        const int tk = w.first + t * a.tokens + r / heads;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (r < a.tokens * heads && tk < w.nq && a.sign != 0) {
+          x = __ldg(reinterpret_cast<const uint4*>(a.q + int64_t(w.q0 + tk) * a.ldq + int64_t(head0 + r % heads) * D) + piece);
+          x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+        }
+        const uint32_t dst = uint32_t(t) * C::kTileBytes + uint32_t(piece >> 3) * C::kAtomBytes + uint32_t(r) * 128u +
+                             (uint32_t((piece ^ r) & 7) << 4);
+        *reinterpret_cast<uint4*>(smem + dst) = x;
+      }
+      fence_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_q);
+    }
+    const uint32_t lanes = uint32_t(warp & 3) << 21;                 // tensor-memory lane 32 * (warp % 4)
+    const uint32_t s_col = tmem + lanes + uint32_t(t) * 128u;
+    const uint32_t o_col = tmem + lanes + 256u + uint32_t(t) * 128u;
+    // first block of this tile with a key that some row does not see
+    const int masked_from = w.limit(min(w.first + t * a.tokens, w.nq - 1), a.causal) / kTile;
+    float m = -INFINITY, l = 0.0f;
+    bool ok = true;
+    for (int j = 0; j < nt; ++j) {
+      if (!mbar_wait(bar_s + 8 * t, j & 1, abort_flag, kSiteSoftmax)) { ok = false; break; }
+      fence_after();
+      float s[kTile];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tmem_load32(s_col + 32 * i, s + 32 * i);
+      tmem_wait_ld();
+      if (j >= masked_from) {
+        const int here = limit - j * kTile;
+#pragma unroll
+        for (int i = 0; i < kTile; ++i) s[i] = i < here ? s[i] : -INFINITY;
+      }
+      float top[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+      for (int i = 4; i < kTile; i += 4) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) top[x] = max_nan(top[x], s[i + x]);
+      }
+      float high = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3])) * a.c;
+      if (high == INFINITY) high = NAN;                              // inf - inf
+      // P of the last block has been read: S of this one was issued after it
+      const bool raise = !(high <= m + 8.0f);
+      if (j == 0) {
+        m = high;
+      } else if (__any_sync(0xffffffffu, raise)) {
+        const float to = raise ? high : m;
+        const float keep = to == -INFINITY ? 1.0f : exp2_fast(m - to);
+        m = to;
+        l *= keep;
+#pragma unroll 1
+        for (int i = 0; i < D / 32; ++i) {
+          float o[32];
+          tmem_load32(o_col + 32 * i, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int x = 0; x < 32; ++x) o[x] *= keep;
+          tmem_store32(o_col + 32 * i, reinterpret_cast<const uint32_t*>(o));
+        }
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+      const f32x2 c2 = pack2(a.c, a.c), r2 = pack2(-ref, -ref);
+      f32x2 sum[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t p[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          float x, y;
+          unpack2(fma2(pack2(s[64 * half + 2 * i], s[64 * half + 2 * i + 1]), c2, r2), x, y);
+          x = exp2_fast(x);
+          y = exp2_fast(y);
+          sum[i & 1] = add2(sum[i & 1], pack2(x, y));
+          p[i] = half2_bits(x, y);
+        }
+        tmem_store32(s_col + 32 * half, p);
+      }
+      {
+        float x, y;
+        unpack2(add2(sum[0], sum[1]), x, y);
+        l += x + y;
+      }
+      tmem_wait_st();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_p + 8 * t);
+    }
+    // ---- output ----
+    if (ok && nt > 0) {
+      ok = mbar_wait(bar_o + 8 * t, 0, abort_flag, kSiteOutput);
+      fence_after();
+    }
+    if (ok) {
+      const bool put_back = nt > 0 && *not_finite != 0;
+      const float inv = limit > 0 ? 1.0f / l : 0.0f;
+      __half* out = a.y + int64_t(w.q0 + token) * a.ldy + int64_t(head) * D;
+#pragma unroll 1
+      for (int i = 0; i < D / 32; ++i) {
+        float o[32];
+        if (nt > 0) {
+          tmem_load32(o_col + 32 * i, o);
+          tmem_wait_ld();
+        }
+#pragma unroll
+        for (int x = 0; x < 32; ++x) o[x] = limit > 0 ? o[x] * inv : 0.0f;
+        if (put_back) {
+          for (int key = ragged / kTile * kTile; key < limit; ++key) {
+            if (key < ragged) continue;
+            const __half* v = a.v + int64_t(w.k0 + key) * a.ldv + int64_t(kv) * D + 32 * i;
+#pragma unroll
+            for (int x = 0; x < 32; ++x) {
+              const float f = __half2float(v[x]);
+              if (!isfinite(f)) o[x] += f;
+            }
+          }
+        }
+        if (live) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            uint4 h;
+            h.x = half2_bits(o[8 * x], o[8 * x + 1]);
+            h.y = half2_bits(o[8 * x + 2], o[8 * x + 3]);
+            h.z = half2_bits(o[8 * x + 4], o[8 * x + 5]);
+            h.w = half2_bits(o[8 * x + 6], o[8 * x + 7]);
+            reinterpret_cast<uint4*>(out + 32 * i)[x] = h;
+          }
+        }
+      }
+    }
+  } else if (warp == 8) {
+    // ================= products =================
+    if (lane == 0 && n > 0) {
+      constexpr uint32_t id_s = idesc(kTile, false), id_o = idesc(D, true);
+      bool ok = mbar_wait(bar_q, 0, abort_flag, kSiteMma);
+      auto full = [&](int i) { return mbar_wait(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1, abort_flag, kSiteMma); };
+      auto scores = [&](int t, int i) {                               // S_t = Q_t K^T from ring entry i
+        const uint32_t k = ring + uint32_t(i % C::kStages) * C::kTileBytes;
+        const uint32_t q = q_smem + uint32_t(t) * C::kTileBytes;
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x) {
+          const uint32_t off = uint32_t(x >> 2) * C::kAtomBytes + uint32_t(x & 3) * 32u;
+          mma_ss(tmem + uint32_t(t) * 128u, desc_k_major(q + off), desc_k_major(k + off), id_s, x > 0);
+        }
+        commit(bar_s + 8 * t);
+      };
+      ok = ok && full(0);
+      fence_after();
+      if (ok) {
+        if (n0 > 0) scores(0, 0);
+        if (n1 > 0) scores(1, 0);
+        if (2 * n > C::kStages) commit(bar_empty);
+      }
+      for (int j = 0; ok && j < n; ++j) {
+        const int ik = 2 * (j + 1), iv = 2 * j + 1;
+        bool have_v = false, have_k = false;
+        for (int t = 0; ok && t < 2; ++t) {
+          const int nt = t == 0 ? n0 : n1;
+          if (j < nt) {
+            ok = mbar_wait(bar_p + 8 * t, j & 1, abort_flag, kSiteMma);
+            if (ok && !have_v) {
+              ok = full(iv);
+              if (ok && j >= ragged / kTile) ok = mbar_wait(bar_guard + 8 * (j - ragged / kTile), 0, abort_flag, kSiteMma);
+              have_v = true;
+            }
+            if (!ok) break;
+            fence_after();
+            const uint32_t v = ring + uint32_t(iv % C::kStages) * C::kTileBytes;
+#pragma unroll
+            for (int x = 0; x < kTile / 16; ++x)
+              mma_ts(tmem + 256u + uint32_t(t) * 128u, tmem + uint32_t(t) * 128u + 8u * x, desc_mn_major(v + 2048u * x), id_o,
+                     (j > 0 || x > 0) ? 1u : 0u);
+            if (j + 1 == nt) commit(bar_o + 8 * t);
+          }
+          if (j + 1 < nt) {
+            if (!have_k) {
+              ok = full(ik);
+              have_k = true;
+              if (!ok) break;
+              fence_after();
+            }
+            scores(t, ik);
+          }
+        }
+        if (ok) {
+          // only entries that are filled again: no arrival is left under way when the CTA ends
+          if (iv + C::kStages < 2 * n) commit(bar_empty + 8 * (iv % C::kStages));
+          if (ik + C::kStages < 2 * n) commit(bar_empty + 8 * (ik % C::kStages));
+        }
+      }
+    }
+  } else if (warp == 9) {
+    // ================= loads: K_0, V_0, K_1, V_1, ... =================
+    if (lane == 0) {
+      for (int i = 0; i < 2 * n; ++i) {
+        const int s = i % C::kStages;
+        if (i >= C::kStages && !mbar_wait(bar_empty + 8 * s, ((i / C::kStages) & 1) ^ 1, abort_flag, kSiteLoad)) break;
+        mbar_expect(bar_full + 8 * s, C::kTileBytes);
+        load_rows<D>(ring + uint32_t(s) * C::kTileBytes, (i & 1) ? &v_map : &k_map, bar_full + 8 * s, kv, w.k0 + (i >> 1) * kTile);
+        if ((i & 1) && (i >> 1) >= ragged / kTile) mbar_arrive(bar_go + 8 * ((i >> 1) - ragged / kTile));
+      }
+    }
+  } else {
+    // ================= value rows that not all rows of the CTA see =================
+    // The rows of a CTA are at most 256 tokens, so at most three blocks: one barrier for each.
+    for (int j = ragged / kTile; j < n; ++j) {
+      const int i = 2 * j + 1, s = i % C::kStages;
+      // once the load is under way the entry's barrier is in this use's phase
+      if (!mbar_wait(bar_go + 8 * (j - ragged / kTile), 0, abort_flag, kSiteGuard)) break;
+      if (!mbar_wait(bar_full + 8 * s, (i / C::kStages) & 1, abort_flag, kSiteGuard)) break;
+      uint8_t* v = smem + (2 + s) * C::kTileBytes;
+      const int from = max(0, ragged - j * kTile), end = w.nk - j * kTile;       // rows to look at; rows past the sequence
+      bool bad = false;
+      for (int x = tid - 320; x < (kTile - from) * (D / 8); x += kGuardThreads) {
+        const int r = from + x / (D / 8), piece = x % (D / 8);
+        uint4* at = reinterpret_cast<uint4*>(v + (piece >> 3) * C::kAtomBytes + r * 128 + (piece & 7) * 16);
+        if (r >= end) {
+          *at = make_uint4(0, 0, 0, 0);
+        } else {
+          uint4 h = *at;
+          uint32_t* u = reinterpret_cast<uint32_t*>(&h);
+          bool found = false;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if ((u[k] & 0x7C00u) == 0x7C00u) { u[k] &= 0xFFFF0000u; found = true; }
+            if ((u[k] & 0x7C000000u) == 0x7C000000u) { u[k] &= 0x0000FFFFu; found = true; }
+          }
+          if (found) *at = h;
+          bad |= found;
+        }
+      }
+      if (bad) *not_finite = 1;
+      __threadfence_block();
+      fence_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_guard + 8 * (j - ragged / kTile));
+    }
+  }
+
+  // ---- wind down ----
+  __syncwarp();
+  if (*abort_flag != 0) {                           // copies and products under way have time to land
+    const unsigned long long t0 = now_ns();
+    while (now_ns() - t0 < kDrainNs) __nanosleep(1000);
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == 8)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+static bool row_map(CUtensorMap* map, const void* p, int64_t cols, int64_t rows, int64_t ld) {
+  TensorMapEncodeFn encode = tensor_map_encoder();
+  if (encode == nullptr) return false;
+  const cuuint64_t dims[2] = {cuuint64_t(cols), cuuint64_t(rows)};
+  const cuuint64_t strides[1] = {cuuint64_t(ld) * 2};
+  const cuuint32_t box[2] = {64, kTile}, steps[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(p), dims, strides, box, steps,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+static int launch(const Args& a, const CUtensorMap& km, const CUtensorMap& vm, int64_t grid, cudaStream_t st) {
+  if (!allow_dynamic_smem(reinterpret_cast<const void*>(&attn_prefill_kernel<D>), Cfg<D>::kSmemBytes)) return SMOOTHROT_CUDA_ERROR;
+  attn_prefill_kernel<D><<<unsigned(grid), kThreads, Cfg<D>::kSmemBytes, st>>>(a, km, vm);
+  count_launch();
+  return launch_status();
 }
 
 }  // namespace prefill
@@ -86,13 +632,21 @@ int smoothrot_prefill_status_word(int* out, int clear) {
   return SMOOTHROT_OK;
 }
 
+int smoothrot_prefill_set_wait_limit_ns(uint64_t ns) {
+  const unsigned long long v = ns == 0 ? smoothrot::prefill::kWaitLimitNs : static_cast<unsigned long long>(ns);
+  return cudaMemcpyToSymbol(smoothrot::prefill::g_prefill_wait_limit_ns, &v, sizeof(v)) == cudaSuccess ? SMOOTHROT_OK
+                                                                                                      : SMOOTHROT_CUDA_ERROR;
+}
+
 int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, const void* K_f16, int64_t ldk, const void* V_f16,
                            int64_t ldv, int64_t total_k, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
                            const int32_t* cu_q, const int32_t* cu_k, int64_t B, int causal, float scale, void* Y_f16,
                            int64_t ldy, void* stream) {
   using namespace smoothrot;
   using namespace smoothrot::prefill;
-  if (total_q < 0 || total_k < 0 || total_q > INT32_MAX || total_k > INT32_MAX || B < 0 || B > 65535) return SMOOTHROT_INVALID_ARG;
+  // row and tile numbers stay well inside 32 bits
+  const int64_t most = int64_t(1) << 30;
+  if (total_q < 0 || total_k < 0 || total_q > most || total_k > most || B < 0 || B > 65535) return SMOOTHROT_INVALID_ARG;
   if (n_heads <= 0 || n_kv_heads <= 0 || n_heads > 65535 || n_heads % n_kv_heads != 0) return SMOOTHROT_INVALID_ARG;
   if (head_dim != 64 && head_dim != 128) return SMOOTHROT_UNSUPPORTED_K;
   if ((causal & ~1) != 0 || !(scale == scale)) return SMOOTHROT_INVALID_ARG;
@@ -103,19 +657,28 @@ int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, cons
   if (!aligned16(Q_f16) || !aligned16(Y_f16) || ldq % 8 != 0 || ldy % 8 != 0) return SMOOTHROT_BAD_ALIGNMENT;
   if (total_k > 0 && (!aligned16(K_f16) || !aligned16(V_f16) || ldk % 8 != 0 || ldv % 8 != 0)) return SMOOTHROT_BAD_ALIGNMENT;
   Args a;
-  a.q = static_cast<const __half*>(Q_f16); a.k = static_cast<const __half*>(K_f16); a.v = static_cast<const __half*>(V_f16);
-  a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldy = ldy;
+  a.q = static_cast<const __half*>(Q_f16);
+  a.v = static_cast<const __half*>(V_f16);
+  a.ldq = ldq; a.ldv = ldv; a.ldy = ldy;
   a.y = static_cast<__half*>(Y_f16);
   a.total_q = total_q; a.total_k = total_k;
   a.cu_q = cu_q; a.cu_k = cu_k;
-  a.batch = int(B); a.n_heads = int(n_heads); a.group = int(n_heads / n_kv_heads); a.causal = causal;
-  a.scale = scale;
-  const dim3 grid(unsigned((total_q + kWarps - 1) / kWarps), unsigned(n_heads));
+  a.batch = int(B); a.causal = causal;
+  a.group = int(n_heads / n_kv_heads);
+  a.heads_per_chunk = a.group < kTile ? a.group : kTile;
+  a.chunks = (a.group + kTile - 1) / kTile;
+  a.tokens = kTile / a.heads_per_chunk;
+  a.units = int(n_kv_heads) * a.chunks;
+  a.sign = scale > 0.0f ? 1 : (scale < 0.0f ? -1 : 0);
+  a.c = scale == 0.0f ? 1.0f : (scale < 0.0f ? -scale : scale) * 1.4426950408889634f;
+  const int64_t grid = (total_q / (2 * a.tokens) + B) * a.units;
+  if (grid > INT32_MAX) return SMOOTHROT_INVALID_ARG;
+  CUtensorMap km, vm;
+  if (total_k > 0) {
+    if (!row_map(&km, K_f16, ckv, total_k, ldk) || !row_map(&vm, V_f16, ckv, total_k, ldv)) return SMOOTHROT_CUDA_ERROR;
+  }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (head_dim == 128) attn_prefill_kernel<128><<<grid, 32 * kWarps, 0, st>>>(a);
-  else attn_prefill_kernel<64><<<grid, 32 * kWarps, 0, st>>>(a);
-  count_launch();
-  return launch_status();
+  return head_dim == 128 ? launch<128>(a, km, vm, grid, st) : launch<64>(a, km, vm, grid, st);
 }
 
 }  // extern "C"

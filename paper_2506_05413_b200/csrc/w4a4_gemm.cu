@@ -46,6 +46,7 @@ extern "C" int smoothrot_decode_status_word(int* value, int clear);
 extern "C" int smoothrot_prefill_status_word(int* value, int clear);
 // defined with the row transform kernels: the limit of their bounded waits
 extern "C" int smoothrot_rotate_set_wait_limit_ns(uint64_t ns);
+extern "C" int smoothrot_prefill_set_wait_limit_ns(uint64_t ns);
 
 namespace smoothrot {
 namespace gemm {
@@ -1958,7 +1959,8 @@ int smoothrot_linear_static_scratch(const uint8_t* Xq, const float* dx, int64_t 
 int smoothrot_debug_set_wait_limit_ns(uint64_t ns) {
   const unsigned long long v = ns == 0 ? smoothrot::gemm::kWaitLimitNs : static_cast<unsigned long long>(ns);
   if (cudaMemcpyToSymbol(smoothrot::gemm::g_wait_limit_ns, &v, sizeof(v)) != cudaSuccess) return SMOOTHROT_CUDA_ERROR;
-  return smoothrot_rotate_set_wait_limit_ns(ns);
+  const int rot = smoothrot_rotate_set_wait_limit_ns(ns);
+  return rot != SMOOTHROT_OK ? rot : smoothrot_prefill_set_wait_limit_ns(ns);
 }
 
 int smoothrot_debug_wait_expiry(void* stream) {
