@@ -11,7 +11,8 @@
 // where a segment reaches over several CTAs, in the workspace: the last CTA to arrive adds the
 // pieces up, in the order of the tiles, so the result does not depend on who came last.
 //
-// A warp streams its tiles through a ring of its own (cp.async, no barrier with other warps) and computes with the
+// A warp streams its tiles through a ring of its own (bulk copies, a lane for each run of rows in one page; no barrier
+// with other warps) and computes with the
 // warp-level matrix instruction (m16n8k16): the keys of a tile are the 16 rows, the query heads the 8 columns, so a group of
 // 4 or 8 heads wastes little, where the tensor-memory instructions would want 128 rows:
 //     S^T [keys x heads] = K Q^T,   O^T [values x heads] += V^T P^T
@@ -20,16 +21,22 @@
 //     x = (q.c - z sum(q)) s_k,   O = sum w c - sum w z,   w = p s_v
 // The weight w is rounded once to fp16, and both sums take the rounded one.  So that w fits fp16 whatever the
 // step, the reference m runs over x + log2(s_v); p itself, summed in fp32 for the denominator, may then exceed 1.
-// m is raised only where it is exceeded by more than 8, so most tiles need no exchange between lanes.
+// m is raised only where a w exceeds 2^8, so most tiles need no exchange between lanes.
 #include "paged.cuh"
+#include "rowquant.cuh"
 
 namespace smoothrot {
 namespace paged {
 
 __device__ int g_decode_status = 0;
+constexpr unsigned long long kDecodeWaitLimitNs = 2000000000ull;
+__device__ unsigned long long g_decode_wait_limit_ns = kDecodeWaitLimitNs;
+constexpr int kDecodeWait = 41;
+constexpr uint32_t kGaveUp = 1u << 31;           // in a warp's phases: a wait ran out, nothing more is loaded
 
 constexpr int kWarps = 8;
 constexpr int kDecodeThreads = 32 * kWarps;
+static_assert(2 * kWarps <= 16, "two records a warp, found by half a warp");
 
 struct DecodeArgs {
   const __half* q;
@@ -45,9 +52,9 @@ struct DecodeArgs {
   int chunks;               // segments per key head
   int units;                // segments per sequence
   float c;                  // scale log2(e)
-  unsigned long long* arrived;   // [batch * units]
+  unsigned long long* arrived;   // [grid][2]
   float* records;           // [grid][2][rows * D + 2 * rows]
-  unsigned long long tag;   // of this call, in the upper 48 bits
+  unsigned long long tag;   // of this call, not 0
 };
 
 template <int D, int kBits, int NT>
@@ -60,6 +67,7 @@ struct Shape {
   static constexpr int kCtas = kBits == 4 && NT == 1 ? 2 : 1;        // resident per SM
   static constexpr int kRecord = 8 * NT * (D + 2);                   // floats, at most
   // a warp's second record goes over its ring, when that is done with
+  // (the weights of the pieces of a segment, 16 floats for each of 2 x 160 CTAs at most, fit over all of them)
   static constexpr int kWarpBytes = kRingBytes > kRecord * 4 ? kRingBytes : kRecord * 4;
 };
 
@@ -74,25 +82,55 @@ __device__ __forceinline__ int clamped_length(const DecodeArgs& a, const Cache& 
 }
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copy8(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(live ? 8 : 0) : "memory");
+__device__ __forceinline__ void copy_rows(uint32_t dst, const void* src, uint32_t size, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(size), "r"(bar)
+               : "memory");
 }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// Wait of a whole warp for a stage's copies, bounded; false (in every lane) if it ran out.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+  bool ok = bar_try(bar, parity);
+  if (!__all_sync(0xffffffffu, ok)) {
+    const unsigned long long t0 = now_ns();
+    while (!ok && now_ns() - t0 <= g_decode_wait_limit_ns) ok = bar_try(bar, parity);
+    if (!__all_sync(0xffffffffu, ok)) {
+      atomicCAS(&g_decode_status, 0, int(kDecodeWait));
+      const unsigned long long t1 = now_ns();    // copies under way have time to land
+      while (now_ns() - t1 < 50000ull) __nanosleep(1000);
+      return false;
+    }
+  }
+  return true;
+}
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -100,10 +138,16 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float log2_fast(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
 
-// Codes k and k + 4 of a word (k = 0 .. 3) as two fp16 whole numbers.  0x6400 is 1024 in fp16 with a last place of 1, so
-// a code or-ed into it is 1024 + code; four places higher it counts 16 times.
+// Codes k and k + 4 of a word (k = 0 .. 3), less 8, as two fp16 whole numbers.  0x6400 is 1024 in fp16 with a last place
+// of 1, so a code or-ed into it is 1024 + code; four places higher it counts 16 times.  The 8 comes off the zero point
+// too: sums of codes around zero are small, and what the tensor core cuts off their last places with them.
 __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t (&h)[4]) {
   const uint32_t up = w >> 8;
   uint32_t x[4];
@@ -111,10 +155,23 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t (&h)[4]) {
   asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(x[1]) : "r"(w));
   asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(x[2]) : "r"(up));
   asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(x[3]) : "r"(up));
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h[0]) : "r"(x[0]), "r"(0x64006400u));
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(h[1]) : "r"(x[1]), "r"(0x2C002C00u), "r"(0xD400D400u));   // x / 16 - 64
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h[2]) : "r"(x[2]), "r"(0x64006400u));
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(h[3]) : "r"(x[3]), "r"(0x2C002C00u), "r"(0xD400D400u));
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h[0]) : "r"(x[0]), "r"(0x64086408u));
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(h[1]) : "r"(x[1]), "r"(0x2C002C00u), "r"(0xD480D480u));   // x / 16 - 72
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h[2]) : "r"(x[2]), "r"(0x64086408u));
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(h[3]) : "r"(x[3]), "r"(0x2C002C00u), "r"(0xD480D480u));
+}
+
+// The same for keys: a code in bits 4..7 over 0x5400 is 64 + code (last place 1/16), which saves the second
+// operation; the 72 = 64 + 8 too many of the odd codes are taken off the score before its sum starts.
+__device__ __forceinline__ void key_codes_to_half(uint32_t w, uint32_t (&h)[4]) {
+  const uint32_t up = w >> 8;
+  uint32_t x[2];
+  asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(x[0]) : "r"(w));
+  asm("lop3.b32 %0, %1, 0x00F000F0, 0x54005400, 0xEA;" : "=r"(h[1]) : "r"(w));
+  asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(x[1]) : "r"(up));
+  asm("lop3.b32 %0, %1, 0x00F000F0, 0x54005400, 0xEA;" : "=r"(h[3]) : "r"(up));
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h[0]) : "r"(x[0]), "r"(0x64086408u));
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h[2]) : "r"(x[1]), "r"(0x64086408u));
 }
 
 // Key of a tile's 16 that stands in row r of the first product, and so in place r of the second's sum.  A lane's
@@ -125,18 +182,21 @@ __device__ __forceinline__ int key_of_row(int r) {
   return (r & 8) + ((r & 1) ? 4 + (t ^ 1) : t);
 }
 
+constexpr float kNoMaximum = 3e38f;              // -m before the first key: exceeded by any finite score
+
 template <int D, int kBits, int NT>
 struct Piece {                                   // what a warp has of a segment
   float o[D / 16][NT][4];                        // [pairs of values][8 heads][(value 2i, head 2t), (2i, 2t+1), (2i+1, 2t), (2i+1, 2t+1)]
-  float m[NT][2], l[NT][2], z[NT][2];            // of heads 2t, 2t + 1; l and z: this lane's share
+  f32x2 neg_m[NT], l[NT], z[NT];                 // of heads 2t, 2t + 1: -m; l and z: this lane's share
 };
 
 // Streams tiles [first, first + count) of a segment.
 template <int D, int kBits, int NT>
 __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c, const Segment& s, int count, uint8_t* ring,
-                                             int lane, Piece<D, kBits, NT>& pc) {
+                                             uint32_t bars, volatile uint32_t* there, uint32_t& phases, int lane,
+                                             Piece<D, kBits, NT>& pc) {
   using S = Shape<D, kBits, NT>;
-  constexpr int MG = S::kKeys / 16;              // groups of 16 keys
+  constexpr int MG = 1;                          // groups of 16 keys at a time
   constexpr int DG = D / 8;                      // values of a lane's stretch of the output
   const int g = lane >> 2, t = lane & 3;
   const int kv = s.unit / a.chunks, chunk = s.unit - kv * a.chunks;
@@ -145,57 +205,104 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
   const int32_t* table = a.table + int64_t(s.b) * a.max_pages;
   const int pgroup = kBits == 4 ? kv * D / kGroup : 0;
 
-  // ---- loads ----
-  auto page_of = [&](int tile) -> int {          // the page of key `lane` of a tile; -1 if there is none
-    const int64_t key = int64_t(tile) * S::kKeys + lane;
-    if (lane >= S::kKeys || key >= s.length) return -1;
+  // ---- loads: a lane copies one run of rows, the part of a tile that lies in one page ----
+  const int run = min(c.page_size, S::kKeys);
+  const int run_shift = min(c.page_shift, S::kKeys == 32 ? 5 : 4);
+  constexpr int kArrays = kBits == 4 ? 4 : 2;    // keys, values, their steps and zero points
+  const int copies = kArrays * (S::kKeys >> run_shift);
+  auto page_of = [&](int tile, int copy) -> int {                    // of a copy's run; -1 if there is none
+    const int64_t key = int64_t(tile) * S::kKeys + (int64_t(copy / kArrays) << run_shift);
+    if (copy >= copies || key >= s.length) return -1;
     const int p = __ldg(table + (key >> c.page_shift));
     if (p >= 0 && p < c.pages) return p;
     atomicCAS(&g_decode_status, 0, int(kDecodeRange));
     return -1;
   };
-  auto issue = [&](int tile, int page, int stage) -> uint32_t {      // returns which keys are there
-    const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
-    const uint32_t at = ring_at + stage * S::kStageBytes;
-    const int offset = (tile * S::kKeys + lane) & (c.page_size - 1);
-    const int64_t row = page >= 0 ? head_row(c, page, kv, offset) : 0;
-    constexpr int kChunks = S::kRowBytes / 16;
-    constexpr int kPer = 32 / kChunks;           // rows that one instruction covers
-#pragma unroll
-    for (int i = 0; i < S::kKeys / kPer; ++i) {
-      const int key = i * kPer + lane / kChunks, ch = lane % kChunks;
-      const int64_t r = __shfl_sync(0xffffffffu, row, key);
-      const bool live = (there >> key) & 1;
-      const uint32_t dst = at + key * S::kRowBytes + ch * 16;
-      const int64_t off = r * S::kRowBytes + ch * 16;
-      copy16(dst, static_cast<const uint8_t*>(c.k) + off, live);
-      copy16(dst + S::kKeys * S::kRowBytes, static_cast<const uint8_t*>(c.v) + off, live);
-    }
-    if (kBits == 4) {
-      const int64_t r = page >= 0 ? param_row(c, page, pgroup, offset) : 0;
-      const uint32_t dst = at + 2 * S::kKeys * S::kRowBytes + lane * 8;
-      copy8(dst, c.k_params + r, page >= 0);
-      copy8(dst + S::kKeys * 8, c.v_params + r, page >= 0);
-    }
-    return there;
-  };
-  uint32_t there[S::kStages];
-#pragma unroll
-  for (int i = 0; i < S::kStages; ++i) {
-    there[i] = 0;
-    if (i < count) there[i] = issue(s.tile + i, page_of(s.tile + i), i);
-    copy_commit();
+  // this lane's copy of a tile that is all there
+  const int my_array = lane % kArrays, my_first = (lane / kArrays) << run_shift;
+  const uint32_t my_bytes = my_array < 2 ? S::kRowBytes : 8;         // a key
+  const uint8_t* my_src = my_array == 0 ? static_cast<const uint8_t*>(c.k) : static_cast<const uint8_t*>(c.v);
+  uint32_t my_dst = ring_at + (my_array * S::kKeys + my_first) * S::kRowBytes;
+  int my_heads = c.kv_heads, my_head = kv;
+  if (my_array >= 2) {
+    my_src = reinterpret_cast<const uint8_t*>(my_array == 2 ? c.k_params : c.v_params);
+    my_dst = ring_at + 2 * S::kKeys * S::kRowBytes + ((my_array - 2) * S::kKeys + my_first) * 8;
+    my_heads = c.groups;
+    my_head = pgroup;
   }
-  int page = S::kStages < count ? page_of(s.tile + S::kStages) : -1;
+  my_src += (int64_t(my_head) << c.page_shift) * my_bytes;
+  const uint32_t my_page = (uint32_t(my_heads) << c.page_shift) * my_bytes;      // below 2^31 (checked)
+  const uint32_t my_size = my_bytes << run_shift;
+  const bool one_each = copies <= 32 && (kBits == 16 || run > 1);
+
+  auto issue = [&](int tile, int page, int stage) {
+    const uint32_t at = ring_at + stage * S::kStageBytes, bar = bars + 8 * stage;
+    if (one_each && (tile + 1) * S::kKeys <= s.length && __all_sync(0xffffffffu, page >= 0 || lane >= copies)) {
+      if (lane == 0) {
+        there[stage] = S::kKeys == 32 ? 0xFFFFFFFFu : 0xFFFFu;
+        bar_expect(bar, S::kStageBytes);
+      }
+      __syncwarp();
+      if (lane < copies) {
+        const uint32_t offset = uint32_t(tile * S::kKeys + my_first) & uint32_t(c.page_size - 1);
+        copy_rows(my_dst + stage * S::kStageBytes, my_src + uint64_t(uint32_t(page)) * my_page + offset * my_bytes, my_size, bar);
+      }
+      return;
+    }
+    uint32_t keys = 0, bytes = 0;
+    for (int copy = lane; copy < copies; copy += 32) {
+      if (copy >= 32) page = page_of(tile, copy);
+      const int array = copy % kArrays, first = (copy / kArrays) << run_shift;
+      const int n = page < 0 ? 0 : min(run, s.length - tile * S::kKeys - first);
+      if (array == 0) keys |= n == 0 ? 0u : (0xFFFFFFFFu >> (32 - n)) << first;
+      if (array < 2) bytes += n * S::kRowBytes;
+      else if (run > 1) bytes += (n + 1) / 2 * 16;                   // a copy is a multiple of 16 bytes
+    }
+    keys = __reduce_or_sync(0xffffffffu, keys);
+    bytes = __reduce_add_sync(0xffffffffu, bytes);
+    if (lane == 0) {
+      there[stage] = keys;
+      bar_expect(bar, bytes);
+    }
+    __syncwarp();
+    if (copies > 32) page = page_of(tile, lane);
+    for (int copy = lane; copy < copies; copy += 32) {
+      if (copy >= 32) page = page_of(tile, copy);
+      const int array = copy % kArrays, first = (copy / kArrays) << run_shift;
+      const int n = page < 0 ? 0 : min(run, s.length - tile * S::kKeys - first);
+      if (n == 0) continue;
+      const int offset = (tile * S::kKeys + first) & (c.page_size - 1);
+      const uint8_t* src;
+      uint32_t dst, size;
+      if (array < 2) {
+        src = static_cast<const uint8_t*>(array ? c.v : c.k) + head_row(c, page, kv, offset) * S::kRowBytes;
+        dst = at + (array * S::kKeys + first) * S::kRowBytes;
+        size = n * S::kRowBytes;
+      } else {
+        src = reinterpret_cast<const uint8_t*>((array == 2 ? c.k_params : c.v_params) + param_row(c, page, pgroup, offset));
+        dst = at + 2 * S::kKeys * S::kRowBytes + ((array - 2) * S::kKeys + first) * 8;
+        size = (n + 1) / 2 * 16;
+        if (run == 1) {                          // pages of one token: 8 bytes
+          const float2 x = *reinterpret_cast<const float2*>(src);
+          asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(dst), "f"(x.x), "f"(x.y) : "memory");
+          continue;
+        }
+      }
+      copy_rows(dst, src, size, bar);
+    }
+  };
+  for (int i = 0; i < S::kStages && i < count; ++i) issue(s.tile + i, page_of(s.tile + i, lane), i);
+  int page = S::kStages < count ? page_of(s.tile + S::kStages, lane) : -1;
 
   // ---- queries: the second operand of K Q^T, heads in columns; column g of group n is head 8 n + g ----
   uint32_t q[NT][D / 16][2];
-  float qsum[NT][2];                             // of heads 2t, 2t + 1
+  f32x2 qsum[NT];                                // of heads 2t, 2t + 1
+  float qodd[NT][2];                             // where the sum of q.c starts: 8 sum(q) - 72 sum over odd values
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int h = 8 * n + g;
     const __half* src = a.q + int64_t(s.b) * a.ldq + (int64_t(kv) * a.group + chunk * a.rows + h) * D;
-    float sum = 0.0f;
+    float sum = 0.0f, odd = 0.0f;
 #pragma unroll
     for (int w = 0; w < D / 32; ++w) {           // 8 values: two steps of 16
       uint4 x = make_uint4(0, 0, 0, 0);
@@ -211,6 +318,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
         for (int i = 0; i < 4; ++i) {
           const float2 f = __half22float2(*reinterpret_cast<const __half2*>(u + i));
           sum += f.x + f.y;
+          odd += f.y;
         }
       } else {
         q[n][2 * w][0] = x.x;
@@ -222,18 +330,18 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
     if (kBits == 4) {
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      qsum[n][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
-      qsum[n][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+      const float s0 = __shfl_sync(0xffffffffu, sum, 8 * t), s1 = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+      qsum[n] = pack2(s0, s1);
+      odd += __shfl_xor_sync(0xffffffffu, odd, 1);
+      odd += __shfl_xor_sync(0xffffffffu, odd, 2);
+      qodd[n][0] = fmaf(-72.0f, __shfl_sync(0xffffffffu, odd, 8 * t), 8.0f * s0);
+      qodd[n][1] = fmaf(-72.0f, __shfl_sync(0xffffffffu, odd, 8 * t + 4), 8.0f * s1);
     }
   }
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      pc.m[n][e] = -INFINITY;
-      pc.l[n][e] = 0.0f;
-      pc.z[n][e] = 0.0f;
-    }
+    pc.neg_m[n] = pack2(kNoMaximum, kNoMaximum);
+    pc.l[n] = pc.z[n] = pack2(0.0f, 0.0f);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -241,26 +349,39 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
   }
 
   const int key_lo = key_of_row(g), key_hi = key_of_row(g + 8);
-  int stage = 0;
-  for (int i = 0; i < count; ++i) {
-    copy_wait<S::kStages - 1>();
-    __syncwarp();
-    const uint8_t* kt = ring + stage * S::kStageBytes;
-    const uint8_t* vt = kt + S::kKeys * S::kRowBytes;
-    const float2* kp = reinterpret_cast<const float2*>(vt + S::kKeys * S::kRowBytes);
-    const float2* vp = kp + S::kKeys;
-    uint32_t seen = 0;
-#pragma unroll
-    for (int x = 0; x < S::kStages; ++x) seen = x == stage ? there[x] : seen;
-
+  constexpr int kParts = S::kKeys / 16;
+  float sc[kParts][NT][4];
+  uint32_t pt[MG][NT][2], seen = 0;              // the second operand of V^T P^T
+  bool full = false;
+  auto arrived = [&](int stage) -> bool {
+    if (!bar_wait(bars + 8 * stage, (phases >> stage) & 1)) {
+      phases = kGaveUp;
+      return false;
+    }
+    phases ^= 1u << stage;
+    seen = there[stage];
+    full = seen == (S::kKeys == 32 ? 0xFFFFFFFFu : 0xFFFFu);
+    if (kBits == 16 && !full) {                  // 0 * NaN is NaN: values of keys that are not there are zeroed
+      for (int x = lane; x < S::kKeys * (S::kRowBytes / 16); x += 32)
+        if (((seen >> (x / (S::kRowBytes / 16))) & 1) == 0)
+          reinterpret_cast<uint4*>(ring + stage * S::kStageBytes + S::kKeys * S::kRowBytes)[x] = make_uint4(0, 0, 0, 0);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+    }
+    return true;
+  };
+  auto scores = [&](int stage, int part) {
+    const uint8_t* kt = ring + stage * S::kStageBytes + part * 16 * S::kRowBytes;
     // ---- S^T = K Q^T ----
-    float sc[MG][NT][4];
+    float sa[NT][4];
 #pragma unroll
     for (int mg = 0; mg < MG; ++mg) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[mg][n][e] = 0.0f;
+        for (int e = 0; e < 4; ++e) {
+          sa[n][e] = kBits == 4 ? qodd[n][e & 1] : 0.0f;
+        }
       const uint8_t* lo = kt + (16 * mg + key_lo) * S::kRowBytes;
       const uint8_t* hi = kt + (16 * mg + key_hi) * S::kRowBytes;
       if (kBits == 4) {
@@ -275,13 +396,13 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
 #pragma unroll
         for (int w = 0; w < D / 32; ++w) {
           uint32_t x[4], y[4];
-          codes_to_half(wl[w], x);
-          codes_to_half(wh[w], y);
+          key_codes_to_half(wl[w], x);
+          key_codes_to_half(wh[w], y);
           const uint32_t a0[4] = {x[0], y[0], x[1], y[1]}, a1[4] = {x[2], y[2], x[3], y[3]};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            mma16816(sc[mg][n], a0, q[n][2 * w][0], q[n][2 * w][1]);
-            mma16816(sc[mg][n], a1, q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
+            mma16816(sa[n], a0, q[n][2 * w][0], q[n][2 * w][1]);
+            mma16816(sa[n], a1, q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
           }
         }
       } else {
@@ -292,99 +413,147 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
           const uint32_t a0[4] = {x.x, y.x, x.y, y.y}, a1[4] = {x.z, y.z, x.w, y.w};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            mma16816(sc[mg][n], a0, q[n][2 * w][0], q[n][2 * w][1]);
-            mma16816(sc[mg][n], a1, q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
+            mma16816(sa[n], a0, q[n][2 * w][0], q[n][2 * w][1]);
+            mma16816(sa[n], a1, q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
           }
         }
       }
-    }
-
-    // ---- weights ----
-    float sv[MG][2], zv[MG][2], high[NT][2], lead[MG][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) high[n][0] = high[n][1] = -INFINITY;
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[part][n][e] = sa[n][e];
+    }
+  };
+  auto weigh = [&](int stage, int part) {
+    const float2* kp = reinterpret_cast<const float2*>(ring + stage * S::kStageBytes + 2 * S::kKeys * S::kRowBytes) + 16 * part;
+    const float2* vp = kp + S::kKeys;
+    const uint32_t seen16 = seen >> (16 * part);
+    // ---- weights ----
+    // x = (q.c - z sum(q)) s_k c, y = x - m, w = 2^y s_v.  Heads 2t and 2t + 1 go through packed arithmetic.
+    float ks[MG][2], kz[MG][2], sv[MG][2], zv[MG][2];
+    f32x2 y[MG][2][NT];
 #pragma unroll
     for (int mg = 0; mg < MG; ++mg) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int key = 16 * mg + (r ? key_hi : key_lo);
-        const bool live = (seen >> key) & 1;
-        float2 k2 = make_float2(1.0f, 0.0f);
+        ks[mg][r] = a.c;
+        kz[mg][r] = 0.0f;
         sv[mg][r] = 1.0f;
         zv[mg][r] = 0.0f;
-        lead[mg][r] = 0.0f;
         if (kBits == 4) {
-          k2 = kp[key];
-          const float2 v2 = vp[key];
+          const float2 k2 = kp[key], v2 = vp[key];
+          ks[mg][r] = k2.x * a.c;
+          kz[mg][r] = -k2.y * ks[mg][r];         // the 8 that the codes lack is in where their sum starts
           sv[mg][r] = v2.x;
-          zv[mg][r] = v2.y;
-          lead[mg][r] = __log2f(v2.x);
+          zv[mg][r] = v2.y - 8.0f;
         }
-        const float ks = k2.x * a.c;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float& x = sc[mg][n][2 * r + e];
-            if (kBits == 4) x = fmaf(-k2.y, qsum[n][e], x);
-            x *= ks;
-            x = live ? x : -INFINITY;
-            high[n][e] = fmaxf(high[n][e], x + lead[mg][r]);
-          }
+          f32x2 u = pc.neg_m[n];
+          if (kBits == 4) u = fma2(pack2(kz[mg][r], kz[mg][r]), qsum[n], u);
+          y[mg][r][n] = fma2(pack2(sc[part][n][2 * r], sc[part][n][2 * r + 1]), pack2(ks[mg][r], ks[mg][r]), u);
         }
       }
     }
-    bool raise = false;
+    if (!full) {                                 // keys that are not there: no weight, whatever their places hold
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int mg = 0; mg < MG; ++mg) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) raise |= high[n][e] > pc.m[n][e] + 8.0f;
-    if (__any_sync(0xffffffffu, raise)) {
+        for (int r = 0; r < 2; ++r) {
+          if ((seen16 >> (16 * mg + (r ? key_hi : key_lo))) & 1) continue;
+          sv[mg][r] = 1.0f;
+          zv[mg][r] = 0.0f;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) y[mg][r][n] = pack2(-INFINITY, -INFINITY);
+        }
+      }
+    }
+    f32x2 p2[MG][2][NT], w2[MG][2][NT];
+    float high = 0.0f;
+    auto weights = [&]() {
+#pragma unroll
+      for (int mg = 0; mg < MG; ++mg) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float y0, y1, w0, w1;
+            unpack2(y[mg][r][n], y0, y1);
+            p2[mg][r][n] = pack2(exp2_fast(y0), exp2_fast(y1));
+            w2[mg][r][n] = kBits == 4 ? mul2(p2[mg][r][n], pack2(sv[mg][r], sv[mg][r])) : p2[mg][r][n];
+            unpack2(w2[mg][r][n], w0, w1);
+            high = fmaxf(high, fmaxf(w0, w1));
+          }
+        }
+      }
+    };
+    weights();
+    if (__any_sync(0xffffffffu, high > 256.0f)) {
+      // a new m, from x itself: y has lost its places where m was far off
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
+        float m[2], to[2], keep[2], qs[2] = {0.0f, 0.0f};
+        unpack2(pc.neg_m[n], m[0], m[1]);
+        if (kBits == 4) unpack2(qsum[n], qs[0], qs[1]);
+        to[0] = -m[0];
+        to[1] = -m[1];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll
-          for (int o = 4; o < 32; o <<= 1) high[n][e] = fmaxf(high[n][e], __shfl_xor_sync(0xffffffffu, high[n][e], o));
-          const float to = fmaxf(pc.m[n][e], high[n][e]);
-          const float keep = to == -INFINITY ? 1.0f : exp2_fast(pc.m[n][e] - to);
-          pc.m[n][e] = to;
-          pc.l[n][e] *= keep;
-          pc.z[n][e] *= keep;
+          for (int mg = 0; mg < MG; ++mg) {
 #pragma unroll
-          for (int x = 0; x < D / 16; ++x) {
-            pc.o[x][n][e] *= keep;
-            pc.o[x][n][2 + e] *= keep;
+            for (int r = 0; r < 2; ++r) {
+              const bool live = (seen16 >> (16 * mg + (r ? key_hi : key_lo))) & 1;
+              const float lead = kBits == 4 ? log2_fast(sv[mg][r]) : 0.0f;
+              float x[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                x[e] = live ? fmaf(sc[part][n][2 * r + e], ks[mg][r], kz[mg][r] * qs[e]) : -INFINITY;
+                if (pass == 0) to[e] = fmaxf(to[e], x[e] + lead);
+              }
+              if (pass == 1) y[mg][r][n] = pack2(x[0] - to[0], x[1] - to[1]);
+            }
+          }
+          if (pass == 0) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+              for (int o = 4; o < 32; o <<= 1) to[e] = fmaxf(to[e], __shfl_xor_sync(0xffffffffu, to[e], o));
+              keep[e] = exp2_fast(-m[e] - to[e]);
+            }
           }
         }
+        pc.neg_m[n] = pack2(-to[0], -to[1]);
+        const f32x2 k2 = pack2(keep[0], keep[1]);
+        pc.l[n] = mul2(pc.l[n], k2);
+        pc.z[n] = mul2(pc.z[n], k2);
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pc.o[x][n][e] *= keep[e & 1];
       }
+      weights();
     }
-    uint32_t pt[MG][NT][2];                      // the second operand of V^T P^T
 #pragma unroll
     for (int mg = 0; mg < MG; ++mg) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          float w[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float ref = pc.m[n][e] == -INFINITY ? 0.0f : pc.m[n][e];
-            const float p = exp2_fast(sc[mg][n][2 * r + e] - ref);
-            pc.l[n][e] += p;
-            w[e] = kBits == 4 ? p * sv[mg][r] : p;
-          }
-          const __half2 h = __floats2half2_rn(w[0], w[1]);
-          if (kBits == 4) {
-            const float2 f = __half22float2(h);
-            pc.z[n][0] = fmaf(f.x, zv[mg][r], pc.z[n][0]);
-            pc.z[n][1] = fmaf(f.y, zv[mg][r], pc.z[n][1]);
-          }
-          pt[mg][n][r] = transposed(*reinterpret_cast<const uint32_t*>(&h));
+          pc.l[n] = add2(pc.l[n], p2[mg][r][n]);
+          float w0, w1;
+          unpack2(w2[mg][r][n], w0, w1);
+          const __half2 h = __floats2half2_rn(w0, w1);
+          const uint32_t bits = *reinterpret_cast<const uint32_t*>(&h);
+          if (kBits == 4) pc.z[n] = fma2(half2_to_f32x2(bits), pack2(zv[mg][r], zv[mg][r]), pc.z[n]);
+          pt[mg][n][r] = transposed(bits);
         }
       }
     }
-
+  };
+  auto values = [&](int stage, int part) {
+    const uint8_t* vt = ring + stage * S::kStageBytes + (S::kKeys + part * 16) * S::kRowBytes;
     // ---- O^T += V^T P^T ----
 #pragma unroll
     for (int mg = 0; mg < MG; ++mg) {
@@ -443,39 +612,48 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
         }
       }
     }
+  };
 
-    // ---- the stage's next tile ----
-    __syncwarp();
-    uint32_t next = 0;
-    if (i + S::kStages < count) {
-      next = issue(s.tile + i + S::kStages, page, stage);
-      page = i + S::kStages + 1 < count ? page_of(s.tile + i + S::kStages + 1) : -1;
-    }
-    copy_commit();
+  int stage = 0;
+  for (int i = 0; i < count; ++i) {
+    if (!arrived(stage)) break;
 #pragma unroll
-    for (int x = 0; x < S::kStages; ++x) there[x] = x == stage ? next : there[x];
+    for (int part = 0; part < kParts; ++part) scores(stage, part);
+#pragma unroll
+    for (int part = 0; part < kParts; ++part) {
+      weigh(stage, part);
+      values(stage, part);
+    }
+    __syncwarp();
+    if (i + S::kStages < count) {
+      issue(s.tile + i + S::kStages, page, stage);
+      page = i + S::kStages + 1 < count ? page_of(s.tile + i + S::kStages + 1, lane) : -1;
+    }
     stage = stage + 1 == S::kStages ? 0 : stage + 1;
   }
-  copy_wait<0>();
   __syncwarp();
   // the lanes' shares of the sums; zero points out of the output
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
+    float l[2], z[2];
+    unpack2(pc.l[n], l[0], l[1]);
+    unpack2(pc.z[n], z[0], z[1]);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) {
-        pc.l[n][e] += __shfl_xor_sync(0xffffffffu, pc.l[n][e], o);
-        if (kBits == 4) pc.z[n][e] += __shfl_xor_sync(0xffffffffu, pc.z[n][e], o);
+        l[e] += __shfl_xor_sync(0xffffffffu, l[e], o);
+        if (kBits == 4) z[e] += __shfl_xor_sync(0xffffffffu, z[e], o);
       }
       if (kBits == 4) {
 #pragma unroll
         for (int x = 0; x < D / 16; ++x) {
-          pc.o[x][n][e] -= pc.z[n][e];
-          pc.o[x][n][2 + e] -= pc.z[n][e];
+          pc.o[x][n][e] -= z[e];
+          pc.o[x][n][2 + e] -= z[e];
         }
       }
     }
+    pc.l[n] = pack2(l[0], l[1]);
   }
 }
 
@@ -486,16 +664,24 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int record = a.rows * (D + 2);                      // floats: output, reference, sum
+  const int stride = (record + 3) / 4 * 4;                  // of the records in the workspace
   uint8_t* ring = smem + warp * S::kWarpBytes;
   float* heads_of = reinterpret_cast<float*>(smem + kWarps * S::kWarpBytes);    // [warp][record]: pieces that began in an earlier warp
-  __shared__ long long s_sums[kDecodeThreads + 1];
+  __shared__ int s_sums[kDecodeThreads + 1];
   __shared__ int s_scan[kWarps], s_most[kWarps];
-  __shared__ int s_seg[2 * kWarps], s_flag[2 * kWarps];     // the records' segments; bit 0: its first tile, bit 1: its last
-  __shared__ int s_last;
+  __shared__ int s_seg[16], s_flag[16];     // the records' segments; bit 0: its first tile, bit 1: its last
+  __shared__ __align__(8) unsigned long long s_bars[kWarps][S::kStages];   // a stage's copies
+  __shared__ uint32_t s_there[kWarps][S::kStages];          // and the keys that they bring
+  __shared__ float s_total[8 * NT];
 
   // ---- the line of tiles: the sequences' tile counts, added up by the whole CTA ----
   const int per = (a.batch + kDecodeThreads - 1) / kDecodeThreads;
-  auto tiles_of = [&](int b) { return (clamped_length(a, c, b) + S::kKeys - 1) / S::kKeys; };
+  // The start of a segment (queries, an empty ring) costs a warp about as much as a tile, and counts as one: tile 0 of
+  // the line's tiles of a segment is no work, tile i + 1 the i-th of its keys.
+  auto tiles_of = [&](int b) {
+    const int n = (clamped_length(a, c, b) + S::kKeys - 1) / S::kKeys;
+    return n == 0 ? 0 : n + 1;
+  };
   int mine = 0, most = 0;
   for (int b = min(a.batch, tid * per); b < min(a.batch, tid * per + per); ++b) {
     const int n = tiles_of(b);
@@ -519,7 +705,11 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   }
   if (lane == 31) s_scan[warp] = incl;
   if (lane == 0) s_most[warp] = most;
-  if (tid < 2 * kWarps) s_seg[tid] = -1;
+  if (tid < 16) s_seg[tid] = -1;
+  const uint32_t bars = smem_addr(&s_bars[warp][0]);
+  if (lane < S::kStages) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * lane) : "memory");
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  uint32_t phases = 0;                                      // bit i: parity of stage i's next use
   __syncthreads();
   for (int i = 0; i < kWarps; ++i) {
     if (i < warp) incl += s_scan[i];
@@ -528,10 +718,10 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   s_sums[tid + 1] = incl;
   if (tid == 0) s_sums[0] = 0;
   __syncthreads();
-  const long long all = s_sums[kDecodeThreads] * a.units;   // tiles in the line
+  const long long all = (long long)s_sums[kDecodeThreads] * a.units;   // tiles in the line
   const int segments = a.batch * a.units;
   // Short sequences: a CTA per segment, so that nothing has to meet in the workspace.  Else equal stretches.
-  const bool whole = segments <= int(gridDim.x) && most <= 4 * kWarps;
+  const bool whole = segments <= int(gridDim.x) && most <= 4 * kWarps + 1;
   const int ctas = whole ? segments : int(min((long long)gridDim.x, (all + kWarps - 1) / kWarps));
   if (int(blockIdx.x) >= ctas) return;
 
@@ -541,16 +731,26 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
     for (int x = i * per; x < b; ++x) at += tiles_of(x);
     return at;
   };
+  // CTA i's stretch starts at tile i * share + min(i, extra)
+  const long long share = all < (1ll << 32) ? (long long)(uint32_t(all) / uint32_t(ctas)) : all / ctas;
+  const int extra = int(all - share * ctas);
+  auto start_of_cta = [&](int i) -> long long { return i * share + min(i, extra); };
+  auto cta_of = [&](long long tile) -> int {
+    const long long bound = extra * (share + 1);
+    return tile < bound ? int(tile / (share + 1)) : extra + int((tile - bound) / share);
+  };
   long long begin, end;                                     // this warp's stretch
   if (whole) {
     const int b = blockIdx.x / a.units, n = tiles_of(b);
     const long long at = start_of_sequence(b) * a.units + (long long)(blockIdx.x - b * a.units) * n;
-    begin = at + n * warp / kWarps;
-    end = at + n * (warp + 1) / kWarps;
+    if (n == 0) return;
+    begin = at + 1 + (n - 1) * warp / kWarps;
+    end = at + 1 + (n - 1) * (warp + 1) / kWarps;
   } else {
-    const long long w = (long long)blockIdx.x * kWarps + warp, ws = (long long)ctas * kWarps;
-    begin = w * all / ws;
-    end = (w + 1) * all / ws;
+    begin = start_of_cta(blockIdx.x);
+    const long long n = start_of_cta(blockIdx.x + 1) - begin;
+    end = begin + n * (warp + 1) / kWarps;
+    begin += n * warp / kWarps;
   }
 
   if (begin < end) {
@@ -559,9 +759,9 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
     int lo = 0, hi = kDecodeThreads;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (s_sums[mid] * a.units <= begin) lo = mid; else hi = mid;
+      if ((long long)s_sums[mid] * a.units <= begin) lo = mid; else hi = mid;
     }
-    long long at = s_sums[lo] * a.units;
+    long long at = (long long)s_sums[lo] * a.units;
     s.b = lo * per;
     s.tiles = tiles_of(s.b);
     while (at + (long long)s.tiles * a.units <= begin) {
@@ -572,13 +772,22 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
     s.tile = int((begin - at) - (long long)s.unit * s.tiles);
     while (true) {
       s.length = clamped_length(a, c, s.b);
-      const int count = int(min((long long)(s.tiles - s.tile), end - begin));
+      const int place = s.tile, steps = int(min((long long)(s.tiles - place), end - begin));
+      const bool first = place <= 1, last = place + steps == s.tiles;
+      const int count = place == 0 ? steps - 1 : steps;
+      s.tile = place == 0 ? 0 : place - 1;
+      if (count > 0) {
       Piece<D, kBits, NT> pc;
-      stream_tiles<D, kBits, NT>(a, c, s, count, ring, lane, pc);
+      stream_tiles<D, kBits, NT>(a, c, s, count, ring, bars, s_there[warp], phases, lane, pc);
       const int g = lane >> 2, t = lane & 3;
       const int kv = s.unit / a.chunks, chunk = s.unit - kv * a.chunks;
       const int rows = min(a.rows, a.group - chunk * a.rows);
-      const bool first = s.tile == 0, last = s.tile + count == s.tiles;
+      float pl[NT][2], pm[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        unpack2(pc.l[n], pl[n][0], pl[n][1]);
+        unpack2(pc.neg_m[n], pm[n][0], pm[n][1]);
+      }
       if (first && last) {                                  // the whole segment
         __half* y = a.y + int64_t(s.b) * a.ldy + (int64_t(kv) * a.group + chunk * a.rows) * D + g * (D / 8);
 #pragma unroll
@@ -587,7 +796,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
           for (int e = 0; e < 2; ++e) {
             const int h = 8 * n + 2 * t + e;
             if (h >= rows) continue;
-            const float inv = 1.0f / pc.l[n][e];
+            const float inv = 1.0f / pl[n][e];
 #pragma unroll
             for (int x = 0; x < D / 64; ++x) {
               uint4 out;
@@ -612,8 +821,8 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
             for (int i = 0; i < D / 16; ++i)
               *reinterpret_cast<float2*>(rec + h * D + g * (D / 8) + 2 * i) = make_float2(pc.o[i][n][e], pc.o[i][n][2 + e]);
             if (g == 0) {
-              rec[a.rows * D + h] = pc.m[n][e];
-              rec[a.rows * D + a.rows + h] = pc.l[n][e];
+              rec[a.rows * D + h] = -pm[n][e];
+              rec[a.rows * D + a.rows + h] = pl[n][e];
             }
           }
         }
@@ -622,8 +831,9 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
           s_flag[slot] = (first ? 1 : 0) | (last ? 2 : 0);
         }
       }
-      begin += count;
-      if (begin >= end) break;
+      }
+      begin += steps;
+      if (begin >= end || (phases & kGaveUp) != 0) break;
       s.tile = 0;
       if (++s.unit == a.units) {
         s.unit = 0;
@@ -634,90 +844,133 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   __syncthreads();
 
   // ---- pieces of one segment within the CTA: neighbours in the list of records ----
-  for (int i0 = 0; i0 < 2 * kWarps;) {
-    const int seg = s_seg[i0];
-    if (seg < 0) {
-      ++i0;
-      continue;
+  auto rec_of = [&](int i) -> float* {
+    return (i & 1) ? reinterpret_cast<float*>(smem + (i >> 1) * S::kWarpBytes) : heads_of + (i >> 1) * record;
+  };
+  int pending[2] = {-1, -1};
+  {
+    // lane i of every warp: record i.  A segment's records find each other by its number.
+    const int i = lane & 15, seg = lane < 16 ? s_seg[i] : -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, lane < 16 && seg >= 0 ? seg : ~lane) ;
+    const uint32_t leads = __ballot_sync(0xffffffffu, seg >= 0 && (same & ((1u << lane) - 1u)) == 0);
+    const uint32_t firsts = __ballot_sync(0xffffffffu, seg >= 0 && (s_flag[i] & 1)), lasts = __ballot_sync(0xffffffffu, seg >= 0 && (s_flag[i] & 2));
+    int task = 0;                                           // (segment, head), a warp each
+    for (uint32_t left = leads; left != 0; left &= left - 1) {
+      const int lead = __ffs(left) - 1, sg = __shfl_sync(0xffffffffu, seg, lead);
+      const uint32_t mask = __shfl_sync(0xffffffffu, same, lead);
+      const bool starts = (firsts & mask) != 0, ends = (lasts & mask) != 0;
+      if (!(starts && ends)) pending[starts ? 1 : 0] = sg;
+      const int b = sg / a.units, unit = sg - b * a.units;
+      const int kv = unit / a.chunks, chunk = unit - kv * a.chunks;
+      const int rows = min(a.rows, a.group - chunk * a.rows);
+      for (int h = 0; h < rows; ++h, ++task) {
+        if (task % kWarps != warp) continue;
+        const bool mine = (mask >> lane) & 1;
+        const float m = mine ? rec_of(i)[a.rows * D + h] : -INFINITY;
+        float l = mine ? rec_of(i)[a.rows * D + a.rows + h] : 0.0f, top = m;
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float f = mine ? (top == -INFINITY ? 1.0f : exp2_fast(m - top)) : 0.0f;
+        l *= f;
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        l = __shfl_sync(0xffffffffu, l, 0);
+        float o[D / 32] = {};
+        for (uint32_t x = mask; x != 0; x &= x - 1) {
+          const int r = __ffs(x) - 1;
+          const float fr = __shfl_sync(0xffffffffu, f, r);
+          const float* at = rec_of(r) + h * D + lane * 2;
+#pragma unroll
+          for (int k = 0; k < D / 64; ++k) {
+            const float2 v = *reinterpret_cast<const float2*>(at + 64 * k);
+            o[2 * k] = fmaf(v.x, fr, o[2 * k]);
+            o[2 * k + 1] = fmaf(v.y, fr, o[2 * k + 1]);
+          }
+        }
+        if (starts && ends) {
+          __half* y = a.y + int64_t(b) * a.ldy + (int64_t(kv) * a.group + chunk * a.rows + h) * D + lane * 2;
+          const float inv = 1.0f / l;
+#pragma unroll
+          for (int k = 0; k < D / 64; ++k)
+            *reinterpret_cast<__half2*>(y + 64 * k) = __floats2half2_rn(o[2 * k] * inv, o[2 * k + 1] * inv);
+        } else {
+          float* out = a.records + (int64_t(blockIdx.x) * 2 + (starts ? 1 : 0)) * stride;
+#pragma unroll
+          for (int k = 0; k < D / 64; ++k)
+            *reinterpret_cast<float2*>(out + h * D + lane * 2 + 64 * k) = make_float2(o[2 * k], o[2 * k + 1]);
+          if (lane == 0) {
+            out[a.rows * D + h] = top;
+            out[a.rows * D + a.rows + h] = l;
+          }
+          __threadfence();
+        }
+      }
     }
-    int i1 = i0 + 1, flag = s_flag[i0];
-    while (i1 < 2 * kWarps && (s_seg[i1] == seg || s_seg[i1] < 0)) {
-      if (s_seg[i1] == seg) flag |= s_flag[i1];
-      ++i1;
-    }
+  }
+
+  // ---- segments that reach over several CTAs: the last of them to arrive adds up ----
+  // Each CTA raises a flag of its own per piece and then looks at all of the segment's: at least the last to raise sees them
+  // all (sequentially consistent fences).  Two that see them both add up, to the same bits; the flags come down again, so
+  // that a replay of the same launch starts anew.  A flag is up when it holds this call's tag, whatever the
+  // workspace held before.
+  if (pending[0] < 0 && pending[1] < 0) return;
+  __syncthreads();
+  if (tid < 2 && pending[tid] >= 0)
+    reinterpret_cast<volatile unsigned long long*>(a.arrived)[blockIdx.x * 2 + tid] = a.tag;
+  __threadfence();
+  float* s_weight = reinterpret_cast<float*>(smem);         // [pieces][rows], over what is done with
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    const int seg = pending[k];
+    if (seg < 0) continue;
     const int b = seg / a.units, unit = seg - b * a.units;
     const int kv = unit / a.chunks, chunk = unit - kv * a.chunks;
     const int rows = min(a.rows, a.group - chunk * a.rows);
-    auto rec_of = [&](int i) -> const float* {
-      return (i & 1) ? reinterpret_cast<const float*>(smem + (i >> 1) * S::kWarpBytes) : heads_of + (i >> 1) * record;
-    };
     __half* y = a.y + int64_t(b) * a.ldy + (int64_t(kv) * a.group + chunk * a.rows) * D;
-    float* out = a.records + (int64_t(blockIdx.x) * 2 + (flag & 1)) * record;
-    for (int x = tid; x < rows * D; x += kDecodeThreads) {
-      const int h = x / D;
-      float m = -INFINITY, l = 0.0f, o = 0.0f;
-      for (int i = i0; i < i1; ++i)
-        if (s_seg[i] == seg) m = fmaxf(m, rec_of(i)[a.rows * D + h]);
-      const float ref = m == -INFINITY ? 0.0f : m;
-      for (int i = i0; i < i1; ++i) {
-        if (s_seg[i] != seg) continue;
-        const float* r = rec_of(i);
-        const float f = exp2_fast(r[a.rows * D + h] - ref);
-        o += r[x] * f;
-        l += r[a.rows * D + a.rows + h] * f;
-      }
-      if (flag == 3) {
-        y[x] = __float2half_rn(o / l);
-      } else {
-        out[x] = o;
-        if (x % D == 0) {
-          out[a.rows * D + h] = m;
-          out[a.rows * D + a.rows + h] = l;
-        }
-      }
-    }
-    if (flag != 3) {                                        // the segment reaches into other CTAs
-      const long long n = tiles_of(b);
-      const long long from = start_of_sequence(b) * a.units + unit * n;
-      // CTA i starts at tile floor(i * all / ctas)
-      const int c0 = int(((from + 1) * ctas + all - 1) / all) - 1, c1 = int(((from + n) * ctas + all - 1) / all) - 1;
+    const long long n = tiles_of(b);
+    const long long from = start_of_sequence(b) * a.units + unit * n;
+    const int c0 = cta_of(from + 1), c1 = cta_of(from + n - 1);
+    bool up = true;
+    __syncthreads();                                        // this CTA's own flags are up
+    for (int i = c0 + tid; i <= c1; i += kDecodeThreads)
+      up &= reinterpret_cast<volatile unsigned long long*>(a.arrived)[i * 2 + (i == c0 ? 1 : 0)] == a.tag;
+    if (__syncthreads_and(up)) {
       __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        // the count of a segment starts with the first arrival of this call: whatever the word held before
-        unsigned long long* word = a.arrived + seg;
-        unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(word), was, now;
-        do {
-          was = old;
-          now = (was >> 16) == (a.tag >> 16) ? was + 1 : a.tag + 1;
-          if (int(now & 0xFFFFu) == c1 - c0 + 1) now = 0;   // the last: a replay of the same launch starts anew
-          old = atomicCAS(word, was, now);
-        } while (old != was);
-        s_last = now == 0;
-      }
-      __syncthreads();
-      if (s_last) {
-        __threadfence();
-        for (int x = tid; x < rows * D; x += kDecodeThreads) {
-          const int h = x / D;
-          float m = -INFINITY, l = 0.0f, o = 0.0f;
-#pragma unroll 4
-          for (int i = c0; i <= c1; ++i) {
-            const float* r = a.records + (int64_t(i) * 2 + (i == c0 ? 1 : 0)) * record;
-            const float rm = __ldcg(r + a.rows * D + h), rl = __ldcg(r + a.rows * D + a.rows + h), ro = __ldcg(r + x);
-            const float to = fmaxf(m, rm);
-            const float ref = to == -INFINITY ? 0.0f : to;
-            const float f0 = exp2_fast(m - ref), f1 = exp2_fast(rm - ref);
-            o = o * f0 + ro * f1;
-            l = l * f0 + rl * f1;
-            m = to;
-          }
-          y[x] = __float2half_rn(o / l);
+      auto piece = [&](int i) -> const float* { return a.records + (int64_t(i) * 2 + (i == c0 ? 1 : 0)) * stride; };
+      // one warp per head: the pieces' references and sums, a lane for every 32nd piece
+      for (int h = warp; h < rows; h += kWarps) {
+        float m = -INFINITY, l = 0.0f;
+        for (int i = c0 + lane; i <= c1; i += 32) m = fmaxf(m, __ldcg(piece(i) + a.rows * D + h));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const float ref = m == -INFINITY ? 0.0f : m;
+        for (int i = c0 + lane; i <= c1; i += 32) {
+          const float f = exp2_fast(__ldcg(piece(i) + a.rows * D + h) - ref);
+          s_weight[(i - c0) * a.rows + h] = f;
+          l += __ldcg(piece(i) + a.rows * D + a.rows + h) * f;
         }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (lane == 0) s_total[h] = l;
       }
       __syncthreads();
+      // a thread per two values
+      for (int x = tid * 2; x < rows * D; x += kDecodeThreads * 2) {
+        const int h = x / D;
+        float o0 = 0.0f, o1 = 0.0f;
+#pragma unroll 16
+        for (int i = c0; i <= c1; ++i) {
+          const float2 r = __ldcg(reinterpret_cast<const float2*>(piece(i) + x));
+          const float f = s_weight[(i - c0) * a.rows + h];
+          o0 = fmaf(r.x, f, o0);
+          o1 = fmaf(r.y, f, o1);
+        }
+        const float inv = 1.0f / s_total[h];
+        *reinterpret_cast<__half2*>(y + x) = __floats2half2_rn(o0 * inv, o1 * inv);
+      }
+      __syncthreads();
+      for (int i = c0 + tid; i <= c1; i += kDecodeThreads) a.arrived[i * 2 + (i == c0 ? 1 : 0)] = 0;
     }
-    i0 = i1;
   }
 }
 
@@ -733,10 +986,11 @@ static int64_t decode_grid() { return int64_t(device_sm_count()) * 2; }
 template <int D, int kBits, int NT>
 static int launch(const DecodeArgs& a, const Cache& c, cudaStream_t st) {
   using S = Shape<D, kBits, NT>;
+  const int grid = device_sm_count() * S::kCtas;
   const int smem = kWarps * (S::kWarpBytes + a.rows * (D + 2) * 4);
   const void* kern = reinterpret_cast<const void*>(&attn_decode_kernel<D, kBits, NT>);
   if (!allow_dynamic_smem(kern, kWarps * (S::kWarpBytes + S::kRecord * 4))) return SMOOTHROT_CUDA_ERROR;
-  attn_decode_kernel<D, kBits, NT><<<unsigned(device_sm_count() * S::kCtas), kDecodeThreads, smem, st>>>(a, c);
+  attn_decode_kernel<D, kBits, NT><<<unsigned(grid), kDecodeThreads, smem, st>>>(a, c);
   count_launch();
   return launch_status();
 }
@@ -750,13 +1004,18 @@ int smoothrot_decode_status_word(int* out, int clear) {
   return smoothrot::paged::read_status_word(smoothrot::paged::g_decode_status, out, clear);
 }
 
+int smoothrot_decode_set_wait_limit_ns(uint64_t ns) {
+  const unsigned long long v = ns == 0 ? smoothrot::paged::kDecodeWaitLimitNs : static_cast<unsigned long long>(ns);
+  return cudaMemcpyToSymbol(smoothrot::paged::g_decode_wait_limit_ns, &v, sizeof(v)) == cudaSuccess ? SMOOTHROT_OK
+                                                                                                   : SMOOTHROT_CUDA_ERROR;
+}
+
 size_t smoothrot_attn_decode_workspace_bytes(int64_t B, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim) {
   using namespace smoothrot::paged;
   if (B <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads != 0 || head_dim <= 0) return 0;
   DecodeArgs a;
   decode_plan(n_heads, n_kv_heads, &a);
-  const int64_t words = (B * a.units * 8 + 15) / 16 * 16;
-  return size_t(words + decode_grid() * 2 * a.rows * (head_dim + 2) * 4);
+  return size_t(decode_grid() * 16 + decode_grid() * 2 * ((a.rows * (head_dim + 2) + 3) / 4 * 4) * 4);
 }
 
 int smoothrot_attn_decode(const void* Q_f16, int64_t ldq, int64_t B, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
@@ -792,14 +1051,12 @@ int smoothrot_attn_decode(const void* Q_f16, int64_t ldq, int64_t B, int64_t n_h
   a.batch = int(B);
   a.c = scale * 1.4426950408889634f;
   a.arrived = static_cast<unsigned long long*>(workspace);
-  a.records = reinterpret_cast<float*>(static_cast<char*>(workspace) + (B * a.units * 8 + 15) / 16 * 16);
+  a.records = reinterpret_cast<float*>(static_cast<char*>(workspace) + decode_grid() * 16);
+  // a number that no other call of this process has, and that stray contents of a workspace hardly hold
   static std::atomic<unsigned long long> calls{0x5A17C0DEull};
-  a.tag = (calls.fetch_add(1, std::memory_order_relaxed) * 0x9E3779B97F4A7C15ull | (1ull << 63)) & ~0xFFFFull;
-  Cache c = make_cache(n_kv_heads, head_dim, bits, pages, page_size, k_cache, v_cache, k_params, v_params);
-  if (pages == 0) {           // no page is valid; the copies of nothing still name an address
-    c.k = c.v = workspace;
-    c.k_params = c.v_params = static_cast<float2*>(workspace);
-  }
+  a.tag = calls.fetch_add(1, std::memory_order_relaxed) * 0x9E3779B97F4A7C15ull;
+  if (a.tag == 0) a.tag = calls.fetch_add(1, std::memory_order_relaxed) * 0x9E3779B97F4A7C15ull;
+  const Cache c = make_cache(n_kv_heads, head_dim, bits, pages, page_size, k_cache, v_cache, k_params, v_params);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = a.rows > 8;
   if (head_dim == 128) {

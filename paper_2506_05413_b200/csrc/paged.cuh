@@ -46,6 +46,7 @@ inline int check_sizes(int64_t kv_heads, int64_t head_dim, int bits, int64_t pag
   if (bits != 4 && bits != 16) return SMOOTHROT_INVALID_ARG;
   if (bits == 4 && kv_heads * head_dim % kGroup != 0) return SMOOTHROT_UNSUPPORTED_K;
   if (!is_pow2(page_size) || page_size > 1024) return SMOOTHROT_INVALID_ARG;
+  if (kv_heads * page_size * head_dim * 2 > INT32_MAX) return SMOOTHROT_INVALID_ARG;   // a page's bytes
   return SMOOTHROT_OK;
 }
 inline int check_pointers(int bits, const void* k, const void* v, const float* k_params, const float* v_params) {

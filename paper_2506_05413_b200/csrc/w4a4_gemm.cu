@@ -47,6 +47,7 @@ extern "C" int smoothrot_prefill_status_word(int* value, int clear);
 // defined with the row transform kernels: the limit of their bounded waits
 extern "C" int smoothrot_rotate_set_wait_limit_ns(uint64_t ns);
 extern "C" int smoothrot_prefill_set_wait_limit_ns(uint64_t ns);
+extern "C" int smoothrot_decode_set_wait_limit_ns(uint64_t ns);
 
 namespace smoothrot {
 namespace gemm {
@@ -1960,7 +1961,9 @@ int smoothrot_debug_set_wait_limit_ns(uint64_t ns) {
   const unsigned long long v = ns == 0 ? smoothrot::gemm::kWaitLimitNs : static_cast<unsigned long long>(ns);
   if (cudaMemcpyToSymbol(smoothrot::gemm::g_wait_limit_ns, &v, sizeof(v)) != cudaSuccess) return SMOOTHROT_CUDA_ERROR;
   const int rot = smoothrot_rotate_set_wait_limit_ns(ns);
-  return rot != SMOOTHROT_OK ? rot : smoothrot_prefill_set_wait_limit_ns(ns);
+  if (rot != SMOOTHROT_OK) return rot;
+  const int pre = smoothrot_prefill_set_wait_limit_ns(ns);
+  return pre != SMOOTHROT_OK ? pre : smoothrot_decode_set_wait_limit_ns(ns);
 }
 
 int smoothrot_debug_wait_expiry(void* stream) {
