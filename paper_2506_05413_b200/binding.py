@@ -4,17 +4,20 @@ Argument marshalling only: every function checks the tensors it is handed,
 passes raw device pointers, sizes and the current CUDA stream to the C entry
 point of the same name, and raises on a non-zero status.  No arithmetic of the
 method happens here, and there is no fallback: if the library is missing or a
-tensor is not on a CUDA device the call fails.
+tensor is not on a CUDA device the call fails.  The cache and attention calls are marshalled by a native
+module (csrc/marshal.cpp) instead of ctypes: a decode step makes them once per layer.
 """
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsmoothrot.so")
+MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
 
 _i64, _f32, _int, _vp, _sz = ctypes.c_int64, ctypes.c_float, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
 
@@ -238,33 +241,24 @@ def kv_dequant(q, step, zero, Y):
                                        _ptr(zero, torch.float32, "zero"), R, C, yp, ld, _stream()))
 
 
-def _cache(k_cache, v_cache, k_params, v_params):
-    """Checks a paged cache's tensors; returns (bits, pages, kv heads, page size, head dim, the four pointers)."""
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype:
-        raise ValueError("k_cache and v_cache must be 4-D tensors of one shape and type")
-    if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
-        raise ValueError("k_cache and v_cache must be contiguous")
-    pages, kv, page, width = k_cache.shape
-    if k_cache.dtype == torch.float16:
-        bits, dim, kp, vp = 16, width, None, None
-    elif k_cache.dtype == torch.uint8:
-        bits, dim = 4, 2 * width
-        want = (pages, kv * dim // KV_GROUP, page, 2)
-        for t, name in ((k_params, "k_params"), (v_params, "v_params")):
-            if t is None or t.dtype != torch.float32 or t.shape != want or not t.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous float32 {list(want)} tensor")
-        kp, vp = _ptr(k_params, None, "k_params"), _ptr(v_params, None, "v_params")
-    else:
-        raise TypeError(f"k_cache must be float16 or uint8 (4-bit codes), got {k_cache.dtype}")
-    return bits, pages, kv, page, dim, _ptr(k_cache, None, "k_cache"), _ptr(v_cache, None, "v_cache"), kp, vp
+_marshal_module = None
 
 
-def _head_rows(t, rows, width, name):
-    """fp16 rows of `width` values with unit inner stride: (pointer, leading dimension)."""
-    p, r, c, ld = _rows(t, torch.float16, name)
-    if (r, c) != (rows, width):
-        raise ValueError(f"{name} must be [{rows}, {width}]")
-    return p, ld
+def _marshal():
+    """The native marshalling of the cache and attention calls (csrc/marshal.cpp), connected to the library."""
+    global _marshal_module
+    if _marshal_module is None:
+        if not os.path.exists(MARSHAL_PATH):
+            raise FileNotFoundError(
+                f"{MARSHAL_PATH} is missing: build it with `python -m paper_2506_05413_b200.build`")
+        spec = importlib.util.spec_from_file_location("_marshal", MARSHAL_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        lib = load()
+        module.connect(*(ctypes.cast(getattr(lib, "smoothrot_" + name), _vp).value
+                         for name in ("kv_append", "kv_gather", "attn_decode", "attn_prefill")))
+        _marshal_module = module
+    return _marshal_module
 
 
 def kv_append(q, k, v, positions, rotary, slots, k_cache, v_cache, k_params=None, v_params=None, *, q_out=None,
@@ -273,36 +267,17 @@ def kv_append(q, k, v, positions, rotary, slots, k_cache, v_cache, k_params=None
     projection); positions [T] int32, rotary [rows, D] float32 (cosines, then sines), slots [T] int64.  Rotated queries go to
     q_out, rotated keys to k_out (optional), keys and values into the cache: fp16 [pages, Hk, page, D], or uint8
     [pages, Hk, page, D/2] with k_params / v_params float32 [pages, Hk * D / 128, page, 2] (step, zero point)."""
-    bits, pages, kv, page, dim, kc, vc, kp, vp = _cache(k_cache, v_cache, k_params, v_params)
-    T = k.shape[0]
-    kptr, ldk = _head_rows(k, T, kv * dim, "k")
-    vptr, ldv = _head_rows(v, T, kv * dim, "v")
-    qptr = qoptr = koptr = None
-    heads = ldq = ldqo = ldko = 0
-    if q is not None:
-        if q_out is None:
-            raise ValueError("q_out is required with q")
-        heads = q.shape[-1] // dim
-        qptr, ldq = _head_rows(q, T, heads * dim, "q")
-        qoptr, ldqo = _head_rows(q_out, T, heads * dim, "q_out")
-    if k_out is not None:
-        koptr, ldko = _head_rows(k_out, T, kv * dim, "k_out")
-    if rotary.dim() != 2 or rotary.shape[1] != dim or not rotary.is_contiguous():
-        raise ValueError(f"rotary must be a contiguous [rows, {dim}] tensor")
-    _check(load().smoothrot_kv_append(
-        qptr, ldq, kptr, ldk, vptr, ldv, T, heads, kv, dim, _vec(positions, T, "positions", torch.int32),
-        _ptr(rotary, torch.float32, "rotary"), rotary.shape[0], int(interleaved), int(walsh), qoptr, ldqo, koptr, ldko,
-        _vec(slots, T, "slots", torch.int64), bits, pages, page, kc, vc, kp, vp, clip, _stream()))
+    status = _marshal().kv_append(q, k, v, positions, rotary, slots, k_cache, v_cache, k_params, v_params, q_out, k_out,
+                                  clip, walsh, interleaved)
+    if status:
+        _check(status)
 
 
 def kv_gather(slots, k_cache, v_cache, k_out, v_out, k_params=None, v_params=None):
     """smoothrot_kv_gather: rows of the cache at slots [T] int64 -> k_out, v_out [T, Hk * D] fp16."""
-    bits, pages, kv, page, dim, kc, vc, kp, vp = _cache(k_cache, v_cache, k_params, v_params)
-    T = slots.shape[0]
-    kptr, ldk = _head_rows(k_out, T, kv * dim, "k_out")
-    vptr, ldv = _head_rows(v_out, T, kv * dim, "v_out")
-    _check(load().smoothrot_kv_gather(_vec(slots, T, "slots", torch.int64), T, kv, dim, bits, pages, page, kc, vc, kp, vp,
-                                      kptr, ldk, vptr, ldv, _stream()))
+    status = _marshal().kv_gather(slots, k_cache, v_cache, k_out, v_out, k_params, v_params)
+    if status:
+        _check(status)
 
 
 def attn_decode_workspace_bytes(B, n_heads, n_kv_heads, head_dim) -> int:
@@ -313,37 +288,17 @@ def attn_decode(q, k_cache, v_cache, block_table, lengths, Y, k_params=None, v_p
     """smoothrot_attn_decode: q [B, H * D] fp16, one new token per sequence, over the paged cache (see kv_append);
     block_table [B, max_pages] int32, lengths [B] int32 -> Y [B, H * D] fp16.  scale: 1 / sqrt(D) if None.
     workspace: at least attn_decode_workspace_bytes(B, H, Hk, D) bytes."""
-    bits, pages, kv, page, dim, kc, vc, kp, vp = _cache(k_cache, v_cache, k_params, v_params)
-    qptr, B, width, ldq = _rows(q, torch.float16, "q")
-    if width == 0 or width % dim:
-        raise ValueError(f"the rows of q must hold whole heads of {dim}")
-    yptr, ldy = _head_rows(Y, B, width, "Y")
-    if block_table.dim() != 2 or block_table.shape[0] != B or not block_table.is_contiguous():
-        raise ValueError(f"block_table must be a contiguous [{B}, max_pages] tensor")
-    wsp = _ptr(workspace, None, "workspace")
-    wsb = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    _check(load().smoothrot_attn_decode(
-        qptr, ldq, B, width // dim, kv, dim, bits, pages, page, kc, vc, kp, vp,
-        _ptr(block_table, torch.int32, "block_table"), block_table.shape[1], _vec(lengths, B, "lengths", torch.int32),
-        dim ** -0.5 if scale is None else scale, yptr, ldy, wsp, wsb, _stream()))
+    status = _marshal().attn_decode(q, k_cache, v_cache, block_table, lengths, Y, k_params, v_params, scale, workspace)
+    if status:
+        _check(status)
 
 
 def attn_prefill(q, k, v, cu_q, cu_k, Y, *, head_dim=128, causal=True, scale=None):
     """smoothrot_attn_prefill: packed prompts, q [total_q, H * D], k, v [total_k, Hk * D] fp16 (rows may be strided),
     cu_q, cu_k [B + 1] int32 -> Y [total_q, H * D] fp16.  scale: 1 / sqrt(D) if None."""
-    qptr, tq, cq, ldq = _rows(q, torch.float16, "q")
-    kptr, tk, ckv, ldk = _rows(k, torch.float16, "k")
-    vptr, ldv = _head_rows(v, tk, ckv, "v")
-    yptr, ldy = _head_rows(Y, tq, cq, "Y")
-    if head_dim <= 0 or cq % head_dim or ckv % head_dim:
-        raise ValueError(f"the rows of q and k must hold whole heads of {head_dim}")
-    n = cu_q.shape[0]
-    if n == 0:
-        raise ValueError("cu_q must have at least one entry")
-    _check(load().smoothrot_attn_prefill(
-        qptr, ldq, tq, kptr, ldk, vptr, ldv, tk, cq // head_dim, ckv // head_dim, head_dim,
-        _vec(cu_q, n, "cu_q", torch.int32), _vec(cu_k, n, "cu_k", torch.int32), n - 1, int(causal),
-        head_dim ** -0.5 if scale is None else scale, yptr, ldy, _stream()))
+    status = _marshal().attn_prefill(q, k, v, cu_q, cu_k, Y, head_dim, causal, scale)
+    if status:
+        _check(status)
 
 
 def workspace_bytes(M, N, K) -> int:
