@@ -21,7 +21,7 @@
 // fp32; a weight is rounded once to fp16, the type of the values that it multiplies.
 //
 // Roles: warps 0-3 and 4-7 the softmax of the two tiles, warp 8 issues the products, warp 9 the TMA
-// loads (keys and values through one ring of 128-row stages), warps 10-11 clean the value rows that not every row
+// loads (queries, then keys and values through one ring of 128-row stages), warps 10-11 clean the value rows that not every row
 // of the CTA sees: a product of a zero weight with NaN or infinity is NaN, so rows past the sequence's end are
 // zeroed, and values that are not finite taken out of causally masked blocks and put back, row by row, at the end.
 // Every mbarrier wait is bounded; on expiry the CTA records a code and winds down.
@@ -43,7 +43,8 @@ __device__ unsigned long long g_prefill_wait_limit_ns = kWaitLimitNs;
 
 constexpr int kTile = 128;         // query rows of a tile, and keys of a block
 constexpr int kThreads = 384;
-constexpr int kSoftmaxThreads = 256;
+constexpr int kSoftmaxWarps = 8;   // 4 a tile, a thread per row
+constexpr int kMmaWarp = kSoftmaxWarps, kLoadWarp = kMmaWarp + 1, kGuardWarp = kLoadWarp + 1;
 constexpr int kGuardThreads = 64;
 
 template <int D>
@@ -55,13 +56,13 @@ struct Cfg {
   static constexpr int kBarriers = 2 * kStages + 2 /*S*/ + 2 /*P*/ + 2 /*O*/ + 1 /*Q*/ + 8 /*guard*/;
   static constexpr int kBarOffset = (2 + kStages) * kTileBytes;
   static constexpr int kMiscOffset = kBarOffset + 8 * kBarriers;
-  static constexpr int kSmemBytes = 1024 /*alignment slack*/ + kMiscOffset + 128;
+  static constexpr int kSmemBytes = kMiscOffset + 256;
   static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
 };
 
 struct Args {
-  const __half *q, *v;
-  int64_t ldq, ldv, ldy;
+  const __half* v;
+  int64_t ldv, ldy;
   __half* y;
   int64_t total_q, total_k;
   const int32_t *cu_q, *cu_k;
@@ -71,7 +72,7 @@ struct Args {
   int tokens;                // per tile: 128 / heads_per_chunk
   int units;                 // kv heads * chunks
   float c;                   // |scale| log2(e), 1 where scale is 0
-  int sign;                  // of scale: queries are multiplied by it
+  int sign;                  // of scale: scores are multiplied by it
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
@@ -193,6 +194,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {      // NaN if eith
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -205,8 +211,8 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, 
 #pragma unroll
   for (int a = 0; a < Cfg<D>::kAtoms; ++a)
     asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-        ::"r"(dst + a * Cfg<D>::kAtomBytes), "l"(map), "r"(bar), "r"(head * D + a * 64), "r"(row)
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst + a * Cfg<D>::kAtomBytes), "l"(map), "r"(bar), "r"(a * 64), "r"(head), "r"(row)
         : "memory");
 }
 
@@ -241,20 +247,51 @@ __device__ __forceinline__ int sequence_tiles(const Args& a, int b, Work* w) {
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
-attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                    const __grid_constant__ CUtensorMap v_map) {
   using C = Cfg<D>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  extern __shared__ __align__(1024) uint8_t smem[];       // the kernel has no other shared memory
   const uint32_t base = smem_u32(smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
+  // ---- barriers, tensor memory ----
+  const uint32_t bars = base + C::kBarOffset;
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * C::kStages, bar_s = bar_empty + 8 * C::kStages, bar_p = bar_s + 16,
+                 bar_o = bar_p + 16, bar_q = bar_o + 16, bar_guard = bar_q + 8, bar_go = bar_guard + 32;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kMiscOffset);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 8);
+  volatile int* not_finite = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 16);
+  if (tid == 0) {
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(bar_full + 8 * i, 1);
+      mbar_init(bar_empty + 8 * i, 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(bar_s + 8 * t, 1);
+      mbar_init(bar_p + 8 * t, 4);
+      mbar_init(bar_o + 8 * t, 1);
+    }
+    mbar_init(bar_q, 1);
+    for (int g = 0; g < 4; ++g) {
+      mbar_init(bar_guard + 8 * g, 2);
+      mbar_init(bar_go + 8 * g, 1);
+    }
+    *abort_flag = 0;
+    *not_finite = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+
   // ---- which sequence and which of its tiles: the sequences' tile counts, added up by the whole CTA ----
-  __shared__ int s_sums[kThreads / 32];
-  __shared__ int s_found, s_local;
+  int* s_sums = reinterpret_cast<int*>(smem + C::kMiscOffset + 32);
+  int& s_found = s_sums[kThreads / 32];
+  int& s_local = s_sums[kThreads / 32 + 1];
   const int unit = int(blockIdx.x) % a.units;
   const int want = int(blockIdx.x) / a.units;
   if (tid == 0) s_found = -1;
-  __syncthreads();
   {
     const int per = (a.batch + kThreads - 1) / kThreads;
     const int b0 = min(a.batch, tid * per), b1 = min(a.batch, b0 + per);
@@ -283,8 +320,14 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
       }
     }
   }
+  fence_before();
   __syncthreads();
-  if (s_found < 0) return;                          // more CTAs than tiles: the grid is an upper bound
+  fence_after();
+  if (s_found < 0) {                                // more CTAs than tiles: the grid is an upper bound
+    if (warp == kMmaWarp)
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*tmem_slot), "r"(512) : "memory");
+    return;
+  }
   Work w;
   sequence_tiles(a, s_found, &w);
   w.first = s_local * 2 * a.tokens;
@@ -296,43 +339,10 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
   // from this key on some row of the CTA does not see everything
   const int ragged = w.limit(w.first, a.causal);
 
-  // ---- barriers, tensor memory ----
-  const uint32_t bars = base + C::kBarOffset;
-  const uint32_t bar_full = bars, bar_empty = bars + 8 * C::kStages, bar_s = bar_empty + 8 * C::kStages, bar_p = bar_s + 16,
-                 bar_o = bar_p + 16, bar_q = bar_o + 16, bar_guard = bar_q + 8, bar_go = bar_guard + 32;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kMiscOffset);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 8);
-  volatile int* not_finite = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 16);
-  if (tid == 0) {
-    for (int i = 0; i < C::kStages; ++i) {
-      mbar_init(bar_full + 8 * i, 1);
-      mbar_init(bar_empty + 8 * i, 1);
-    }
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(bar_s + 8 * t, 1);
-      mbar_init(bar_p + 8 * t, 4);
-      mbar_init(bar_o + 8 * t, 1);
-    }
-    mbar_init(bar_q, 8);
-    for (int g = 0; g < 4; ++g) {
-      mbar_init(bar_guard + 8 * g, 2);
-      mbar_init(bar_go + 8 * g, 1);
-    }
-    *abort_flag = 0;
-    *not_finite = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == 8) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  fence_before();
-  __syncthreads();
-  fence_after();
   const uint32_t tmem = *tmem_slot;
   const uint32_t q_smem = base, ring = base + 2 * C::kTileBytes;
 
-  if (warp < 8) {
+  if (warp < kSoftmaxWarps) {
     // ================= softmax of tile t: one thread per row =================
     const int t = warp >> 2;
     const int row = tid & 127;
@@ -341,27 +351,6 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
     const bool live = row < a.tokens * heads && token < w.nq;
     const int limit = live ? w.limit(token, a.causal) : 0;
     const int nt = t == 0 ? n0 : n1;
-    {
-      // the row's queries into shared memory, K-major with the 128-byte swizzle.  Consecutive threads take consecutive
-      // 16-byte pieces of a row.
-      constexpr int kPieces = D / 8;
-      const uint32_t flip = a.sign < 0 ? 0x80008000u : 0u;
-      for (int i = row; i < kTile * kPieces; i += kTile) {
-        const int r = i / kPieces, piece = i % kPieces;
-        const int tk = w.first + t * a.tokens + r / heads;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (r < a.tokens * heads && tk < w.nq && a.sign != 0) {
-          x = __ldg(reinterpret_cast<const uint4*>(a.q + int64_t(w.q0 + tk) * a.ldq + int64_t(head0 + r % heads) * D) + piece);
-          x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
-        }
-        const uint32_t dst = uint32_t(t) * C::kTileBytes + uint32_t(piece >> 3) * C::kAtomBytes + uint32_t(r) * 128u +
-                             (uint32_t((piece ^ r) & 7) << 4);
-        *reinterpret_cast<uint4*>(smem + dst) = x;
-      }
-      fence_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_q);
-    }
     const uint32_t lanes = uint32_t(warp & 3) << 21;                 // tensor-memory lane 32 * (warp % 4)
     const uint32_t s_col = tmem + lanes + uint32_t(t) * 128u;
     const uint32_t o_col = tmem + lanes + 256u + uint32_t(t) * 128u;
@@ -376,6 +365,10 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll
       for (int i = 0; i < 4; ++i) tmem_load32(s_col + 32 * i, s + 32 * i);
       tmem_wait_ld();
+      if (a.sign != 1) {                                             // a scale that is not positive
+#pragma unroll
+        for (int i = 0; i < kTile; ++i) s[i] *= float(a.sign);
+      }
       if (j >= masked_from) {
         const int here = limit - j * kTile;
 #pragma unroll
@@ -383,11 +376,13 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
       }
       float top[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-      for (int i = 4; i < kTile; i += 4) {
+      for (int i = 4; i < kTile - 4; i += 8) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) top[x] = max_nan(top[x], s[i + x]);
+        for (int x = 0; x < 4; ++x) top[x] = max_nan(top[x], s[i + x], s[i + 4 + x]);
       }
-      float high = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3])) * a.c;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) top[x] = max_nan(top[x], s[kTile - 4 + x]);
+      float high = max_nan(max_nan(top[0], top[1], top[2]), top[3]) * a.c;
       if (high == INFINITY) high = NAN;                              // inf - inf
       // P of the last block has been read: S of this one was issued after it
       const bool raise = !(high <= m + 8.0f);
@@ -454,8 +449,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
 #pragma unroll
         for (int x = 0; x < 32; ++x) o[x] = limit > 0 ? o[x] * inv : 0.0f;
         if (put_back) {
-          for (int key = ragged / kTile * kTile; key < limit; ++key) {
-            if (key < ragged) continue;
+          for (int key = ragged; key < limit; ++key) {
             const __half* v = a.v + int64_t(w.k0 + key) * a.ldv + int64_t(kv) * D + 32 * i;
 #pragma unroll
             for (int x = 0; x < 32; ++x) {
@@ -477,7 +471,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
         }
       }
     }
-  } else if (warp == 8) {
+  } else if (warp == kMmaWarp) {
     // ================= products =================
     if (lane == 0 && n > 0) {
       constexpr uint32_t id_s = idesc(kTile, false), id_o = idesc(D, true);
@@ -538,9 +532,18 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
         }
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == kLoadWarp) {
     // ================= loads: K_0, V_0, K_1, V_1, ... =================
-    if (lane == 0) {
+    if (lane == 0 && n > 0) {
+      // rows of a query tile: the chunk's heads of one token after another; what lies past the sequence is never stored
+      mbar_expect(bar_q, (n1 > 0 ? 2 : 1) * C::kAtoms * 128 * a.heads_per_chunk * a.tokens);
+      for (int t = 0; t < (n1 > 0 ? 2 : 1); ++t)
+        for (int x = 0; x < C::kAtoms; ++x)
+          asm volatile(
+              "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+              ::"r"(q_smem + t * C::kTileBytes + x * C::kAtomBytes), "l"(&q_map), "r"(bar_q), "r"(x * 64), "r"(head0),
+              "r"(w.q0 + w.first + t * a.tokens)
+              : "memory");
       for (int i = 0; i < 2 * n; ++i) {
         const int s = i % C::kStages;
         if (i >= C::kStages && !mbar_wait(bar_empty + 8 * s, ((i / C::kStages) & 1) ^ 1, abort_flag, kSiteLoad)) break;
@@ -560,7 +563,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
       uint8_t* v = smem + (2 + s) * C::kTileBytes;
       const int from = max(0, ragged - j * kTile), end = w.nk - j * kTile;       // rows to look at; rows past the sequence
       bool bad = false;
-      for (int x = tid - 320; x < (kTile - from) * (D / 8); x += kGuardThreads) {
+      for (int x = tid - 32 * kGuardWarp; x < (kTile - from) * (D / 8); x += kGuardThreads) {
         const int r = from + x / (D / 8), piece = x % (D / 8);
         uint4* at = reinterpret_cast<uint4*>(v + (piece >> 3) * C::kAtomBytes + r * 128 + (piece & 7) * 16);
         if (r >= end) {
@@ -595,25 +598,27 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, con
   fence_before();
   __syncthreads();
   fence_after();
-  if (warp == 8)
+  if (warp == kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-static bool row_map(CUtensorMap* map, const void* p, int64_t cols, int64_t rows, int64_t ld) {
+// fp16 rows of `heads` heads of `dim` values: 64 values of `box_heads` heads of `box_rows` rows are copied at a time.
+static bool row_map(CUtensorMap* map, const void* p, int64_t heads, int64_t dim, int64_t rows, int64_t ld, int box_heads,
+                    int box_rows) {
   TensorMapEncodeFn encode = tensor_map_encoder();
   if (encode == nullptr) return false;
-  const cuuint64_t dims[2] = {cuuint64_t(cols), cuuint64_t(rows)};
-  const cuuint64_t strides[1] = {cuuint64_t(ld) * 2};
-  const cuuint32_t box[2] = {64, kTile}, steps[2] = {1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(p), dims, strides, box, steps,
+  const cuuint64_t dims[3] = {cuuint64_t(dim), cuuint64_t(heads), cuuint64_t(rows)};
+  const cuuint64_t strides[2] = {cuuint64_t(dim) * 2, cuuint64_t(ld) * 2};
+  const cuuint32_t box[3] = {64, cuuint32_t(box_heads), cuuint32_t(box_rows)}, steps[3] = {1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims, strides, box, steps,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int D>
-static int launch(const Args& a, const CUtensorMap& km, const CUtensorMap& vm, int64_t grid, cudaStream_t st) {
+static int launch(const Args& a, const CUtensorMap& qm, const CUtensorMap& km, const CUtensorMap& vm, int64_t grid, cudaStream_t st) {
   if (!allow_dynamic_smem(reinterpret_cast<const void*>(&attn_prefill_kernel<D>), Cfg<D>::kSmemBytes)) return SMOOTHROT_CUDA_ERROR;
-  attn_prefill_kernel<D><<<unsigned(grid), kThreads, Cfg<D>::kSmemBytes, st>>>(a, km, vm);
+  attn_prefill_kernel<D><<<unsigned(grid), kThreads, Cfg<D>::kSmemBytes, st>>>(a, qm, km, vm);
   count_launch();
   return launch_status();
 }
@@ -657,9 +662,8 @@ int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, cons
   if (!aligned16(Q_f16) || !aligned16(Y_f16) || ldq % 8 != 0 || ldy % 8 != 0) return SMOOTHROT_BAD_ALIGNMENT;
   if (total_k > 0 && (!aligned16(K_f16) || !aligned16(V_f16) || ldk % 8 != 0 || ldv % 8 != 0)) return SMOOTHROT_BAD_ALIGNMENT;
   Args a;
-  a.q = static_cast<const __half*>(Q_f16);
   a.v = static_cast<const __half*>(V_f16);
-  a.ldq = ldq; a.ldv = ldv; a.ldy = ldy;
+  a.ldv = ldv; a.ldy = ldy;
   a.y = static_cast<__half*>(Y_f16);
   a.total_q = total_q; a.total_k = total_k;
   a.cu_q = cu_q; a.cu_k = cu_k;
@@ -673,12 +677,15 @@ int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, cons
   a.c = scale == 0.0f ? 1.0f : (scale < 0.0f ? -scale : scale) * 1.4426950408889634f;
   const int64_t grid = (total_q / (2 * a.tokens) + B) * a.units;
   if (grid > INT32_MAX) return SMOOTHROT_INVALID_ARG;
-  CUtensorMap km, vm;
+  CUtensorMap qm, km, vm;
+  if (!row_map(&qm, Q_f16, n_heads, head_dim, total_q, ldq, a.heads_per_chunk, a.tokens)) return SMOOTHROT_CUDA_ERROR;
   if (total_k > 0) {
-    if (!row_map(&km, K_f16, ckv, total_k, ldk) || !row_map(&vm, V_f16, ckv, total_k, ldv)) return SMOOTHROT_CUDA_ERROR;
+    if (!row_map(&km, K_f16, n_kv_heads, head_dim, total_k, ldk, 1, kTile) ||
+        !row_map(&vm, V_f16, n_kv_heads, head_dim, total_k, ldv, 1, kTile))
+      return SMOOTHROT_CUDA_ERROR;
   }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return head_dim == 128 ? launch<128>(a, km, vm, grid, st) : launch<64>(a, km, vm, grid, st);
+  return head_dim == 128 ? launch<128>(a, qm, km, vm, grid, st) : launch<64>(a, qm, km, vm, grid, st);
 }
 
 }  // extern "C"
