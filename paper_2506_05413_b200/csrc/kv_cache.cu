@@ -31,6 +31,16 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
   return raw;
 }
 
+// Products of two pairs, each rounded to fp32.  Not mul2: the compiler may make one fma of a packed product and the packed
+// sum that takes it, and the rotation and the codes are defined with the product rounded by itself (a
+// code at a rounding boundary moves with it).
+__device__ __forceinline__ f32x2 rounded_product(f32x2 a, f32x2 b) {
+  float a0, a1, b0, b1;
+  unpack2(a, a0, a1);
+  unpack2(b, b0, b1);
+  return pack2(__fmul_rn(a0, b0), __fmul_rn(a1, b1));
+}
+
 struct AppendArgs {
   const __half *q, *k, *v;
   int64_t ldq, ldk, ldv;
@@ -139,7 +149,7 @@ kv_append_kernel(AppendArgs a, Cache c) {
             o[i] = half2_to_f32x2(other);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = add2(mul2(y[i], cs[i]), mul2(o[i], sn[i]));
+          for (int i = 0; i < 4; ++i) y[i] = add2(rounded_product(y[i], cs[i]), rounded_product(o[i], sn[i]));
           if (a.walsh) {                           // y H_D / sqrt(D), butterflies of stride 1, 2, 4, then between lanes
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -216,7 +226,7 @@ kv_append_kernel(AppendArgs a, Cache c) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               float u0, u1;
-              unpack2(add2(add2(mul2(pack2(x[2 * i], x[2 * i + 1]), inv2), magic2), zero2), u0, u1);
+              unpack2(add2(add2(rounded_product(pack2(x[2 * i], x[2 * i + 1]), inv2), magic2), zero2), u0, u1);
               u0 = fminf(fmaxf(u0, 12582912.0f), 12582927.0f);
               u1 = fminf(fmaxf(u1, 12582912.0f), 12582927.0f);
               packed += (__float_as_uint(u0) - 0x4B400000u) * weight;

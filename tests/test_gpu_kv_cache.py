@@ -143,6 +143,37 @@ def test_gather_matches_the_plain_form(sr, pu, T, kv, D, page, bits):
     assert torch.isnan(out[:, kv * D:kv * D + 8]).all() and torch.isnan(out[:, 2 * kv * D + 8:]).all()
 
 
+@pytest.mark.parametrize("D,kv,inter", [(128, 8, False), (128, 8, True), (64, 16, False)])
+def test_append_rounds_every_product(sr, pu, D, kv, inter):
+    """Enough values that some lie at rounding boundaries: the rotation equals separate fp32 operations bit for bit, and the
+    codes those of the row quantizer."""
+    import torch
+    T = 4096
+    gen = _gen(6)
+    q, k, v = pu.rows(gen, T, 8 * D), pu.rows(gen, T, kv * D, outliers=(5, 40)), pu.rows(gen, T, kv * D, 0.5)
+    pos = torch.arange(T, dtype=torch.int32, device=pu.DEV)
+    table = pu.rotary_table(T, D)
+    slots = torch.randperm(T, generator=gen, device=pu.DEV)
+    cache = pu.Cache(T // 64, 64, kv, D, 4)
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    sr.kv_append(q, k, v, pos, table, slots, *cache.tensors(), q_out=qo, k_out=ko, interleaved=inter)
+    torch.cuda.synchronize()
+    c, s = table[:, None, :D // 2], table[:, None, D // 2:]
+    for got, x in ((qo, q), (ko, k)):
+        x = x.float().reshape(T, -1, D)
+        a, b = (x[..., 0::2], x[..., 1::2]) if inter else (x[..., :D // 2], x[..., D // 2:])
+        ac, bs, bc, as_ = a * c, b * s, b * c, a * s          # each rounded by itself
+        one, two = ac - bs, bc + as_
+        want = torch.stack([one, two], -1).flatten(-2) if inter else torch.cat([one, two], -1)
+        assert torch.equal(got, want.reshape(T, -1).half())
+    qv = torch.empty(T, kv * D // 2, dtype=torch.uint8, device=pu.DEV)
+    st, ze = (torch.empty(T, kv * D // 128, device=pu.DEV) for _ in range(2))
+    sr.kv_quant(v, 0.95, qv, st, ze)
+    p, o = slots // 64, slots % 64
+    assert torch.equal(cache.v[p, :, o].flatten(1), qv)
+    assert torch.equal(cache.vp[p, :, o][..., 0], st) and torch.equal(cache.vp[p, :, o][..., 1], ze)
+
+
 def test_constant_and_far_off_groups(sr, pu):
     """Groups whose values are all equal, and groups far from zero (a zero point far outside 0..15)."""
     import torch
