@@ -350,7 +350,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
 
   const int key_lo = key_of_row(g), key_hi = key_of_row(g + 8);
   constexpr int kParts = S::kKeys / 16;
-  float sc[kParts][NT][4];
+  float sc2[kParts][NT][4];
   uint32_t pt[MG][NT][2], seen = 0;              // the second operand of V^T P^T
   bool full = false;
   auto arrived = [&](int stage) -> bool {
@@ -421,7 +421,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[part][n][e] = sa[n][e];
+        for (int e = 0; e < 4; ++e) sc2[part][n][e] = sa[n][e];
     }
   };
   auto weigh = [&](int stage, int part) {
@@ -452,7 +452,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
         for (int n = 0; n < NT; ++n) {
           f32x2 u = pc.neg_m[n];
           if (kBits == 4) u = fma2(pack2(kz[mg][r], kz[mg][r]), qsum[n], u);
-          y[mg][r][n] = fma2(pack2(sc[part][n][2 * r], sc[part][n][2 * r + 1]), pack2(ks[mg][r], ks[mg][r]), u);
+          y[mg][r][n] = fma2(pack2(sc2[part][n][2 * r], sc2[part][n][2 * r + 1]), pack2(ks[mg][r], ks[mg][r]), u);
         }
       }
     }
@@ -509,7 +509,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
               float x[2];
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                x[e] = live ? fmaf(sc[part][n][2 * r + e], ks[mg][r], kz[mg][r] * qs[e]) : -INFINITY;
+                x[e] = live ? fmaf(sc2[part][n][2 * r + e], ks[mg][r], kz[mg][r] * qs[e]) : -INFINITY;
                 if (pass == 0) to[e] = fmaxf(to[e], x[e] + lead);
               }
               if (pass == 1) y[mg][r][n] = pack2(x[0] - to[0], x[1] - to[1]);
@@ -718,39 +718,38 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   s_sums[tid + 1] = incl;
   if (tid == 0) s_sums[0] = 0;
   __syncthreads();
-  const long long all = (long long)s_sums[kDecodeThreads] * a.units;   // tiles in the line
+  const int all = s_sums[kDecodeThreads] * a.units;         // tiles in the line: below 2^31 (checked)
   const int segments = a.batch * a.units;
   // Short sequences: a CTA per segment, so that nothing has to meet in the workspace.  Else equal stretches.
   const bool whole = segments <= int(gridDim.x) && most <= 4 * kWarps + 1;
-  const int ctas = whole ? segments : int(min((long long)gridDim.x, (all + kWarps - 1) / kWarps));
+  const int ctas = whole ? segments : min(int(gridDim.x), (all + kWarps - 1) / kWarps);
   if (int(blockIdx.x) >= ctas) return;
 
-  auto start_of_sequence = [&](int b) -> long long {        // tiles per unit before sequence b
+  auto start_of_sequence = [&](int b) -> int {              // tiles per unit before sequence b
     const int i = b / per;
-    long long at = s_sums[i];
+    int at = s_sums[i];
     for (int x = i * per; x < b; ++x) at += tiles_of(x);
     return at;
   };
   // CTA i's stretch starts at tile i * share + min(i, extra)
-  const long long share = all < (1ll << 32) ? (long long)(uint32_t(all) / uint32_t(ctas)) : all / ctas;
-  const int extra = int(all - share * ctas);
-  auto start_of_cta = [&](int i) -> long long { return i * share + min(i, extra); };
-  auto cta_of = [&](long long tile) -> int {
-    const long long bound = extra * (share + 1);
-    return tile < bound ? int(tile / (share + 1)) : extra + int((tile - bound) / share);
+  const int share = all / ctas, extra = all - share * ctas;
+  auto start_of_cta = [&](int i) -> int { return i * share + min(i, extra); };
+  auto cta_of = [&](int tile) -> int {
+    const int bound = extra * (share + 1);
+    return tile < bound ? tile / (share + 1) : extra + (tile - bound) / share;
   };
-  long long begin, end;                                     // this warp's stretch
+  int begin, end;                                           // this warp's stretch
   if (whole) {
     const int b = blockIdx.x / a.units, n = tiles_of(b);
-    const long long at = start_of_sequence(b) * a.units + (long long)(blockIdx.x - b * a.units) * n;
+    const int at = start_of_sequence(b) * a.units + (blockIdx.x - b * a.units) * n;
     if (n == 0) return;
     begin = at + 1 + (n - 1) * warp / kWarps;
     end = at + 1 + (n - 1) * (warp + 1) / kWarps;
   } else {
     begin = start_of_cta(blockIdx.x);
-    const long long n = start_of_cta(blockIdx.x + 1) - begin;
-    end = begin + n * (warp + 1) / kWarps;
-    begin += n * warp / kWarps;
+    const int n = share + (int(blockIdx.x) < extra ? 1 : 0), each = n / kWarps, more = n % kWarps;
+    begin += warp * each + min(warp, more);
+    end = begin + each + (warp < more ? 1 : 0);
   }
 
   if (begin < end) {
@@ -759,20 +758,20 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
     int lo = 0, hi = kDecodeThreads;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if ((long long)s_sums[mid] * a.units <= begin) lo = mid; else hi = mid;
+      if (s_sums[mid] * a.units <= begin) lo = mid; else hi = mid;
     }
-    long long at = (long long)s_sums[lo] * a.units;
+    int at = s_sums[lo] * a.units;
     s.b = lo * per;
     s.tiles = tiles_of(s.b);
-    while (at + (long long)s.tiles * a.units <= begin) {
-      at += (long long)s.tiles * a.units;
+    while (at + s.tiles * a.units <= begin) {
+      at += s.tiles * a.units;
       s.tiles = tiles_of(++s.b);
     }
-    s.unit = int((begin - at) / s.tiles);
-    s.tile = int((begin - at) - (long long)s.unit * s.tiles);
+    s.unit = (begin - at) / s.tiles;
+    s.tile = (begin - at) - s.unit * s.tiles;
     while (true) {
       s.length = clamped_length(a, c, s.b);
-      const int place = s.tile, steps = int(min((long long)(s.tiles - place), end - begin));
+      const int place = s.tile, steps = min(s.tiles - place, end - begin);
       const bool first = place <= 1, last = place + steps == s.tiles;
       const int count = place == 0 ? steps - 1 : steps;
       s.tile = place == 0 ? 0 : place - 1;
@@ -902,7 +901,6 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
             out[a.rows * D + h] = top;
             out[a.rows * D + a.rows + h] = l;
           }
-          __threadfence();
         }
       }
     }
@@ -910,14 +908,18 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
 
   // ---- segments that reach over several CTAs: the last of them to arrive adds up ----
   // Each CTA raises a flag of its own per piece and then looks at all of the segment's: at least the last to raise sees them
-  // all (sequentially consistent fences).  Two that see them both add up, to the same bits; the flags come down again, so
-  // that a replay of the same launch starts anew.  A flag is up when it holds this call's tag, whatever the
-  // workspace held before.
+  // all (sequentially consistent fences).  Of those that do, the one that takes the first piece's flag down adds up; it
+  // takes the others down too, so that a replay of the same launch starts anew.  A flag is up when it holds this
+  // call's tag, whatever the workspace held before.
   if (pending[0] < 0 && pending[1] < 0) return;
   __syncthreads();
-  if (tid < 2 && pending[tid] >= 0)
-    reinterpret_cast<volatile unsigned long long*>(a.arrived)[blockIdx.x * 2 + tid] = a.tag;
-  __threadfence();
+  if (tid == 0) {
+    __threadfence();                                        // the records, all threads', before the flags
+    volatile unsigned long long* flags = reinterpret_cast<volatile unsigned long long*>(a.arrived) + blockIdx.x * 2;
+    if (pending[0] >= 0) flags[0] = a.tag;
+    if (pending[1] >= 0) flags[1] = a.tag;
+    __threadfence();                                        // and the flags before any other is looked at
+  }
   float* s_weight = reinterpret_cast<float*>(smem);         // [pieces][rows], over what is done with
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {
@@ -927,41 +929,64 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
     const int kv = unit / a.chunks, chunk = unit - kv * a.chunks;
     const int rows = min(a.rows, a.group - chunk * a.rows);
     __half* y = a.y + int64_t(b) * a.ldy + (int64_t(kv) * a.group + chunk * a.rows) * D;
-    const long long n = tiles_of(b);
-    const long long from = start_of_sequence(b) * a.units + unit * n;
+    const int n = tiles_of(b);
+    const int from = start_of_sequence(b) * a.units + unit * n;
     const int c0 = cta_of(from + 1), c1 = cta_of(from + n - 1);
     bool up = true;
     __syncthreads();                                        // this CTA's own flags are up
     for (int i = c0 + tid; i <= c1; i += kDecodeThreads)
       up &= reinterpret_cast<volatile unsigned long long*>(a.arrived)[i * 2 + (i == c0 ? 1 : 0)] == a.tag;
-    if (__syncthreads_and(up)) {
+    bool won = __syncthreads_and(up) != 0;
+    if (won) won = __syncthreads_or(tid == 0 && atomicCAS(a.arrived + c0 * 2 + 1, a.tag, 0ull) == a.tag) != 0;
+    if (won) {
       __threadfence();
       auto piece = [&](int i) -> const float* { return a.records + (int64_t(i) * 2 + (i == c0 ? 1 : 0)) * stride; };
-      // one warp per head: the pieces' references and sums, a lane for every 32nd piece
-      for (int h = warp; h < rows; h += kWarps) {
+      // Everything is asked for at once: the pieces' references and sums, to shared memory, and the first kEarly pieces of this
+      // thread's two values.
+      const int pieces = c1 - c0 + 1;
+      constexpr int kEarly = 8;
+      float2 early[kEarly];
+      const bool mine = tid * 2 < rows * D;
+#pragma unroll
+      for (int i = 0; i < kEarly; ++i)
+        early[i] = mine && i < pieces ? __ldcg(reinterpret_cast<const float2*>(piece(c0 + i) + tid * 2)) : make_float2(0.0f, 0.0f);
+      for (int x = tid; x < pieces * rows; x += kDecodeThreads) {
+        const int i = x / rows, h = x - i * rows;
+        s_weight[x] = __ldcg(piece(c0 + i) + a.rows * D + h);
+        s_weight[pieces * rows + x] = __ldcg(piece(c0 + i) + a.rows * D + a.rows + h);
+      }
+      __syncthreads();
+      for (int h = warp; h < rows; h += kWarps) {           // a warp per head: weights and sum
         float m = -INFINITY, l = 0.0f;
-        for (int i = c0 + lane; i <= c1; i += 32) m = fmaxf(m, __ldcg(piece(i) + a.rows * D + h));
+        for (int i = lane; i < pieces; i += 32) m = fmaxf(m, s_weight[i * rows + h]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         const float ref = m == -INFINITY ? 0.0f : m;
-        for (int i = c0 + lane; i <= c1; i += 32) {
-          const float f = exp2_fast(__ldcg(piece(i) + a.rows * D + h) - ref);
-          s_weight[(i - c0) * a.rows + h] = f;
-          l += __ldcg(piece(i) + a.rows * D + a.rows + h) * f;
+        for (int i = lane; i < pieces; i += 32) {
+          const float f = exp2_fast(s_weight[i * rows + h] - ref);
+          s_weight[i * rows + h] = f;
+          l += s_weight[(pieces + i) * rows + h] * f;
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
         if (lane == 0) s_total[h] = l;
       }
       __syncthreads();
-      // a thread per two values
       for (int x = tid * 2; x < rows * D; x += kDecodeThreads * 2) {
         const int h = x / D;
         float o0 = 0.0f, o1 = 0.0f;
-#pragma unroll 16
-        for (int i = c0; i <= c1; ++i) {
-          const float2 r = __ldcg(reinterpret_cast<const float2*>(piece(i) + x));
-          const float f = s_weight[(i - c0) * a.rows + h];
+        if (x == tid * 2) {
+#pragma unroll
+          for (int i = 0; i < kEarly; ++i) {
+            const float f = i < pieces ? s_weight[i * rows + h] : 0.0f;
+            o0 = fmaf(early[i].x, f, o0);
+            o1 = fmaf(early[i].y, f, o1);
+          }
+        }
+#pragma unroll 8
+        for (int i = x == tid * 2 ? kEarly : 0; i < pieces; ++i) {
+          const float2 r = __ldcg(reinterpret_cast<const float2*>(piece(c0 + i) + x));
+          const float f = s_weight[i * rows + h];
           o0 = fmaf(r.x, f, o0);
           o1 = fmaf(r.y, f, o1);
         }
@@ -969,7 +994,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
         *reinterpret_cast<__half2*>(y + x) = __floats2half2_rn(o0 * inv, o1 * inv);
       }
       __syncthreads();
-      for (int i = c0 + tid; i <= c1; i += kDecodeThreads) a.arrived[i * 2 + (i == c0 ? 1 : 0)] = 0;
+      for (int i = c0 + 1 + tid; i <= c1; i += kDecodeThreads) a.arrived[i * 2] = 0;
     }
   }
 }
@@ -1030,7 +1055,8 @@ int smoothrot_attn_decode(const void* Q_f16, int64_t ldq, int64_t B, int64_t n_h
   if (sizes != SMOOTHROT_OK) return sizes;
   if (n_heads % n_kv_heads != 0 || !(scale == scale)) return SMOOTHROT_INVALID_ARG;
   // a length is an int32, and the tiles of all sequences are counted in one
-  if (max_pages * page_size > INT32_MAX || B * max_pages * page_size > (int64_t(1) << 34)) return SMOOTHROT_INVALID_ARG;
+  if (max_pages * page_size > INT32_MAX || B * (max_pages * page_size / 16 + 2) > INT32_MAX / n_kv_heads / ((n_heads / n_kv_heads + 15) / 16))
+    return SMOOTHROT_INVALID_ARG;
   if (B == 0) return SMOOTHROT_OK;
   if (Q_f16 == nullptr || Y_f16 == nullptr || lengths == nullptr || ldq < n_heads * head_dim || ldy < n_heads * head_dim)
     return SMOOTHROT_INVALID_ARG;
