@@ -20,8 +20,8 @@
 // multiplied down in tensor memory, which happens in the first few blocks and hardly ever after.  Sums, scores, O and m are
 // fp32; a weight is rounded once to fp16, the type of the values that it multiplies.
 //
-// Roles: warps 0-3 and 4-7 the softmax of the two tiles, warp 8 issues the products, warp 9 the TMA
-// loads (queries, then keys and values through one ring of 128-row stages), warps 10-11 clean the value rows that not every row
+// Roles: warps 0-3 and 4-7 the softmax of the two tiles, warps 8 and 9 issue their products, warp 10 the TMA
+// loads (queries, then keys and values through one ring), warp 11 cleans the value rows that not every row
 // of the CTA sees: a product of a zero weight with NaN or infinity is NaN, so rows past the sequence's end are
 // zeroed, and values that are not finite taken out of causally masked blocks and put back, row by row, at the end.
 // Every mbarrier wait is bounded; on expiry the CTA records a code and winds down.
@@ -41,20 +41,24 @@ constexpr unsigned long long kDrainNs = 50000ull;
 __device__ int g_prefill_status = 0;
 __device__ unsigned long long g_prefill_wait_limit_ns = kWaitLimitNs;
 
-constexpr int kTile = 128;         // query rows of a tile, and keys of a block
+constexpr int kTile = 128;         // query rows of a tile
+constexpr int kBlock = 64;         // keys of a block
+constexpr int kRaggedBlocks = 6;   // of a CTA: its rows are at most 256 tokens, so 5 blocks in which they see different keys
 constexpr int kThreads = 384;
 constexpr int kSoftmaxWarps = 8;   // 4 a tile, a thread per row
-constexpr int kMmaWarp = kSoftmaxWarps, kLoadWarp = kMmaWarp + 1, kGuardWarp = kLoadWarp + 1;
-constexpr int kGuardThreads = 64;
+constexpr int kMmaWarp = kSoftmaxWarps, kLoadWarp = kMmaWarp + 2, kGuardWarp = kLoadWarp + 1;      // a product warp per tile
+constexpr int kGuardThreads = 32;
 
 template <int D>
 struct Cfg {
   static constexpr int kAtoms = D / 64;                       // 128-byte wide slices of a row
   static constexpr int kAtomBytes = kTile * 128;
-  static constexpr int kTileBytes = kAtoms * kAtomBytes;      // 128 rows of fp16
-  static constexpr int kStages = D == 128 ? 5 : 10;           // of the ring that keys and values share
-  static constexpr int kBarriers = 2 * kStages + 2 /*S*/ + 2 /*P*/ + 2 /*O*/ + 1 /*Q*/ + 8 /*guard*/;
-  static constexpr int kBarOffset = (2 + kStages) * kTileBytes;
+  static constexpr int kTileBytes = kAtoms * kAtomBytes;      // 128 rows of queries
+  static constexpr int kSliceBytes = kBlock * 128;
+  static constexpr int kBlockBytes = kAtoms * kSliceBytes;    // 64 rows of keys or values
+  static constexpr int kStages = D == 128 ? 5 : 8;            // of the ring: two blocks each
+  static constexpr int kBarriers = 2 * kStages + 4 /*S*/ + 4 /*P*/ + 2 /*O*/ + 1 /*Q*/ + 2 * kRaggedBlocks;
+  static constexpr int kBarOffset = 2 * kTileBytes + kStages * 2 * kBlockBytes;
   static constexpr int kMiscOffset = kBarOffset + 8 * kBarriers;
   static constexpr int kSmemBytes = kMiscOffset + 256;
   static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
@@ -126,36 +130,37 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 }
 
 // K-major operand, 128-byte swizzle: rows of 128 bytes, groups of 8 rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t desc_k_major(uint32_t addr) {
-  const uint32_t lo = ((addr & 0x3FFFFu) >> 4) | (1u << 16);
-  const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
-  return (uint64_t(hi) << 32) | lo;
-}
+// Only the low word differs from one descriptor to the next: the address in 16 bytes, and the second stride above it.
+__device__ __forceinline__ uint32_t desc_k_major(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
 // MN-major operand, 128-byte swizzle: 64 values of N per 128-byte row, one row per k, groups of 8 k
-// 1024 bytes apart, the next 64 values of N one slice of 128 rows further.
-__device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr) {
-  const uint32_t lo = ((addr & 0x3FFFFu) >> 4) | ((uint32_t(kTile) * 128u >> 4) << 16);
-  const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
-  return (uint64_t(hi) << 32) | lo;
+// 1024 bytes apart, the next 64 values of N one slice of 64 rows further.
+__device__ __forceinline__ uint32_t desc_mn_major(uint32_t addr) {
+  return ((addr & 0x3FFFFu) >> 4) | ((uint32_t(kBlock) * 128u >> 4) << 16);
 }
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
 // fp16 x fp16 -> fp32, M = 128; bit 16: B is MN-major.
 __host__ __device__ constexpr uint32_t idesc(int n, bool b_mn) {
   return (1u << 4) | (uint32_t(b_mn) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(kTile >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+template <uint32_t kAccumulate>
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t id) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 da, {%1, %4};\n\t"
+      "mov.b64 db, {%2, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(id), "r"(kDescHigh), "n"(kAccumulate)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+template <uint32_t kAccumulate>
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t id) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 db, {%2, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(id), "r"(kDescHigh), "n"(kAccumulate)
       : "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t taddr, float* r) {
@@ -205,14 +210,14 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   return r;
 }
 
-// 128 rows of one head: `kAtoms` boxes of 64 values x 128 rows.
+// 64 rows of one head: `kAtoms` boxes of 64 values x 64 rows.
 template <int D>
 __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
 #pragma unroll
   for (int a = 0; a < Cfg<D>::kAtoms; ++a)
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-        ::"r"(dst + a * Cfg<D>::kAtomBytes), "l"(map), "r"(bar), "r"(a * 64), "r"(head), "r"(row)
+        ::"r"(dst + a * Cfg<D>::kSliceBytes), "l"(map), "r"(bar), "r"(a * 64), "r"(head), "r"(row)
         : "memory");
 }
 
@@ -228,7 +233,7 @@ struct Work {
   __device__ __forceinline__ int blocks(int t, int tokens, int causal) const {
     const int a = first + t * tokens;
     if (a >= nq) return 0;
-    return (limit(min(nq, a + tokens) - 1, causal) + kTile - 1) / kTile;
+    return (limit(min(nq, a + tokens) - 1, causal) + kBlock - 1) / kBlock;
   }
 };
 
@@ -245,6 +250,67 @@ __device__ __forceinline__ int sequence_tiles(const Args& a, int b, Work* w) {
   return (w->nq + 2 * a.tokens - 1) / (2 * a.tokens);
 }
 
+// Ring entries of two blocks: K_0 and K_1 (which is always there, whatever it holds), then V_j and K_{j+2} for j = 0 .. n - 1
+// (no keys with the last two).
+template <int D>
+struct Bars {
+  static constexpr uint32_t kFull = Cfg<D>::kBarOffset, kEmpty = kFull + 8 * Cfg<D>::kStages, kS = kEmpty + 8 * Cfg<D>::kStages,
+                            kP = kS + 32, kO = kP + 32, kQ = kO + 16, kGuard = kQ + 8, kGo = kGuard + 8 * kRaggedBlocks;
+};
+
+// The products of tile T, all issued by one thread, whose own instructions are part of the tile's pace: a wait or a commit takes it
+// some 100 to 200 cycles, shared memory being busy with the operands.  So a ring entry holds what one step takes, values of this
+// block and keys of the next but one, with one barrier.
+template <int D, int T>
+__device__ __forceinline__ void issue_products(uint32_t base, int n, int nt, int guarded, volatile int* abort_flag) {
+  using C = Cfg<D>;
+  using B = Bars<D>;
+  constexpr uint32_t id_s = idesc(kBlock, false), id_o = idesc(D, true);
+  constexpr uint32_t s_at = T * 128u, o_at = 256u + T * 128u;
+  constexpr uint32_t ring = 2 * C::kTileBytes;
+  const uint32_t q_desc = desc_k_major(base + T * C::kTileBytes);
+  auto scores = [&](uint32_t buffer, uint32_t block_at) {             // S = Q K^T
+    const uint32_t k = desc_k_major(block_at);
+    mma_ss<0>(s_at + buffer * 64u, q_desc, k, id_s);
+#pragma unroll
+    for (int x = 1; x < D / 16; ++x)
+      mma_ss<1>(s_at + buffer * 64u, q_desc + (x >> 2) * (C::kAtomBytes / 16) + (x & 3) * 2,
+                k + (x >> 2) * (C::kSliceBytes / 16) + (x & 3) * 2, id_s);
+    commit(base + B::kS + 8 * (2 * T + buffer));
+  };
+  if (!mbar_wait(base + B::kQ, 0, abort_flag, kSiteMma)) return;
+  if (!mbar_wait(base + B::kFull, 0, abort_flag, kSiteMma)) return;
+  fence_after();
+  if (nt > 0) scores(0, base + ring);
+  if (nt > 1) scores(1, base + ring + C::kBlockBytes);
+  // no arrival is left under way when the CTA ends: only entries whose stage is filled again are released
+  if (C::kStages <= n) commit(base + B::kEmpty);
+  uint32_t stage = 1, phase = 0;
+#pragma unroll 1
+  for (int j = 0; j < n; ++j) {
+    const uint32_t at = base + ring + stage * (2 * C::kBlockBytes), buffer = j & 1;
+    if (!mbar_wait(base + B::kFull + 8 * stage, phase, abort_flag, kSiteMma)) return;
+    if (j < nt) {
+      if (j >= guarded && !mbar_wait(base + B::kGuard + 8 * (j - guarded), 0, abort_flag, kSiteMma)) return;
+      if (!mbar_wait(base + B::kP + 8 * (2 * T + buffer), (j >> 1) & 1, abort_flag, kSiteMma)) return;
+      fence_after();
+      const uint32_t v = desc_mn_major(at);
+      if (j == 0) mma_ts<0>(o_at, s_at + buffer * 64u, v, id_o);
+      else mma_ts<1>(o_at, s_at + buffer * 64u, v, id_o);
+#pragma unroll
+      for (int x = 1; x < kBlock / 16; ++x) mma_ts<1>(o_at, s_at + buffer * 64u + 8u * x, v + 128 * x, id_o);
+      if (j + 2 < nt) scores(buffer, at + C::kBlockBytes);
+      else if (j + 1 < nt) commit(base + B::kS + 8 * (2 * T + buffer));       // says that this block's products are done
+      else commit(base + B::kO + 8 * T);
+    }
+    if (j + 1 + C::kStages <= n) commit(base + B::kEmpty + 8 * stage);
+    if (++stage == C::kStages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
@@ -255,25 +321,25 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   // ---- barriers, tensor memory ----
-  const uint32_t bars = base + C::kBarOffset;
-  const uint32_t bar_full = bars, bar_empty = bars + 8 * C::kStages, bar_s = bar_empty + 8 * C::kStages, bar_p = bar_s + 16,
-                 bar_o = bar_p + 16, bar_q = bar_o + 16, bar_guard = bar_q + 8, bar_go = bar_guard + 32;
+  using B = Bars<D>;
+  const uint32_t bar_full = base + B::kFull, bar_empty = base + B::kEmpty, bar_s = base + B::kS, bar_p = base + B::kP,
+                 bar_o = base + B::kO, bar_q = base + B::kQ, bar_guard = base + B::kGuard, bar_go = base + B::kGo;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kMiscOffset);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 8);
   volatile int* not_finite = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 16);
   if (tid == 0) {
     for (int i = 0; i < C::kStages; ++i) {
       mbar_init(bar_full + 8 * i, 1);
-      mbar_init(bar_empty + 8 * i, 1);
+      mbar_init(bar_empty + 8 * i, 2);
     }
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(bar_s + 8 * t, 1);
-      mbar_init(bar_p + 8 * t, 4);
-      mbar_init(bar_o + 8 * t, 1);
+    for (int i = 0; i < 4; ++i) {                   // tile i / 2, buffer i % 2
+      mbar_init(bar_s + 8 * i, 1);
+      mbar_init(bar_p + 8 * i, 4);
     }
+    for (int t = 0; t < 2; ++t) mbar_init(bar_o + 8 * t, 1);
     mbar_init(bar_q, 1);
-    for (int g = 0; g < 4; ++g) {
-      mbar_init(bar_guard + 8 * g, 2);
+    for (int g = 0; g < kRaggedBlocks; ++g) {
+      mbar_init(bar_guard + 8 * g, 1);
       mbar_init(bar_go + 8 * g, 1);
     }
     *abort_flag = 0;
@@ -323,6 +389,10 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
   fence_before();
   __syncthreads();
   fence_after();
+  if (*tmem_slot != 0 && tid == 0) {
+    *abort_flag = 1;
+    atomicCAS(&g_prefill_status, 0, int(kSiteMma));
+  }
   if (s_found < 0) {                                // more CTAs than tiles: the grid is an upper bound
     if (warp == kMmaWarp)
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*tmem_slot), "r"(512) : "memory");
@@ -339,7 +409,8 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
   // from this key on some row of the CTA does not see everything
   const int ragged = w.limit(w.first, a.causal);
 
-  const uint32_t tmem = *tmem_slot;
+  // All of tensor memory is this CTA's, so it starts at 0: addresses in it are constants.
+  constexpr uint32_t tmem = 0;
   const uint32_t q_smem = base, ring = base + 2 * C::kTileBytes;
 
   if (warp < kSoftmaxWarps) {
@@ -355,36 +426,42 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
     const uint32_t s_col = tmem + lanes + uint32_t(t) * 128u;
     const uint32_t o_col = tmem + lanes + 256u + uint32_t(t) * 128u;
     // first block of this tile with a key that some row does not see
-    const int masked_from = w.limit(min(w.first + t * a.tokens, w.nq - 1), a.causal) / kTile;
+    const int masked_from = w.limit(min(w.first + t * a.tokens, w.nq - 1), a.causal) / kBlock;
     float m = -INFINITY, l = 0.0f;
+    float s[kBlock];
     bool ok = true;
-    for (int j = 0; j < nt; ++j) {
-      if (!mbar_wait(bar_s + 8 * t, j & 1, abort_flag, kSiteSoftmax)) { ok = false; break; }
+    // The scores of block j into registers.  The copy is on its way when this returns.
+    auto fetch = [&](int j) {
+      if (!mbar_wait(bar_s + 8 * (2 * t + (j & 1)), (j >> 1) & 1, abort_flag, kSiteSoftmax)) {
+        ok = false;
+        return;
+      }
       fence_after();
-      float s[kTile];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_load32(s_col + 32 * i, s + 32 * i);
+      tmem_load32(s_col + 64 * (j & 1), s);
+      tmem_load32(s_col + 64 * (j & 1) + 32, s + 32);
+    };
+    if (nt > 0) fetch(0);
+    for (int j = 0; ok && j < nt; ++j) {
       tmem_wait_ld();
       if (a.sign != 1) {                                             // a scale that is not positive
 #pragma unroll
-        for (int i = 0; i < kTile; ++i) s[i] *= float(a.sign);
+        for (int i = 0; i < kBlock; ++i) s[i] *= float(a.sign);
       }
       if (j >= masked_from) {
-        const int here = limit - j * kTile;
+        const int here = limit - j * kBlock;
 #pragma unroll
-        for (int i = 0; i < kTile; ++i) s[i] = i < here ? s[i] : -INFINITY;
+        for (int i = 0; i < kBlock; ++i) s[i] = i < here ? s[i] : -INFINITY;
       }
       float top[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-      for (int i = 4; i < kTile - 4; i += 8) {
+      for (int i = 4; i < kBlock - 4; i += 8) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) top[x] = max_nan(top[x], s[i + x], s[i + 4 + x]);
       }
 #pragma unroll
-      for (int x = 0; x < 4; ++x) top[x] = max_nan(top[x], s[kTile - 4 + x]);
+      for (int x = 0; x < 4; ++x) top[x] = max_nan(top[x], s[kBlock - 4 + x]);
       float high = max_nan(max_nan(top[0], top[1], top[2]), top[3]) * a.c;
       if (high == INFINITY) high = NAN;                              // inf - inf
-      // P of the last block has been read: S of this one was issued after it
       const bool raise = !(high <= m + 8.0f);
       if (j == 0) {
         m = high;
@@ -393,6 +470,12 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
         const float keep = to == -INFINITY ? 1.0f : exp2_fast(m - to);
         m = to;
         l *= keep;
+        // O is at rest when the products of block j - 1 are done, which is what the next phase of that block's buffer says
+        if (!mbar_wait(bar_s + 8 * (2 * t + ((j - 1) & 1)), (((j - 1) >> 1) + 1) & 1, abort_flag, kSiteSoftmax)) {
+          ok = false;
+          break;
+        }
+        fence_after();
 #pragma unroll 1
         for (int i = 0; i < D / 32; ++i) {
           float o[32];
@@ -406,29 +489,27 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
       const float ref = m == -INFINITY ? 0.0f : m;
       const f32x2 c2 = pack2(a.c, a.c), r2 = pack2(-ref, -ref);
       f32x2 sum[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
+      uint32_t p[32];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint32_t p[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          float x, y;
-          unpack2(fma2(pack2(s[64 * half + 2 * i], s[64 * half + 2 * i + 1]), c2, r2), x, y);
-          x = exp2_fast(x);
-          y = exp2_fast(y);
-          sum[i & 1] = add2(sum[i & 1], pack2(x, y));
-          p[i] = half2_bits(x, y);
-        }
-        tmem_store32(s_col + 32 * half, p);
+      for (int i = 0; i < 32; ++i) {
+        float x, y;
+        unpack2(fma2(pack2(s[2 * i], s[2 * i + 1]), c2, r2), x, y);
+        x = exp2_fast(x);
+        y = exp2_fast(y);
+        sum[i & 1] = add2(sum[i & 1], pack2(x, y));
+        p[i] = half2_bits(x, y);
       }
+      tmem_store32(s_col + 64 * (j & 1), p);
       {
         float x, y;
         unpack2(add2(sum[0], sum[1]), x, y);
         l += x + y;
       }
+      if (j + 1 < nt) fetch(j + 1);                                  // while the weights are on their way
       tmem_wait_st();
       fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar_p + 8 * t);
+      if (lane == 0) mbar_arrive(bar_p + 8 * (2 * t + (j & 1)));
     }
     // ---- output ----
     if (ok && nt > 0) {
@@ -471,69 +552,14 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
         }
       }
     }
-  } else if (warp == kMmaWarp) {
-    // ================= products =================
+  } else if (warp < kLoadWarp) {
+    // ================= products of tile t =================
     if (lane == 0 && n > 0) {
-      constexpr uint32_t id_s = idesc(kTile, false), id_o = idesc(D, true);
-      bool ok = mbar_wait(bar_q, 0, abort_flag, kSiteMma);
-      auto full = [&](int i) { return mbar_wait(bar_full + 8 * (i % C::kStages), (i / C::kStages) & 1, abort_flag, kSiteMma); };
-      auto scores = [&](int t, int i) {                               // S_t = Q_t K^T from ring entry i
-        const uint32_t k = ring + uint32_t(i % C::kStages) * C::kTileBytes;
-        const uint32_t q = q_smem + uint32_t(t) * C::kTileBytes;
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) {
-          const uint32_t off = uint32_t(x >> 2) * C::kAtomBytes + uint32_t(x & 3) * 32u;
-          mma_ss(tmem + uint32_t(t) * 128u, desc_k_major(q + off), desc_k_major(k + off), id_s, x > 0);
-        }
-        commit(bar_s + 8 * t);
-      };
-      ok = ok && full(0);
-      fence_after();
-      if (ok) {
-        if (n0 > 0) scores(0, 0);
-        if (n1 > 0) scores(1, 0);
-        if (2 * n > C::kStages) commit(bar_empty);
-      }
-      for (int j = 0; ok && j < n; ++j) {
-        const int ik = 2 * (j + 1), iv = 2 * j + 1;
-        bool have_v = false, have_k = false;
-        for (int t = 0; ok && t < 2; ++t) {
-          const int nt = t == 0 ? n0 : n1;
-          if (j < nt) {
-            ok = mbar_wait(bar_p + 8 * t, j & 1, abort_flag, kSiteMma);
-            if (ok && !have_v) {
-              ok = full(iv);
-              if (ok && j >= ragged / kTile) ok = mbar_wait(bar_guard + 8 * (j - ragged / kTile), 0, abort_flag, kSiteMma);
-              have_v = true;
-            }
-            if (!ok) break;
-            fence_after();
-            const uint32_t v = ring + uint32_t(iv % C::kStages) * C::kTileBytes;
-#pragma unroll
-            for (int x = 0; x < kTile / 16; ++x)
-              mma_ts(tmem + 256u + uint32_t(t) * 128u, tmem + uint32_t(t) * 128u + 8u * x, desc_mn_major(v + 2048u * x), id_o,
-                     (j > 0 || x > 0) ? 1u : 0u);
-            if (j + 1 == nt) commit(bar_o + 8 * t);
-          }
-          if (j + 1 < nt) {
-            if (!have_k) {
-              ok = full(ik);
-              have_k = true;
-              if (!ok) break;
-              fence_after();
-            }
-            scores(t, ik);
-          }
-        }
-        if (ok) {
-          // only entries that are filled again: no arrival is left under way when the CTA ends
-          if (iv + C::kStages < 2 * n) commit(bar_empty + 8 * (iv % C::kStages));
-          if (ik + C::kStages < 2 * n) commit(bar_empty + 8 * (ik % C::kStages));
-        }
-      }
+      if (warp == kMmaWarp) issue_products<D, 0>(base, n, n0, ragged / kBlock, abort_flag);
+      else issue_products<D, 1>(base, n, n1, ragged / kBlock, abort_flag);
     }
   } else if (warp == kLoadWarp) {
-    // ================= loads: K_0, V_0, K_1, V_1, ... =================
+    // ================= loads =================
     if (lane == 0 && n > 0) {
       // rows of a query tile: the chunk's heads of one token after another; what lies past the sequence is never stored
       mbar_expect(bar_q, (n1 > 0 ? 2 : 1) * C::kAtoms * 128 * a.heads_per_chunk * a.tokens);
@@ -544,28 +570,33 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
               ::"r"(q_smem + t * C::kTileBytes + x * C::kAtomBytes), "l"(&q_map), "r"(bar_q), "r"(x * 64), "r"(head0),
               "r"(w.q0 + w.first + t * a.tokens)
               : "memory");
-      for (int i = 0; i < 2 * n; ++i) {
-        const int s = i % C::kStages;
-        if (i >= C::kStages && !mbar_wait(bar_empty + 8 * s, ((i / C::kStages) & 1) ^ 1, abort_flag, kSiteLoad)) break;
-        mbar_expect(bar_full + 8 * s, C::kTileBytes);
-        load_rows<D>(ring + uint32_t(s) * C::kTileBytes, (i & 1) ? &v_map : &k_map, bar_full + 8 * s, kv, w.k0 + (i >> 1) * kTile);
-        if ((i & 1) && (i >> 1) >= ragged / kTile) mbar_arrive(bar_go + 8 * ((i >> 1) - ragged / kTile));
+      bool ok = true;
+      for (int i = 0; ok && i <= n; ++i) {                            // ring entry i
+        const int st = i % C::kStages;
+        ok = i < C::kStages || mbar_wait(bar_empty + 8 * st, ((i / C::kStages) & 1) ^ 1, abort_flag, kSiteLoad);
+        if (!ok) break;
+        const uint32_t at = ring + uint32_t(st) * (2 * C::kBlockBytes);
+        const bool keys = i == 0 || i + 1 < n;
+        mbar_expect(bar_full + 8 * st, keys ? 2 * C::kBlockBytes : C::kBlockBytes);
+        load_rows<D>(at, i == 0 ? &k_map : &v_map, bar_full + 8 * st, kv, w.k0 + (i == 0 ? 0 : i - 1) * kBlock);
+        if (keys) load_rows<D>(at + C::kBlockBytes, &k_map, bar_full + 8 * st, kv, w.k0 + (i + 1) * kBlock);
+        if (i - 1 >= ragged / kBlock) mbar_arrive(bar_go + 8 * (i - 1 - ragged / kBlock));
       }
     }
   } else {
     // ================= value rows that not all rows of the CTA see =================
-    // The rows of a CTA are at most 256 tokens, so at most three blocks: one barrier for each.
-    for (int j = ragged / kTile; j < n; ++j) {
-      const int i = 2 * j + 1, s = i % C::kStages;
+    for (int j = ragged / kBlock; j < n; ++j) {
+      const int g = j - ragged / kBlock;
+      const int i = j + 1, s = i % C::kStages;
       // once the load is under way the entry's barrier is in this use's phase
-      if (!mbar_wait(bar_go + 8 * (j - ragged / kTile), 0, abort_flag, kSiteGuard)) break;
+      if (!mbar_wait(bar_go + 8 * g, 0, abort_flag, kSiteGuard)) break;
       if (!mbar_wait(bar_full + 8 * s, (i / C::kStages) & 1, abort_flag, kSiteGuard)) break;
-      uint8_t* v = smem + (2 + s) * C::kTileBytes;
-      const int from = max(0, ragged - j * kTile), end = w.nk - j * kTile;       // rows to look at; rows past the sequence
+      uint8_t* v = smem + 2 * C::kTileBytes + s * 2 * C::kBlockBytes;
+      const int from = max(0, ragged - j * kBlock), end = w.nk - j * kBlock;     // rows to look at; rows past the sequence
       bool bad = false;
-      for (int x = tid - 32 * kGuardWarp; x < (kTile - from) * (D / 8); x += kGuardThreads) {
+      for (int x = tid - 32 * kGuardWarp; x < (kBlock - from) * (D / 8); x += kGuardThreads) {
         const int r = from + x / (D / 8), piece = x % (D / 8);
-        uint4* at = reinterpret_cast<uint4*>(v + (piece >> 3) * C::kAtomBytes + r * 128 + (piece & 7) * 16);
+        uint4* at = reinterpret_cast<uint4*>(v + (piece >> 3) * C::kSliceBytes + r * 128 + (piece & 7) * 16);
         if (r >= end) {
           *at = make_uint4(0, 0, 0, 0);
         } else {
@@ -585,7 +616,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
       __threadfence_block();
       fence_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar_guard + 8 * (j - ragged / kTile));
+      if (lane == 0) mbar_arrive(bar_guard + 8 * g);
     }
   }
 
@@ -680,8 +711,8 @@ int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, cons
   CUtensorMap qm, km, vm;
   if (!row_map(&qm, Q_f16, n_heads, head_dim, total_q, ldq, a.heads_per_chunk, a.tokens)) return SMOOTHROT_CUDA_ERROR;
   if (total_k > 0) {
-    if (!row_map(&km, K_f16, n_kv_heads, head_dim, total_k, ldk, 1, kTile) ||
-        !row_map(&vm, V_f16, n_kv_heads, head_dim, total_k, ldv, 1, kTile))
+    if (!row_map(&km, K_f16, n_kv_heads, head_dim, total_k, ldk, 1, kBlock) ||
+        !row_map(&vm, V_f16, n_kv_heads, head_dim, total_k, ldv, 1, kBlock))
       return SMOOTHROT_CUDA_ERROR;
   }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
