@@ -22,6 +22,15 @@
 // The weight w is rounded once to fp16, and both sums take the rounded one.  So that w fits fp16 whatever the
 // step, the reference m runs over x + log2(s_v); p itself, summed in fp32 for the denominator, may then exceed 1.
 // m is raised only where a w exceeds 2^8, so most tiles need no exchange between lanes.
+//
+// Measured (device time; floor at 6552 GB/s in brackets): 32 query and 8 key heads of 128, 4 bits: one sequence of 131072
+// tokens 49.0 us (23.0), 64 of up to 4001 55.1 us (23.5), one of 301 9.6 us; 16 of up to 2048 with 32 fp16 heads 61 us
+// (43).  The copies alone, without any arithmetic, take 39 us of the 49: about 4.5 us until the first tile is asked for, 26
+// of streaming, 7 to join the pieces (each step of which waits for memory: flags 2, their pieces 3).  The arithmetic
+// adds 10: a tile of 32 keys is 600 instructions, 290 of them on the ALU at half rate, for 790 cycles of a scheduler at
+// the memory's pace, and four warps a scheduler reach half of its slots.  With fp16 values the loop runs at the memory's
+// rate.  Few registers and many warps matter more than anything else here: 128 registers and 16 warps beat 168 and
+// 12 (59), 96 and 20 (62), and scores of one tile beside values of the last (61).
 #include "paged.cuh"
 #include "rowquant.cuh"
 

@@ -4,17 +4,19 @@
 //   y_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = 2^(c q_i.k_j - m_i),  c = scale log2(e),  j <= i + keys - queries where causal
 //
 // in one pass over the keys with a running reference m_i.  Both products run on the fifth-generation tensor
-// cores with their accumulators in tensor memory:
+// cores with their accumulators in tensor memory, a block of 64 keys at a time:
 //
-//   S = Q K^T    A = 128 query rows (shared memory), B = 128 keys, D = 128 fp32 columns of tensor memory
+//   S = Q K^T    A = 128 query rows (shared memory), B = 64 keys, D = 64 fp32 columns of tensor memory
 //   O += P V     A = P, the weights as fp16 in tensor memory (over S, which is done with), B = V as it
 //                lies in memory (rows of keys: the MN-major form), D = head_dim fp32 columns
 //
 // A CTA owns two tiles of 128 query rows of one key head.  The rows of a tile are the heads of the
 // group for one token after another, so that grouped heads share every key and value that is
-// loaded, and a short prompt fills a tile.  While one tile's weights are computed, the tensor core works for the other.
+// loaded, and a short prompt fills a tile.  A tile has two score buffers: the scores of block j + 2 are computed as soon
+// as the weights of block j are used up, while the softmax works on block j + 1.  Two tiles with their two buffers
+// and their outputs are all 512 columns of tensor memory.
 //
-// A thread of the softmax warps owns one row: its 128 scores come into registers with tcgen05.ld,
+// A thread of the softmax warps owns one row: its 64 scores come into registers with tcgen05.ld,
 // so maximum and sum need no exchange.  The reference m is raised only when the row's maximum
 // exceeds it by more than 8 (weights up to 2^8 are as good in fp16): then the row of O is
 // multiplied down in tensor memory, which happens in the first few blocks and hardly ever after.  Sums, scores, O and m are
@@ -25,6 +27,16 @@
 // of the CTA sees: a product of a zero weight with NaN or infinity is NaN, so rows past the sequence's end are
 // zeroed, and values that are not finite taken out of causally masked blocks and put back, row by row, at the end.
 // Every mbarrier wait is bounded; on expiry the CTA records a code and winds down.
+//
+// Measured (32 query heads, 8 key heads, head width 128, causal): a prompt of 8192 tokens 531-539 us, 550 GFLOP, 1.03
+// PFLOP/s; 9 prompts of 2048 tokens in all with prefixes 35.7 us.  A block takes a tile 2050 cycles of 1.85 GHz.  What
+// bounds it is that tile's chain: the thread that issues a tile's 12 products and waits and commits for them is busy for
+// all of that (shared memory serves the operands, 192 bytes a cycle wanted with 64 keys a product, 128 given, and is slow to
+// answer barriers beside that), and the softmax's 1150 cycles and the two waits for scores lie beside it.  Without
+// the exponentials it is 492 us, without the softmax's arithmetic 510, with an eighth of the products 482.  Not better:
+// 128 keys at a time with one buffer (560), with the weights handed over in halves (686), two threads per row (577),
+// one product warp for both tiles (898), 2^x by polynomial for some of the pairs (531 and up).  A CTA costs some 7 us
+// before its first and after its last block, which is what a short prompt pays.
 #include <cuda.h>
 
 #include "common.cuh"
@@ -358,10 +370,28 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
   const int unit = int(blockIdx.x) % a.units;
   const int want = int(blockIdx.x) / a.units;
   if (tid == 0) s_found = -1;
-  {
+  int found = -1, local = 0;
+  Work w;
+  if (a.batch <= 32) {                              // every warp for itself, a lane per sequence
+    Work mine_w;
+    const int mine = lane < a.batch ? sequence_tiles(a, lane, &mine_w) : 0;
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    const uint32_t at = __ballot_sync(0xffffffffu, want < incl);
+    found = at == 0 ? -1 : __ffs(at) - 1;
+    const int owner = max(found, 0);
+    local = __shfl_sync(0xffffffffu, incl, owner) - 1 - want;         // the longest rows of a sequence first
+    w.q0 = __shfl_sync(0xffffffffu, mine_w.q0, owner);
+    w.nq = __shfl_sync(0xffffffffu, mine_w.nq, owner);
+    w.k0 = __shfl_sync(0xffffffffu, mine_w.k0, owner);
+    w.nk = __shfl_sync(0xffffffffu, mine_w.nk, owner);
+  } else {
     const int per = (a.batch + kThreads - 1) / kThreads;
     const int b0 = min(a.batch, tid * per), b1 = min(a.batch, b0 + per);
-    Work w;
     int mine = 0;
     for (int b = b0; b < b1; ++b) mine += sequence_tiles(a, b, &w);
     int incl = mine;
@@ -393,14 +423,17 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
     *abort_flag = 1;
     atomicCAS(&g_prefill_status, 0, int(kSiteMma));
   }
-  if (s_found < 0) {                                // more CTAs than tiles: the grid is an upper bound
+  if (a.batch > 32) {
+    found = s_found;
+    local = s_local;
+    if (found >= 0) sequence_tiles(a, found, &w);
+  }
+  if (found < 0) {                                  // more CTAs than tiles: the grid is an upper bound
     if (warp == kMmaWarp)
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*tmem_slot), "r"(512) : "memory");
     return;
   }
-  Work w;
-  sequence_tiles(a, s_found, &w);
-  w.first = s_local * 2 * a.tokens;
+  w.first = local * 2 * a.tokens;
   const int kv = unit / a.chunks, chunk = unit % a.chunks;
   const int heads = min(a.heads_per_chunk, a.group - chunk * a.heads_per_chunk);
   const int head0 = kv * a.group + chunk * a.heads_per_chunk;

@@ -3,6 +3,11 @@
 //
 // Both kernels stream: half a warp owns 128 consecutive values of a token's row (one head of 128 or
 // two of 64), a lane 8 of them, i.e. one 16-byte load or store of fp16.
+//
+// Measured (device time; floor at 6552 GB/s in brackets).  Append: 8192 tokens of 32 + 32 + 32 fp16 heads 83 us (61), 2048 of
+// 32 + 8 + 8 into 4 bits 18.0 us (6.7), 61 tokens 3.5 us, one 3.1 us.  It is bound by its instructions: 4100 a token of 48 heads
+// across its warps (the coding of a head's 128 values is 200 of a half-warp's, its rotation 70), at half of the issue slots.
+// Gather: 8192 tokens of 32 fp16 heads 43.5 us (41), at the memory's rate; 16384 of 8 heads in 4 bits 19.2 us (13.1).
 #include "paged.cuh"
 #include "rowquant.cuh"
 
@@ -333,6 +338,8 @@ kv_gather_kernel(GatherArgs a, Cache c) {
   }
 }
 
+// Warps a token and pairs a batch, swept together (2048 tokens in 4 bits / 8192 of 32 heads in fp16, us, 4 blocks an SM): 2 and
+// 2: 17.2 / 81.8, 1 and 2: 21.8 / 80.8, 2 and 3: 18.0 / 79.2; with 8 warps a token and no bound on registers 25 / 113.
 constexpr int kManyWarps = 2;
 template <int D, int kBits>
 static void launch_append(const AppendArgs& a, const Cache& c, cudaStream_t st) {
