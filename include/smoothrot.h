@@ -270,11 +270,13 @@ int smoothrot_kv_dequant(const uint8_t* q, const float* step, const float* zero,
  * token's row of n_kv_heads * head_dim values (groups = n_kv_heads * head_dim / 128; with heads of
  * 64 two heads share a group, so n_kv_heads must be even).  A value is (code - zero) * step.  k_params and v_params are
  * ignored with `bits` 16.  All 16-byte aligned.  page_size is a power of two up to 1024, head_dim is
- * 64 or 128 (else SMOOTHROT_UNSUPPORTED_K).  A slot is page * page_size + offset.
+ * 64 or 128 (else SMOOTHROT_UNSUPPORTED_K); n_kv_heads * page_size * head_dim * 2 must stay below 2^31.
+ * A slot is page * page_size + offset; offsets into a cache are 64-bit.
  *
  * Values that only the device sees (slots, positions, pages, lengths) are checked by the kernels: what is out of range is
  * left out as each call says, nothing is read or written outside the buffers, and smoothrot_device_status reports
- * a code from 32 on.
+ * a code: 32 to 35, named at each call, or 36 to 41 when a bounded wait inside an attention kernel has run out (its
+ * output is then incomplete).
  */
 
 /*
@@ -319,7 +321,8 @@ int smoothrot_kv_gather(const int64_t* slots, int64_t T, int64_t n_kv_heads, int
  *     y = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * q.k_j - max)
  * with fp32 scores, statistics and sums; y = 0 for an empty sequence.  Token j of sequence b lies in page
  * block_table[b * max_pages + j / page_size] at offset j % page_size.  Q [B x ldq] and Y [B x ldy] fp16
- * rows of n_heads * head_dim values; n_heads a multiple of n_kv_heads; B <= 8192.
+ * rows of n_heads * head_dim values; n_heads a multiple of n_kv_heads; B <= 8192, max_pages * page_size < 2^31 and
+ * B * (max_pages * page_size / 16 + 2) * n_kv_heads * ceil(n_heads / n_kv_heads / 16) < 2^31.
  * A length outside [0, max_pages * page_size] is clamped and a token on a page outside [0, pages) left out, both
  * with status code 34.  The order of all sums is fixed by the shapes and lengths: a call repeated gives the same bits.
  * `workspace`: smoothrot_attn_decode_workspace_bytes(...) bytes, 16-byte aligned, contents on entry do not matter; calls
@@ -343,6 +346,7 @@ int smoothrot_attn_decode(const void* Q_f16, int64_t ldq, int64_t B, int64_t n_h
  * query that sees no key gives y = 0.  What a query does not see has no part in its output, whatever its values.
  * Q [total_q x ldq], K [total_k x ldk], V [total_k x ldv], Y [total_q x ldy] fp16 rows of heads.
  * Rows that belong to no sequence are not written; a sequence that leaves the buffers is left out, status code 35.
+ * total_q, total_k <= 2^30, B <= 65535.
  */
 int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, const void* K_f16,
                            int64_t ldk, const void* V_f16, int64_t ldv, int64_t total_k,
@@ -433,7 +437,7 @@ int smoothrot_base_matrix(int order, int8_t* out_host);
 /*
  * Host, synchronous.  Kernels never spin without bound: a wait that runs out
  * records a non-zero code in a device-side status word and the kernel
- * returns; the cache and attention calls record a code from 32 on for a slot, position, page or
+ * returns; the cache and attention calls record 32 to 35 for a slot, position, page or
  * length out of range.  This call copies that word for the current device into
  * *status_host (0 = none so far) and clears it when `clear` is non-zero.
  */

@@ -1,7 +1,7 @@
 // Argument marshalling of the cache and attention calls in native code: what binding.py does for the other entry
 // points through ctypes, for the calls that a decode step makes once per layer.  Checking some ten tensors
-// and converting thirty arguments in Python takes longer than the kernels of a small step run (15 us
-// a call measured, 5 here).  Same checks, same exceptions; a call returns the library's status.
+// and converting thirty arguments in Python takes longer than the kernels of a small step run (17 us
+// a call measured, 4.3 here).  Same checks, same exceptions; a call returns the library's status.
 //
 // The module holds no pointer into the library of its own: binding.py hands over the entry points' addresses.
 #include <Python.h>
