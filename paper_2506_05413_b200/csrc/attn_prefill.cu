@@ -28,15 +28,15 @@
 // zeroed, and values that are not finite taken out of causally masked blocks and put back, row by row, at the end.
 // Every mbarrier wait is bounded; on expiry the CTA records a code and winds down.
 //
-// Measured (32 query heads, 8 key heads, head width 128, causal): a prompt of 8192 tokens 531-539 us, 550 GFLOP, 1.03
-// PFLOP/s; 9 prompts of 2048 tokens in all with prefixes 35.7 us.  A block takes a tile 2050 cycles of 1.85 GHz.  What
+// Measured (32 query heads, 8 key heads, head width 128, causal): a prompt of 8192 tokens 519 us, 550 GFLOP, 1.06
+// PFLOP/s; 9 prompts of 2048 tokens in all with prefixes 34.1 us.  A block takes a tile 2050 cycles of 1.85 GHz.  What
 // bounds it is that tile's chain: the thread that issues a tile's 12 products and waits and commits for them is busy for
 // all of that (shared memory serves the operands, 192 bytes a cycle wanted with 64 keys a product, 128 given, and is slow to
-// answer barriers beside that), and the softmax's 1150 cycles and the two waits for scores lie beside it.  Without
-// the exponentials it is 492 us, without the softmax's arithmetic 510, with an eighth of the products 482.  Not better:
-// 128 keys at a time with one buffer (560), with the weights handed over in halves (686), two threads per row (577),
-// one product warp for both tiles (898), 2^x by polynomial for some of the pairs (531 and up).  A CTA costs some 7 us
-// before its first and after its last block, which is what a short prompt pays.
+// answer barriers beside that), and the softmax's 1150 cycles and the two waits for scores lie beside it.  Of an
+// earlier 531 us it was 492 without the exponentials, 510 without the softmax's arithmetic, 482 with an eighth of the
+// products.  Not better: 128 keys at a time with one buffer (560), with the weights handed over in halves (686), two threads per row (577),
+// one product warp for both tiles (898), 2^x by polynomial for some of the pairs (531 and up).  A CTA costs some 6 us
+// before its first and after its last block, which is what a short prompt pays (7 with every thread storing its own row).
 #include <cuda.h>
 
 #include "common.cuh"
@@ -128,6 +128,25 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
       if (now_ns() - t0 > g_prefill_wait_limit_ns) {
         *abort_flag = 1;
         atomicCAS(&g_prefill_status, 0, site);
+        return false;
+      }
+    }
+  }
+}
+// The same for a whole warp, with one answer for all of its lanes: what follows has instructions of the whole warp.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int site) {
+  constexpr uint32_t all = 0xffffffffu;
+  if (__all_sync(all, mbar_try(bar, parity))) return true;
+  const unsigned long long t0 = now_ns();
+  for (uint32_t spin = 1;; ++spin) {
+    if (__all_sync(all, mbar_try(bar, parity))) return true;
+    if ((spin & 63u) == 0u) {
+      const bool late = now_ns() - t0 > g_prefill_wait_limit_ns;
+      if (__any_sync(all, late || *abort_flag != 0)) {
+        if (late) {
+          *abort_flag = 1;
+          atomicCAS(&g_prefill_status, 0, site);
+        }
         return false;
       }
     }
@@ -358,6 +377,11 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
     *not_finite = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (warp == kLoadWarp && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+  }
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -465,7 +489,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
     bool ok = true;
     // The scores of block j into registers.  The copy is on its way when this returns.
     auto fetch = [&](int j) {
-      if (!mbar_wait(bar_s + 8 * (2 * t + (j & 1)), (j >> 1) & 1, abort_flag, kSiteSoftmax)) {
+      if (!mbar_wait_warp(bar_s + 8 * (2 * t + (j & 1)), (j >> 1) & 1, abort_flag, kSiteSoftmax)) {
         ok = false;
         return;
       }
@@ -504,7 +528,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
         m = to;
         l *= keep;
         // O is at rest when the products of block j - 1 are done, which is what the next phase of that block's buffer says
-        if (!mbar_wait(bar_s + 8 * (2 * t + ((j - 1) & 1)), (((j - 1) >> 1) + 1) & 1, abort_flag, kSiteSoftmax)) {
+        if (!mbar_wait_warp(bar_s + 8 * (2 * t + ((j - 1) & 1)), (((j - 1) >> 1) + 1) & 1, abort_flag, kSiteSoftmax)) {
           ok = false;
           break;
         }
@@ -545,14 +569,19 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
       if (lane == 0) mbar_arrive(bar_p + 8 * (2 * t + (j & 1)));
     }
     // ---- output ----
-    if (ok && nt > 0) {
-      ok = mbar_wait(bar_o + 8 * t, 0, abort_flag, kSiteOutput);
+    if (ok && n > 0) {                               // a tile that sees no keys: its queries are still on their way
+      ok = mbar_wait_warp(nt > 0 ? bar_o + 8 * t : bar_q, 0, abort_flag, kSiteOutput);
       fence_after();
     }
     if (ok) {
       const bool put_back = nt > 0 && *not_finite != 0;
       const float inv = limit > 0 ? 1.0f / l : 0.0f;
       __half* out = a.y + int64_t(w.q0 + token) * a.ldy + int64_t(head) * D;
+      // Rows leave through the shared memory of the tile's queries, whose products are done, so that half a warp stores a row
+      // at a time: a lane storing its own row would touch 32 lines an instruction.
+      constexpr int kPieces = D / 8, kRowsAtOnce = 32 / kPieces;     // 16 bytes
+      uint4* rows = reinterpret_cast<uint4*>(smem + t * C::kTileBytes) + (warp & 3) * 32 * kPieces;     // of this warp
+      uint4* own = rows + lane * kPieces;
 #pragma unroll 1
       for (int i = 0; i < D / 32; ++i) {
         float o[32];
@@ -572,17 +601,24 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
             }
           }
         }
-        if (live) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            uint4 h;
-            h.x = half2_bits(o[8 * x], o[8 * x + 1]);
-            h.y = half2_bits(o[8 * x + 2], o[8 * x + 3]);
-            h.z = half2_bits(o[8 * x + 4], o[8 * x + 5]);
-            h.w = half2_bits(o[8 * x + 6], o[8 * x + 7]);
-            reinterpret_cast<uint4*>(out + 32 * i)[x] = h;
-          }
+        for (int x = 0; x < 4; ++x) {
+          uint4 h;
+          h.x = half2_bits(o[8 * x], o[8 * x + 1]);
+          h.y = half2_bits(o[8 * x + 2], o[8 * x + 3]);
+          h.z = half2_bits(o[8 * x + 4], o[8 * x + 5]);
+          h.w = half2_bits(o[8 * x + 6], o[8 * x + 7]);
+          own[(4 * i + x) ^ (lane & 7)] = h;
         }
+      }
+      __syncwarp();
+      const uint64_t to = live ? reinterpret_cast<uint64_t>(out) : 0;
+#pragma unroll 4
+      for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
+        const int r = i * kRowsAtOnce + lane / kPieces, piece = lane % kPieces;
+        uint4* at = reinterpret_cast<uint4*>(__shfl_sync(0xffffffffu, to, r));
+        const uint4 h = rows[r * kPieces + (piece ^ (r & 7))];
+        if (at != nullptr) at[piece] = h;
       }
     }
   } else if (warp < kLoadWarp) {
@@ -622,8 +658,8 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
       const int g = j - ragged / kBlock;
       const int i = j + 1, s = i % C::kStages;
       // once the load is under way the entry's barrier is in this use's phase
-      if (!mbar_wait(bar_go + 8 * g, 0, abort_flag, kSiteGuard)) break;
-      if (!mbar_wait(bar_full + 8 * s, (i / C::kStages) & 1, abort_flag, kSiteGuard)) break;
+      if (!mbar_wait_warp(bar_go + 8 * g, 0, abort_flag, kSiteGuard)) break;
+      if (!mbar_wait_warp(bar_full + 8 * s, (i / C::kStages) & 1, abort_flag, kSiteGuard)) break;
       uint8_t* v = smem + 2 * C::kTileBytes + s * 2 * C::kBlockBytes;
       const int from = max(0, ragged - j * kBlock), end = w.nk - j * kBlock;     // rows to look at; rows past the sequence
       bool bad = false;
@@ -743,6 +779,7 @@ int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, cons
   if (grid > INT32_MAX) return SMOOTHROT_INVALID_ARG;
   CUtensorMap qm, km, vm;
   if (!row_map(&qm, Q_f16, n_heads, head_dim, total_q, ldq, a.heads_per_chunk, a.tokens)) return SMOOTHROT_CUDA_ERROR;
+  km = vm = qm;                                     // the kernel prefetches all three
   if (total_k > 0) {
     if (!row_map(&km, K_f16, n_kv_heads, head_dim, total_k, ldk, 1, kBlock) ||
         !row_map(&vm, V_f16, n_kv_heads, head_dim, total_k, ldv, 1, kBlock))

@@ -330,6 +330,16 @@ def test_prefill_matches_the_plain_form(sr, pu, seqs, H, kv, D, causal):
     assert torch.equal(y, _prefill(sr, pu, q, k, v, cq, ck, D, causal))
 
 
+@pytest.mark.parametrize("H,kv,D,seqs", [(32, 8, 128, [(64, -44), (60, -40), (63, -33), (128, -100)]), (8, 8, 64, [(256, -140), (200, -130)])])
+def test_prefill_a_tile_without_keys_beside_one_with_keys(sr, pu, H, kv, D, seqs):
+    """The first tile of a pair sees no key and answers at once, while its queries are still being loaded."""
+    gen = _gen(27)
+    q, k, v, cq, ck, nq, nk = _packed(pu, gen, seqs, H, kv, D)
+    for _ in range(20):
+        y = _prefill(sr, pu, q, k, v, cq, ck, D, True)
+        _check_prefill(pu, y, q, k, v, nq, nk, D, kv, True, 1 / math.sqrt(D))
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("spread,scale", [(30.0, None), (1.0, 0.0), (1.0, -0.1), (4.0, 1.5)])
 def test_prefill_scores_of_any_size(sr, pu, D, spread, scale):
