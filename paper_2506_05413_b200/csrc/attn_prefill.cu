@@ -268,11 +268,17 @@ struct Work {
   }
 };
 
-__device__ __forceinline__ int sequence_tiles(const Args& a, int b, Work* w) {
-  w->q0 = a.cu_q[b];
-  w->nq = a.cu_q[b + 1] - w->q0;
-  w->k0 = a.cu_k[b];
-  w->nk = a.cu_k[b + 1] - w->k0;
+struct Ends {
+  int q0, q1, k0, k1;
+};
+__device__ __forceinline__ Ends sequence_ends(const Args& a, int b) {
+  return {a.cu_q[b], a.cu_q[b + 1], a.cu_k[b], a.cu_k[b + 1]};
+}
+__device__ __forceinline__ int sequence_tiles(const Args& a, const Ends& e, Work* w) {
+  w->q0 = e.q0;
+  w->nq = e.q1 - e.q0;
+  w->k0 = e.k0;
+  w->nk = e.k1 - e.k0;
   if (w->nq <= 0) return 0;
   if (w->q0 < 0 || w->nq > a.total_q - w->q0 || w->k0 < 0 || w->nk < 0 || w->nk > a.total_k - w->k0) {
     atomicCAS(&g_prefill_status, 0, kRange);
@@ -358,7 +364,10 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kMiscOffset);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 8);
   volatile int* not_finite = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 16);
-  if (tid == 0) {
+  // a sequence per lane where a warp has enough of them: asked for before anything else
+  Ends ends{0, 0, 0, 0};
+  if (a.batch <= 32 && lane < a.batch) ends = sequence_ends(a, lane);
+  if (tid == kThreads - 32) {
     for (int i = 0; i < C::kStages; ++i) {
       mbar_init(bar_full + 8 * i, 1);
       mbar_init(bar_empty + 8 * i, 2);
@@ -398,7 +407,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
   Work w;
   if (a.batch <= 32) {                              // every warp for itself, a lane per sequence
     Work mine_w;
-    const int mine = lane < a.batch ? sequence_tiles(a, lane, &mine_w) : 0;
+    const int mine = sequence_tiles(a, ends, &mine_w);
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -417,7 +426,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
     const int per = (a.batch + kThreads - 1) / kThreads;
     const int b0 = min(a.batch, tid * per), b1 = min(a.batch, b0 + per);
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += sequence_tiles(a, b, &w);
+    for (int b = b0; b < b1; ++b) mine += sequence_tiles(a, sequence_ends(a, b), &w);
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -430,7 +439,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
     int at = incl - mine;
     if (want >= at && want < incl) {
       for (int b = b0; b < b1; ++b) {
-        const int n = sequence_tiles(a, b, &w);
+        const int n = sequence_tiles(a, sequence_ends(a, b), &w);
         if (want < at + n) {
           s_found = b;
           s_local = n - 1 - (want - at);            // the longest rows of a sequence first
@@ -450,7 +459,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
   if (a.batch > 32) {
     found = s_found;
     local = s_local;
-    if (found >= 0) sequence_tiles(a, found, &w);
+    if (found >= 0) sequence_tiles(a, sequence_ends(a, found), &w);
   }
   if (found < 0) {                                  // more CTAs than tiles: the grid is an upper bound
     if (warp == kMmaWarp)
@@ -583,32 +592,33 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
       uint4* rows = reinterpret_cast<uint4*>(smem + t * C::kTileBytes) + (warp & 3) * 32 * kPieces;     // of this warp
       uint4* own = rows + lane * kPieces;
 #pragma unroll 1
-      for (int i = 0; i < D / 32; ++i) {
-        float o[32];
+      for (int i = 0; i < D / 64; ++i) {
+        float o[64];
         if (nt > 0) {
-          tmem_load32(o_col + 32 * i, o);
+          tmem_load32(o_col + 64 * i, o);
+          tmem_load32(o_col + 64 * i + 32, o + 32);
           tmem_wait_ld();
         }
 #pragma unroll
-        for (int x = 0; x < 32; ++x) o[x] = limit > 0 ? o[x] * inv : 0.0f;
+        for (int x = 0; x < 64; ++x) o[x] = limit > 0 ? o[x] * inv : 0.0f;
         if (put_back) {
           for (int key = ragged; key < limit; ++key) {
-            const __half* v = a.v + int64_t(w.k0 + key) * a.ldv + int64_t(kv) * D + 32 * i;
+            const __half* v = a.v + int64_t(w.k0 + key) * a.ldv + int64_t(kv) * D + 64 * i;
 #pragma unroll
-            for (int x = 0; x < 32; ++x) {
+            for (int x = 0; x < 64; ++x) {
               const float f = __half2float(v[x]);
               if (!isfinite(f)) o[x] += f;
             }
           }
         }
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
+        for (int x = 0; x < 8; ++x) {
           uint4 h;
           h.x = half2_bits(o[8 * x], o[8 * x + 1]);
           h.y = half2_bits(o[8 * x + 2], o[8 * x + 3]);
           h.z = half2_bits(o[8 * x + 4], o[8 * x + 5]);
           h.w = half2_bits(o[8 * x + 6], o[8 * x + 7]);
-          own[(4 * i + x) ^ (lane & 7)] = h;
+          own[(8 * i + x) ^ (lane & 7)] = h;
         }
       }
       __syncwarp();
@@ -663,6 +673,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
       uint8_t* v = smem + 2 * C::kTileBytes + s * 2 * C::kBlockBytes;
       const int from = max(0, ragged - j * kBlock), end = w.nk - j * kBlock;     // rows to look at; rows past the sequence
       bool bad = false;
+#pragma unroll 4
       for (int x = tid - 32 * kGuardWarp; x < (kBlock - from) * (D / 8); x += kGuardThreads) {
         const int r = from + x / (D / 8), piece = x % (D / 8);
         uint4* at = reinterpret_cast<uint4*>(v + (piece >> 3) * C::kSliceBytes + r * 128 + (piece & 7) * 16);
