@@ -5,8 +5,8 @@
 // two of 64), a lane 8 of them, i.e. one 16-byte load or store of fp16.
 //
 // Measured (device time; floor at 6552 GB/s in brackets).  Append: 8192 tokens of 32 + 32 + 32 fp16 heads 83 us (61), 2048 of
-// 32 + 8 + 8 into 4 bits 18.0 us (6.7), 61 tokens 3.5 us, one 3.1 us.  It is bound by its instructions: 4100 a token of 48 heads
-// across its warps (the coding of a head's 128 values is 200 of a half-warp's, its rotation 70), at half of the issue slots.
+// 32 + 8 + 8 into 4 bits 18.0 us (6.7), 61 tokens 3.5 us, one 3.1 us.  It is bound by its instructions: 5200 a token of 48 heads
+// across its warps, two heads an instruction, at two thirds of the issue slots (profiled at 2048 tokens).
 // Gather: 8192 tokens of 32 fp16 heads 43.5 us (41), at the memory's rate; 16384 of 8 heads in 4 bits 19.2 us (13.1).
 #include "paged.cuh"
 #include "rowquant.cuh"
