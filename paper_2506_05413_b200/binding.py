@@ -105,7 +105,7 @@ def _ptr(t, dtype=None, name="tensor"):
 
 def _rows(t, dtype, name):
     """A 2-D tensor whose rows are contiguous; returns (ptr, rows, cols, leading dim)."""
-    if t.dim() != 2 or (t.shape[0] > 1 and t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dim() != 2 or (t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be 2-D with unit inner stride")
     ld = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
     return _ptr(t, dtype, name), t.shape[0], t.shape[1], ld

@@ -57,10 +57,10 @@ struct Rows {
   void* p = nullptr;
   int64_t rows = 0, cols = 0, ld = 0;
 };
-// fp16 rows with unit inner stride
+// fp16 rows with unit inner stride, of a single row too: the library takes a row's values as neighbours
 Rows rows_of(PyObject* o, const char* name) {
   const at::Tensor& t = tensor(o, name);
-  if (t.dim() != 2 || (t.size(0) > 1 && t.size(1) > 1 && t.stride(1) != 1))
+  if (t.dim() != 2 || (t.size(0) > 0 && t.size(1) > 1 && t.stride(1) != 1))
     throw BadValue(std::string(name) + " must be 2-D with unit inner stride");
   typed(o, at::kHalf, name);
   Rows r;
