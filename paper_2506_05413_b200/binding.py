@@ -119,6 +119,15 @@ def _vec(t, n, name, dtype=torch.float32):
     return _ptr(t, dtype, name)
 
 
+def _workspace(t):
+    """(pointer, bytes) of a workspace, which has to be contiguous: its elements are counted to tell how much memory it is."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return _ptr(t, None, "workspace"), t.numel() * t.element_size()
+
+
 def _stream():
     return torch.cuda.current_stream().cuda_stream
 
@@ -168,8 +177,7 @@ def fuse_weights_search(W, pre, lowest_ratio, ratio_count, Wq_out, dw_out, best_
     wp, N, K, ld = _rows(W, torch.float16, "W")
     if Wq_out.dtype != torch.uint8 or tuple(Wq_out.shape) != (N, K // 2) or not Wq_out.is_contiguous():
         raise ValueError(f"Wq_out must be a contiguous uint8 [{N}, {K // 2}] tensor")
-    wsp = _ptr(workspace, None, "workspace")
-    wsb = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    wsp, wsb = _workspace(workspace)
     _check(load().smoothrot_fuse_weights_search(
         wp, N, K, ld, _vec(pre, K, "pre"), float(lowest_ratio), int(ratio_count),
         _ptr(Wq_out, torch.uint8, "Wq_out"), _vec(dw_out, N, "dw_out"),
@@ -325,8 +333,7 @@ def linear(Xq, dx, Wq, dw, Y, workspace=None):
     yp, My, Ny, ldy = _rows(Y, torch.float16, "Y")
     if (My, Ny) != (M, N):
         raise ValueError(f"Y must be [{M}, {N}]")
-    wsp = _ptr(workspace, None, "workspace")
-    wsb = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    wsp, wsb = _workspace(workspace)
     _check(load().smoothrot_linear(xp, _vec(dx, M, "dx"), M, wp, _vec(dw, N, "dw"), N, K, yp, ldy,
                                    wsp, wsb, _stream()))
 
@@ -415,8 +422,7 @@ def debug_gemm_i32(Xq, Wq, acc, workspace=None):
         raise ValueError("Xq and Wq disagree on K")
     if acc.dtype != torch.int32 or tuple(acc.shape) != (M, N) or not acc.is_contiguous():
         raise ValueError("acc must be a contiguous int32 [M, N] tensor")
-    wsp = _ptr(workspace, None, "workspace")
-    wsb = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    wsp, wsb = _workspace(workspace)
     _check(load().smoothrot_debug_gemm_i32(xp, M, wp, N, K, _ptr(acc, torch.int32, "acc"), wsp, wsb, _stream()))
 
 

@@ -219,6 +219,7 @@ PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     size_t bytes = 0;
     if (a[9] != Py_None) {
       const at::Tensor& w = tensor(a[9], "workspace");
+      if (!w.is_contiguous()) throw BadValue("workspace must be contiguous");
       ws = address(w);
       bytes = size_t(w.numel()) * w.element_size();
     }
