@@ -196,7 +196,7 @@ constexpr float kNoMaximum = 3e38f;              // -m before the first key: exc
 template <int D, int kBits, int NT>
 struct Piece {                                   // what a warp has of a segment
   float o[D / 16][NT][4];                        // [pairs of values][8 heads][(value 2i, head 2t), (2i, 2t+1), (2i+1, 2t), (2i+1, 2t+1)]
-  f32x2 neg_m[NT], l[NT], z[NT];                 // of heads 2t, 2t + 1: -m; l and z: this lane's share
+  f32x2 neg_m[NT], l[NT], z[NT];                 // of heads 2t, 2t + 1: -m, infinite without a key; l and z: this lane's share
 };
 
 // Streams tiles [first, first + count) of a segment.
@@ -360,7 +360,8 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
   const int key_lo = key_of_row(g), key_hi = key_of_row(g + 8);
   constexpr int kParts = S::kKeys / 16;
   float sc2[kParts][NT][4];
-  uint32_t pt[MG][NT][2], seen = 0;              // the second operand of V^T P^T
+  uint32_t pt[MG][NT][2];                        // the second operand of V^T P^T
+  uint32_t seen = 0, any = 0;                    // keys of this tile, of all tiles
   bool full = false;
   auto arrived = [&](int stage) -> bool {
     if (!bar_wait(bars + 8 * stage, (phases >> stage) & 1)) {
@@ -369,6 +370,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
     }
     phases ^= 1u << stage;
     seen = there[stage];
+    any |= seen;
     full = seen == (S::kKeys == 32 ? 0xFFFFFFFFu : 0xFFFFu);
     if (kBits == 16 && !full) {                  // 0 * NaN is NaN: values of keys that are not there are zeroed
       for (int x = lane; x < S::kKeys * (S::kRowBytes / 16); x += 32)
@@ -663,6 +665,8 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
       }
     }
     pc.l[n] = pack2(l[0], l[1]);
+    // a piece of which every token was left out is told from one whose scores are all -infinity: its m is -infinity
+    if (any == 0) pc.neg_m[n] = pack2(INFINITY, INFINITY);
   }
 }
 
@@ -804,7 +808,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
           for (int e = 0; e < 2; ++e) {
             const int h = 8 * n + 2 * t + e;
             if (h >= rows) continue;
-            const float inv = 1.0f / pl[n][e];
+            const float inv = pm[n][e] == INFINITY ? 0.0f : 1.0f / pl[n][e];      // no token: 0
 #pragma unroll
             for (int x = 0; x < D / 64; ++x) {
               uint4 out;
@@ -897,7 +901,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
         }
         if (starts && ends) {
           __half* y = a.y + int64_t(b) * a.ldy + (int64_t(kv) * a.group + chunk * a.rows + h) * D + lane * 2;
-          const float inv = 1.0f / l;
+          const float inv = __shfl_sync(0xffffffffu, top, 0) == -INFINITY ? 0.0f : 1.0f / l;      // no token: 0
 #pragma unroll
           for (int k = 0; k < D / 64; ++k)
             *reinterpret_cast<__half2*>(y + 64 * k) = __floats2half2_rn(o[2 * k] * inv, o[2 * k + 1] * inv);
@@ -978,7 +982,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        if (lane == 0) s_total[h] = l;
+        if (lane == 0) s_total[h] = m == -INFINITY ? INFINITY : l;            // no token: 0
       }
       __syncthreads();
       for (int x = tid * 2; x < rows * D; x += kDecodeThreads * 2) {
