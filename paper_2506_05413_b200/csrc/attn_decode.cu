@@ -40,6 +40,9 @@ namespace paged {
 __device__ int g_decode_status = 0;
 constexpr unsigned long long kDecodeWaitLimitNs = 2000000000ull;
 __device__ unsigned long long g_decode_wait_limit_ns = kDecodeWaitLimitNs;
+constexpr unsigned long long kAtOnceNs = 1000;   // a limit below this is taken as run out before the first wait (for tests: no copy is
+                                                 // late by itself, and a single try waits longer)
+constexpr unsigned long long kDecodeDrainNs = 1000000ull;
 constexpr int kDecodeWait = 41;
 constexpr uint32_t kGaveUp = 1u << 31;           // in a warp's phases: a wait ran out, nothing more is loaded
 
@@ -63,7 +66,7 @@ struct DecodeArgs {
   float c;                  // scale log2(e)
   unsigned long long* arrived;   // [grid][2]
   float* records;           // [grid][2][rows * D + 2 * rows]
-  unsigned long long tag;   // of this call, not 0
+  unsigned long long tag;   // of this call, even and not 0
 };
 
 template <int D, int kBits, int NT>
@@ -121,12 +124,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
   if (!__all_sync(0xffffffffu, ok)) {
     const unsigned long long t0 = now_ns();
     while (!ok && now_ns() - t0 <= g_decode_wait_limit_ns) ok = bar_try(bar, parity);
-    if (!__all_sync(0xffffffffu, ok)) {
-      atomicCAS(&g_decode_status, 0, int(kDecodeWait));
-      const unsigned long long t1 = now_ns();    // copies under way have time to land
-      while (now_ns() - t1 < 50000ull) __nanosleep(1000);
-      return false;
-    }
+    return __all_sync(0xffffffffu, ok);
   }
   return true;
 }
@@ -364,10 +362,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
   uint32_t seen = 0, any = 0;                    // keys of this tile, of all tiles
   bool full = false;
   auto arrived = [&](int stage) -> bool {
-    if (!bar_wait(bars + 8 * stage, (phases >> stage) & 1)) {
-      phases = kGaveUp;
-      return false;
-    }
+    if (!bar_wait(bars + 8 * stage, (phases >> stage) & 1)) return false;
     phases ^= 1u << stage;
     seen = there[stage];
     any |= seen;
@@ -625,8 +620,9 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
     }
   };
 
-  int stage = 0;
-  for (int i = 0; i < count; ++i) {
+  int stage = 0, i = 0;
+  const int stop = g_decode_wait_limit_ns < kAtOnceNs ? 0 : count;
+  for (; i < stop; ++i) {
     if (!arrived(stage)) break;
 #pragma unroll
     for (int part = 0; part < kParts; ++part) scores(stage, part);
@@ -643,6 +639,16 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
     stage = stage + 1 == S::kStages ? 0 : stage + 1;
   }
   __syncwarp();
+  if (i < count) {                               // a wait ran out: copies under way have time to land
+    if (lane == 0) atomicCAS(&g_decode_status, 0, int(kDecodeWait));
+    for (int left = min(S::kStages, count - i); left > 0; --left) {
+      const unsigned long long t0 = now_ns();
+      while (!bar_try(bars + 8 * stage, (phases >> stage) & 1) && now_ns() - t0 < kDecodeDrainNs) {}
+      stage = stage + 1 == S::kStages ? 0 : stage + 1;
+    }
+    __syncwarp();
+    phases = kGaveUp;
+  }
   // the lanes' shares of the sums; zero points out of the output
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -686,6 +692,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   __shared__ __align__(8) unsigned long long s_bars[kWarps][S::kStages];   // a stage's copies
   __shared__ uint32_t s_there[kWarps][S::kStages];          // and the keys that they bring
   __shared__ float s_total[8 * NT];
+  __shared__ int s_missing;                                 // 1 + k: a CTA has not got its piece of pending segment k
 
   // ---- the line of tiles: the sequences' tile counts, added up by the whole CTA ----
   const int per = (a.batch + kDecodeThreads - 1) / kDecodeThreads;
@@ -765,23 +772,28 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
     end = begin + each + (warp < more ? 1 : 0);
   }
 
-  if (begin < end) {
-    // the segment of tile `begin`: sequence b with start(b) * units <= begin < start(b + 1) * units
+  // the segment of a tile of the line, and the tile's place in it: sequence b with start(b) * units <= tile < start(b + 1) * units
+  auto segment_of = [&](int tile) -> Segment {
     Segment s;
     int lo = 0, hi = kDecodeThreads;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (s_sums[mid] * a.units <= begin) lo = mid; else hi = mid;
+      if (s_sums[mid] * a.units <= tile) lo = mid; else hi = mid;
     }
     int at = s_sums[lo] * a.units;
     s.b = lo * per;
     s.tiles = tiles_of(s.b);
-    while (at + s.tiles * a.units <= begin) {
+    while (at + s.tiles * a.units <= tile) {
       at += s.tiles * a.units;
       s.tiles = tiles_of(++s.b);
     }
-    s.unit = (begin - at) / s.tiles;
-    s.tile = (begin - at) - s.unit * s.tiles;
+    s.unit = (tile - at) / s.tiles;
+    s.tile = (tile - at) - s.unit * s.tiles;
+    return s;
+  };
+
+  if (begin < end) {
+    Segment s = segment_of(begin);
     while (true) {
       s.length = clamped_length(a, c, s.b);
       const int place = s.tile, steps = min(s.tiles - place, end - begin);
@@ -853,14 +865,24 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
       }
     }
   }
-  __syncthreads();
+  const bool gave_up = __syncthreads_or((phases & kGaveUp) != 0) != 0;
 
   // ---- pieces of one segment within the CTA: neighbours in the list of records ----
   auto rec_of = [&](int i) -> float* {
     return (i & 1) ? reinterpret_cast<float*>(smem + (i >> 1) * S::kWarpBytes) : heads_of + (i >> 1) * record;
   };
   int pending[2] = {-1, -1};
-  {
+  if (gave_up) {
+    // Output is missing, and the status says so.  The flags of the pieces that this CTA has, found from the line, go up all the
+    // same, marked: a flag that stays down leaves the others of its segment up, and a replay of this launch, whose tag is
+    // the same, would take them for its own.
+    if (!whole) {
+      const Segment head = segment_of(start_of_cta(blockIdx.x)), tail = segment_of(start_of_cta(blockIdx.x + 1) - 1);
+      const int first = head.b * a.units + head.unit, last = tail.b * a.units + tail.unit;
+      if (head.tile > 1) pending[0] = first;
+      if (tail.tile >= 1 && tail.tile + 1 < tail.tiles && last != pending[0]) pending[1] = last;
+    }
+  } else {
     // lane i of every warp: record i.  A segment's records find each other by its number.
     const int i = lane & 15, seg = lane < 16 ? s_seg[i] : -1;
     const uint32_t same = __match_any_sync(0xffffffffu, lane < 16 && seg >= 0 ? seg : ~lane) ;
@@ -923,14 +945,16 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   // Each CTA raises a flag of its own per piece and then looks at all of the segment's: at least the last to raise sees them
   // all (sequentially consistent fences).  Of those that do, the one that takes the first piece's flag down adds up; it
   // takes the others down too, so that a replay of the same launch starts anew.  A flag is up when it holds this
-  // call's tag, whatever the workspace held before.
+  // call's tag, whatever the workspace held before; the tag's last bit says that the piece is not there (its CTA gave
+  // up), and then the segment's flags are taken down and nothing else.
   if (pending[0] < 0 && pending[1] < 0) return;
   __syncthreads();
   if (tid == 0) {
     __threadfence();                                        // the records, all threads', before the flags
     volatile unsigned long long* flags = reinterpret_cast<volatile unsigned long long*>(a.arrived) + blockIdx.x * 2;
-    if (pending[0] >= 0) flags[0] = a.tag;
-    if (pending[1] >= 0) flags[1] = a.tag;
+    if (pending[0] >= 0) flags[0] = a.tag | (gave_up ? 1 : 0);
+    if (pending[1] >= 0) flags[1] = a.tag | (gave_up ? 1 : 0);
+    s_missing = 0;
     __threadfence();                                        // and the flags before any other is looked at
   }
   float* s_weight = reinterpret_cast<float*>(smem);         // [pieces][rows], over what is done with
@@ -947,11 +971,22 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
     const int c0 = cta_of(from + 1), c1 = cta_of(from + n - 1);
     bool up = true;
     __syncthreads();                                        // this CTA's own flags are up
-    for (int i = c0 + tid; i <= c1; i += kDecodeThreads)
-      up &= reinterpret_cast<volatile unsigned long long*>(a.arrived)[i * 2 + (i == c0 ? 1 : 0)] == a.tag;
+    for (int i = c0 + tid; i <= c1; i += kDecodeThreads) {
+      const unsigned long long flag = reinterpret_cast<volatile unsigned long long*>(a.arrived)[i * 2 + (i == c0 ? 1 : 0)];
+      up &= (flag & ~1ull) == a.tag;
+      if (flag == (a.tag | 1)) s_missing = 1 + k;
+    }
     bool won = __syncthreads_and(up) != 0;
-    if (won) won = __syncthreads_or(tid == 0 && atomicCAS(a.arrived + c0 * 2 + 1, a.tag, 0ull) == a.tag) != 0;
     if (won) {
+      bool taken = false;
+      if (tid == 0) {
+        unsigned long long* flag = a.arrived + c0 * 2 + 1;
+        const unsigned long long held = atomicCAS(flag, a.tag, 0ull);
+        taken = held == a.tag || (held == (a.tag | 1) && atomicCAS(flag, held, 0ull) == held);
+      }
+      won = __syncthreads_or(taken) != 0;
+    }
+    if (won && s_missing != 1 + k) {
       __threadfence();
       auto piece = [&](int i) -> const float* { return a.records + (int64_t(i) * 2 + (i == c0 ? 1 : 0)) * stride; };
       // Everything is asked for at once: the pieces' references and sums, to shared memory, and the first kEarly pieces of this
@@ -1007,8 +1042,9 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
         *reinterpret_cast<__half2*>(y + x) = __floats2half2_rn(o0 * inv, o1 * inv);
       }
       __syncthreads();
-      for (int i = c0 + 1 + tid; i <= c1; i += kDecodeThreads) a.arrived[i * 2] = 0;
     }
+    if (won)
+      for (int i = c0 + 1 + tid; i <= c1; i += kDecodeThreads) a.arrived[i * 2] = 0;
   }
 }
 
@@ -1093,8 +1129,7 @@ int smoothrot_attn_decode(const void* Q_f16, int64_t ldq, int64_t B, int64_t n_h
   a.records = reinterpret_cast<float*>(static_cast<char*>(workspace) + decode_grid() * 16);
   // a number that no other call of this process has, and that stray contents of a workspace hardly hold
   static std::atomic<unsigned long long> calls{0x5A17C0DEull};
-  a.tag = calls.fetch_add(1, std::memory_order_relaxed) * 0x9E3779B97F4A7C15ull;
-  if (a.tag == 0) a.tag = calls.fetch_add(1, std::memory_order_relaxed) * 0x9E3779B97F4A7C15ull;
+  a.tag = (calls.fetch_add(1, std::memory_order_relaxed) * 0x9E3779B97F4A7C15ull) << 1;
   const Cache c = make_cache(n_kv_heads, head_dim, bits, pages, page_size, k_cache, v_cache, k_params, v_params);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = a.rows > 8;
