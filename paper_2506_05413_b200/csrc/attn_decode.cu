@@ -297,6 +297,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
       }
       copy_rows(dst, src, size, bar);
     }
+    __syncwarp();                                // those stores are seen by the other lanes: the barrier waits for copies only
   };
   for (int i = 0; i < S::kStages && i < count; ++i) issue(s.tile + i, page_of(s.tile + i, lane), i);
   int page = S::kStages < count ? page_of(s.tile + S::kStages, lane) : -1;
