@@ -244,7 +244,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
 
   auto issue = [&](int tile, int page, int stage) {
     const uint32_t at = ring_at + stage * S::kStageBytes, bar = bars + 8 * stage;
-    if (one_each && (tile + 1) * S::kKeys <= s.length && __all_sync(0xffffffffu, page >= 0 || lane >= copies)) {
+    if (one_each && s.length - tile * S::kKeys >= S::kKeys && __all_sync(0xffffffffu, page >= 0 || lane >= copies)) {
       if (lane == 0) {
         there[stage] = S::kKeys == 32 ? 0xFFFFFFFFu : 0xFFFFu;
         bar_expect(bar, S::kStageBytes);
@@ -700,8 +700,8 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   // The start of a segment (queries, an empty ring) costs a warp about as much as a tile, and counts as one: tile 0 of
   // the line's tiles of a segment is no work, tile i + 1 the i-th of its keys.
   auto tiles_of = [&](int b) {
-    const int n = (clamped_length(a, c, b) + S::kKeys - 1) / S::kKeys;
-    return n == 0 ? 0 : n + 1;
+    const int n = clamped_length(a, c, b);                  // may be just below 2^31: rounded up without a sum
+    return n == 0 ? 0 : (n - 1) / S::kKeys + 2;
   };
   int mine = 0, most = 0;
   for (int b = min(a.batch, tid * per); b < min(a.batch, tid * per + per); ++b) {
