@@ -21,7 +21,9 @@
 //     x = (q.c - z sum(q)) s_k,   O = sum w c - sum w z,   w = p s_v
 // The weight w is rounded once to fp16, and both sums take the rounded one.  So that w fits fp16 whatever the
 // step, the reference m runs over x + log2(s_v); p itself, summed in fp32 for the denominator, may then exceed 1.
-// m is raised only where a w exceeds 2^8, so most tiles need no exchange between lanes.
+// m is set so that the largest w is 2^7 and raised only where one exceeds 2^15, half of what fp16 holds: most tiles need no
+// exchange between lanes, and a weight keeps its 11 bits down to 2^-21 of the largest and counts down to 2^-31 (small weights
+// of many keys add up).  Steps of one sequence that differ by more than 2^21 cost the smaller ones bits.
 //
 // Measured (device time; floor at 6552 GB/s in brackets): 32 query and 8 key heads of 128, 4 bits: one sequence of 131072
 // tokens 49.0 us (23.0), 64 of up to 4001 55.1 us (23.5), one of 301 9.6 us; 16 of up to 2048 with 32 fp16 heads 61 us
@@ -496,7 +498,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
       }
     };
     weights();
-    if (__any_sync(0xffffffffu, high > 256.0f)) {
+    if (__any_sync(0xffffffffu, high > 32768.0f)) {
       // a new m, from x itself: y has lost its places where m was far off
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -517,7 +519,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
                 x[e] = live ? fmaf(sc2[part][n][2 * r + e], ks[mg][r], kz[mg][r] * qs[e]) : -INFINITY;
-                if (pass == 0) to[e] = fmaxf(to[e], x[e] + lead);
+                if (pass == 0) to[e] = fmaxf(to[e], x[e] + lead - 7.0f);
               }
               if (pass == 1) y[mg][r][n] = pack2(x[0] - to[0], x[1] - to[1]);
             }
