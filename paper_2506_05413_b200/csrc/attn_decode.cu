@@ -23,7 +23,9 @@
 // step, the reference m runs over x + log2(s_v); p itself, summed in fp32 for the denominator, may then exceed 1.
 // m is set so that the largest w is 2^7 and raised only where one exceeds 2^15, half of what fp16 holds: most tiles need no
 // exchange between lanes, and a weight keeps its 11 bits down to 2^-21 of the largest and counts down to 2^-31 (small weights
-// of many keys add up).  Steps of one sequence that differ by more than 2^21 cost the smaller ones bits.
+// of many keys add up).  Steps of one sequence that differ by more than 2^21 cost the smaller ones bits.  A group of equal
+// values has the step 1, so a row of zeros would set the reference for values of any size: its step is taken as 2^-60,
+// which leaves its value what it is.
 //
 // Measured (device time; floor at 6552 GB/s in brackets): 32 query and 8 key heads of 128, 4 bits: one sequence of 131072
 // tokens 49.0 us (23.0), 64 of up to 4001 55.1 us (23.5), one of 301 9.6 us; 16 of up to 2048 with 32 fp16 heads 61 us
@@ -192,6 +194,7 @@ __device__ __forceinline__ int key_of_row(int r) {
 }
 
 constexpr float kNoMaximum = 3e38f;              // -m before the first key: exceeded by any finite score
+constexpr float kStepOfZeros = 8.673617379884035e-19f;     // 2^-60: neither its weight nor the sum of the p overflows
 
 template <int D, int kBits, int NT>
 struct Piece {                                   // what a warp has of a segment
@@ -376,6 +379,23 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
           reinterpret_cast<uint4*>(ring + stage * S::kStageBytes + S::kKeys * S::kRowBytes)[x] = make_uint4(0, 0, 0, 0);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
+    }
+    if (kBits == 4) {                            // rows of zeros among the values: a lane per key
+      uint8_t* const at = ring + stage * S::kStageBytes;
+      float2* const params = reinterpret_cast<float2*>(at + 2 * S::kKeys * S::kRowBytes) + S::kKeys + lane;
+      const float2 vp = *params;
+      const bool flat = vp.x == 1.0f && vp.y == 0.0f;
+      if (__any_sync(0xffffffffu, flat)) {
+        if (flat) {
+          const uint4* row = reinterpret_cast<const uint4*>(at + (S::kKeys + lane) * S::kRowBytes);
+          uint32_t codes = 0;
+#pragma unroll
+          for (int i = 0; i < S::kRowBytes / 16; ++i) codes |= row[i].x | row[i].y | row[i].z | row[i].w;
+          if (codes == 0) params->x = kStepOfZeros;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
     }
     return true;
   };
