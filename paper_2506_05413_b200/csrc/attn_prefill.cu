@@ -17,10 +17,11 @@
 // and their outputs are all 512 columns of tensor memory.
 //
 // A thread of the softmax warps owns one row: its 64 scores come into registers with tcgen05.ld,
-// so maximum and sum need no exchange.  The reference m is raised only when the row's maximum
-// exceeds it by more than 8 (weights up to 2^8 are as good in fp16): then the row of O is
-// multiplied down in tensor memory, which happens in the first few blocks and hardly ever after.  Sums, scores, O and m are
-// fp32; a weight is rounded once to fp16, the type of the values that it multiplies.
+// so maximum and sum need no exchange.  The reference m is set 7 below the row's maximum and raised only when a maximum
+// exceeds it by more than 15: then the row of O is multiplied down in tensor memory, which happens in the first few blocks
+// and hardly ever after.  Sums, scores, O and m are fp32; a weight is rounded once to fp16, the type of the values that it
+// multiplies.  It is at most 2^15 and keeps its 11 bits down to 2^-21 of the row's largest, and counts down to 2^-31: small
+// weights add up over a long prompt.
 //
 // Roles: warps 0-3 and 4-7 the softmax of the two tiles, warps 8 and 9 issue their products, warp 10 the TMA
 // loads (queries, then keys and values through one ring), warp 11 cleans the value rows that not every row
@@ -63,6 +64,7 @@ constexpr int kThreads = 384;
 constexpr int kSoftmaxWarps = 8;   // 4 a tile, a thread per row
 constexpr int kMmaWarp = kSoftmaxWarps, kLoadWarp = kMmaWarp + 2, kGuardWarp = kLoadWarp + 1;      // a product warp per tile
 constexpr int kGuardThreads = 32;
+constexpr float kLead = 7.0f, kHeadroom = 15.0f;   // log2 of a row's largest weight when its reference is set, and at most
 
 template <int D>
 struct Cfg {
@@ -531,11 +533,11 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
       for (int x = 0; x < 4; ++x) top[x] = max_nan(top[x], s[kBlock - 4 + x]);
       float high = max_nan(max_nan(top[0], top[1], top[2]), top[3]) * a.c;
       if (high == INFINITY) high = NAN;                              // inf - inf
-      const bool raise = !(high <= m + 8.0f);
+      const bool raise = !(high <= m + kHeadroom);
       if (j == 0) {
-        m = high;
+        m = high - kLead;
       } else if (__any_sync(0xffffffffu, raise)) {
-        const float to = raise ? high : m;
+        const float to = raise ? high - kLead : m;
         const float keep = to == -INFINITY ? 1.0f : exp2_fast(m - to);
         m = to;
         l *= keep;
