@@ -533,7 +533,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
       for (int x = 0; x < 4; ++x) top[x] = max_nan(top[x], s[kBlock - 4 + x]);
       float high = max_nan(max_nan(top[0], top[1], top[2]), top[3]) * a.c;
       if (high == INFINITY) high = NAN;                              // inf - inf
-      const bool raise = !(high <= m + kHeadroom);
+      const bool raise = limit > 0 && !(high <= m + kHeadroom);     // not for a row that is thrown away, whatever it holds
       if (j == 0) {
         m = high - kLead;
       } else if (__any_sync(0xffffffffu, raise)) {
