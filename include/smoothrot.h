@@ -417,13 +417,17 @@ int smoothrot_debug_gemm_i32(const uint8_t* Xq, int64_t M, const uint8_t* Wq, in
  * anything).
  *   smoothrot_debug_set_wait_limit_ns: host, synchronous.  Sets the limit of every bounded wait
  *     of the library's kernels on the current device, in nanoseconds; 0 restores the default
- *     (two seconds).
+ *     (two seconds).  Below 1000 the attention kernels take their first wait as run out at once: their output
+ *     is then missing, and smoothrot_device_status reports 36 or 41.
  *   smoothrot_debug_wait_expiry: enqueues one warp that waits, through the same bounded wait as
  *     the GEMM kernels, on a barrier nobody arrives on.  When the limit has passed the warp
  *     records code 7 in the status word smoothrot_device_status reads, and the kernel returns.
+ *   smoothrot_debug_attn_wait_expiry: the same through the waits of the attention kernels; `code` is the one to record,
+ *     36 to 40 for smoothrot_attn_prefill's and 41 for smoothrot_attn_decode's.
  */
 int smoothrot_debug_set_wait_limit_ns(uint64_t ns);
 int smoothrot_debug_wait_expiry(void* stream);
+int smoothrot_debug_attn_wait_expiry(int code, void* stream);
 
 /* Host. Writes the library's own order-28 Paley matrix, row-major, entries
  * +1 / -1, into out[784] (a host buffer). */

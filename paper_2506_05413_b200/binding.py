@@ -53,6 +53,7 @@ SIGNATURES = {
     "smoothrot_debug_gemm_i32": (_int, [_vp, _i64, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
     "smoothrot_debug_set_wait_limit_ns": (_int, [ctypes.c_uint64]),
     "smoothrot_debug_wait_expiry": (_int, [_vp]),
+    "smoothrot_debug_attn_wait_expiry": (_int, [_int, _vp]),
     "smoothrot_paley28": (_int, [_vp]),
     "smoothrot_base_matrix": (_int, [_int, _vp]),
     "smoothrot_device_status": (_int, [ctypes.POINTER(_int), _int]),
@@ -449,6 +450,11 @@ def debug_set_wait_limit_ns(ns: int) -> None:
 def debug_wait_expiry() -> None:
     """Enqueues the probe whose bounded wait is certain to run out (it returns normally)."""
     _check(load().smoothrot_debug_wait_expiry(_stream()))
+
+
+def debug_attn_wait_expiry(code: int) -> None:
+    """The same through the attention kernels' waits: `code` 36 to 40 for attn_prefill's, 41 for attn_decode's."""
+    _check(load().smoothrot_debug_attn_wait_expiry(int(code), _stream()))
 
 
 def device_status(clear: bool = True) -> int:

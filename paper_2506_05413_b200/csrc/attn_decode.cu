@@ -38,6 +38,9 @@
 #include "paged.cuh"
 #include "rowquant.cuh"
 
+// defined with the attention over prompts: a probe of its waits
+extern "C" int smoothrot_prefill_wait_expiry(int site, void* stream);
+
 namespace smoothrot {
 namespace paged {
 
@@ -1071,6 +1074,16 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   }
 }
 
+// Test probe: a warp waits, through the kernel's own bounded wait, on a barrier that nobody arrives on.
+__global__ void decode_wait_expiry_kernel() {
+  __shared__ __align__(8) unsigned long long bar_storage;
+  const uint32_t bar = smem_addr(&bar_storage);
+  if (threadIdx.x == 0) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar) : "memory");
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncwarp();
+  if (!bar_wait(bar, 0) && threadIdx.x == 0) atomicCAS(&g_decode_status, 0, int(kDecodeWait));
+}
+
 static void decode_plan(int64_t n_heads, int64_t n_kv, DecodeArgs* a) {
   a->group = int(n_heads / n_kv);
   a->chunks = (a->group + 15) / 16;
@@ -1105,6 +1118,14 @@ int smoothrot_decode_set_wait_limit_ns(uint64_t ns) {
   const unsigned long long v = ns == 0 ? smoothrot::paged::kDecodeWaitLimitNs : static_cast<unsigned long long>(ns);
   return cudaMemcpyToSymbol(smoothrot::paged::g_decode_wait_limit_ns, &v, sizeof(v)) == cudaSuccess ? SMOOTHROT_OK
                                                                                                    : SMOOTHROT_CUDA_ERROR;
+}
+
+int smoothrot_debug_attn_wait_expiry(int code, void* stream) {
+  if (code < 36 || code > smoothrot::paged::kDecodeWait) return SMOOTHROT_INVALID_ARG;
+  if (code < smoothrot::paged::kDecodeWait) return smoothrot_prefill_wait_expiry(code, stream);
+  smoothrot::paged::decode_wait_expiry_kernel<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>();
+  smoothrot::count_launch();
+  return smoothrot::launch_status();
 }
 
 size_t smoothrot_attn_decode_workspace_bytes(int64_t B, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim) {

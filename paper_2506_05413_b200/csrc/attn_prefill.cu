@@ -53,6 +53,7 @@ constexpr int kRange = 35;
 enum Site { kSiteLoad = 36, kSiteMma = 37, kSiteSoftmax = 38, kSiteGuard = 39, kSiteOutput = 40 };
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 constexpr unsigned long long kDrainNs = 50000ull;
+constexpr unsigned long long kAtOnceNs = 1000;   // a limit below this: the loads give up before the first copy (for tests)
 
 __device__ int g_prefill_status = 0;
 __device__ unsigned long long g_prefill_wait_limit_ns = kWaitLimitNs;
@@ -369,6 +370,7 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kMiscOffset);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 8);
   volatile int* not_finite = reinterpret_cast<volatile int*>(smem + C::kMiscOffset + 16);
+  const unsigned long long wait_limit = warp == kLoadWarp ? g_prefill_wait_limit_ns : kWaitLimitNs;
   // a sequence per lane where a warp has enough of them: asked for before anything else
   Ends ends{0, 0, 0, 0};
   if (a.batch <= 32 && lane < a.batch) ends = sequence_ends(a, lane);
@@ -644,7 +646,10 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
     }
   } else if (warp == kLoadWarp) {
     // ================= loads =================
-    if (lane == 0 && n > 0) {
+    if (lane == 0 && n > 0 && wait_limit < kAtOnceNs) {
+      *abort_flag = 1;
+      atomicCAS(&g_prefill_status, 0, int(kSiteLoad));
+    } else if (lane == 0 && n > 0) {
       // rows of a query tile: the chunk's heads of one token after another; what lies past the sequence is never stored
       mbar_expect(bar_q, (n1 > 0 ? 2 : 1) * C::kAtoms * 128 * a.heads_per_chunk * a.tokens);
       for (int t = 0; t < (n1 > 0 ? 2 : 1); ++t)
@@ -718,6 +723,21 @@ attn_prefill_kernel(const Args a, const __grid_constant__ CUtensorMap q_map, con
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
+// Test probe: a warp waits, through the kernel's own bounded waits, on a barrier that nobody arrives on.
+__global__ void wait_expiry_kernel(int site) {
+  __shared__ __align__(8) unsigned long long bar_storage;
+  __shared__ int abort_word;
+  const uint32_t bar = smem_u32(&bar_storage);
+  if (threadIdx.x == 0) {
+    abort_word = 0;
+    mbar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  if (site != kSiteLoad && site != kSiteMma) (void)mbar_wait_warp(bar, 0, &abort_word, site);
+  else if (threadIdx.x == 0) (void)mbar_wait(bar, 0, &abort_word, site);
+}
+
 // fp16 rows of `heads` heads of `dim` values: 64 values of `box_heads` heads of `box_rows` rows are copied at a time.
 static bool row_map(CUtensorMap* map, const void* p, int64_t heads, int64_t dim, int64_t rows, int64_t ld, int box_heads,
                     int box_rows) {
@@ -757,6 +777,12 @@ int smoothrot_prefill_set_wait_limit_ns(uint64_t ns) {
   const unsigned long long v = ns == 0 ? smoothrot::prefill::kWaitLimitNs : static_cast<unsigned long long>(ns);
   return cudaMemcpyToSymbol(smoothrot::prefill::g_prefill_wait_limit_ns, &v, sizeof(v)) == cudaSuccess ? SMOOTHROT_OK
                                                                                                       : SMOOTHROT_CUDA_ERROR;
+}
+
+int smoothrot_prefill_wait_expiry(int site, void* stream) {
+  smoothrot::prefill::wait_expiry_kernel<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>(site);
+  smoothrot::count_launch();
+  return smoothrot::launch_status();
 }
 
 int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, const void* K_f16, int64_t ldk, const void* V_f16,

@@ -67,6 +67,7 @@ def attend(q, k, v, D, kv, scale, seen=None, key_step=None, step=None):
       2 ds A               a score is an fp32 sum of D products with the tensor cores' wider alignment: ds = 2^-20 scale sum |q||k|,
                            with 4-bit keys of |q| times what is multiplied, a code with up to 72 added, times the step
       2^-18 A              exponentials and sums in fp32, over at most some thousand terms a lane
+    Not counted: with 4-bit values the kernel sums codes less 8, so an output near 0 also carries the last fp32 place of some 8 steps.
     """
     m, n = q.shape[0], k.shape[0]
     H = q.shape[1] // D
