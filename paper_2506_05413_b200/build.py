@@ -64,7 +64,11 @@ def build_marshal() -> str:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu file for sm_100a and link the shared library; returns its path."""
+    """Compile every .cu file for sm_100a and link the shared library; returns its path.
+
+    The library needs nvcc alone and is linked whatever becomes of the binding's module, which needs torch's headers and a
+    C++ compiler: where that fails, the error is raised with the library in place for users of its C interface.
+    """
     if not force and is_current():
         return LIB
     nvcc = _nvcc()
@@ -84,10 +88,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
     with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as pool:
         marshal = pool.submit(build_marshal)
         objs = list(pool.map(compile_one, SOURCES))
+        tmp = LIB + f".tmp{os.getpid()}"
+        subprocess.check_call([nvcc, "-shared", "-Wno-deprecated-gpu-targets", "-o", tmp, *objs])
+        os.replace(tmp, LIB)
         marshal.result()
-    tmp = LIB + f".tmp{os.getpid()}"
-    subprocess.check_call([nvcc, "-shared", "-Wno-deprecated-gpu-targets", "-o", tmp, *objs])
-    os.replace(tmp, LIB)
     return LIB
 
 
