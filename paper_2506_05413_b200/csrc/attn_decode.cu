@@ -24,8 +24,8 @@
 // m is set so that the largest w is 2^7 and raised only where one exceeds 2^15, half of what fp16 holds: most tiles need no
 // exchange between lanes, and a weight keeps its 11 bits down to 2^-21 of the largest and counts down to 2^-31 (small weights
 // of many keys add up).  Steps of one sequence that differ by more than 2^21 cost the smaller ones bits.  A group of equal
-// values has the step 1, so a row of zeros would set the reference for values of any size: its step is taken as 2^-60,
-// which leaves its value what it is.
+// values has the step 1, so a row of zeros would set the reference for values of any size: where one asks for a higher
+// reference its step is taken as 2^-60, which leaves its value what it is.
 //
 // Measured (device time; floor at 6552 GB/s in brackets): 32 query and 8 key heads of 128, 4 bits: one sequence of 131072
 // tokens 49.0 us (23.0), 64 of up to 4001 55.1 us (23.5), one of 301 9.6 us; 16 of up to 2048 with 32 fp16 heads 61 us
@@ -47,11 +47,12 @@ namespace paged {
 __device__ int g_decode_status = 0;
 constexpr unsigned long long kDecodeWaitLimitNs = 2000000000ull;
 __device__ unsigned long long g_decode_wait_limit_ns = kDecodeWaitLimitNs;
-constexpr unsigned long long kAtOnceNs = 1000;   // a limit below this is taken as run out before the first wait (for tests: no copy is
+constexpr unsigned long long kAtOnceNs = 1000;   // a limit below this is taken as run out before the first copy (for tests: no copy is
                                                  // late by itself, and a single try waits longer)
 constexpr unsigned long long kDecodeDrainNs = 1000000ull;
 constexpr int kDecodeWait = 41;
 constexpr uint32_t kGaveUp = 1u << 31;           // in a warp's phases: a wait ran out, nothing more is loaded
+constexpr uint32_t kNoKey = 1u << 30;            // every token of this piece so far was left out
 
 constexpr int kWarps = 8;
 constexpr int kDecodeThreads = 32 * kWarps;
@@ -252,7 +253,7 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
 
   auto issue = [&](int tile, int page, int stage) {
     const uint32_t at = ring_at + stage * S::kStageBytes, bar = bars + 8 * stage;
-    if (one_each && s.length - tile * S::kKeys >= S::kKeys && __all_sync(0xffffffffu, page >= 0 || lane >= copies)) {
+    if (one_each && uint32_t(tile + 1) * S::kKeys <= uint32_t(s.length) && __all_sync(0xffffffffu, page >= 0 || lane >= copies)) {
       if (lane == 0) {
         there[stage] = S::kKeys == 32 ? 0xFFFFFFFFu : 0xFFFFu;
         bar_expect(bar, S::kStageBytes);
@@ -367,38 +368,21 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
   const int key_lo = key_of_row(g), key_hi = key_of_row(g + 8);
   constexpr int kParts = S::kKeys / 16;
   float sc2[kParts][NT][4];
-  uint32_t pt[MG][NT][2];                        // the second operand of V^T P^T
-  uint32_t seen = 0, any = 0;                    // keys of this tile, of all tiles
+  uint32_t pt[MG][NT][2], seen = 0;              // the second operand of V^T P^T; keys of this tile
   bool full = false;
   auto arrived = [&](int stage) -> bool {
     if (!bar_wait(bars + 8 * stage, (phases >> stage) & 1)) return false;
-    phases ^= 1u << stage;
     seen = there[stage];
-    any |= seen;
     full = seen == (S::kKeys == 32 ? 0xFFFFFFFFu : 0xFFFFu);
+    const uint32_t none = phases & kNoKey;
+    phases = (phases ^ (1u << stage)) & ~kNoKey;
+    if (!full && seen == 0) phases |= none;
     if (kBits == 16 && !full) {                  // 0 * NaN is NaN: values of keys that are not there are zeroed
       for (int x = lane; x < S::kKeys * (S::kRowBytes / 16); x += 32)
         if (((seen >> (x / (S::kRowBytes / 16))) & 1) == 0)
           reinterpret_cast<uint4*>(ring + stage * S::kStageBytes + S::kKeys * S::kRowBytes)[x] = make_uint4(0, 0, 0, 0);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-    }
-    if (kBits == 4) {                            // rows of zeros among the values: a lane per key
-      uint8_t* const at = ring + stage * S::kStageBytes;
-      float2* const params = reinterpret_cast<float2*>(at + 2 * S::kKeys * S::kRowBytes) + S::kKeys + lane;
-      const float2 vp = *params;
-      const bool flat = vp.x == 1.0f && vp.y == 0.0f;
-      if (__any_sync(0xffffffffu, flat)) {
-        if (flat) {
-          const uint4* row = reinterpret_cast<const uint4*>(at + (S::kKeys + lane) * S::kRowBytes);
-          uint32_t codes = 0;
-#pragma unroll
-          for (int i = 0; i < S::kRowBytes / 16; ++i) codes |= row[i].x | row[i].y | row[i].z | row[i].w;
-          if (codes == 0) params->x = kStepOfZeros;
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-      }
     }
     return true;
   };
@@ -522,6 +506,23 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
     };
     weights();
     if (__any_sync(0xffffffffu, high > 32768.0f)) {
+      if (kBits == 4) {                          // rows of zeros among the values: the four lanes of a key look at a quarter each
+        bool flat[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) flat[r] = sv[0][r] == 1.0f && zv[0][r] == -8.0f;
+        if (__any_sync(0xffffffffu, flat[0] || flat[1])) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const uint8_t* row = ring + stage * S::kStageBytes + (S::kKeys + 16 * part + (r ? key_hi : key_lo)) * S::kRowBytes;
+            uint32_t codes = 0;
+#pragma unroll
+            for (int i = 0; i < S::kRowBytes / 16; ++i) codes |= reinterpret_cast<const uint32_t*>(row)[t * (S::kRowBytes / 16) + i];
+            codes |= __shfl_xor_sync(0xffffffffu, codes, 1);
+            codes |= __shfl_xor_sync(0xffffffffu, codes, 2);
+            if (flat[r] && codes == 0) sv[0][r] = kStepOfZeros;
+          }
+        }
+      }
       // a new m, from x itself: y has lost its places where m was far off
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -646,9 +647,9 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
     }
   };
 
+  phases |= kNoKey;
   int stage = 0, i = 0;
-  const int stop = g_decode_wait_limit_ns < kAtOnceNs ? 0 : count;
-  for (; i < stop; ++i) {
+  for (; i < count; ++i) {
     if (!arrived(stage)) break;
 #pragma unroll
     for (int part = 0; part < kParts; ++part) scores(stage, part);
@@ -697,8 +698,11 @@ __device__ __forceinline__ void stream_tiles(const DecodeArgs& a, const Cache& c
       }
     }
     pc.l[n] = pack2(l[0], l[1]);
-    // a piece of which every token was left out is told from one whose scores are all -infinity: its m is -infinity
-    if (any == 0) pc.neg_m[n] = pack2(INFINITY, INFINITY);
+  }
+  // told from a piece whose scores are all -infinity
+  if ((phases & kNoKey) != 0) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) pc.neg_m[n] = pack2(INFINITY, INFINITY);
   }
 }
 
@@ -714,7 +718,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   float* heads_of = reinterpret_cast<float*>(smem + kWarps * S::kWarpBytes);    // [warp][record]: pieces that began in an earlier warp
   __shared__ int s_sums[kDecodeThreads + 1];
   __shared__ int s_scan[kWarps], s_most[kWarps];
-  __shared__ int s_seg[16], s_flag[16];     // the records' segments; bit 0: its first tile, bit 1: its last
+  __shared__ int s_seg[16], s_flag[16];     // the records' segments; bit 0: its first tile, bit 1: its last, bit 2: the record is not there
   __shared__ __align__(8) unsigned long long s_bars[kWarps][S::kStages];   // a stage's copies
   __shared__ uint32_t s_there[kWarps][S::kStages];          // and the keys that they bring
   __shared__ float s_total[8 * NT];
@@ -725,8 +729,8 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   // The start of a segment (queries, an empty ring) costs a warp about as much as a tile, and counts as one: tile 0 of
   // the line's tiles of a segment is no work, tile i + 1 the i-th of its keys.
   auto tiles_of = [&](int b) {
-    const int n = clamped_length(a, c, b);                  // may be just below 2^31: rounded up without a sum
-    return n == 0 ? 0 : (n - 1) / S::kKeys + 2;
+    const int n = int((uint32_t(clamped_length(a, c, b)) + S::kKeys - 1) / S::kKeys);      // a length may be just below 2^31
+    return n == 0 ? 0 : n + 1;
   };
   int mine = 0, most = 0;
   for (int b = min(a.batch, tid * per); b < min(a.batch, tid * per + per); ++b) {
@@ -755,7 +759,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   const uint32_t bars = smem_addr(&s_bars[warp][0]);
   if (lane < S::kStages) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * lane) : "memory");
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  uint32_t phases = 0;                                      // bit i: parity of stage i's next use
+  uint32_t phases = g_decode_wait_limit_ns < kAtOnceNs ? kGaveUp : 0;     // bit i: parity of stage i's next use
   __syncthreads();
   for (int i = 0; i < kWarps; ++i) {
     if (i < warp) incl += s_scan[i];
@@ -798,28 +802,24 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
     end = begin + each + (warp < more ? 1 : 0);
   }
 
-  // the segment of a tile of the line, and the tile's place in it: sequence b with start(b) * units <= tile < start(b + 1) * units
-  auto segment_of = [&](int tile) -> Segment {
+  if ((phases & kGaveUp) != 0 && lane == 0) atomicCAS(&g_decode_status, 0, int(kDecodeWait));
+  if (begin < end) {
+    // the segment of tile `begin`: sequence b with start(b) * units <= begin < start(b + 1) * units
     Segment s;
     int lo = 0, hi = kDecodeThreads;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (s_sums[mid] * a.units <= tile) lo = mid; else hi = mid;
+      if (s_sums[mid] * a.units <= begin) lo = mid; else hi = mid;
     }
     int at = s_sums[lo] * a.units;
     s.b = lo * per;
     s.tiles = tiles_of(s.b);
-    while (at + s.tiles * a.units <= tile) {
+    while (at + s.tiles * a.units <= begin) {
       at += s.tiles * a.units;
       s.tiles = tiles_of(++s.b);
     }
-    s.unit = (tile - at) / s.tiles;
-    s.tile = (tile - at) - s.unit * s.tiles;
-    return s;
-  };
-
-  if (begin < end) {
-    Segment s = segment_of(begin);
+    s.unit = (begin - at) / s.tiles;
+    s.tile = (begin - at) - s.unit * s.tiles;
     while (true) {
       s.length = clamped_length(a, c, s.b);
       const int place = s.tile, steps = min(s.tiles - place, end - begin);
@@ -828,7 +828,8 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
       s.tile = place == 0 ? 0 : place - 1;
       if (count > 0) {
       Piece<D, kBits, NT> pc;
-      stream_tiles<D, kBits, NT>(a, c, s, count, ring, bars, s_there[warp], phases, lane, pc);
+      if ((phases & kGaveUp) == 0) stream_tiles<D, kBits, NT>(a, c, s, count, ring, bars, s_there[warp], phases, lane, pc);
+      const bool lost = (phases & kGaveUp) != 0;            // this piece, as all that follow in this warp
       const int g = lane >> 2, t = lane & 3;
       const int kv = s.unit / a.chunks, chunk = s.unit - kv * a.chunks;
       const int rows = min(a.rows, a.group - chunk * a.rows);
@@ -839,6 +840,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
         unpack2(pc.neg_m[n], pm[n][0], pm[n][1]);
       }
       if (first && last) {                                  // the whole segment
+        if (!lost) {
         __half* y = a.y + int64_t(s.b) * a.ldy + (int64_t(kv) * a.group + chunk * a.rows) * D + g * (D / 8);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -858,6 +860,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
             }
           }
         }
+        }
       } else {
         const int slot = 2 * warp + (first ? 1 : 0);
         float* rec = first ? reinterpret_cast<float*>(ring) : heads_of + warp * record;
@@ -866,7 +869,7 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int h = 8 * n + 2 * t + e;
-            if (h >= rows) continue;
+            if (h >= rows || lost) continue;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
               *reinterpret_cast<float2*>(rec + h * D + g * (D / 8) + 2 * i) = make_float2(pc.o[i][n][e], pc.o[i][n][2 + e]);
@@ -878,12 +881,12 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
         }
         if (lane == 0) {
           s_seg[slot] = s.b * a.units + s.unit;
-          s_flag[slot] = (first ? 1 : 0) | (last ? 2 : 0);
+          s_flag[slot] = (first ? 1 : 0) | (last ? 2 : 0) | (lost ? 4 : 0);
         }
       }
       }
       begin += steps;
-      if (begin >= end || (phases & kGaveUp) != 0) break;
+      if (begin >= end) break;
       s.tile = 0;
       if (++s.unit == a.units) {
         s.unit = 0;
@@ -891,35 +894,32 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
       }
     }
   }
-  const bool gave_up = __syncthreads_or((phases & kGaveUp) != 0) != 0;
+  __syncthreads();
 
   // ---- pieces of one segment within the CTA: neighbours in the list of records ----
   auto rec_of = [&](int i) -> float* {
     return (i & 1) ? reinterpret_cast<float*>(smem + (i >> 1) * S::kWarpBytes) : heads_of + (i >> 1) * record;
   };
   int pending[2] = {-1, -1};
-  if (gave_up) {
-    // Output is missing, and the status says so.  The flags of the pieces that this CTA has, found from the line, go up all the
-    // same, marked: a flag that stays down leaves the others of its segment up, and a replay of this launch, whose tag is
-    // the same, would take them for its own.
-    if (!whole) {
-      const Segment head = segment_of(start_of_cta(blockIdx.x)), tail = segment_of(start_of_cta(blockIdx.x + 1) - 1);
-      const int first = head.b * a.units + head.unit, last = tail.b * a.units + tail.unit;
-      if (head.tile > 1) pending[0] = first;
-      if (tail.tile >= 1 && tail.tile + 1 < tail.tiles && last != pending[0]) pending[1] = last;
-    }
-  } else {
+  uint32_t missing = 0;                                     // bit k: pending piece k is not there
+  {
     // lane i of every warp: record i.  A segment's records find each other by its number.
     const int i = lane & 15, seg = lane < 16 ? s_seg[i] : -1;
     const uint32_t same = __match_any_sync(0xffffffffu, lane < 16 && seg >= 0 ? seg : ~lane) ;
     const uint32_t leads = __ballot_sync(0xffffffffu, seg >= 0 && (same & ((1u << lane) - 1u)) == 0);
     const uint32_t firsts = __ballot_sync(0xffffffffu, seg >= 0 && (s_flag[i] & 1)), lasts = __ballot_sync(0xffffffffu, seg >= 0 && (s_flag[i] & 2));
+    const uint32_t losts = __ballot_sync(0xffffffffu, seg >= 0 && (s_flag[i] & 4));
     int task = 0;                                           // (segment, head), a warp each
     for (uint32_t left = leads; left != 0; left &= left - 1) {
       const int lead = __ffs(left) - 1, sg = __shfl_sync(0xffffffffu, seg, lead);
       const uint32_t mask = __shfl_sync(0xffffffffu, same, lead);
       const bool starts = (firsts & mask) != 0, ends = (lasts & mask) != 0;
-      if (!(starts && ends)) pending[starts ? 1 : 0] = sg;
+      const bool lost = (losts & mask) != 0;
+      if (!(starts && ends)) {
+        pending[starts ? 1 : 0] = sg;
+        missing |= lost ? (starts ? 2u : 1u) : 0u;
+      }
+      if (lost) continue;
       const int b = sg / a.units, unit = sg - b * a.units;
       const int kv = unit / a.chunks, chunk = unit - kv * a.chunks;
       const int rows = min(a.rows, a.group - chunk * a.rows);
@@ -971,15 +971,16 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   // Each CTA raises a flag of its own per piece and then looks at all of the segment's: at least the last to raise sees them
   // all (sequentially consistent fences).  Of those that do, the one that takes the first piece's flag down adds up; it
   // takes the others down too, so that a replay of the same launch starts anew.  A flag is up when it holds this
-  // call's tag, whatever the workspace held before; the tag's last bit says that the piece is not there (its CTA gave
-  // up), and then the segment's flags are taken down and nothing else.
+  // call's tag, whatever the workspace held before.  A piece that is not there, a wait for it having run out, raises its flag
+  // all the same, with the tag's last bit: a flag that stays down would leave the others of its segment up, and a replay of
+  // this launch, whose tag is the same, would take them for its own.  Such a segment's flags are taken down and nothing else.
   if (pending[0] < 0 && pending[1] < 0) return;
   __syncthreads();
   if (tid == 0) {
     __threadfence();                                        // the records, all threads', before the flags
     volatile unsigned long long* flags = reinterpret_cast<volatile unsigned long long*>(a.arrived) + blockIdx.x * 2;
-    if (pending[0] >= 0) flags[0] = a.tag | (gave_up ? 1 : 0);
-    if (pending[1] >= 0) flags[1] = a.tag | (gave_up ? 1 : 0);
+    if (pending[0] >= 0) flags[0] = a.tag | (missing & 1);
+    if (pending[1] >= 0) flags[1] = a.tag | (missing >> 1);
     s_missing = 0;
     __threadfence();                                        // and the flags before any other is looked at
   }
