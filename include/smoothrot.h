@@ -324,7 +324,9 @@ int smoothrot_kv_gather(const int64_t* slots, int64_t T, int64_t n_kv_heads, int
  * rows of n_heads * head_dim values; n_heads a multiple of n_kv_heads; B <= 8192, max_pages * page_size < 2^31 and
  * B * (max_pages * page_size / 16 + 2) * n_kv_heads * ceil(n_heads / n_kv_heads / 16) < 2^31.
  * A length outside [0, max_pages * page_size] is clamped and a token on a page outside [0, pages) left out, both
- * with status code 34.  The order of all sums is fixed by the shapes and lengths: a call repeated gives the same bits.
+ * with status code 34; y = 0 where none is left.  Weights are rounded to fp16 before they multiply the values: 11 bits down to
+ * 2^-21 of the largest, counted down to 2^-31; with `bits` 4 of the weight times the value's step, so tokens whose steps
+ * are more than 2^21 below another's lose bits.  The order of all sums is fixed by the shapes and lengths: a call repeated gives the same bits.
  * `workspace`: smoothrot_attn_decode_workspace_bytes(...) bytes, 16-byte aligned, contents on entry do not matter; calls
  * that may overlap on the GPU need one each.
  */
@@ -345,6 +347,7 @@ int smoothrot_attn_decode(const void* Q_f16, int64_t ldq, int64_t B, int64_t n_h
  * sequence's start): the sequences' ends are aligned, a prefix of earlier keys is visible to all, and a
  * query that sees no key gives y = 0.  What a query does not see has no part in its output, whatever its values.
  * Q [total_q x ldq], K [total_k x ldk], V [total_k x ldv], Y [total_q x ldy] fp16 rows of heads.
+ * Weights are rounded to fp16 as above (`bits` 16).
  * Rows that belong to no sequence are not written; a sequence that leaves the buffers is left out, status code 35.
  * total_q, total_k <= 2^30, B <= 65535.
  */

@@ -19,7 +19,7 @@
 // P leaves S's registers for the second product through movmatrix.  4-bit codes become fp16 whole numbers (exact) in
 // registers; step and zero point are applied to the small side:
 //     x = (q.c - z sum(q)) s_k,   O = sum w c - sum w z,   w = p s_v
-// The weight w is rounded once to fp16, and both sums take the rounded one.  So that w fits fp16 whatever the
+// The weight w is rounded once to fp16, and both sums take the rounded one (the denominator sums p before it is rounded).  So that w fits fp16 whatever the
 // step, the reference m runs over x + log2(s_v); p itself, summed in fp32 for the denominator, may then exceed 1.
 // m is set so that the largest w is 2^7 and raised only where one exceeds 2^15, half of what fp16 holds: most tiles need no
 // exchange between lanes, and a weight keeps its 11 bits down to 2^-21 of the largest and counts down to 2^-31 (small weights
@@ -28,10 +28,12 @@
 // reference its step is taken as 2^-60, which leaves its value what it is.
 //
 // Measured (device time; floor at 6552 GB/s in brackets): 32 query and 8 key heads of 128, 4 bits: one sequence of 131072
-// tokens 49.0 us (23.0), 64 of up to 4001 55.1 us (23.5), one of 301 9.6 us; 16 of up to 2048 with 32 fp16 heads 61 us
-// (43).  The copies alone, without any arithmetic, take 39 us of the 49: about 4.5 us until the first tile is asked for, 26
+// tokens 47.9 us (23.0), 64 of up to 4001 55.3 us (23.5), one of 301 9.6 us; 16 of up to 2048 with 32 fp16 heads 61 us
+// (43).  Pages are of 16 tokens in all but the first (64); the 64 sequences take 157 us with pages of 1, 108 with 2, 69 with 4,
+// 60 with 8, 54 with 256 and more: a tile is then several copies, and with fewer than 4 tokens a page more than one a lane.
+// The copies alone, without any arithmetic, take 39 us of the 48: about 4.5 us until the first tile is asked for, 26
 // of streaming, 7 to join the pieces (each step of which waits for memory: flags 2, their pieces 3).  The arithmetic
-// adds 10: a tile of 32 keys is 600 instructions, 290 of them on the ALU at half rate, for 790 cycles of a scheduler at
+// adds 9: a tile of 32 keys is 600 instructions, 290 of them on the ALU at half rate, for 790 cycles of a scheduler at
 // the memory's pace, and four warps a scheduler reach half of its slots.  With fp16 values the loop runs at the memory's
 // rate.  Few registers and many warps matter more than anything else here: 128 registers and 16 warps beat 168 and
 // 12 (59), 96 and 20 (62), and scores of one tile beside values of the last (61).
@@ -770,7 +772,11 @@ attn_decode_kernel(const DecodeArgs a, const Cache c) {
   __syncthreads();
   const int all = s_sums[kDecodeThreads] * a.units;         // tiles in the line: below 2^31 (checked)
   const int segments = a.batch * a.units;
-  // Short sequences: a CTA per segment, so that nothing has to meet in the workspace.  Else equal stretches.
+  // Short sequences: a CTA per segment, so that nothing has to meet in the workspace.  Else equal stretches.  This / the other, us, at
+  // equal lengths, 32 + 8 heads of 128 in 4 bits: 1 sequence of 64 tokens 7.8 / 12.3, 512 10.1 / 13.4, 1024 13.3 / 13.6, 1200
+  // 15.1 / 13.1, 4096 34 / 15; 32 sequences (256 segments, nearly a CTA each anyway) 512 12.8 / 18.3, 1024 17.9 / 23.9, 2048
+  // 28.0 / 32.2, 4096 47.4 / 48.1, which this rule leaves to the other.  fp16, 32 + 32 heads, 1 sequence: 64 6.4 / 11.3, 512 11.5 / 12.1,
+  // 768 13.8 / 13.2.
   const bool whole = segments <= int(gridDim.x) && most <= 4 * kWarps + 1;
   const int ctas = whole ? segments : min(int(gridDim.x), (all + kWarps - 1) / kWarps);
   if (int(blockIdx.x) >= ctas) return;

@@ -29,14 +29,16 @@
 // zeroed, and values that are not finite taken out of causally masked blocks and put back, row by row, at the end.
 // Every mbarrier wait is bounded; on expiry the CTA records a code and winds down.
 //
-// Measured (32 query heads, 8 key heads, head width 128, causal): a prompt of 8192 tokens 519-530 us, 550 GFLOP, 1.04 to
-// 1.06 PFLOP/s; 9 prompts of 2048 tokens in all with prefixes 33.3 us.  A block takes a tile 1900 cycles of 1.85 GHz.  What
-// bounds it is that tile's chain: the thread that issues a tile's 12 products and waits and commits for them is busy for
+// Measured (32 query heads, 8 key heads, head width 128, causal): a prompt of 8192 tokens, 550 GFLOP, 519-530 us in graph replays
+// of milliseconds (1.04 to 1.06 PFLOP/s) and 565 to 609 in repeated calls over tenths of a second, where the power cap
+// lowers the clock (0.90 to 0.97); 9 prompts of 2048 tokens in all with prefixes 31 to 33 us.  A block takes a tile 1900 cycles of
+// 1.85 GHz.  What bounds it is that tile's chain: the thread that issues a tile's 12 products and waits and commits for them is busy for
 // all of that (shared memory serves the operands, 192 bytes a cycle wanted with 64 keys a product, 128 given, and is slow to
 // answer barriers beside that), and the softmax's 1150 cycles and the two waits for scores lie beside it.  Of an
 // earlier 531 us it was 492 without the exponentials, 510 without the softmax's arithmetic, 482 with an eighth of the
-// products.  Not better: 128 keys at a time with one buffer (560), with the weights handed over in halves (686), two threads per row (577),
-// one product warp for both tiles (898), 2^x by polynomial for some of the pairs (531 and up).  Beside
+// products.  Not better: the weights of 128 keys handed over in halves (686), two threads per row (577), one product warp for both
+// tiles (898), 2^x by polynomial for some of the pairs (531 and up).  128 keys at a time with one buffer was 560 with one product
+// warp and a descriptor worked out for every product; with the present issue of products it has not been measured.  Beside
 // its blocks a CTA costs some 6 us, which is what a short prompt pays: 860 ns between two CTAs on an SM, 1900 cycles to set up,
 // 3500 until the first scores, 2000 to 3000 from the last weights to the output, 3600 for the output (7 us in all with every thread storing its own
 // row).  A CTA that takes on the work of CTAs that have not started (clusterlaunchcontrol) and loads ahead saves the first three, but

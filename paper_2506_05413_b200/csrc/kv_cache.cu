@@ -346,7 +346,9 @@ static void launch_append(const AppendArgs& a, const Cache& c, cudaStream_t st) 
   const int64_t sms = device_sm_count();
   const int pairs = (a.q_units + 1) / 2 + (a.kv_units + 1) / 2 * 2;
   if (a.tokens <= sms * 4) {
-    // few tokens: a warp per pair of units
+    // Few tokens: a warp per pair of units.  With Walsh, this form / the other, us: 32 + 8 heads of 128 in 4 bits, 1 token 2.6 / 8.0,
+    // 148 3.8 / 9.4, 592 9.0 / 9.6, 740 11.0 / 12.1, 888 12.6 / 12.0, 1184 15.9 / 12.1; 32 + 32 heads in fp16, 1 token 2.6 / 12.0,
+    // 592 13.7 / 13.6, 888 19.4 / 16.7; 12 + 4 heads of 64 in 4 bits, 592 3.7 / 3.8, 740 5.2 / 4.2.
     const unsigned split = unsigned((pairs + 7) / 8);
     kv_append_kernel<D, kBits, 8><<<dim3(unsigned(a.tokens), split > 65535u ? 65535u : split), kThreads, 0, st>>>(a, c);
   } else {
