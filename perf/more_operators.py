@@ -239,8 +239,6 @@ def prepare(case, seed):
             s["codes"], s["inner_codes"] = _room(m, k, g), _room(m, f, g)
             if g == 16:  # the steps of the inner values are calibrated beforehand
                 s["inner_codes"]["step"].fill_(2.0 ** -6)
-    # scratch of the caller's, used again from call to call
-    s["scratch"] = torch.empty(64 << 20, dtype=torch.uint8, device=DEVICE)
     return s
 
 
@@ -306,19 +304,19 @@ def _own(s):
         return {"h": s["h_out"], "x": s["x"]}
     if s["op"] == "linear":
         x, w = s["x"], s["w"]
-        sr.mx_linear(x["q"], x["s"], w["q"], w["s"], s["out"], group=s["group"], x_step=x["step"], w_step=w["step"], workspace=s["scratch"])
+        sr.mx_linear(x["q"], x["s"], w["q"], w["s"], s["out"], group=s["group"], x_step=x["step"], w_step=w["step"])
         return s["out"]
     a, b = s["gate"], s["up"]
     if s["op"] == "glu":
         x = s["x"]
         sr.mx_glu(x["q"], x["s"], a["q"], a["s"], b["q"], b["s"], group=s["group"], x_step=x["step"], gate_step=a["step"], up_step=b["step"],
-                  h_out=s["out"], workspace=s["scratch"])
+                  h_out=s["out"])
         return s["out"]
     c, h, w = s["codes"], s["inner_codes"], s["down"]
     sr.mx_quant(s["x"], c["q"], c["s"], c["step"], group=s["group"])
     sr.mx_glu(c["q"], c["s"], a["q"], a["s"], b["q"], b["s"], group=s["group"], x_step=c["step"], gate_step=a["step"], up_step=b["step"],
-              q_out=h["q"], scale_out=h["s"], h_step=h["step"], walsh=s["walsh"], workspace=s["scratch"])
-    sr.mx_linear(h["q"], h["s"], w["q"], w["s"], s["out"], group=s["group"], x_step=h["step"], w_step=w["step"], workspace=s["scratch"])
+              q_out=h["q"], scale_out=h["s"], h_step=h["step"], walsh=s["walsh"])
+    sr.mx_linear(h["q"], h["s"], w["q"], w["s"], s["out"], group=s["group"], x_step=h["step"], w_step=w["step"])
     return s["out"]
 
 
