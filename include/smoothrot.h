@@ -358,6 +358,87 @@ int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, cons
                            float scale, void* Y_f16, int64_t ldy, void* stream);
 
 /*
+ * Microscaled 4-bit floating point: the same layers with codes that the tensor cores multiply as they are.  (An addition of
+ * this library; the paper's codes are integers with a step per row.)
+ *
+ * A code is e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign in bit 3, two to a byte along the row, value 2i in bits 0-3.
+ * Conversions round to the nearest, ties to the even code, and saturate at 6.  A value is code * scale (* step):
+ *   group 32: a scale per 32 neighbouring values, a power of two, held as exponent + 127 in a byte (255: NaN);
+ *             steps are not needed
+ *   group 16: a scale per 16 neighbouring values, e4m3, and a step per row, fp32
+ * Codes are [rows x K/2] bytes.  Scales lie in blocks of 512 bytes for 128 rows and 4 neighbouring groups, blocks along
+ * the row first: row r and group g are at
+ *     ((r / 128) * (K / group / 4) + g / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + g % 4
+ * of smoothrot_mx_scale_bytes(rows, K, group) bytes.  Bytes of rows past the last are not written, and their contents do
+ * not matter to the calls that read the rest.  Codes and scales are 16-byte aligned, K is a multiple of 128.
+ */
+
+/* Host. Bytes of the scales of `rows` rows of K values; 0 for a group or K that is not supported. */
+size_t smoothrot_mx_scale_bytes(int64_t rows, int64_t K, int64_t group);
+
+/*
+ * Quantizer, for weights and activations alike.  For every row, in fp32, each product and sum rounded by itself:
+ *     v = X[m][:] * pre                                    pre [K] or NULL: d / s or s * d as in smoothrot_quant_act
+ *     v = v (I (x) H_n) / sqrt(n)                          n = walsh: Walsh rotation of blocks of 32, 64 or 128, 0: none
+ *     group 32: scale = 2^E with the least E such that max|v of the group| <= 7 * 2^E, -127 <= E  (2^0 for a group of zeros)
+ *               code = e2m1(v / scale)
+ *     group 16: step[m] = the least power of two with max|v of the row| <= 2688 * step, at least 2^-100  (1 for zeros)
+ *               scale = e4m3(max|v of the group| / (6 step)),  code = e2m1(v / (scale * step)), 0 where the scale is 0
+ * X rotated in blocks of n needs weights that are rotated in the same blocks.  An infinity or NaN makes its group's
+ * scale (group 32) or its row's step (group 16) NaN, and with it every product that it takes part in.
+ * X [M x ldx] fp16; step_out [M] with group 16, NULL with 32.  K <= 32768.
+ */
+int smoothrot_mx_quant(const void* X_f16, int64_t M, int64_t K, int64_t ldx, int64_t group, const float* pre, int walsh,
+                       uint8_t* q_out, uint8_t* scale_out, float* step_out, void* stream);
+
+/* Codes back to values: Y[m][k] = fp16(code * (scale * step[m])), step NULL: 1.  Y [M x ldy] fp16. */
+int smoothrot_mx_dequant(const uint8_t* q, const uint8_t* scale, const float* step, int64_t M, int64_t K, int64_t group,
+                         void* Y_f16, int64_t ldy, void* stream);
+
+/*
+ * The layer on microscaled codes:
+ *     Y[m][n] = fp16( (sum over groups of x_scale w_scale (sum of x w)) * x_step[m] * w_step[n] )       fp32 sums
+ * Xq, x_scale [M rows], Wq, w_scale [N rows], both of K values in groups of `group`; x_step [M], w_step [N] or NULL (1).
+ * Y [M x ldy] fp16.  Any M >= 0, N a multiple of 8, K <= 2^20.  A call repeated gives the same bits.  No workspace.
+ */
+int smoothrot_mx_linear(const uint8_t* Xq, const uint8_t* x_scale, const float* x_step, int64_t M, const uint8_t* Wq,
+                        const uint8_t* w_scale, const float* w_step, int64_t N, int64_t K, int64_t group, void* Y_f16,
+                        int64_t ldy, void* stream);
+
+/*
+ * Both projections of a gated feed-forward block, its activation and product in one kernel:
+ *     h[m][f] = SiLU(gate) * up,  gate = x . gate_row[f],  up = x . up_row[f]  as in smoothrot_mx_linear, in fp32
+ *     walsh = 32: h rotated in blocks of 32 neighbouring features by H_32 / sqrt(32), for a down projection whose
+ *                 weights went through smoothrot_mx_quant with walsh = 32;  0: none
+ * and either H [M x ldh] = fp16(h), or, with q_out and scale_out in place of H, h in codes for the down projection, as
+ * smoothrot_mx_quant makes them except that with group 16 the steps h_step [M] are the caller's (calibrated: a row's
+ * maximum is not known while its first features leave); where a row's values exceed 2688 steps they saturate.
+ * h_step is NULL with group 32.  F a multiple of 8, of 32 with walsh, of 128 with codes.
+ */
+int smoothrot_mx_glu(const uint8_t* Xq, const uint8_t* x_scale, const float* x_step, int64_t M, const uint8_t* gate_q,
+                     const uint8_t* gate_scale, const float* gate_step, const uint8_t* up_q, const uint8_t* up_scale,
+                     const float* up_step, int64_t F, int64_t K, int64_t group, int walsh, void* H_f16, int64_t ldh,
+                     uint8_t* q_out, uint8_t* scale_out, const float* h_step, void* stream);
+
+/*
+ * The residual stream between two blocks, with the norms after the one and before the other:
+ *     z = Y[m][:],  with post_norm = 1:  z = Y * rstd(Y) * post_w                     post_w [K] or NULL: 1
+ *     H' = fp16( residual_scale * H + block_scale * (gate * z) )                      gate [K] or NULL: 1
+ *     x = fp16( H' * rstd(H') * pre_w )                                               pre_w [K] or NULL: 1
+ *     rstd(r) = 1 / sqrt(mean(r^2) + eps), the mean in more than 32 bits, rstd rounded to fp32;
+ *     products from the left, each and the sum rounded to fp32 by itself
+ * Y NULL: H' = fp16(residual_scale * H), H NULL: H' = fp16(block_scale * (gate * z)).  Written are, of H_out [M x ldho], X_out [M x ldxo]
+ * (fp16) and the codes of x, those that are asked for: `codes` 0 none; 4 what smoothrot_quant_act_plain makes of X_out
+ * with ratio `clip` (step_out: dx_out); 16 or 32 what smoothrot_mx_quant makes of X_out in groups of that size.
+ * H_out may be H or Y and X_out may be H or Y, with the same leading dimension, but not one and the same.
+ * K a multiple of 8, of 128 with codes 16 and 32; K <= 32768.  eps > 0.
+ */
+int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_t ldh, int64_t M, int64_t K, int post_norm,
+                       const float* post_w, const float* gate, float block_scale, float residual_scale,
+                       const float* pre_w, float eps, void* H_out_f16, int64_t ldho, void* X_out_f16, int64_t ldxo,
+                       int codes, float clip, uint8_t* q_out, uint8_t* scale_out, float* step_out, void* stream);
+
+/*
  * The whole online layer for a handful of tokens in one kernel: the online activation path
  * followed by smoothrot_linear (Fig. 2: ["hadamard" ->] "quantize" -> the quantized projection; Eq. 2
  * on Eq. 1's integer codes), for decode steps, where two launches cost more than the work.  Every
@@ -427,10 +508,12 @@ int smoothrot_debug_gemm_i32(const uint8_t* Xq, int64_t M, const uint8_t* Wq, in
  *     records code 7 in the status word smoothrot_device_status reads, and the kernel returns.
  *   smoothrot_debug_attn_wait_expiry: the same through the waits of the attention kernels; `code` is the one to record,
  *     36 to 40 for smoothrot_attn_prefill's and 41 for smoothrot_attn_decode's.
+ *   smoothrot_debug_mx_wait_expiry: the same through the waits of the microscaled products, code 49.
  */
 int smoothrot_debug_set_wait_limit_ns(uint64_t ns);
 int smoothrot_debug_wait_expiry(void* stream);
 int smoothrot_debug_attn_wait_expiry(int code, void* stream);
+int smoothrot_debug_mx_wait_expiry(void* stream);
 
 /* Host. Writes the library's own order-28 Paley matrix, row-major, entries
  * +1 / -1, into out[784] (a host buffer). */
@@ -444,7 +527,7 @@ int smoothrot_base_matrix(int order, int8_t* out_host);
 /*
  * Host, synchronous.  Kernels never spin without bound: a wait that runs out
  * records a non-zero code in a device-side status word and the kernel
- * returns; the cache and attention calls record 32 to 35 for a slot, position, page or
+ * returns (42 to 48 in the microscaled products); the cache and attention calls record 32 to 35 for a slot, position, page or
  * length out of range.  This call copies that word for the current device into
  * *status_host (0 = none so far) and clears it when `clear` is non-zero.
  */

@@ -4,7 +4,7 @@ Argument marshalling only: every function checks the tensors it is handed,
 passes raw device pointers, sizes and the current CUDA stream to the C entry
 point of the same name, and raises on a non-zero status.  No arithmetic of the
 method happens here, and there is no fallback: if the library is missing or a
-tensor is not on a CUDA device the call fails.  The cache and attention calls are marshalled by a native
+tensor is not on a CUDA device the call fails.  The cache, attention, microscaled and norm calls are marshalled by a native
 module (csrc/marshal.cpp) instead of ctypes: a decode step makes them once per layer.
 """
 from __future__ import annotations
@@ -42,6 +42,14 @@ SIGNATURES = {
                                      _vp, _f32, _vp, _i64, _vp, _sz, _vp]),
     "smoothrot_attn_prefill": (_int, [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _i64, _int,
                                       _f32, _vp, _i64, _vp]),
+    "smoothrot_mx_scale_bytes": (_sz, [_i64, _i64, _i64]),
+    "smoothrot_mx_quant": (_int, [_vp, _i64, _i64, _i64, _i64, _vp, _int, _vp, _vp, _vp, _vp]),
+    "smoothrot_mx_dequant": (_int, [_vp, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _vp]),
+    "smoothrot_mx_linear": (_int, [_vp, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _vp]),
+    "smoothrot_mx_glu": (_int, [_vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _int, _vp, _i64, _vp, _vp,
+                                _vp, _vp]),
+    "smoothrot_add_norm": (_int, [_vp, _i64, _vp, _i64, _i64, _i64, _int, _vp, _vp, _f32, _f32, _vp, _f32, _vp, _i64, _vp, _i64,
+                                  _int, _f32, _vp, _vp, _vp, _vp]),
     "smoothrot_linear": (_int, [_vp, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _vp, _sz, _vp]),
     "smoothrot_linear_static_scratch": (_int, [_vp, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _vp]),
     "smoothrot_linear_decode_heads": (_int, [_vp, _i64, _i64, _i64, _i64, _vp, _f32, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp]),
@@ -54,6 +62,7 @@ SIGNATURES = {
     "smoothrot_debug_set_wait_limit_ns": (_int, [ctypes.c_uint64]),
     "smoothrot_debug_wait_expiry": (_int, [_vp]),
     "smoothrot_debug_attn_wait_expiry": (_int, [_int, _vp]),
+    "smoothrot_debug_mx_wait_expiry": (_int, [_vp]),
     "smoothrot_paley28": (_int, [_vp]),
     "smoothrot_base_matrix": (_int, [_int, _vp]),
     "smoothrot_device_status": (_int, [ctypes.POINTER(_int), _int]),
@@ -266,6 +275,8 @@ def _marshal():
         lib = load()
         module.connect(*(ctypes.cast(getattr(lib, "smoothrot_" + name), _vp).value
                          for name in ("kv_append", "kv_gather", "attn_decode", "attn_prefill")))
+        module.connect_mx(*(ctypes.cast(getattr(lib, "smoothrot_" + name), _vp).value
+                            for name in ("mx_quant", "mx_dequant", "mx_linear", "mx_glu", "add_norm", "mx_scale_bytes")))
         _marshal_module = module
     return _marshal_module
 
@@ -306,6 +317,62 @@ def attn_prefill(q, k, v, cu_q, cu_k, Y, *, head_dim=128, causal=True, scale=Non
     """smoothrot_attn_prefill: packed prompts, q [total_q, H * D], k, v [total_k, Hk * D] fp16 (rows may be strided),
     cu_q, cu_k [B + 1] int32 -> Y [total_q, H * D] fp16.  scale: 1 / sqrt(D) if None."""
     status = _marshal().attn_prefill(q, k, v, cu_q, cu_k, Y, head_dim, causal, scale)
+    if status:
+        _check(status)
+
+
+def mx_scale_bytes(rows, K, group=32) -> int:
+    """Bytes of the scales of `rows` rows of K values in groups of 32 or 16 (0: not supported)."""
+    return int(load().smoothrot_mx_scale_bytes(int(rows), int(K), int(group)))
+
+
+def mx_quant(X, q_out, scale_out, step_out=None, *, group=32, pre=None, walsh=0):
+    """smoothrot_mx_quant: X [M, K] fp16 (rows may be strided) -> q_out [M, K/2] u8, scale_out u8 of at least
+    mx_scale_bytes(M, K, group) bytes and, with group 16, step_out [M] f32.  pre [K] f32; walsh 0, 32, 64 or 128."""
+    status = _marshal().mx_quant(X, q_out, scale_out, step_out, group, pre, walsh)
+    if status:
+        _check(status)
+
+
+def mx_dequant(q, scale, step, Y, *, group=32):
+    """smoothrot_mx_dequant: what codes stand for -> Y [M, K] fp16.  step [M] f32 or None."""
+    status = _marshal().mx_dequant(q, scale, step, Y, group)
+    if status:
+        _check(status)
+
+
+def mx_linear(Xq, x_scale, Wq, w_scale, Y, *, group=32, x_step=None, w_step=None):
+    """smoothrot_mx_linear: Y [M, N] fp16 = the product of coded rows Xq [M, K/2] and Wq [N, K/2] (see mx_quant);
+    x_step [M], w_step [N] f32 or None."""
+    status = _marshal().mx_linear(Xq, x_scale, x_step, Wq, w_scale, w_step, Y, group)
+    if status:
+        _check(status)
+
+
+def mx_glu(Xq, x_scale, gate_q, gate_scale, up_q, up_scale, *, group=32, x_step=None, gate_step=None, up_step=None,
+           h_out=None, q_out=None, scale_out=None, h_step=None, walsh=0):
+    """smoothrot_mx_glu: SiLU(x . gate) * (x . up) of coded rows Xq [M, K/2], gate_q and up_q [F, K/2] -> h_out [M, F]
+    fp16, or q_out [M, F/2] and scale_out in codes for the down projection (with group 16 under the given steps
+    h_step [M]); walsh = 32 rotates it in blocks of 32."""
+    status = _marshal().mx_glu(Xq, x_scale, x_step, gate_q, gate_scale, gate_step, up_q, up_scale, up_step, h_out, q_out, scale_out,
+                               h_step, group, walsh)
+    if status:
+        _check(status)
+
+
+_NORM_CODES = {None: 0, "int4": 4, "mx16": 16, "mx32": 32}
+
+
+def add_norm(y, h, pre_weight=None, *, h_out=None, x_out=None, q_out=None, scale_out=None, step_out=None, codes=None,
+             post_norm=None, post_weight=None, gate=None, block_scale=1.0, residual_scale=1.0, eps=1e-5, clip=0.9):
+    """smoothrot_add_norm: the block output y [M, K] fp16 (or None), normalised if post_norm (None: if there is a
+    post_weight), gated and scaled, plus residual_scale times the stream h [M, K] (or None) -> h_out, its norm
+    -> x_out and / or codes "int4" (q_out [M, K/2], step_out [M]), "mx16" (and scale_out) or "mx32" (no step_out)."""
+    if codes not in _NORM_CODES:
+        raise ValueError("codes must be None, 'int4', 'mx16' or 'mx32'")
+    status = _marshal().add_norm(y, h, pre_weight, h_out, x_out, q_out, scale_out, step_out, _NORM_CODES[codes],
+                                 post_weight is not None if post_norm is None else post_norm, post_weight, gate, block_scale,
+                                 residual_scale, eps, clip)
     if status:
         _check(status)
 
@@ -455,6 +522,11 @@ def debug_wait_expiry() -> None:
 def debug_attn_wait_expiry(code: int) -> None:
     """The same through the attention kernels' waits: `code` 36 to 40 for attn_prefill's, 41 for attn_decode's."""
     _check(load().smoothrot_debug_attn_wait_expiry(int(code), _stream()))
+
+
+def debug_mx_wait_expiry() -> None:
+    """The same through the waits of the microscaled products (code 49)."""
+    _check(load().smoothrot_debug_mx_wait_expiry(_stream()))
 
 
 def device_status(clear: bool = True) -> int:

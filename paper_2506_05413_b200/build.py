@@ -20,7 +20,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsmoothrot.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ("rotate_quant.cu", "calibrate.cu", "w4a4_gemm.cu", "clip_search.cu", "kv_quant.cu", "heads_quant.cu", "decode_fused.cu", "plain_quant.cu",
-           "kv_cache.cu", "attn_decode.cu", "attn_prefill.cu")
+           "kv_cache.cu", "attn_decode.cu", "attn_prefill.cu", "mx_quant.cu", "mx_gemm.cu", "add_norm.cu")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
 

@@ -1,4 +1,4 @@
-// Argument marshalling of the cache and attention calls in native code: what binding.py does for the other entry
+// Argument marshalling of the cache, attention, microscaled and norm calls in native code: what binding.py does for the other entry
 // points through ctypes, for the calls that a decode step makes once per layer.  Checking some ten tensors
 // and converting thirty arguments in Python takes longer than the kernels of a small step run (17 us
 // a call measured, 4.3 here).  Same checks, same exceptions; a call returns the library's status.
@@ -34,10 +34,27 @@ typedef int (*DecodeFn)(const void*, int64_t, int64_t, int64_t, int64_t, int64_t
 typedef int (*PrefillFn)(const void*, int64_t, int64_t, const void*, int64_t, const void*, int64_t, int64_t, int64_t, int64_t,
                          int64_t, const int32_t*, const int32_t*, int64_t, int, float, void*, int64_t, void*);
 
+typedef int (*MxQuantFn)(const void*, int64_t, int64_t, int64_t, int64_t, const float*, int, uint8_t*, uint8_t*, float*, void*);
+typedef int (*MxDequantFn)(const uint8_t*, const uint8_t*, const float*, int64_t, int64_t, int64_t, void*, int64_t, void*);
+typedef int (*MxLinearFn)(const uint8_t*, const uint8_t*, const float*, int64_t, const uint8_t*, const uint8_t*, const float*,
+                          int64_t, int64_t, int64_t, void*, int64_t, void*);
+typedef int (*MxGluFn)(const uint8_t*, const uint8_t*, const float*, int64_t, const uint8_t*, const uint8_t*, const float*,
+                       const uint8_t*, const uint8_t*, const float*, int64_t, int64_t, int64_t, int, void*, int64_t, uint8_t*,
+                       uint8_t*, const float*, void*);
+typedef int (*AddNormFn)(const void*, int64_t, const void*, int64_t, int64_t, int64_t, int, const float*, const float*, float,
+                         float, const float*, float, void*, int64_t, void*, int64_t, int, float, uint8_t*, uint8_t*, float*, void*);
+typedef size_t (*MxScaleBytesFn)(int64_t, int64_t, int64_t);
+
 AppendFn g_append = nullptr;
 GatherFn g_gather = nullptr;
 DecodeFn g_decode = nullptr;
 PrefillFn g_prefill = nullptr;
+MxQuantFn g_mx_quant = nullptr;
+MxDequantFn g_mx_dequant = nullptr;
+MxLinearFn g_mx_linear = nullptr;
+MxGluFn g_mx_glu = nullptr;
+AddNormFn g_add_norm = nullptr;
+MxScaleBytesFn g_mx_scale_bytes = nullptr;
 
 const at::Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) throw TypeMismatch(std::string(name) + " must be a CUDA tensor");
@@ -249,7 +266,165 @@ PyObject* attn_prefill(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// The addresses of the library's four entry points.
+// ---- microscaled codes and norms ----
+
+// The work goes to the current device's current stream: its tensors have to be there too.
+void here(const at::Tensor& t, const char* name) {
+  if (t.device().index() != c10::cuda::current_device())
+    throw BadValue(std::string(name) + " is not on the current CUDA device");
+}
+float* step_of(PyObject* o, int64_t n, const char* name) {
+  if (o == Py_None) return nullptr;
+  float* p = static_cast<float*>(vector_of(o, n, at::kFloat, name));
+  here(THPVariable_Unpack(o), name);
+  return p;
+}
+Rows half_rows(PyObject* o, const char* name) {
+  const Rows r = rows_of(o, name);
+  here(THPVariable_Unpack(o), name);
+  return r;
+}
+Rows half_rows(PyObject* o, int64_t rows, int64_t cols, const char* name) {
+  const Rows r = rows_of(o, rows, cols, name);
+  here(THPVariable_Unpack(o), name);
+  return r;
+}
+int64_t whole(PyObject* o, const char* name) {
+  const int64_t x = PyLong_AsLongLong(o);
+  if (x == -1 && PyErr_Occurred()) throw TypeMismatch(std::string(name) + " must be a whole number");
+  return x;
+}
+
+struct Coded {
+  uint8_t *q = nullptr, *scale = nullptr;
+  int64_t rows = 0, K = 0;
+};
+uint8_t* codes_of(PyObject* o, int64_t rows, int64_t bytes, const char* name) {
+  const at::Tensor& t = typed(o, at::kByte, name);
+  here(t, name);
+  if (t.dim() != 2 || !t.is_contiguous()) throw BadValue(std::string(name) + " must be a contiguous 2-D uint8 tensor");
+  if (bytes >= 0 && (t.size(0) != rows || t.size(1) != bytes))
+    throw BadValue(std::string(name) + " must be [" + std::to_string(rows) + ", " + std::to_string(bytes) + "]");
+  return static_cast<uint8_t*>(address(t));
+}
+uint8_t* scales_of(PyObject* o, int64_t rows, int64_t K, int64_t group, const char* name) {
+  const at::Tensor& t = typed(o, at::kByte, name);
+  here(t, name);
+  const int64_t need = int64_t(g_mx_scale_bytes(rows, K, group));
+  if (!t.is_contiguous() || t.numel() < need)
+    throw BadValue(std::string(name) + " must be a contiguous uint8 tensor of at least " + std::to_string(need) + " bytes");
+  return static_cast<uint8_t*>(address(t));
+}
+Coded coded(PyObject* q, PyObject* scale, int64_t group, const char* q_name, const char* scale_name) {
+  Coded c;
+  c.q = codes_of(q, 0, -1, q_name);
+  const at::Tensor& t = THPVariable_Unpack(q);
+  c.rows = t.size(0);
+  c.K = 2 * t.size(1);
+  c.scale = scales_of(scale, c.rows, c.K, group, scale_name);
+  return c;
+}
+
+// X, q_out, scale_out, step_out, group, pre, walsh
+PyObject* mx_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> int {
+    const Rows x = half_rows(a[0], "X");
+    const int64_t group = whole(a[4], "group");
+    uint8_t* q = codes_of(a[1], x.rows, x.cols / 2, "q_out");
+    uint8_t* scale = scales_of(a[2], x.rows, x.cols, group, "scale_out");
+    return g_mx_quant(x.p, x.rows, x.cols, x.ld, group, step_of(a[5], x.cols, "pre"), int(whole(a[6], "walsh")), q, scale,
+                      step_of(a[3], x.rows, "step_out"), stream());
+  });
+}
+
+// q, scale, step, Y, group
+PyObject* mx_dequant(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 5, [&]() -> int {
+    const int64_t group = whole(a[4], "group");
+    const Coded c = coded(a[0], a[1], group, "q", "scale");
+    const Rows y = half_rows(a[3], c.rows, c.K, "Y");
+    return g_mx_dequant(c.q, c.scale, step_of(a[2], c.rows, "step"), c.rows, c.K, group, y.p, y.ld, stream());
+  });
+}
+
+// Xq, x_scale, x_step, Wq, w_scale, w_step, Y, group
+PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> int {
+    const int64_t group = whole(a[7], "group");
+    const Coded x = coded(a[0], a[1], group, "Xq", "x_scale"), w = coded(a[3], a[4], group, "Wq", "w_scale");
+    if (x.K != w.K) throw BadValue("Xq and Wq disagree on K");
+    const Rows y = half_rows(a[6], x.rows, w.rows, "Y");
+    return g_mx_linear(x.q, x.scale, step_of(a[2], x.rows, "x_step"), x.rows, w.q, w.scale, step_of(a[5], w.rows, "w_step"), w.rows,
+                       x.K, group, y.p, y.ld, stream());
+  });
+}
+
+// Xq, x_scale, x_step, gate_q, gate_scale, gate_step, up_q, up_scale, up_step, h_out, q_out, scale_out, h_step, group, walsh
+PyObject* mx_glu(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 15, [&]() -> int {
+    const int64_t group = whole(a[13], "group");
+    const Coded x = coded(a[0], a[1], group, "Xq", "x_scale");
+    const Coded g = coded(a[3], a[4], group, "gate_q", "gate_scale"), u = coded(a[6], a[7], group, "up_q", "up_scale");
+    if (x.K != g.K || x.K != u.K) throw BadValue("Xq, gate_q and up_q disagree on K");
+    if (g.rows != u.rows) throw BadValue("gate_q and up_q must have the same shape");
+    Rows h;
+    uint8_t *q = nullptr, *scale = nullptr;
+    if ((a[9] == Py_None) == (a[10] == Py_None)) throw BadValue("one of h_out and q_out is wanted");
+    if (a[9] != Py_None) {
+      h = half_rows(a[9], x.rows, g.rows, "h_out");
+      if (a[11] != Py_None || a[12] != Py_None) throw BadValue("scale_out and h_step go with q_out");
+    } else {
+      if (a[11] == Py_None) throw BadValue("scale_out is required with q_out");
+      if (g.rows % 128 != 0) throw BadValue("codes need a multiple of 128 features");
+      q = codes_of(a[10], x.rows, g.rows / 2, "q_out");
+      scale = scales_of(a[11], x.rows, g.rows, group, "scale_out");
+    }
+    return g_mx_glu(x.q, x.scale, step_of(a[2], x.rows, "x_step"), x.rows, g.q, g.scale, step_of(a[5], g.rows, "gate_step"), u.q,
+                    u.scale, step_of(a[8], u.rows, "up_step"), g.rows, x.K, group, int(whole(a[14], "walsh")), h.p, h.ld, q, scale,
+                    step_of(a[12], x.rows, "h_step"), stream());
+  });
+}
+
+// y, h, pre_weight, h_out, x_out, q_out, scale_out, step_out, codes, post_norm, post_weight, gate, block_scale,
+// residual_scale, eps, clip
+PyObject* add_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 16, [&]() -> int {
+    if (a[0] == Py_None && a[1] == Py_None) throw BadValue("one of y and h is required");
+    Rows y, h, ho, xo;
+    if (a[0] != Py_None) y = half_rows(a[0], "y");
+    if (a[1] != Py_None) h = a[0] != Py_None ? half_rows(a[1], y.rows, y.cols, "h") : half_rows(a[1], "h");
+    const int64_t rows = a[0] != Py_None ? y.rows : h.rows, K = a[0] != Py_None ? y.cols : h.cols;
+    if (a[3] != Py_None) ho = half_rows(a[3], rows, K, "h_out");
+    if (a[4] != Py_None) xo = half_rows(a[4], rows, K, "x_out");
+    const int64_t codes = whole(a[8], "codes");
+    uint8_t *q = nullptr, *scale = nullptr;
+    float* step = nullptr;
+    if (codes != 0) {
+      if (a[5] == Py_None || (codes >= 16 && a[6] == Py_None)) throw BadValue("codes need q_out, and scale_out where they are microscaled");
+      q = codes_of(a[5], rows, K / 2, "q_out");
+      if (codes >= 16) scale = scales_of(a[6], rows, K, codes, "scale_out");
+      step = step_of(a[7], rows, "step_out");
+    }
+    return g_add_norm(y.p, y.ld, h.p, h.ld, rows, K, truth(a[9]), step_of(a[10], K, "post_weight"), step_of(a[11], K, "gate"),
+                      float(number(a[12])), float(number(a[13])), step_of(a[2], K, "pre_weight"), float(number(a[14])), ho.p,
+                      ho.ld, xo.p, xo.ld, int(codes), float(number(a[15])), q, scale, step, stream());
+  });
+}
+
+// The addresses of the entry points for microscaled codes and norms.
+PyObject* connect_mx(PyObject*, PyObject* args) {
+  unsigned long long quant, dequant, linear, glu, norm, bytes;
+  if (!PyArg_ParseTuple(args, "KKKKKK", &quant, &dequant, &linear, &glu, &norm, &bytes)) return nullptr;
+  g_mx_quant = reinterpret_cast<MxQuantFn>(quant);
+  g_mx_dequant = reinterpret_cast<MxDequantFn>(dequant);
+  g_mx_linear = reinterpret_cast<MxLinearFn>(linear);
+  g_mx_glu = reinterpret_cast<MxGluFn>(glu);
+  g_add_norm = reinterpret_cast<AddNormFn>(norm);
+  g_mx_scale_bytes = reinterpret_cast<MxScaleBytesFn>(bytes);
+  Py_RETURN_NONE;
+}
+
+// The addresses of the cache's and the attention's entry points.
 PyObject* connect(PyObject*, PyObject* args) {
   unsigned long long append, gather, decode, prefill;
   if (!PyArg_ParseTuple(args, "KKKK", &append, &gather, &decode, &prefill)) return nullptr;
@@ -266,6 +441,12 @@ PyMethodDef kMethods[] = {
     {"kv_gather", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_gather)), METH_FASTCALL, nullptr},
     {"attn_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attn_decode)), METH_FASTCALL, nullptr},
     {"attn_prefill", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attn_prefill)), METH_FASTCALL, nullptr},
+    {"connect_mx", connect_mx, METH_VARARGS, nullptr},
+    {"mx_quant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx_quant)), METH_FASTCALL, nullptr},
+    {"mx_dequant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx_dequant)), METH_FASTCALL, nullptr},
+    {"mx_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx_linear)), METH_FASTCALL, nullptr},
+    {"mx_glu", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx_glu)), METH_FASTCALL, nullptr},
+    {"add_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(add_norm)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,994 @@
+// Products of microscaled 4-bit floating point on tcgen05, which multiplies e2m1 codes and applies the groups' scales
+// itself: the linear layer  Y = fp16(step_x[m] step_w[n] sum_g s_x s_w sum_{k in g} x w)  and the gated pair of
+// projections  h = SiLU(gate) * up  with the next layer's encoding behind it.
+//
+// Nothing is widened or rearranged on the way: TMA brings packed codes (128 bytes = 256 codes a row and k-block,
+// 128-byte swizzle) and whole blocks of scales into shared memory, tcgen05.cp copies the scales to tensor memory,
+// tcgen05.mma reads both.  Two kernels:
+//
+//   pair    many tokens.  A cluster of two CTAs on a 256 x 256 tile (cta_group::2), persistent.
+//   stream  few tokens.  The weights on the 128-row axis, the tokens on the other, K split over a cluster whose
+//           partial sums meet in shared memory: bound by the one pass over the weights.
+//
+// Every wait on an mbarrier is bounded in wall time, as in the other kernels of the library.
+#include <cuda.h>
+
+#include "mx.cuh"
+
+namespace smoothrot {
+namespace mx {
+
+constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s
+constexpr unsigned long long kDrainNs = 50000ull;            // pause before leaving after a timeout
+
+__device__ int g_mx_status = 0;
+__device__ unsigned long long g_mx_wait_limit_ns = kWaitLimitNs;
+
+enum Site { kPairLoad = 42, kPairAcc = 43, kPairFull = 44, kPairEpilogue = 45, kStreamLoad = 46, kStreamFull = 47,
+            kStreamEpilogue = 48, kProbe = 49 };
+
+namespace {
+
+constexpr int kTile = 128;            // rows of an operand in one CTA's shared memory
+constexpr int kRowBytes = 128;        // of a k-block
+constexpr int kBlockK = 256;          // codes of a k-block
+constexpr int kStepsPerBlock = 4;     // an instruction takes 64 codes
+constexpr int kTileBytes = kTile * kRowBytes;
+
+// ---- PTX ----
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// arrival on a barrier of this CTA or another of the cluster
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// Waits for a phase; false if the limit has passed or another role of the CTA gave up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int site) {
+  if (bar_try(bar, parity)) return true;
+  const unsigned long long t0 = now_ns();
+  for (uint32_t spin = 1;; ++spin) {
+    if (bar_try(bar, parity)) return true;
+    if ((spin & 63u) == 0u) {
+      if (*abort_flag != 0) return false;
+      if (now_ns() - t0 > g_mx_wait_limit_ns) {
+        *abort_flag = 1;
+        atomicCAS(&g_mx_status, 0, site);
+        return false;
+      }
+    }
+  }
+}
+// The same for a whole warp, with one answer for all of its lanes.
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int site) {
+  return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag, site));
+}
+// After a timeout copies and products that this CTA started may still be on their way: they land in microseconds.
+__device__ __forceinline__ void drain_after_abort(volatile int* abort_flag) {
+  if (*abort_flag == 0) return;
+  const unsigned long long t0 = now_ns();
+  while (now_ns() - t0 < kDrainNs) __nanosleep(1000);
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t map_to_cta(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+// the same with a barrier that may be the other CTA's of the pair
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+               ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// K-major operand, 128-byte swizzle: rows of 128 bytes, groups of 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_codes(uint32_t addr) {
+  return (uint64_t((1024u >> 4) | (1u << 14) | (2u << 29)) << 32) | ((addr & 0x3FFFFu) >> 4) | (1u << 16);
+}
+// A block of scales: 32 rows of 16 bytes, no swizzle, groups of 8 rows 128 bytes apart.
+__device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
+  return (uint64_t((128u >> 4) | (1u << 14)) << 32) | ((addr & 0x3FFFFu) >> 4) | (1u << 16);
+}
+// Instruction descriptor: e2m1 x e2m1 -> fp32, K-major; which of a word's bytes are the scales of this
+// step: bits 4-5 (B) and 29-30 (A); bit 23: scales are powers of two.
+template <int GROUP>
+__host__ __device__ constexpr uint32_t instruction(int m, int n, uint32_t scale_byte) {
+  return (1u << 7) | (1u << 10) | (uint32_t(n >> 3) << 17) | (uint32_t(GROUP == 32) << 23) | (uint32_t(m >> 4) << 24) |
+         (scale_byte << 4) | (scale_byte << 29);
+}
+template <int GROUP, int CTAS>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t inst, uint32_t scale_a, uint32_t scale_b,
+                                    uint32_t accumulate) {
+#define SR_MX_MMA(CG, KIND)                                                                                       \
+  asm volatile(                                                                                                   \
+      "{\n\t.reg .pred p;\n\t"                                                                                    \
+      "setp.ne.b32 p, %6, 0;\n\t"                                                                                 \
+      "tcgen05.mma.cta_group::" CG "." KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),                    \
+      "l"(a), "l"(b), "r"(inst), "r"(scale_a), "r"(scale_b), "r"(accumulate)                                      \
+      : "memory")
+  if constexpr (GROUP == 32 && CTAS == 2) SR_MX_MMA("2", "kind::mxf4.block_scale.scale_vec::2X");
+  if constexpr (GROUP == 32 && CTAS == 1) SR_MX_MMA("1", "kind::mxf4.block_scale.scale_vec::2X");
+  if constexpr (GROUP == 16 && CTAS == 2) SR_MX_MMA("2", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+  if constexpr (GROUP == 16 && CTAS == 1) SR_MX_MMA("1", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+#undef SR_MX_MMA
+}
+template <int CTAS>
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+  if constexpr (CTAS == 2)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+  const uint16_t both = 3;
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(bar), "h"(both) : "memory");
+}
+template <int CTAS>
+__device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t cols) {
+  if constexpr (CTAS == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+}
+template <int CTAS>
+__device__ __forceinline__ void tmem_free(uint32_t base, uint32_t cols) {
+  if constexpr (CTAS == 2)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
+  else
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// ---- what the epilogues share ----
+
+// g / (1 + exp(-g)) * u; an exponential beyond the range gives 0 or g
+__device__ __forceinline__ float silu_times(float g, float u) {
+  return __fdividef(g, 1.0f + __expf(-g)) * u;
+}
+
+// Walsh rotation of a thread's 32 values: strides 1, 2, 4, ..., then 1 / sqrt(32).
+__device__ __forceinline__ void walsh_32(float (&v)[32], float norm) {
+#pragma unroll
+  for (int s = 1; s < 32; s *= 2)
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if ((i & s) == 0) {
+        const float a = v[i], b = v[i + s];
+        v[i] = __fadd_rn(a, b);
+        v[i + s] = __fsub_rn(a, b);
+      }
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __fmul_rn(v[i], norm);
+}
+
+// A thread's 32 neighbouring values to codes; the scale bytes of their one or two groups in the low bits of the result.
+template <int GROUP>
+__device__ __forceinline__ uint32_t encode_values(const float (&v)[32], float step, uint4* codes) {
+  uint32_t bytes = 0;
+  uint32_t* out = reinterpret_cast<uint32_t*>(codes);
+#pragma unroll
+  for (int g = 0; g < 32 / GROUP; ++g) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) top = max(top, abs_bits(v[g * GROUP + i]));
+    float d = 1.0f, inv;
+    uint32_t byte;
+    if constexpr (GROUP == 32) {
+      byte = scale_byte_32(top);
+      inv = inverse_scale_32(byte);
+    } else {
+      byte = to_e4m3(__fdiv_rn(__uint_as_float(top), __fmul_rn(6.0f, step)));
+      d = __fmul_rn(from_e4m3(byte), step);
+      inv = d == 0.0f ? 0.0f : __frcp_rn(d);
+    }
+    bytes |= byte << (8 * g);
+#pragma unroll
+    for (int c = 0; c < GROUP / 8; ++c) {
+      float q[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = v[g * GROUP + 8 * c + i];
+        q[i] = GROUP == 32 ? __fmul_rn(x, inv) : quotient(x, d, inv);
+      }
+      out[g * (GROUP / 8) + c] = to_codes(q);
+    }
+  }
+  return bytes;
+}
+
+enum Mode { kLinear = 0, kGatedHalf = 1, kGatedCodes = 2 };
+
+struct Args {
+  int M, N;                   // tokens, output channels (of one projection)
+  int kblocks, last_steps;    // k-blocks, instructions of the last one
+  int tiles_a, tiles_b;
+  const float *x_step, *w_step, *up_step;   // per row, or null
+  __half* y;
+  int64_t ldy;
+  uint8_t *q_out, *scale_out;
+  const float* h_step;
+  int walsh;
+  float norm;
+};
+
+// ---------------------------------------------------------------------------
+// Many tokens: 256 x 256 tiles over a pair of CTAs.
+//
+// Each CTA stages 128 token rows and half of the 256 weight rows (gated: one CTA the gate's 128 rows, the other the
+// up projection's), the pair's tensor cores share the halves.  Scales of the weights are applied column by
+// column in both CTAs, so each holds all of them.  A 4-bit operand row of an instruction is 32 bytes like any other
+// type's, so the pair moves 16 KB through shared memory per CTA and 128-clock instruction: the layout with the least.
+//
+// Tensor memory: two accumulators of 256 columns and the scales of a k-block (24 or 48 columns) are more than 512, so the
+// second accumulator starts 224 (208) columns after the first and they share 32 (48).  The epilogue drains the shared columns
+// first and hands them over at once; by then all of the accumulator before is drained too.  The tensor core waits a
+// microsecond's fraction per tile for that instead of a whole epilogue.
+//
+// Warps: 0 TMA, 1 products (of the first CTA), 2..9 epilogue, two to a quadrant of tensor-memory lanes.
+// ---------------------------------------------------------------------------
+template <int GROUP>
+struct Pair {
+  static constexpr int kAtoms = kBlockK / GROUP / kAtomGroups;      // blocks of scales per 128 rows and k-block
+  static constexpr int kScaleBytes = kAtoms * kAtomBytes;
+  static constexpr int kStageBytes = 2 * kTileBytes + 3 * kScaleBytes;
+  static constexpr int kStages = 5;
+  static constexpr int kEpiWarps = 8, kThreads = 32 * (2 + kEpiWarps);
+  static constexpr int kBoxBytes = 32 * 128;                        // 32 rows x 64 fp16
+  static constexpr int kOutBytes = kEpiWarps * kBoxBytes;
+  static constexpr int kBarriers = 2 * kStages + 4;
+  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kOutBytes + kBarriers * 8 + 16;
+  static constexpr int kSecond = GROUP == 32 ? 224 : 208;           // first column of the second accumulator
+  static constexpr int kScaleCol = kSecond + 256;                   // scales of A, then of B
+  static_assert(kScaleCol + 12 * kAtoms <= 512, "tensor memory");
+  static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+  static_assert(kStageBytes % 1024 == 0, "swizzled tiles start on 1024 bytes");
+};
+
+template <int GROUP, int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Pair<GROUP>::kThreads, 1)
+mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_sa,
+               const __grid_constant__ CUtensorMap map_sb, const __grid_constant__ CUtensorMap map_su,
+               const __grid_constant__ CUtensorMap map_y, const Args p) {
+  using T = Pair<GROUP>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw_addr = smem_u32(smem_raw);
+  const uint32_t base = (raw_addr + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (base - raw_addr);
+  const uint32_t out_base = base + T::kStages * T::kStageBytes;
+  const uint32_t bar_base = out_base + T::kOutBytes;
+  auto full = [&](int s) { return bar_base + 8u * s; };                       // in the first CTA, for both
+  auto empty = [&](int s) { return bar_base + 8u * (T::kStages + s); };       // in each
+  const uint32_t acc_full = bar_base + 8u * (2 * T::kStages);                 // one per accumulator, in each
+  const uint32_t acc_empty = acc_full + 16u;                                  // in the first CTA
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + (bar_base - base) + 8 * T::kBarriers);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < T::kStages; ++s) {
+      bar_init(full(s), 1);
+      bar_init(empty(s), 1);
+    }
+    bar_init(acc_full, 1);
+    bar_init(acc_full + 8u, 1);
+    bar_init(acc_empty, 2 * T::kEpiWarps);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+  }
+  if (warp == 1) tmem_alloc<2>(smem_u32(tmem_slot), 512);
+  fence_before();
+  __syncthreads();
+  cluster_sync();
+  fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int tiles = p.tiles_a * p.tiles_b;
+  const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const CUtensorMap* mb = MODE != kLinear && rank == 1 ? &map_u : &map_b;
+      const CUtensorMap* ms1 = MODE != kLinear ? &map_su : &map_sb;
+      prefetch_map(&map_a);
+      prefetch_map(mb);
+      prefetch_map(&map_sa);
+      prefetch_map(&map_sb);
+      prefetch_map(ms1);
+      uint32_t it = 0;
+      bool ok = true;
+      for (int tile = first; tile < tiles && ok; tile += step) {
+        const int ta = tile % p.tiles_a, tb = tile / p.tiles_a;
+        const int row_a = ta * 256 + int(rank) * kTile;
+        const int row_b = MODE != kLinear ? tb * kTile : tb * 256 + int(rank) * kTile;
+        const int sb0 = MODE != kLinear ? tb : 2 * tb, sb1 = MODE != kLinear ? tb : 2 * tb + 1;
+        for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+          const int s = it % T::kStages;
+          if (!bar_wait(empty(s), ((it / T::kStages) & 1u) ^ 1u, abort_flag, kPairLoad)) { ok = false; break; }
+          if (rank == 0) bar_expect(full(s), 2u * T::kStageBytes);
+          const uint32_t bar = map_to_cta(full(s), 0);
+          const uint32_t dst = base + s * T::kStageBytes, sc = dst + 2 * kTileBytes;
+          tma_load_pair(dst, &map_a, bar, kb * kRowBytes, row_a);
+          tma_load_pair(dst + kTileBytes, mb, bar, kb * kRowBytes, row_b);
+          const int x = kb * (T::kScaleBytes / 8);
+          tma_load_pair(sc, &map_sa, bar, x, row_a / kTile);
+          tma_load_pair(sc + T::kScaleBytes, &map_sb, bar, x, sb0);
+          tma_load_pair(sc + 2 * T::kScaleBytes, ms1, bar, x, sb1);
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (rank == 0 && lane == 0) {
+      uint32_t it = 0, n = 0;
+      bool ok = true;
+      const uint32_t sa = tmem + T::kScaleCol, sb = sa + 4 * T::kAtoms;
+      for (int tile = first; tile < tiles && ok; tile += step, ++n) {
+        // the tile before has left the columns that this one's accumulator shares with it
+        if (!bar_wait(acc_empty, (n & 1u) ^ 1u, abort_flag, kPairAcc)) break;
+        fence_after();
+        const uint32_t acc = tmem + ((n & 1u) ? T::kSecond : 0);
+        for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+          const int s = it % T::kStages;
+          if (!bar_wait(full(s), (it / T::kStages) & 1u, abort_flag, kPairFull)) { ok = false; break; }
+          fence_after();
+          const uint32_t src = base + s * T::kStageBytes, sc = src + 2 * kTileBytes;
+          const int steps = kb + 1 < p.kblocks ? kStepsPerBlock : p.last_steps;
+          constexpr int kStepsPerAtom = kStepsPerBlock / T::kAtoms;
+#pragma unroll
+          for (int j = 0; j < kStepsPerBlock; ++j) {
+            if (j >= steps) break;
+            const int atom = j / kStepsPerAtom;
+            if (j % kStepsPerAtom == 0) {
+              copy_scales<2>(sa + 4 * atom, desc_scales(sc + atom * kAtomBytes));
+              copy_scales<2>(sb + 8 * atom, desc_scales(sc + T::kScaleBytes + atom * kAtomBytes));
+              copy_scales<2>(sb + 8 * atom + 4, desc_scales(sc + 2 * T::kScaleBytes + atom * kAtomBytes));
+            }
+            mma<GROUP, 2>(acc, desc_codes(src + 32 * j), desc_codes(src + kTileBytes + 32 * j),
+                          instruction<GROUP>(256, 256, GROUP == 32 ? 2 * (j % 2) : 0), sa + 4 * atom, sb + 8 * atom,
+                          kb > 0 || j > 0);
+          }
+          commit_pair(empty(s));
+        }
+        if (ok) commit_pair(acc_full + 8u * (n & 1u));
+      }
+    }
+  } else {
+    const int q = warp & 3;                    // quadrant of tensor-memory lanes
+    const int half = (warp - 2) >> 2;          // which of the column chunks
+    const uint32_t box = out_base + uint32_t(warp - 2) * T::kBoxBytes;
+    const uint32_t acc_free = map_to_cta(acc_empty, 0);
+    uint32_t n = 0;
+    for (int tile = first; tile < tiles; tile += step, ++n) {
+      const int ta = tile % p.tiles_a, tb = tile / p.tiles_a;
+      const int row0 = ta * 256 + int(rank) * kTile + q * 32, m = row0 + lane;
+      const float xs = p.x_step != nullptr && m < p.M ? __ldg(p.x_step + m) : 1.0f;
+      if (!bar_wait_warp(acc_full + 8u * (n & 1u), (n >> 1) & 1u, abort_flag, kPairEpilogue)) break;
+      fence_after();
+      const uint32_t acc = tmem + (uint32_t(q * 32) << 16) + ((n & 1u) ? T::kSecond : 0);
+#pragma unroll 1
+      for (int i = 0; i < 2; ++i) {
+        // The shared columns are the last of the first accumulator and the first of the second.
+        const int chunk = (n & 1u) ? 2 * i + half : 3 - (2 * i + half);
+        float a[32], b[32];
+        tmem_load32(acc + (MODE == kLinear ? 64 * chunk : 32 * chunk), a);
+        tmem_load32(acc + (MODE == kLinear ? 64 * chunk + 32 : 128 + 32 * chunk), b);
+        tmem_wait_ld();
+        if (i == 0) {
+          fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive_cluster(acc_free);
+        }
+        if constexpr (MODE == kLinear) {
+          const int n0 = tb * 256 + chunk * 64;
+          if (p.w_step != nullptr || p.x_step != nullptr) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const float wa = p.w_step != nullptr && n0 + j < p.N ? __ldg(p.w_step + n0 + j) : 1.0f;
+              const float wb = p.w_step != nullptr && n0 + 32 + j < p.N ? __ldg(p.w_step + n0 + 32 + j) : 1.0f;
+              a[j] *= xs * wa;
+              b[j] *= xs * wb;
+            }
+          }
+          if (lane == 0) store_wait_read<0>();
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            uint32_t o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const __half2 h = j < 4 ? __floats2half2_rn(a[8 * (j & 3) + 2 * e], a[8 * (j & 3) + 2 * e + 1])
+                                      : __floats2half2_rn(b[8 * (j & 3) + 2 * e], b[8 * (j & 3) + 2 * e + 1]);
+              o[e] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                         ::"r"(box + uint32_t(lane) * 128u + ((uint32_t(j) ^ uint32_t(lane & 7)) << 4)), "r"(o[0]), "r"(o[1]),
+                           "r"(o[2]), "r"(o[3]) : "memory");
+          }
+          fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            if (n0 < p.N && row0 < p.M) tma_store(&map_y, box, n0, row0);      // clipped at the matrix's edges
+            store_commit();
+          }
+        } else {
+          const int f0 = tb * kTile + chunk * 32;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const float gs = p.w_step != nullptr && f0 + j < p.N ? __ldg(p.w_step + f0 + j) : 1.0f;
+            const float us = p.up_step != nullptr && f0 + j < p.N ? __ldg(p.up_step + f0 + j) : 1.0f;
+            a[j] = silu_times(a[j] * (xs * gs), b[j] * (xs * us));
+          }
+          if (p.walsh) walsh_32(a, p.norm);
+          if constexpr (MODE == kGatedCodes) {
+            uint4 codes;
+            const float hs = GROUP == 16 && m < p.M ? __ldg(p.h_step + m) : 1.0f;
+            const uint32_t bytes = encode_values<GROUP>(a, hs, &codes);
+            if (m < p.M && f0 < p.N) {
+              __stcs(reinterpret_cast<uint4*>(p.q_out + int64_t(m) * (p.N / 2) + f0 / 2), codes);
+              const int quads = p.N / (4 * GROUP);
+              uint8_t* to = p.scale_out + scale_word(m, f0 / (4 * GROUP), quads) + (f0 / GROUP & 3);
+              if constexpr (GROUP == 32) *to = uint8_t(bytes);
+              else *reinterpret_cast<uint16_t*>(to) = uint16_t(bytes);
+            }
+          } else {
+            if (lane == 0) store_wait_read<0>();
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t o[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const __half2 h = __floats2half2_rn(a[8 * j + 2 * e], a[8 * j + 2 * e + 1]);
+                o[e] = *reinterpret_cast<const uint32_t*>(&h);
+              }
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                           ::"r"(box + uint32_t(lane) * 64u + ((uint32_t(j) ^ uint32_t((lane >> 1) & 3)) << 4)), "r"(o[0]),
+                             "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) {
+              if (f0 < p.N && row0 < p.M) tma_store(&map_y, box, f0, row0);
+              store_commit();
+            }
+          }
+        }
+      }
+    }
+    if (MODE != kGatedCodes && lane == 0) store_wait_all();
+  }
+
+  // a CTA that gave up tells the other, which waits for it before it leaves
+  if (*abort_flag != 0)
+    asm volatile("st.shared::cluster.u32 [%0], %1;"
+                 ::"r"(map_to_cta(smem_u32(const_cast<const int*>(abort_flag)), rank ^ 1u)), "r"(1u) : "memory");
+  drain_after_abort(abort_flag);
+  fence_before();
+  __syncthreads();
+  cluster_sync();
+  if (warp == 1) {
+    __syncwarp();
+    fence_after();
+    tmem_free<2>(tmem, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Few tokens: the weights on the 128-row axis, BN tokens on the other.
+//
+// The one pass over the weights is what such a call costs, so the kernel keeps as much of it in flight as shared memory holds:
+// a ring of 16 KB weight tiles (gated: one of each projection) with their scales, and the tokens' BN rows beside them.
+// One CTA computes a tile of 128 channels over one part of K; the parts of a tile are a cluster, leave their sums in their own
+// shared memory, and after a cluster barrier each adds up some of the tokens over all parts, in the parts' order: the
+// same bits from call to call.  A warp finishes 32 channels of a token, a group of the next layer's codes.
+//
+// Warps: 0 TMA, 1 products, 2..5 read the accumulator; all six finish.
+// ---------------------------------------------------------------------------
+template <int GROUP, int BN, bool GATED>
+struct Stream {
+  static constexpr int kMats = GATED ? 2 : 1;
+  static constexpr int kAtoms = kBlockK / GROUP / kAtomGroups;
+  static constexpr int kScaleBytes = kAtoms * kAtomBytes;
+  static constexpr int kTokenBytes = BN * kRowBytes;
+  static constexpr int kStageBytes = kMats * (kTileBytes + kScaleBytes) + kTokenBytes + kScaleBytes;
+  static constexpr int kStages = 200 * 1024 / kStageBytes;
+  static constexpr int kThreads = 192;
+  static constexpr int kBarriers = 2 * kStages + 1;
+  static constexpr int kRingBytes = kStages * kStageBytes;
+  static constexpr int kSumBytes = kMats * BN * kTile * 4;       // over the ring, once it has been used
+  static constexpr int kSmemBytes = 1024 + kRingBytes + kBarriers * 8 + 16;
+  static constexpr int kScaleCol = kMats * BN;
+  static constexpr int kCols = kScaleCol + 4 * kAtoms * (kMats + 1);
+  static constexpr int kTmemCols = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+  static_assert(kCols <= 512, "tensor memory");
+  static_assert(kSumBytes <= kRingBytes && kSmemBytes <= 227 * 1024, "shared memory");
+  static_assert(kStageBytes % 1024 == 0, "swizzled tiles start on 1024 bytes");
+};
+
+__device__ __forceinline__ float load_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int GROUP, int BN, int MODE>
+__global__ void __launch_bounds__(192, 1)
+mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u,
+                 const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_sw,
+                 const __grid_constant__ CUtensorMap map_su, const __grid_constant__ CUtensorMap map_sx, const Args p,
+                 const int parts) {
+  constexpr bool GATED = MODE != kLinear;
+  using T = Stream<GROUP, BN, GATED>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw_addr = smem_u32(smem_raw);
+  const uint32_t base = (raw_addr + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (base - raw_addr);
+  const uint32_t bar_base = base + T::kRingBytes;
+  auto full = [&](int s) { return bar_base + 8u * s; };
+  auto empty = [&](int s) { return bar_base + 8u * (T::kStages + s); };
+  const uint32_t done = bar_base + 8u * (2 * T::kStages);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + T::kRingBytes + 8 * T::kBarriers);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int part = int(blockIdx.x) % parts;                 // rank in the cluster
+  const int tile = int(blockIdx.x) / parts;
+  const int m0 = int(blockIdx.y) * BN, n0 = tile * kTile;
+  const int k0 = int(int64_t(p.kblocks) * part / parts), k1 = int(int64_t(p.kblocks) * (part + 1) / parts);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < T::kStages; ++s) {
+      bar_init(full(s), 1);
+      bar_init(empty(s), 1);
+    }
+    bar_init(done, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+  }
+  if (warp == 1) tmem_alloc<1>(smem_u32(tmem_slot), T::kTmemCols);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int kb = k0; kb < k1; ++kb) {
+        const int it = kb - k0, s = it % T::kStages;
+        if (it >= T::kStages && !bar_wait(empty(s), ((it / T::kStages) & 1) ^ 1, abort_flag, kStreamLoad)) break;
+        bar_expect(full(s), uint32_t(T::kStageBytes));
+        const uint32_t dst = base + s * T::kStageBytes, sc = dst + T::kMats * kTileBytes + T::kTokenBytes;
+        const int x = kb * (T::kScaleBytes / 8);
+        tma_load(dst, &map_w, full(s), kb * kRowBytes, n0);
+        if (GATED) tma_load(dst + kTileBytes, &map_u, full(s), kb * kRowBytes, n0);
+        tma_load(dst + T::kMats * kTileBytes, &map_x, full(s), kb * kRowBytes, m0);
+        tma_load(sc, &map_sw, full(s), x, tile);
+        if (GATED) tma_load(sc + T::kScaleBytes, &map_su, full(s), x, tile);
+        tma_load(sc + T::kMats * T::kScaleBytes, &map_sx, full(s), x, m0 / kTile);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t sa = tmem + T::kScaleCol, sb = sa + 4 * T::kAtoms * T::kMats;
+      for (int kb = k0; kb < k1; ++kb) {
+        const int it = kb - k0, s = it % T::kStages;
+        if (!bar_wait(full(s), (it / T::kStages) & 1, abort_flag, kStreamFull)) { ok = false; break; }
+        fence_after();
+        const uint32_t src = base + s * T::kStageBytes, tok = src + T::kMats * kTileBytes, sc = tok + T::kTokenBytes;
+        const int steps = kb + 1 < p.kblocks ? kStepsPerBlock : p.last_steps;
+        constexpr int kStepsPerAtom = kStepsPerBlock / T::kAtoms;
+#pragma unroll
+        for (int j = 0; j < kStepsPerBlock; ++j) {
+          if (j >= steps) break;
+          const int atom = j / kStepsPerAtom;
+          if (j % kStepsPerAtom == 0) {
+#pragma unroll
+            for (int w = 0; w <= T::kMats; ++w)      // the tokens' scales follow the weights'
+              copy_scales<1>(sa + 4 * (T::kAtoms * w + atom), desc_scales(sc + w * T::kScaleBytes + atom * kAtomBytes));
+          }
+#pragma unroll
+          for (int w = 0; w < T::kMats; ++w)
+            mma<GROUP, 1>(tmem + w * BN, desc_codes(src + w * kTileBytes + 32 * j), desc_codes(tok + 32 * j),
+                          instruction<GROUP>(128, BN, GROUP == 32 ? 2 * (j % 2) : 0), sa + 4 * (T::kAtoms * w + atom),
+                          sb + 4 * atom, kb > k0 || j > 0);
+        }
+        commit(empty(s));
+      }
+      if (ok) commit(done);
+    }
+  } else if (bar_wait_warp(done, 0, abort_flag, kStreamEpilogue)) {
+    // the ring has been read to its end: the sums take its place, [matrix][token][channel]
+    fence_after();
+    const int q = warp & 3;
+    const uint32_t acc = tmem + (uint32_t(q * 32) << 16);
+    float* sums = reinterpret_cast<float*>(smem) + q * 32 + lane;
+    const int cols = min(BN, p.M - m0);
+#pragma unroll 1
+    for (int c = 0; c < T::kMats * BN; c += 16) {
+      if ((c & (BN - 1)) >= cols) continue;
+      float v[16];
+      tmem_load16(acc + c, v);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sums[(c + i) * kTile] = v[i];
+    }
+  }
+  drain_after_abort(abort_flag);
+  fence_before();
+  __syncwarp();
+  if (parts > 1) cluster_sync();
+  else __syncthreads();
+  if (*abort_flag == 0) {
+    const uint32_t mine = base + uint32_t(lane) * 4u;
+    const int cols = min(BN, p.M - m0);
+    for (int unit = warp; ; unit += T::kThreads / 32) {
+      const int c = (unit >> 2) * parts + part, g = unit & 3;
+      if (c >= cols) break;
+      const int m = m0 + c, n = n0 + g * 32 + lane;
+      if (n - lane >= p.N) continue;
+      const bool on = n < p.N;
+      float a = 0.0f, b = 0.0f;
+      const uint32_t at = mine + uint32_t((c * kTile + g * 32) * 4);
+      for (int r = 0; r < parts; ++r) {
+        const uint32_t src = parts > 1 ? map_to_cta(at, r) : at;
+        a += load_cluster(src);
+        if (GATED) b += load_cluster(src + uint32_t(BN * kTile * 4));
+      }
+      const float xs = p.x_step != nullptr ? __ldg(p.x_step + m) : 1.0f;
+      a *= xs * (on && p.w_step != nullptr ? __ldg(p.w_step + n) : 1.0f);
+      if constexpr (GATED) {
+        b *= xs * (on && p.up_step != nullptr ? __ldg(p.up_step + n) : 1.0f);
+        a = silu_times(a, b);
+        if (p.walsh) {
+#pragma unroll
+          for (int x = 1; x < 32; x *= 2) a = __fmaf_rn((lane & x) ? -1.0f : 1.0f, a, __shfl_xor_sync(0xffffffffu, a, x));
+          a = __fmul_rn(a, p.norm);
+        }
+      }
+      if constexpr (MODE == kGatedCodes) {
+        uint32_t top = abs_bits(a), byte;
+#pragma unroll
+        for (int x = 1; x < GROUP; x *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
+        float v;
+        if constexpr (GROUP == 32) {
+          byte = scale_byte_32(top);
+          v = __fmul_rn(a, inverse_scale_32(byte));
+        } else {
+          const float hs = __ldg(p.h_step + m);
+          byte = to_e4m3(__fdiv_rn(__uint_as_float(top), __fmul_rn(6.0f, hs)));
+          const float d = __fmul_rn(from_e4m3(byte), hs);
+          v = quotient(a, d, d == 0.0f ? 0.0f : __frcp_rn(d));
+        }
+        float q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = __shfl_sync(0xffffffffu, v, (lane & 3) * 8 + i);
+        const uint32_t word = to_codes(q);
+        if (lane < 4) *reinterpret_cast<uint32_t*>(p.q_out + int64_t(m) * (p.N / 2) + (n - lane) / 2 + lane * 4) = word;
+        if ((lane & (GROUP - 1)) == 0)
+          p.scale_out[scale_word(m, n / (4 * GROUP), p.N / (4 * GROUP)) + (n / GROUP & 3)] = uint8_t(byte);
+      } else {
+        if (on) p.y[int64_t(m) * p.ldy + n] = __float2half_rn(a);
+      }
+    }
+  }
+  __syncwarp();
+  if (parts > 1) cluster_sync();        // nobody leaves while its sums may still be read
+  else __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    fence_after();
+    tmem_free<1>(tmem, T::kTmemCols);
+  }
+}
+
+// Test probe: one warp waits, through the kernels' bounded wait, on a barrier that nobody arrives on.
+__global__ void mx_wait_probe_kernel() {
+  __shared__ __align__(8) unsigned long long storage;
+  __shared__ int abort_word;
+  const uint32_t bar = smem_u32(&storage);
+  if (threadIdx.x == 0) {
+    abort_word = 0;
+    bar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  (void)bar_wait(bar, 0u, &abort_word, kProbe);
+  drain_after_abort(&abort_word);
+}
+
+// ---- host ----
+
+// Packed codes [rows x K/2] bytes, `box` rows of 128 bytes at a time, 128-byte swizzle.  Past the edges: zeros.
+bool map_codes(CUtensorMap* map, const uint8_t* p, int64_t rows, int64_t K, int box) {
+  const cuuint64_t dims[2] = {cuuint64_t(K / 2), cuuint64_t(rows)};
+  const cuuint64_t strides[1] = {cuuint64_t(K / 2)};
+  const cuuint32_t boxes[2] = {kRowBytes, cuuint32_t(box)}, ones[2] = {1, 1};
+  return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p), dims, strides, boxes, ones,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Blocks of scales, 8 bytes an element: those of 128 rows in a line, a k-block's at a time.
+bool map_scales(CUtensorMap* map, const uint8_t* p, int64_t rows, int64_t K, int group) {
+  const int64_t quads = K / group / kAtomGroups;
+  const cuuint64_t dims[2] = {cuuint64_t(quads * (kAtomBytes / 8)), cuuint64_t((rows + kAtomRows - 1) / kAtomRows)};
+  const cuuint64_t strides[1] = {cuuint64_t(quads * kAtomBytes)};
+  const cuuint32_t boxes[2] = {cuuint32_t(kBlockK / group / kAtomGroups * (kAtomBytes / 8)), 1}, ones[2] = {1, 1};
+  return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_INT64, 2, const_cast<uint8_t*>(p), dims, strides, boxes, ones,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// fp16 output [M x N], boxes of 32 rows and `cols` columns for stores.
+bool map_half(CUtensorMap* map, __half* y, int64_t M, int64_t N, int64_t ldy, int cols) {
+  const cuuint64_t dims[2] = {cuuint64_t(N), cuuint64_t(M)};
+  const cuuint64_t strides[1] = {cuuint64_t(ldy) * sizeof(__half)};
+  const cuuint32_t boxes[2] = {cuuint32_t(cols), 32}, ones[2] = {1, 1};
+  return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, y, dims, strides, boxes, ones,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Call {
+  const uint8_t *x, *sx, *w, *sw, *u, *su;
+  int64_t M, N, K;
+  Args args;
+  cudaStream_t stream;
+};
+
+template <int GROUP, int MODE>
+int launch_pair(const Call& c) {
+  using T = Pair<GROUP>;
+  constexpr bool gated = MODE != kLinear;
+  CUtensorMap a, b, u, sa, sb, su, y;
+  if (!map_codes(&a, c.x, c.M, c.K, kTile) || !map_codes(&b, c.w, c.N, c.K, kTile) ||
+      !map_scales(&sa, c.sx, c.M, c.K, GROUP) || !map_scales(&sb, c.sw, c.N, c.K, GROUP))
+    return SMOOTHROT_CUDA_ERROR;
+  u = b;
+  su = sb;
+  if (gated && (!map_codes(&u, c.u, c.N, c.K, kTile) || !map_scales(&su, c.su, c.N, c.K, GROUP))) return SMOOTHROT_CUDA_ERROR;
+  y = a;
+  if (MODE != kGatedCodes && !map_half(&y, c.args.y, c.M, c.N, c.args.ldy, gated ? 32 : 64)) return SMOOTHROT_CUDA_ERROR;
+  Args p = c.args;
+  const int width = gated ? kTile : 256;
+  p.tiles_a = int((c.M + 255) / 256);
+  p.tiles_b = int((c.N + width - 1) / width);
+  auto kern = mx_pair_kernel<GROUP, MODE>;
+  if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), T::kSmemBytes)) return SMOOTHROT_CUDA_ERROR;
+  const int64_t tiles = int64_t(p.tiles_a) * p.tiles_b, pairs = device_sm_count() / 2;
+  kern<<<unsigned(2 * (tiles < pairs ? tiles : pairs)), T::kThreads, T::kSmemBytes, c.stream>>>(a, b, u, sa, sb, su, y, p);
+  count_launch();
+  return launch_status();
+}
+
+template <int GROUP, int BN, int MODE>
+int launch_stream(const Call& c, int parts) {
+  using T = Stream<GROUP, BN, MODE != kLinear>;
+  CUtensorMap w, u, x, sw, su, sx;
+  if (!map_codes(&w, c.w, c.N, c.K, kTile) || !map_codes(&x, c.x, c.M, c.K, BN) ||
+      !map_scales(&sw, c.sw, c.N, c.K, GROUP) || !map_scales(&sx, c.sx, c.M, c.K, GROUP))
+    return SMOOTHROT_CUDA_ERROR;
+  u = w;
+  su = sw;
+  if (MODE != kLinear && (!map_codes(&u, c.u, c.N, c.K, kTile) || !map_scales(&su, c.su, c.N, c.K, GROUP))) return SMOOTHROT_CUDA_ERROR;
+  auto kern = mx_stream_kernel<GROUP, BN, MODE>;
+  if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), T::kSmemBytes)) return SMOOTHROT_CUDA_ERROR;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned((c.N + kTile - 1) / kTile * parts), unsigned((c.M + BN - 1) / BN), 1);
+  cfg.blockDim = dim3(T::kThreads, 1, 1);
+  cfg.dynamicSmemBytes = T::kSmemBytes;
+  cfg.stream = c.stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = unsigned(parts);
+  attr.val.clusterDim.y = 1;
+  attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kern, w, u, x, sw, su, sx, c.args, parts) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SMOOTHROT_CUDA_ERROR;
+  }
+  count_launch();
+  return launch_status();
+}
+
+template <int GROUP, int MODE>
+int run(const Call& c) {
+  if (c.M > 128) return launch_pair<GROUP, MODE>(c);
+  const int64_t tiles = (c.N + kTile - 1) / kTile;
+  int parts = 1;
+  while (parts < 8 && 2 * parts * tiles <= device_sm_count() && c.args.kblocks >= 2 * parts) parts *= 2;
+  if (c.M <= 16) return launch_stream<GROUP, 16, MODE>(c, parts);
+  if (c.M <= 32) return launch_stream<GROUP, 32, MODE>(c, parts);
+  if (c.M <= 64) return launch_stream<GROUP, 64, MODE>(c, parts);
+  return launch_stream<GROUP, 128, MODE>(c, parts);
+}
+
+int check_operand(const uint8_t* q, const uint8_t* s) {
+  if (q == nullptr || s == nullptr) return SMOOTHROT_INVALID_ARG;
+  return aligned16(q) && aligned16(s) ? SMOOTHROT_OK : SMOOTHROT_BAD_ALIGNMENT;
+}
+
+int check_sizes(int64_t M, int64_t N, int64_t K, int64_t group) {
+  if (M < 0 || N < 0 || K <= 0 || !group_ok(group)) return SMOOTHROT_INVALID_ARG;
+  if (K % 128 != 0 || K > (int64_t(1) << 20)) return SMOOTHROT_UNSUPPORTED_K;
+  if (N % 8 != 0 || M > 0x7fffffffLL / 2 || N > 0x7fffffffLL / 2) return SMOOTHROT_INVALID_ARG;
+  return SMOOTHROT_OK;
+}
+
+}  // namespace
+}  // namespace mx
+}  // namespace smoothrot
+
+extern "C" {
+
+int smoothrot_mx_status_word(int* out, int clear) {
+  int v = 0;
+  if (cudaMemcpyFromSymbol(&v, smoothrot::mx::g_mx_status, sizeof(int)) != cudaSuccess) return SMOOTHROT_CUDA_ERROR;
+  *out = v;
+  if (clear && v != 0) {
+    const int zero = 0;
+    if (cudaMemcpyToSymbol(smoothrot::mx::g_mx_status, &zero, sizeof(int)) != cudaSuccess) return SMOOTHROT_CUDA_ERROR;
+  }
+  return SMOOTHROT_OK;
+}
+
+int smoothrot_mx_set_wait_limit_ns(uint64_t ns) {
+  const unsigned long long v = ns == 0 ? smoothrot::mx::kWaitLimitNs : static_cast<unsigned long long>(ns);
+  return cudaMemcpyToSymbol(smoothrot::mx::g_mx_wait_limit_ns, &v, sizeof(v)) == cudaSuccess ? SMOOTHROT_OK
+                                                                                               : SMOOTHROT_CUDA_ERROR;
+}
+
+int smoothrot_debug_mx_wait_expiry(void* stream) {
+  smoothrot::mx::mx_wait_probe_kernel<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>();
+  smoothrot::count_launch();
+  return smoothrot::launch_status();
+}
+
+int smoothrot_mx_linear(const uint8_t* Xq, const uint8_t* x_scale, const float* x_step, int64_t M, const uint8_t* Wq,
+                        const uint8_t* w_scale, const float* w_step, int64_t N, int64_t K, int64_t group, void* Y_f16,
+                        int64_t ldy, void* stream) {
+  using namespace smoothrot;
+  using namespace smoothrot::mx;
+  int rc = check_sizes(M, N, K, group);
+  if (rc != SMOOTHROT_OK || M == 0 || N == 0) return rc;
+  if (Y_f16 == nullptr || ldy < N) return SMOOTHROT_INVALID_ARG;
+  if ((rc = check_operand(Xq, x_scale)) != SMOOTHROT_OK || (rc = check_operand(Wq, w_scale)) != SMOOTHROT_OK) return rc;
+  if (!aligned16(Y_f16) || ldy % 8 != 0) return SMOOTHROT_BAD_ALIGNMENT;
+  if (tensor_map_encoder() == nullptr) return SMOOTHROT_CUDA_ERROR;
+  Call c{Xq, x_scale, Wq, w_scale, nullptr, nullptr, M, N, K, Args{}, static_cast<cudaStream_t>(stream)};
+  c.args.M = int(M);
+  c.args.N = int(N);
+  c.args.kblocks = int((K + kBlockK - 1) / kBlockK);
+  c.args.last_steps = K % kBlockK == 0 ? kStepsPerBlock : kStepsPerBlock / 2;
+  c.args.x_step = x_step;
+  c.args.w_step = w_step;
+  c.args.y = static_cast<__half*>(Y_f16);
+  c.args.ldy = ldy;
+  return group == 32 ? run<32, kLinear>(c) : run<16, kLinear>(c);
+}
+
+int smoothrot_mx_glu(const uint8_t* Xq, const uint8_t* x_scale, const float* x_step, int64_t M, const uint8_t* gate_q,
+                     const uint8_t* gate_scale, const float* gate_step, const uint8_t* up_q, const uint8_t* up_scale,
+                     const float* up_step, int64_t F, int64_t K, int64_t group, int walsh, void* H_f16, int64_t ldh,
+                     uint8_t* q_out, uint8_t* scale_out, const float* h_step, void* stream) {
+  using namespace smoothrot;
+  using namespace smoothrot::mx;
+  int rc = check_sizes(M, F, K, group);
+  if (rc != SMOOTHROT_OK) return rc;
+  if (walsh != 0 && walsh != 32) return SMOOTHROT_INVALID_ARG;
+  const bool codes = q_out != nullptr;
+  if ((codes && F % 128 != 0) || (walsh != 0 && F % 32 != 0)) return SMOOTHROT_UNSUPPORTED_K;
+  if (M == 0 || F == 0) return SMOOTHROT_OK;
+  if (codes == (H_f16 != nullptr)) return SMOOTHROT_INVALID_ARG;      // one of the two forms
+  if (codes && (scale_out == nullptr || (group == 16) != (h_step != nullptr))) return SMOOTHROT_INVALID_ARG;
+  if (!codes && (ldh < F || scale_out != nullptr || h_step != nullptr)) return SMOOTHROT_INVALID_ARG;
+  if ((rc = check_operand(Xq, x_scale)) != SMOOTHROT_OK || (rc = check_operand(gate_q, gate_scale)) != SMOOTHROT_OK ||
+      (rc = check_operand(up_q, up_scale)) != SMOOTHROT_OK)
+    return rc;
+  if (codes ? !aligned16(q_out) || !aligned16(scale_out) : !aligned16(H_f16) || ldh % 8 != 0) return SMOOTHROT_BAD_ALIGNMENT;
+  if (tensor_map_encoder() == nullptr) return SMOOTHROT_CUDA_ERROR;
+  Call c{Xq, x_scale, gate_q, gate_scale, up_q, up_scale, M, F, K, Args{}, static_cast<cudaStream_t>(stream)};
+  c.args.M = int(M);
+  c.args.N = int(F);
+  c.args.kblocks = int((K + kBlockK - 1) / kBlockK);
+  c.args.last_steps = K % kBlockK == 0 ? kStepsPerBlock : kStepsPerBlock / 2;
+  c.args.x_step = x_step;
+  c.args.w_step = gate_step;
+  c.args.up_step = up_step;
+  c.args.y = static_cast<__half*>(H_f16);
+  c.args.ldy = ldh;
+  c.args.q_out = q_out;
+  c.args.scale_out = scale_out;
+  c.args.h_step = h_step;
+  c.args.walsh = walsh;
+  c.args.norm = walsh != 0 ? float(1.0 / sqrt(double(walsh))) : 1.0f;
+  if (codes) return group == 32 ? run<32, kGatedCodes>(c) : run<16, kGatedCodes>(c);
+  return group == 32 ? run<32, kGatedHalf>(c) : run<16, kGatedHalf>(c);
+}
+
+}  // extern "C"

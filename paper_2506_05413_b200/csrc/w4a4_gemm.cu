@@ -44,10 +44,12 @@ extern "C" int smoothrot_rotate_status_word(int* value, int clear);
 extern "C" int smoothrot_cache_status_word(int* value, int clear);
 extern "C" int smoothrot_decode_status_word(int* value, int clear);
 extern "C" int smoothrot_prefill_status_word(int* value, int clear);
+extern "C" int smoothrot_mx_status_word(int* value, int clear);
 // defined with the row transform kernels: the limit of their bounded waits
 extern "C" int smoothrot_rotate_set_wait_limit_ns(uint64_t ns);
 extern "C" int smoothrot_prefill_set_wait_limit_ns(uint64_t ns);
 extern "C" int smoothrot_decode_set_wait_limit_ns(uint64_t ns);
+extern "C" int smoothrot_mx_set_wait_limit_ns(uint64_t ns);
 
 namespace smoothrot {
 namespace gemm {
@@ -1963,7 +1965,9 @@ int smoothrot_debug_set_wait_limit_ns(uint64_t ns) {
   const int rot = smoothrot_rotate_set_wait_limit_ns(ns);
   if (rot != SMOOTHROT_OK) return rot;
   const int pre = smoothrot_prefill_set_wait_limit_ns(ns);
-  return pre != SMOOTHROT_OK ? pre : smoothrot_decode_set_wait_limit_ns(ns);
+  if (pre != SMOOTHROT_OK) return pre;
+  const int mx = smoothrot_mx_set_wait_limit_ns(ns);
+  return mx != SMOOTHROT_OK ? mx : smoothrot_decode_set_wait_limit_ns(ns);
 }
 
 int smoothrot_debug_wait_expiry(void* stream) {
@@ -2006,14 +2010,15 @@ int smoothrot_debug_gemm_i32(const uint8_t* Xq, int64_t M, const uint8_t* Wq, in
 
 int smoothrot_device_status(int* status_host, int clear) {
   if (status_host == nullptr) return SMOOTHROT_INVALID_ARG;
-  int v = 0, rot = 0, cache = 0, dec = 0, pre = 0;
+  int v = 0, rot = 0, cache = 0, dec = 0, pre = 0, mx = 0;
   if (cudaMemcpyFromSymbol(&v, smoothrot::gemm::g_device_status, sizeof(int)) != cudaSuccess)
     return SMOOTHROT_CUDA_ERROR;
   if (smoothrot_rotate_status_word(&rot, clear) != SMOOTHROT_OK) return SMOOTHROT_CUDA_ERROR;
   if (smoothrot_cache_status_word(&cache, clear) != SMOOTHROT_OK) return SMOOTHROT_CUDA_ERROR;
   if (smoothrot_decode_status_word(&dec, clear) != SMOOTHROT_OK) return SMOOTHROT_CUDA_ERROR;
   if (smoothrot_prefill_status_word(&pre, clear) != SMOOTHROT_OK) return SMOOTHROT_CUDA_ERROR;
-  *status_host = v != 0 ? v : (rot != 0 ? rot : (cache != 0 ? cache : (dec != 0 ? dec : pre)));
+  if (smoothrot_mx_status_word(&mx, clear) != SMOOTHROT_OK) return SMOOTHROT_CUDA_ERROR;
+  *status_host = v != 0 ? v : (rot != 0 ? rot : (cache != 0 ? cache : (dec != 0 ? dec : (pre != 0 ? pre : mx))));
   if (clear && v != 0) {
     const int zero = 0;
     if (cudaMemcpyToSymbol(smoothrot::gemm::g_device_status, &zero, sizeof(int)) != cudaSuccess)
