@@ -130,14 +130,12 @@ template <int LEFT>
 __device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
 __device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
+// Matrix descriptors: only the low word, the address in 16 bytes, differs from one to the next.
 // K-major operand, 128-byte swizzle: rows of 128 bytes, groups of 8 rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t desc_codes(uint32_t addr) {
-  return (uint64_t((1024u >> 4) | (1u << 14) | (2u << 29)) << 32) | ((addr & 0x3FFFFu) >> 4) | (1u << 16);
-}
+constexpr uint32_t kCodesHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
 // A block of scales: 32 rows of 16 bytes, no swizzle, groups of 8 rows 128 bytes apart.
-__device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
-  return (uint64_t((128u >> 4) | (1u << 14)) << 32) | ((addr & 0x3FFFFu) >> 4) | (1u << 16);
-}
+constexpr uint32_t kScalesHigh = (128u >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
 // Instruction descriptor: e2m1 x e2m1 -> fp32, K-major; which of a word's bytes are the scales of this
 // step: bits 4-5 (B) and 29-30 (A); bit 23: scales are powers of two.
 template <int GROUP>
@@ -145,15 +143,20 @@ __host__ __device__ constexpr uint32_t instruction(int m, int n, uint32_t scale_
   return (1u << 7) | (1u << 10) | (uint32_t(n >> 3) << 17) | (uint32_t(GROUP == 32) << 23) | (uint32_t(m >> 4) << 24) |
          (scale_byte << 4) | (scale_byte << 29);
 }
+// These are issued by one thread at one a few dozen clocks, against 128 clocks that the tensor core takes for the largest: a
+// warp that is known to be of one mind, one elected lane and 32-bit operands keep the issue short (67 clocks a product with a
+// lane that was told apart by its number and whole 64-bit descriptors, 39 so).
 template <int GROUP, int CTAS>
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t inst, uint32_t scale_a, uint32_t scale_b,
+__device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint32_t b, uint32_t inst, uint32_t scale_a, uint32_t scale_b,
                                     uint32_t accumulate) {
 #define SR_MX_MMA(CG, KIND)                                                                                       \
   asm volatile(                                                                                                   \
-      "{\n\t.reg .pred p;\n\t"                                                                                    \
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"                                                             \
       "setp.ne.b32 p, %6, 0;\n\t"                                                                                 \
-      "tcgen05.mma.cta_group::" CG "." KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),                    \
-      "l"(a), "l"(b), "r"(inst), "r"(scale_a), "r"(scale_b), "r"(accumulate)                                      \
+      "mov.b64 da, {%1, %7};\n\t"                                                                                 \
+      "mov.b64 db, {%2, %7};\n\t"                                                                                 \
+      "tcgen05.mma.cta_group::" CG "." KIND " [%0], da, db, %3, [%4], [%5], p;\n\t}" ::"r"(d),                    \
+      "r"(a), "r"(b), "r"(inst), "r"(scale_a), "r"(scale_b), "r"(accumulate), "r"(kCodesHigh)                     \
       : "memory")
   if constexpr (GROUP == 32 && CTAS == 2) SR_MX_MMA("2", "kind::mxf4.block_scale.scale_vec::2X");
   if constexpr (GROUP == 32 && CTAS == 1) SR_MX_MMA("1", "kind::mxf4.block_scale.scale_vec::2X");
@@ -161,13 +164,35 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
   if constexpr (GROUP == 16 && CTAS == 1) SR_MX_MMA("1", "kind::mxf4nvf4.block_scale.scale_vec::4X");
 #undef SR_MX_MMA
 }
+// 512 bytes of scales to 4 columns of tensor memory
 template <int CTAS>
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t desc) {
   if constexpr (CTAS == 2)
-    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    asm volatile("{\n\t.reg .b64 d;\n\tmov.b64 d, {%1, %2};\n\ttcgen05.cp.cta_group::2.32x128b.warpx4 [%0], d;\n\t}"
+                 ::"r"(tmem), "r"(desc), "r"(kScalesHigh) : "memory");
   else
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    asm volatile("{\n\t.reg .b64 d;\n\tmov.b64 d, {%1, %2};\n\ttcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t}"
+                 ::"r"(tmem), "r"(desc), "r"(kScalesHigh) : "memory");
 }
+__device__ __forceinline__ bool elected() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+// The warp's number, as a value that is the same in all its lanes.
+__device__ __forceinline__ int warp_number() { return __shfl_sync(0xffffffffu, int(threadIdx.x >> 5), 0); }
+// A place in a ring of N stages and the parity of the phase that it is in.
+template <int N>
+struct Ring {
+  int s = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++s == N) {
+      s = 0;
+      phase ^= 1u;
+    }
+  }
+};
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -327,6 +352,24 @@ struct Pair {
   static_assert(kStageBytes % 1024 == 0, "swizzled tiles start on 1024 bytes");
 };
 
+// A k-block's scale copies and products; `sc` is the block's scales (A, then the two halves of B), all as low words.
+template <int GROUP, int STEPS>
+__device__ __forceinline__ void pair_block(uint32_t acc, uint32_t a, uint32_t b, uint32_t sc, uint32_t sa, uint32_t sb, bool fresh) {
+  using T = Pair<GROUP>;
+  constexpr int per = kStepsPerBlock / T::kAtoms;      // products that an atom of scales serves
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) {
+    const int atom = j / per;
+    if (j % per == 0) {
+      copy_scales<2>(sa + 4 * atom, sc + atom * (kAtomBytes / 16));
+      copy_scales<2>(sb + 8 * atom, sc + (T::kScaleBytes + atom * kAtomBytes) / 16);
+      copy_scales<2>(sb + 8 * atom + 4, sc + (2 * T::kScaleBytes + atom * kAtomBytes) / 16);
+    }
+    mma<GROUP, 2>(acc, a + 2 * j, b + 2 * j, instruction<GROUP>(256, 256, GROUP == 32 ? 2 * (j % 2) : 0), sa + 4 * atom,
+                  sb + 8 * atom, j > 0 || !fresh);
+  }
+}
+
 template <int GROUP, int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Pair<GROUP>::kThreads, 1)
 mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -347,7 +390,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + (bar_base - base) + 8 * T::kBarriers);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = warp_number(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   if (threadIdx.x == 0) {
     for (int s = 0; s < T::kStages; ++s) {
@@ -366,32 +409,36 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   __syncthreads();
   cluster_sync();
   fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
   const int tiles = p.tiles_a * p.tiles_b;
   const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
 
   if (warp == 0) {
-    if (lane == 0) {
-      const CUtensorMap* mb = MODE != kLinear && rank == 1 ? &map_u : &map_b;
-      const CUtensorMap* ms1 = MODE != kLinear ? &map_su : &map_sb;
+    const bool one = elected();
+    const CUtensorMap* mb = MODE != kLinear && rank == 1 ? &map_u : &map_b;
+    const CUtensorMap* ms1 = MODE != kLinear ? &map_su : &map_sb;
+    if (one) {
       prefetch_map(&map_a);
       prefetch_map(mb);
       prefetch_map(&map_sa);
       prefetch_map(&map_sb);
       prefetch_map(ms1);
-      uint32_t it = 0;
-      bool ok = true;
-      for (int tile = first; tile < tiles && ok; tile += step) {
-        const int ta = tile % p.tiles_a, tb = tile / p.tiles_a;
-        const int row_a = ta * 256 + int(rank) * kTile;
-        const int row_b = MODE != kLinear ? tb * kTile : tb * 256 + int(rank) * kTile;
-        const int sb0 = MODE != kLinear ? tb : 2 * tb, sb1 = MODE != kLinear ? tb : 2 * tb + 1;
-        for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-          const int s = it % T::kStages;
-          if (!bar_wait(empty(s), ((it / T::kStages) & 1u) ^ 1u, abort_flag, kPairLoad)) { ok = false; break; }
-          if (rank == 0) bar_expect(full(s), 2u * T::kStageBytes);
-          const uint32_t bar = map_to_cta(full(s), 0);
-          const uint32_t dst = base + s * T::kStageBytes, sc = dst + 2 * kTileBytes;
+    }
+    Ring<T::kStages> r;
+    const uint32_t lead = map_to_cta(bar_base, 0);
+    bool ok = true;
+    for (int tile = first; tile < tiles && ok; tile += step) {
+      const int ta = tile % p.tiles_a, tb = tile / p.tiles_a;
+      const int row_a = ta * 256 + int(rank) * kTile;
+      const int row_b = MODE != kLinear ? tb * kTile : tb * 256 + int(rank) * kTile;
+      const int sb0 = MODE != kLinear ? tb : 2 * tb, sb1 = MODE != kLinear ? tb : 2 * tb + 1;
+      for (int kb = 0; kb < p.kblocks; ++kb, r.next()) {
+        ok = bar_wait_warp(empty(r.s), r.phase ^ 1u, abort_flag, kPairLoad);
+        if (!ok) break;
+        if (one) {
+          if (rank == 0) bar_expect(full(r.s), 2u * T::kStageBytes);
+          const uint32_t bar = lead + 8u * r.s;
+          const uint32_t dst = base + r.s * T::kStageBytes, sc = dst + 2 * kTileBytes;
           tma_load_pair(dst, &map_a, bar, kb * kRowBytes, row_a);
           tma_load_pair(dst + kTileBytes, mb, bar, kb * kRowBytes, row_b);
           const int x = kb * (T::kScaleBytes / 8);
@@ -399,41 +446,38 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           tma_load_pair(sc + T::kScaleBytes, &map_sb, bar, x, sb0);
           tma_load_pair(sc + 2 * T::kScaleBytes, ms1, bar, x, sb1);
         }
+        __syncwarp();
       }
     }
   } else if (warp == 1) {
-    if (rank == 0 && lane == 0) {
-      uint32_t it = 0, n = 0;
-      bool ok = true;
+    if (rank == 0) {
+      const bool one = elected();
       const uint32_t sa = tmem + T::kScaleCol, sb = sa + 4 * T::kAtoms;
+      Ring<T::kStages> r;
+      uint32_t n = 0;
+      bool ok = true;
       for (int tile = first; tile < tiles && ok; tile += step, ++n) {
         // the tile before has left the columns that this one's accumulator shares with it
-        if (!bar_wait(acc_empty, (n & 1u) ^ 1u, abort_flag, kPairAcc)) break;
+        if (!bar_wait_warp(acc_empty, (n & 1u) ^ 1u, abort_flag, kPairAcc)) break;
         fence_after();
         const uint32_t acc = tmem + ((n & 1u) ? T::kSecond : 0);
-        for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-          const int s = it % T::kStages;
-          if (!bar_wait(full(s), (it / T::kStages) & 1u, abort_flag, kPairFull)) { ok = false; break; }
+        for (int kb = 0; kb < p.kblocks; ++kb, r.next()) {
+          ok = bar_wait_warp(full(r.s), r.phase, abort_flag, kPairFull);
+          if (!ok) break;
           fence_after();
-          const uint32_t src = base + s * T::kStageBytes, sc = src + 2 * kTileBytes;
-          const int steps = kb + 1 < p.kblocks ? kStepsPerBlock : p.last_steps;
-          constexpr int kStepsPerAtom = kStepsPerBlock / T::kAtoms;
-#pragma unroll
-          for (int j = 0; j < kStepsPerBlock; ++j) {
-            if (j >= steps) break;
-            const int atom = j / kStepsPerAtom;
-            if (j % kStepsPerAtom == 0) {
-              copy_scales<2>(sa + 4 * atom, desc_scales(sc + atom * kAtomBytes));
-              copy_scales<2>(sb + 8 * atom, desc_scales(sc + T::kScaleBytes + atom * kAtomBytes));
-              copy_scales<2>(sb + 8 * atom + 4, desc_scales(sc + 2 * T::kScaleBytes + atom * kAtomBytes));
-            }
-            mma<GROUP, 2>(acc, desc_codes(src + 32 * j), desc_codes(src + kTileBytes + 32 * j),
-                          instruction<GROUP>(256, 256, GROUP == 32 ? 2 * (j % 2) : 0), sa + 4 * atom, sb + 8 * atom,
-                          kb > 0 || j > 0);
+          if (one) {
+            const uint32_t src = desc_low(base + r.s * T::kStageBytes);
+            const uint32_t b = src + kTileBytes / 16, sc = src + 2 * kTileBytes / 16;
+            if (kb + 1 < p.kblocks || p.last_steps == kStepsPerBlock)
+              pair_block<GROUP, kStepsPerBlock>(acc, src, b, sc, sa, sb, kb == 0);
+            else
+              pair_block<GROUP, kStepsPerBlock / 2>(acc, src, b, sc, sa, sb, kb == 0);
+            commit_pair(empty(r.s));
           }
-          commit_pair(empty(s));
+          __syncwarp();
         }
-        if (ok) commit_pair(acc_full + 8u * (n & 1u));
+        if (ok && one) commit_pair(acc_full + 8u * (n & 1u));
+        __syncwarp();
       }
     }
   } else {
@@ -595,6 +639,29 @@ __device__ __forceinline__ float load_cluster(uint32_t addr) {
   return v;
 }
 
+// A k-block's scale copies and products; `src` is the stage's low word, `sa` the first column of scales.
+template <int GROUP, int BN, bool GATED, int STEPS>
+__device__ __forceinline__ void stream_block(uint32_t acc, uint32_t src, uint32_t sa, bool fresh) {
+  using T = Stream<GROUP, BN, GATED>;
+  constexpr int per = kStepsPerBlock / T::kAtoms;
+  const uint32_t tokens = src + T::kMats * kTileBytes / 16, sc = tokens + T::kTokenBytes / 16;
+  const uint32_t sb = sa + 4 * T::kAtoms * T::kMats;       // the tokens' scales follow the weights'
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) {
+    const int atom = j / per;
+    if (j % per == 0) {
+#pragma unroll
+      for (int w = 0; w <= T::kMats; ++w)
+        copy_scales<1>(sa + 4 * (T::kAtoms * w + atom), sc + (w * T::kScaleBytes + atom * kAtomBytes) / 16);
+    }
+#pragma unroll
+    for (int w = 0; w < T::kMats; ++w)
+      mma<GROUP, 1>(acc + w * BN, src + (w * kTileBytes) / 16 + 2 * j, tokens + 2 * j,
+                    instruction<GROUP>(128, BN, GROUP == 32 ? 2 * (j % 2) : 0), sa + 4 * (T::kAtoms * w + atom), sb + 4 * atom,
+                    j > 0 || !fresh);
+  }
+}
+
 template <int GROUP, int BN, int MODE>
 __global__ void __launch_bounds__(192, 1)
 mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u,
@@ -614,7 +681,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + T::kRingBytes + 8 * T::kBarriers);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = warp_number(), lane = threadIdx.x & 31;
   const int part = int(blockIdx.x) % parts;                 // rank in the cluster
   const int tile = int(blockIdx.x) / parts;
   const int m0 = int(blockIdx.y) * BN, n0 = tile * kTile;
@@ -633,54 +700,48 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
 
-  bool ok = true;
   if (warp == 0) {
-    if (lane == 0) {
-      for (int kb = k0; kb < k1; ++kb) {
-        const int it = kb - k0, s = it % T::kStages;
-        if (it >= T::kStages && !bar_wait(empty(s), ((it / T::kStages) & 1) ^ 1, abort_flag, kStreamLoad)) break;
-        bar_expect(full(s), uint32_t(T::kStageBytes));
-        const uint32_t dst = base + s * T::kStageBytes, sc = dst + T::kMats * kTileBytes + T::kTokenBytes;
+    const bool one = elected();
+    Ring<T::kStages> r;
+    for (int kb = k0; kb < k1; ++kb, r.next()) {
+      if (!bar_wait_warp(empty(r.s), r.phase ^ 1u, abort_flag, kStreamLoad)) break;
+      if (one) {
+        const uint32_t bar = full(r.s);
+        bar_expect(bar, uint32_t(T::kStageBytes));
+        const uint32_t dst = base + r.s * T::kStageBytes, sc = dst + T::kMats * kTileBytes + T::kTokenBytes;
         const int x = kb * (T::kScaleBytes / 8);
-        tma_load(dst, &map_w, full(s), kb * kRowBytes, n0);
-        if (GATED) tma_load(dst + kTileBytes, &map_u, full(s), kb * kRowBytes, n0);
-        tma_load(dst + T::kMats * kTileBytes, &map_x, full(s), kb * kRowBytes, m0);
-        tma_load(sc, &map_sw, full(s), x, tile);
-        if (GATED) tma_load(sc + T::kScaleBytes, &map_su, full(s), x, tile);
-        tma_load(sc + T::kMats * T::kScaleBytes, &map_sx, full(s), x, m0 / kTile);
+        tma_load(dst, &map_w, bar, kb * kRowBytes, n0);
+        if (GATED) tma_load(dst + kTileBytes, &map_u, bar, kb * kRowBytes, n0);
+        tma_load(dst + T::kMats * kTileBytes, &map_x, bar, kb * kRowBytes, m0);
+        tma_load(sc, &map_sw, bar, x, tile);
+        if (GATED) tma_load(sc + T::kScaleBytes, &map_su, bar, x, tile);
+        tma_load(sc + T::kMats * T::kScaleBytes, &map_sx, bar, x, m0 / kTile);
       }
+      __syncwarp();
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t sa = tmem + T::kScaleCol, sb = sa + 4 * T::kAtoms * T::kMats;
-      for (int kb = k0; kb < k1; ++kb) {
-        const int it = kb - k0, s = it % T::kStages;
-        if (!bar_wait(full(s), (it / T::kStages) & 1, abort_flag, kStreamFull)) { ok = false; break; }
-        fence_after();
-        const uint32_t src = base + s * T::kStageBytes, tok = src + T::kMats * kTileBytes, sc = tok + T::kTokenBytes;
-        const int steps = kb + 1 < p.kblocks ? kStepsPerBlock : p.last_steps;
-        constexpr int kStepsPerAtom = kStepsPerBlock / T::kAtoms;
-#pragma unroll
-        for (int j = 0; j < kStepsPerBlock; ++j) {
-          if (j >= steps) break;
-          const int atom = j / kStepsPerAtom;
-          if (j % kStepsPerAtom == 0) {
-#pragma unroll
-            for (int w = 0; w <= T::kMats; ++w)      // the tokens' scales follow the weights'
-              copy_scales<1>(sa + 4 * (T::kAtoms * w + atom), desc_scales(sc + w * T::kScaleBytes + atom * kAtomBytes));
-          }
-#pragma unroll
-          for (int w = 0; w < T::kMats; ++w)
-            mma<GROUP, 1>(tmem + w * BN, desc_codes(src + w * kTileBytes + 32 * j), desc_codes(tok + 32 * j),
-                          instruction<GROUP>(128, BN, GROUP == 32 ? 2 * (j % 2) : 0), sa + 4 * (T::kAtoms * w + atom),
-                          sb + 4 * atom, kb > k0 || j > 0);
-        }
-        commit(empty(s));
+    const bool one = elected();
+    const uint32_t sa = tmem + T::kScaleCol;
+    Ring<T::kStages> r;
+    bool ok = true;
+    for (int kb = k0; kb < k1; ++kb, r.next()) {
+      ok = bar_wait_warp(full(r.s), r.phase, abort_flag, kStreamFull);
+      if (!ok) break;
+      fence_after();
+      if (one) {
+        const uint32_t src = desc_low(base + r.s * T::kStageBytes);
+        if (kb + 1 < p.kblocks || p.last_steps == kStepsPerBlock)
+          stream_block<GROUP, BN, GATED, kStepsPerBlock>(tmem, src, sa, kb == k0);
+        else
+          stream_block<GROUP, BN, GATED, kStepsPerBlock / 2>(tmem, src, sa, kb == k0);
+        commit(empty(r.s));
       }
-      if (ok) commit(done);
+      __syncwarp();
     }
+    if (ok && one) commit(done);
+    __syncwarp();
   } else if (bar_wait_warp(done, 0, abort_flag, kStreamEpilogue)) {
     // the ring has been read to its end: the sums take its place, [matrix][token][channel]
     fence_after();
