@@ -13,6 +13,8 @@
 // Every wait on an mbarrier is bounded in wall time, as in the other kernels of the library.
 #include <cuda.h>
 
+#include <initializer_list>
+
 #include "mx.cuh"
 
 namespace smoothrot {
@@ -233,7 +235,7 @@ __device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&v)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16]) {
+__device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[16]) {
   uint32_t r[16];
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -244,6 +246,15 @@ __device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16]) {
       : "memory");
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[8]) {
+  uint32_t r[8];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -304,6 +315,45 @@ __device__ __forceinline__ uint32_t encode_values(const float (&v)[32], float st
   return bytes;
 }
 
+// 32 columns of a row times its step and the columns' (null: 1).
+__device__ __forceinline__ void times_steps(float (&v)[32], float row, const float* step, int n0, int n) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    float4 w = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+    if (step != nullptr && n0 + j < n) w = __ldg(reinterpret_cast<const float4*>(step + n0 + j));
+    v[j] *= row * w.x;
+    v[j + 1] *= row * w.y;
+    v[j + 2] *= row * w.z;
+    v[j + 3] *= row * w.w;
+  }
+}
+
+// A warp's 32 rows x 32 columns to fp16 through its box in shared memory (64-byte swizzle) and TMA, which clips at the matrix's
+// edges: rows of 64 bytes leave whole.
+__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t box, const float (&v)[32], int x, int y, int n, int m,
+                                          int lane) {
+  if (lane == 0) store_wait_read<0>();
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __half2 h = __floats2half2_rn(v[8 * j + 2 * e], v[8 * j + 2 * e + 1]);
+      o[e] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                 ::"r"(box + uint32_t(lane) * 64u + ((uint32_t(j) ^ uint32_t((lane >> 1) & 3)) << 4)), "r"(o[0]), "r"(o[1]),
+                   "r"(o[2]), "r"(o[3]) : "memory");
+  }
+  fence_async();
+  __syncwarp();
+  if (lane == 0) {
+    if (x < n && y < m) tma_store(map, box, x, y);
+    store_commit();
+  }
+}
+
 enum Mode { kLinear = 0, kGatedHalf = 1, kGatedCodes = 2 };
 
 struct Args {
@@ -328,11 +378,11 @@ struct Args {
 // type's, so the pair moves 16 KB through shared memory per CTA and 128-clock instruction: the layout with the least.
 //
 // Tensor memory: two accumulators of 256 columns and the scales of a k-block (24 or 48 columns) are more than 512, so the
-// second accumulator starts 224 (208) columns after the first and they share 32 (48).  The epilogue drains the shared columns
-// first and hands them over at once; by then all of the accumulator before is drained too.  The tensor core waits a
-// microsecond's fraction per tile for that instead of a whole epilogue.
+// second accumulator starts 224 (208) columns after the first and they share 32 (48).  The epilogue's
+// warps take all of an accumulator into registers at once and hand it over before they work on it.
 //
-// Warps: 0 TMA, 1 products (of the first CTA), 2..9 epilogue, two to a quadrant of tensor-memory lanes.
+// Warps: 0 TMA, 1 products (of the first CTA), 2..17 epilogue, four to a quadrant of tensor-memory lanes, a chunk of columns
+// each: with two to a quadrant a gated tile's activation and encoding took longer than its products.
 // ---------------------------------------------------------------------------
 template <int GROUP>
 struct Pair {
@@ -340,8 +390,8 @@ struct Pair {
   static constexpr int kScaleBytes = kAtoms * kAtomBytes;
   static constexpr int kStageBytes = 2 * kTileBytes + 3 * kScaleBytes;
   static constexpr int kStages = 5;
-  static constexpr int kEpiWarps = 8, kThreads = 32 * (2 + kEpiWarps);
-  static constexpr int kBoxBytes = 32 * 128;                        // 32 rows x 64 fp16
+  static constexpr int kEpiWarps = 16, kThreads = 32 * (2 + kEpiWarps);
+  static constexpr int kBoxBytes = 32 * 64;                         // 32 rows x 32 fp16
   static constexpr int kOutBytes = kEpiWarps * kBoxBytes;
   static constexpr int kBarriers = 2 * kStages + 4;
   static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kOutBytes + kBarriers * 8 + 16;
@@ -482,103 +532,50 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
   } else {
     const int q = warp & 3;                    // quadrant of tensor-memory lanes
-    const int half = (warp - 2) >> 2;          // which of the column chunks
     const uint32_t box = out_base + uint32_t(warp - 2) * T::kBoxBytes;
     const uint32_t acc_free = map_to_cta(acc_empty, 0);
+    const bool steps = p.x_step != nullptr || p.w_step != nullptr || p.up_step != nullptr;
     uint32_t n = 0;
     for (int tile = first; tile < tiles; tile += step, ++n) {
       const int ta = tile % p.tiles_a, tb = tile / p.tiles_a;
       const int row0 = ta * 256 + int(rank) * kTile + q * 32, m = row0 + lane;
       const float xs = p.x_step != nullptr && m < p.M ? __ldg(p.x_step + m) : 1.0f;
+      const int chunk = (warp - 2) >> 2;
+      // the chunk's first column of the output, and where its two parts of 32 columns lie in the accumulator
+      const int n0 = MODE == kLinear ? tb * 256 + 64 * chunk : tb * kTile + 32 * chunk;
+      const int col_a = MODE == kLinear ? 64 * chunk : 32 * chunk, col_b = MODE == kLinear ? col_a + 32 : 128 + col_a;
       if (!bar_wait_warp(acc_full + 8u * (n & 1u), (n >> 1) & 1u, abort_flag, kPairEpilogue)) break;
       fence_after();
       const uint32_t acc = tmem + (uint32_t(q * 32) << 16) + ((n & 1u) ? T::kSecond : 0);
-#pragma unroll 1
-      for (int i = 0; i < 2; ++i) {
-        // The shared columns are the last of the first accumulator and the first of the second.
-        const int chunk = (n & 1u) ? 2 * i + half : 3 - (2 * i + half);
-        float a[32], b[32];
-        tmem_load32(acc + (MODE == kLinear ? 64 * chunk : 32 * chunk), a);
-        tmem_load32(acc + (MODE == kLinear ? 64 * chunk + 32 : 128 + 32 * chunk), b);
-        tmem_wait_ld();
-        if (i == 0) {
-          fence_before();
-          __syncwarp();
-          if (lane == 0) bar_arrive_cluster(acc_free);
-        }
-        if constexpr (MODE == kLinear) {
-          const int n0 = tb * 256 + chunk * 64;
-          if (p.w_step != nullptr || p.x_step != nullptr) {
+      float a[32], b[32];
+      tmem_load32(acc + col_a, a);
+      tmem_load32(acc + col_b, b);
+      tmem_wait_ld();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive_cluster(acc_free);
+      if (steps) {
+        times_steps(a, xs, p.w_step, n0, p.N);
+        times_steps(b, xs, MODE == kLinear ? p.w_step : p.up_step, MODE == kLinear ? n0 + 32 : n0, p.N);
+      }
+      if constexpr (MODE == kLinear) {
+        store_box(&map_y, box, a, n0, row0, p.N, p.M, lane);
+        store_box(&map_y, box, b, n0 + 32, row0, p.N, p.M, lane);
+      } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float wa = p.w_step != nullptr && n0 + j < p.N ? __ldg(p.w_step + n0 + j) : 1.0f;
-              const float wb = p.w_step != nullptr && n0 + 32 + j < p.N ? __ldg(p.w_step + n0 + 32 + j) : 1.0f;
-              a[j] *= xs * wa;
-              b[j] *= xs * wb;
-            }
-          }
-          if (lane == 0) store_wait_read<0>();
-          __syncwarp();
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            uint32_t o[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const __half2 h = j < 4 ? __floats2half2_rn(a[8 * (j & 3) + 2 * e], a[8 * (j & 3) + 2 * e + 1])
-                                      : __floats2half2_rn(b[8 * (j & 3) + 2 * e], b[8 * (j & 3) + 2 * e + 1]);
-              o[e] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                         ::"r"(box + uint32_t(lane) * 128u + ((uint32_t(j) ^ uint32_t(lane & 7)) << 4)), "r"(o[0]), "r"(o[1]),
-                           "r"(o[2]), "r"(o[3]) : "memory");
-          }
-          fence_async();
-          __syncwarp();
-          if (lane == 0) {
-            if (n0 < p.N && row0 < p.M) tma_store(&map_y, box, n0, row0);      // clipped at the matrix's edges
-            store_commit();
-          }
+        for (int j = 0; j < 32; ++j) a[j] = silu_times(a[j], b[j]);
+        if (p.walsh) walsh_32(a, p.norm);
+        if constexpr (MODE == kGatedHalf) {
+          store_box(&map_y, box, a, n0, row0, p.N, p.M, lane);
         } else {
-          const int f0 = tb * kTile + chunk * 32;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float gs = p.w_step != nullptr && f0 + j < p.N ? __ldg(p.w_step + f0 + j) : 1.0f;
-            const float us = p.up_step != nullptr && f0 + j < p.N ? __ldg(p.up_step + f0 + j) : 1.0f;
-            a[j] = silu_times(a[j] * (xs * gs), b[j] * (xs * us));
-          }
-          if (p.walsh) walsh_32(a, p.norm);
-          if constexpr (MODE == kGatedCodes) {
-            uint4 codes;
-            const float hs = GROUP == 16 && m < p.M ? __ldg(p.h_step + m) : 1.0f;
-            const uint32_t bytes = encode_values<GROUP>(a, hs, &codes);
-            if (m < p.M && f0 < p.N) {
-              __stcs(reinterpret_cast<uint4*>(p.q_out + int64_t(m) * (p.N / 2) + f0 / 2), codes);
-              const int quads = p.N / (4 * GROUP);
-              uint8_t* to = p.scale_out + scale_word(m, f0 / (4 * GROUP), quads) + (f0 / GROUP & 3);
-              if constexpr (GROUP == 32) *to = uint8_t(bytes);
-              else *reinterpret_cast<uint16_t*>(to) = uint16_t(bytes);
-            }
-          } else {
-            if (lane == 0) store_wait_read<0>();
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              uint32_t o[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const __half2 h = __floats2half2_rn(a[8 * j + 2 * e], a[8 * j + 2 * e + 1]);
-                o[e] = *reinterpret_cast<const uint32_t*>(&h);
-              }
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                           ::"r"(box + uint32_t(lane) * 64u + ((uint32_t(j) ^ uint32_t((lane >> 1) & 3)) << 4)), "r"(o[0]),
-                             "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-            }
-            fence_async();
-            __syncwarp();
-            if (lane == 0) {
-              if (f0 < p.N && row0 < p.M) tma_store(&map_y, box, f0, row0);
-              store_commit();
-            }
+          uint4 codes;
+          const float hs = GROUP == 16 && m < p.M ? __ldg(p.h_step + m) : 1.0f;
+          const uint32_t bytes = encode_values<GROUP>(a, hs, &codes);
+          if (m < p.M && n0 < p.N) {
+            __stcs(reinterpret_cast<uint4*>(p.q_out + int64_t(m) * (p.N / 2) + n0 / 2), codes);
+            uint8_t* to = p.scale_out + scale_word(m, n0 / (4 * GROUP), p.N / (4 * GROUP)) + (n0 / GROUP & 3);
+            if constexpr (GROUP == 32) *to = uint8_t(bytes);
+            else *reinterpret_cast<uint16_t*>(to) = uint16_t(bytes);
           }
         }
       }
@@ -610,8 +607,10 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // shared memory, and after a cluster barrier each adds up some of the tokens over all parts, in the parts' order: the
 // same bits from call to call.  A warp finishes 32 channels of a token, a group of the next layer's codes.
 //
-// Warps: 0 TMA, 1 products, 2..5 read the accumulator; all six finish.
+// Warps: 0 TMA, 1 products, 2..9 read the accumulator, two to a quadrant of its lanes, and finish.
 // ---------------------------------------------------------------------------
+constexpr int kStreamThreads = 320;
+
 template <int GROUP, int BN, bool GATED>
 struct Stream {
   static constexpr int kMats = GATED ? 2 : 1;
@@ -620,7 +619,7 @@ struct Stream {
   static constexpr int kTokenBytes = BN * kRowBytes;
   static constexpr int kStageBytes = kMats * (kTileBytes + kScaleBytes) + kTokenBytes + kScaleBytes;
   static constexpr int kStages = 200 * 1024 / kStageBytes;
-  static constexpr int kThreads = 192;
+  static constexpr int kThreads = kStreamThreads;
   static constexpr int kBarriers = 2 * kStages + 1;
   static constexpr int kRingBytes = kStages * kStageBytes;
   static constexpr int kSumBytes = kMats * BN * kTile * 4;       // over the ring, once it has been used
@@ -663,7 +662,7 @@ __device__ __forceinline__ void stream_block(uint32_t acc, uint32_t src, uint32_
 }
 
 template <int GROUP, int BN, int MODE>
-__global__ void __launch_bounds__(192, 1)
+__global__ void __launch_bounds__(kStreamThreads, 1)
 mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u,
                  const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_sw,
                  const __grid_constant__ CUtensorMap map_su, const __grid_constant__ CUtensorMap map_sx, const Args p,
@@ -686,26 +685,24 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   const int tile = int(blockIdx.x) / parts;
   const int m0 = int(blockIdx.y) * BN, n0 = tile * kTile;
   const int k0 = int(int64_t(p.kblocks) * part / parts), k1 = int(int64_t(p.kblocks) * (part + 1) / parts);
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < T::kStages; ++s) {
-      bar_init(full(s), 1);
-      bar_init(empty(s), 1);
-    }
-    bar_init(done, 1);
-    *abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    fence_async();
-  }
-  if (warp == 1) tmem_alloc<1>(smem_u32(tmem_slot), T::kTmemCols);
-  fence_before();
-  __syncthreads();
-  fence_after();
-  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-
+  auto set_up = [] { asm volatile("bar.sync 1, %0;" ::"n"(kStreamThreads) : "memory"); };
+  // Warp 0 sets up the barriers and has loads on their way before the others have their tensor memory.
   if (warp == 0) {
     const bool one = elected();
+    if (one) {
+      for (int s = 0; s < T::kStages; ++s) {
+        bar_init(full(s), 1);
+        bar_init(empty(s), 1);
+      }
+      bar_init(done, 1);
+      *abort_flag = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      fence_async();
+    }
+    __syncwarp();
     Ring<T::kStages> r;
     for (int kb = k0; kb < k1; ++kb, r.next()) {
+      if (kb == k0 + T::kStages) set_up();       // the others may go on: the ring's first round is under way
       if (!bar_wait_warp(empty(r.s), r.phase ^ 1u, abort_flag, kStreamLoad)) break;
       if (one) {
         const uint32_t bar = full(r.s);
@@ -721,6 +718,16 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       }
       __syncwarp();
     }
+    if (k1 - k0 <= T::kStages) set_up();
+  } else {
+    if (warp == 1) tmem_alloc<1>(smem_u32(tmem_slot), T::kTmemCols);
+    fence_before();
+    set_up();
+    fence_after();
+  }
+  const uint32_t tmem = warp == 0 ? 0u : __shfl_sync(0xffffffffu, *tmem_slot, 0);
+
+  if (warp == 0) {
   } else if (warp == 1) {
     const bool one = elected();
     const uint32_t sa = tmem + T::kScaleCol;
@@ -745,18 +752,19 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   } else if (bar_wait_warp(done, 0, abort_flag, kStreamEpilogue)) {
     // the ring has been read to its end: the sums take its place, [matrix][token][channel]
     fence_after();
-    const int q = warp & 3;
+    const int q = warp & 3, half = (warp - 2) >> 2;
     const uint32_t acc = tmem + (uint32_t(q * 32) << 16);
     float* sums = reinterpret_cast<float*>(smem) + q * 32 + lane;
     const int cols = min(BN, p.M - m0);
+    constexpr int kRead = BN >= 32 ? 16 : 8;       // tokens at a time
 #pragma unroll 1
-    for (int c = 0; c < T::kMats * BN; c += 16) {
+    for (int c = half * kRead; c < T::kMats * BN; c += 2 * kRead) {
       if ((c & (BN - 1)) >= cols) continue;
-      float v[16];
-      tmem_load16(acc + c, v);
+      float v[kRead];
+      tmem_load(acc + c, v);
       tmem_wait_ld();
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sums[(c + i) * kTile] = v[i];
+      for (int i = 0; i < kRead; ++i) sums[(c + i) * kTile] = v[i];
     }
   }
   drain_after_abort(abort_flag);
@@ -764,56 +772,73 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   __syncwarp();
   if (parts > 1) cluster_sync();
   else __syncthreads();
-  if (*abort_flag == 0) {
-    const uint32_t mine = base + uint32_t(lane) * 4u;
-    const int cols = min(BN, p.M - m0);
-    for (int unit = warp; ; unit += T::kThreads / 32) {
-      const int c = (unit >> 2) * parts + part, g = unit & 3;
-      if (c >= cols) break;
-      const int m = m0 + c, n = n0 + g * 32 + lane;
-      if (n - lane >= p.N) continue;
-      const bool on = n < p.N;
-      float a = 0.0f, b = 0.0f;
-      const uint32_t at = mine + uint32_t((c * kTile + g * 32) * 4);
-      for (int r = 0; r < parts; ++r) {
-        const uint32_t src = parts > 1 ? map_to_cta(at, r) : at;
-        a += load_cluster(src);
-        if (GATED) b += load_cluster(src + uint32_t(BN * kTile * 4));
-      }
-      const float xs = p.x_step != nullptr ? __ldg(p.x_step + m) : 1.0f;
-      a *= xs * (on && p.w_step != nullptr ? __ldg(p.w_step + n) : 1.0f);
-      if constexpr (GATED) {
-        b *= xs * (on && p.up_step != nullptr ? __ldg(p.up_step + n) : 1.0f);
-        a = silu_times(a, b);
-        if (p.walsh) {
+  if (*abort_flag == 0 && warp >= 2) {
+    // this CTA's tokens are m0 + part, m0 + part + parts, ..; four of them at a time, a lane per channel
+    const int g = warp & 3, cols = min(BN, p.M - m0), n = n0 + g * 32 + lane;
+    const bool on = n < p.N;
+    if (n - lane < p.N) {
+      const float ws = on && p.w_step != nullptr ? __ldg(p.w_step + n) : 1.0f;
+      const float us = GATED && on && p.up_step != nullptr ? __ldg(p.up_step + n) : 1.0f;
+      const uint32_t mine = base + uint32_t((g * 32 + lane) * 4);
+      constexpr int U = 4;
+      for (int i0 = (warp - 2) >> 2; i0 * parts + part < cols; i0 += 2 * U) {
+        float a[U], b[U];
+        int m[U];
 #pragma unroll
-          for (int x = 1; x < 32; x *= 2) a = __fmaf_rn((lane & x) ? -1.0f : 1.0f, a, __shfl_xor_sync(0xffffffffu, a, x));
-          a = __fmul_rn(a, p.norm);
+        for (int u = 0; u < U; ++u) {
+          m[u] = (i0 + 2 * u) * parts + part;        // past the last token: its place, and nothing is written
+          a[u] = 0.0f;
+          b[u] = 0.0f;
         }
-      }
-      if constexpr (MODE == kGatedCodes) {
-        uint32_t top = abs_bits(a), byte;
+        for (int r = 0; r < parts; ++r) {
 #pragma unroll
-        for (int x = 1; x < GROUP; x *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
-        float v;
-        if constexpr (GROUP == 32) {
-          byte = scale_byte_32(top);
-          v = __fmul_rn(a, inverse_scale_32(byte));
-        } else {
-          const float hs = __ldg(p.h_step + m);
-          byte = to_e4m3(__fdiv_rn(__uint_as_float(top), __fmul_rn(6.0f, hs)));
-          const float d = __fmul_rn(from_e4m3(byte), hs);
-          v = quotient(a, d, d == 0.0f ? 0.0f : __frcp_rn(d));
+          for (int u = 0; u < U; ++u) {
+            const uint32_t at = mine + uint32_t(min(m[u], cols - 1) * kTile * 4);
+            const uint32_t src = parts > 1 ? map_to_cta(at, r) : at;
+            a[u] += load_cluster(src);
+            if (GATED) b[u] += load_cluster(src + uint32_t(BN * kTile * 4));
+          }
         }
-        float q[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = __shfl_sync(0xffffffffu, v, (lane & 3) * 8 + i);
-        const uint32_t word = to_codes(q);
-        if (lane < 4) *reinterpret_cast<uint32_t*>(p.q_out + int64_t(m) * (p.N / 2) + (n - lane) / 2 + lane * 4) = word;
-        if ((lane & (GROUP - 1)) == 0)
-          p.scale_out[scale_word(m, n / (4 * GROUP), p.N / (4 * GROUP)) + (n / GROUP & 3)] = uint8_t(byte);
-      } else {
-        if (on) p.y[int64_t(m) * p.ldy + n] = __float2half_rn(a);
+        for (int u = 0; u < U; ++u) {
+          const bool there = m[u] < cols;
+          m[u] = m0 + min(m[u], cols - 1);
+          const float xs = p.x_step != nullptr ? __ldg(p.x_step + m[u]) : 1.0f;
+          float h = a[u] * (xs * ws);
+          if constexpr (GATED) {
+            h = silu_times(h, b[u] * (xs * us));
+            if (p.walsh) {
+#pragma unroll
+              for (int x = 1; x < 32; x *= 2) h = __fmaf_rn((lane & x) ? -1.0f : 1.0f, h, __shfl_xor_sync(0xffffffffu, h, x));
+              h = __fmul_rn(h, p.norm);
+            }
+          }
+          if constexpr (MODE == kGatedCodes) {
+            uint32_t top = abs_bits(h), byte;
+#pragma unroll
+            for (int x = 1; x < GROUP; x *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
+            float v;
+            if constexpr (GROUP == 32) {
+              byte = scale_byte_32(top);
+              v = __fmul_rn(h, inverse_scale_32(byte));
+            } else {
+              const float hs = __ldg(p.h_step + m[u]);
+              byte = to_e4m3(__fdiv_rn(__uint_as_float(top), __fmul_rn(6.0f, hs)));
+              const float d = __fmul_rn(from_e4m3(byte), hs);
+              v = quotient(h, d, d == 0.0f ? 0.0f : __frcp_rn(d));
+            }
+            float c8[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c8[i] = __shfl_sync(0xffffffffu, v, (lane & 3) * 8 + i);
+            const uint32_t word = to_codes(c8);
+            if (there && lane < 4)
+              *reinterpret_cast<uint32_t*>(p.q_out + int64_t(m[u]) * (p.N / 2) + (n - lane) / 2 + lane * 4) = word;
+            if (there && (lane & (GROUP - 1)) == 0)
+              p.scale_out[scale_word(m[u], n / (4 * GROUP), p.N / (4 * GROUP)) + (n / GROUP & 3)] = uint8_t(byte);
+          } else {
+            if (there && on) p.y[int64_t(m[u]) * p.ldy + n] = __float2half_rn(h);
+          }
+        }
       }
     }
   }
@@ -863,13 +888,13 @@ bool map_scales(CUtensorMap* map, const uint8_t* p, int64_t rows, int64_t K, int
                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// fp16 output [M x N], boxes of 32 rows and `cols` columns for stores.
-bool map_half(CUtensorMap* map, __half* y, int64_t M, int64_t N, int64_t ldy, int cols) {
+// fp16 output [M x N], boxes of 32 rows and 32 columns for stores.
+bool map_half(CUtensorMap* map, __half* y, int64_t M, int64_t N, int64_t ldy) {
   const cuuint64_t dims[2] = {cuuint64_t(N), cuuint64_t(M)};
   const cuuint64_t strides[1] = {cuuint64_t(ldy) * sizeof(__half)};
-  const cuuint32_t boxes[2] = {cuuint32_t(cols), 32}, ones[2] = {1, 1};
+  const cuuint32_t boxes[2] = {32, 32}, ones[2] = {1, 1};
   return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, y, dims, strides, boxes, ones,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
                               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -892,7 +917,7 @@ int launch_pair(const Call& c) {
   su = sb;
   if (gated && (!map_codes(&u, c.u, c.N, c.K, kTile) || !map_scales(&su, c.su, c.N, c.K, GROUP))) return SMOOTHROT_CUDA_ERROR;
   y = a;
-  if (MODE != kGatedCodes && !map_half(&y, c.args.y, c.M, c.N, c.args.ldy, gated ? 32 : 64)) return SMOOTHROT_CUDA_ERROR;
+  if (MODE != kGatedCodes && !map_half(&y, c.args.y, c.M, c.N, c.args.ldy)) return SMOOTHROT_CUDA_ERROR;
   Args p = c.args;
   const int width = gated ? kTile : 256;
   p.tiles_a = int((c.M + 255) / 256);
@@ -954,6 +979,13 @@ int check_operand(const uint8_t* q, const uint8_t* s) {
   return aligned16(q) && aligned16(s) ? SMOOTHROT_OK : SMOOTHROT_BAD_ALIGNMENT;
 }
 
+// a step per row, read four at a time where it is the weights'
+bool bad_steps(std::initializer_list<const float*> steps) {
+  for (const float* p : steps)
+    if (p != nullptr && !aligned16(p)) return true;
+  return false;
+}
+
 int check_sizes(int64_t M, int64_t N, int64_t K, int64_t group) {
   if (M < 0 || N < 0 || K <= 0 || !group_ok(group)) return SMOOTHROT_INVALID_ARG;
   if (K % 128 != 0 || K > (int64_t(1) << 20)) return SMOOTHROT_UNSUPPORTED_K;
@@ -999,7 +1031,7 @@ int smoothrot_mx_linear(const uint8_t* Xq, const uint8_t* x_scale, const float* 
   if (rc != SMOOTHROT_OK || M == 0 || N == 0) return rc;
   if (Y_f16 == nullptr || ldy < N) return SMOOTHROT_INVALID_ARG;
   if ((rc = check_operand(Xq, x_scale)) != SMOOTHROT_OK || (rc = check_operand(Wq, w_scale)) != SMOOTHROT_OK) return rc;
-  if (!aligned16(Y_f16) || ldy % 8 != 0) return SMOOTHROT_BAD_ALIGNMENT;
+  if (!aligned16(Y_f16) || ldy % 8 != 0 || bad_steps({w_step})) return SMOOTHROT_BAD_ALIGNMENT;
   if (tensor_map_encoder() == nullptr) return SMOOTHROT_CUDA_ERROR;
   Call c{Xq, x_scale, Wq, w_scale, nullptr, nullptr, M, N, K, Args{}, static_cast<cudaStream_t>(stream)};
   c.args.M = int(M);
@@ -1032,6 +1064,7 @@ int smoothrot_mx_glu(const uint8_t* Xq, const uint8_t* x_scale, const float* x_s
       (rc = check_operand(up_q, up_scale)) != SMOOTHROT_OK)
     return rc;
   if (codes ? !aligned16(q_out) || !aligned16(scale_out) : !aligned16(H_f16) || ldh % 8 != 0) return SMOOTHROT_BAD_ALIGNMENT;
+  if (bad_steps({gate_step, up_step})) return SMOOTHROT_BAD_ALIGNMENT;
   if (tensor_map_encoder() == nullptr) return SMOOTHROT_CUDA_ERROR;
   Call c{Xq, x_scale, gate_q, gate_scale, up_q, up_scale, M, F, K, Args{}, static_cast<cudaStream_t>(stream)};
   c.args.M = int(M);
