@@ -508,7 +508,7 @@ int smoothrot_debug_gemm_i32(const uint8_t* Xq, int64_t M, const uint8_t* Wq, in
  *     records code 7 in the status word smoothrot_device_status reads, and the kernel returns.
  *   smoothrot_debug_attn_wait_expiry: the same through the waits of the attention kernels; `code` is the one to record,
  *     36 to 40 for smoothrot_attn_prefill's and 41 for smoothrot_attn_decode's.
- *   smoothrot_debug_mx_wait_expiry: the same through the waits of the microscaled products, code 49.
+ *   smoothrot_debug_mx_wait_expiry: the same through the waits of the microscaled products, code 50.
  */
 int smoothrot_debug_set_wait_limit_ns(uint64_t ns);
 int smoothrot_debug_wait_expiry(void* stream);
@@ -527,7 +527,7 @@ int smoothrot_base_matrix(int order, int8_t* out_host);
 /*
  * Host, synchronous.  Kernels never spin without bound: a wait that runs out
  * records a non-zero code in a device-side status word and the kernel
- * returns (42 to 48 in the microscaled products); the cache and attention calls record 32 to 35 for a slot, position, page or
+ * returns (42 to 49 in the microscaled products); the cache and attention calls record 32 to 35 for a slot, position, page or
  * length out of range.  This call copies that word for the current device into
  * *status_host (0 = none so far) and clears it when `clear` is non-zero.
  */

@@ -525,7 +525,7 @@ def debug_attn_wait_expiry(code: int) -> None:
 
 
 def debug_mx_wait_expiry() -> None:
-    """The same through the waits of the microscaled products (code 49)."""
+    """The same through the waits of the microscaled products (code 50)."""
     _check(load().smoothrot_debug_mx_wait_expiry(_stream()))
 
 

@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a)
     for (int c = 0; c < CH; ++c) h[c] = a.h != nullptr && t + c * T < chunks ? __ldcs(hs + t + c * T) : zero;
   };
   int m = blockIdx.x;
+  after_the_call_before();
   if (m < a.rows) fetch(m);
   // the sums' slots of one row and the next are two sets in turn
   for (int parity = 0; m < a.rows; m += gridDim.x, parity ^= 1) {
@@ -285,16 +286,12 @@ int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_
   const int T = ((chunks + ch - 1) / ch + 31) / 32 * 32;
   const int64_t cap = sms * (1024 / T > 0 ? 1024 / T : 1);
   const int64_t grid = M < cap ? M : cap;
-  auto launch = [&](auto kern) {
-    kern<<<unsigned(grid), unsigned(T), 0, static_cast<cudaStream_t>(stream)>>>(a);
-    count_launch();
-    return launch_status();
-  };
+  auto go = [&](auto kern) { return launch(kern, dim3(unsigned(grid)), T, 0, 0, static_cast<cudaStream_t>(stream), a); };
   switch (codes) {
-    case 0: return ch == 1 ? launch(add_norm_kernel<0, 1>) : launch(add_norm_kernel<0, 4>);
-    case 4: return ch == 1 ? launch(add_norm_kernel<4, 1>) : launch(add_norm_kernel<4, 4>);
-    case 16: return ch == 1 ? launch(add_norm_kernel<16, 1>) : launch(add_norm_kernel<16, 4>);
-    default: return ch == 1 ? launch(add_norm_kernel<32, 1>) : launch(add_norm_kernel<32, 4>);
+    case 0: return ch == 1 ? go(add_norm_kernel<0, 1>) : go(add_norm_kernel<0, 4>);
+    case 4: return ch == 1 ? go(add_norm_kernel<4, 1>) : go(add_norm_kernel<4, 4>);
+    case 16: return ch == 1 ? go(add_norm_kernel<16, 1>) : go(add_norm_kernel<16, 4>);
+    default: return ch == 1 ? go(add_norm_kernel<32, 1>) : go(add_norm_kernel<32, 4>);
   }
 }
 

@@ -24,7 +24,41 @@ __host__ __device__ __forceinline__ int64_t scale_word(int64_t row, int quad, in
   return ((row >> 7) * quads + quad) * kAtomBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
 }
 
+// Host: launches such a kernel, in clusters of `cluster` CTAs (0: as the kernel says).  A chain of short calls takes a
+// microsecond less for each.
+template <typename... Params, typename... Given>
+inline int launch(void (*kern)(Params...), dim3 grid, int threads, int smem, int cluster, cudaStream_t stream, Given&&... given) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(unsigned(threads), 1, 1);
+  cfg.dynamicSmemBytes = size_t(smem);
+  cfg.stream = stream;
+  cudaLaunchAttribute attrs[2] = {};
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = unsigned(cluster);
+  attrs[1].val.clusterDim.y = 1;
+  attrs[1].val.clusterDim.z = 1;
+  cfg.attrs = attrs;
+  cfg.numAttrs = cluster > 0 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kern, given...) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SMOOTHROT_CUDA_ERROR;
+  }
+  count_launch();
+  return launch_status();
+}
+
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Kernels of this kind are launched so that one may be set up while the one before it in the stream finishes; each
+// waits here, before it reads or writes what others may use.
+// The wait comes first: a call that follows and waits for the end of this one has then waited for all before it too.
+__device__ __forceinline__ void after_the_call_before() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 
 // Eight values to eight codes, round to nearest, ties to the even code, saturating at 6.
 __device__ __forceinline__ uint32_t to_codes(const float (&q)[8]) {

@@ -27,7 +27,7 @@ __device__ int g_mx_status = 0;
 __device__ unsigned long long g_mx_wait_limit_ns = kWaitLimitNs;
 
 enum Site { kPairLoad = 42, kPairAcc = 43, kPairFull = 44, kPairEpilogue = 45, kStreamLoad = 46, kStreamFull = 47,
-            kStreamEpilogue = 48, kProbe = 49 };
+            kStreamMixed = 48, kStreamEpilogue = 49, kProbe = 50 };
 
 namespace {
 
@@ -455,6 +455,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     fence_async();
   }
   if (warp == 1) tmem_alloc<2>(smem_u32(tmem_slot), 512);
+  after_the_call_before();
   fence_before();
   __syncthreads();
   cluster_sync();
@@ -602,33 +603,38 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // Few tokens: the weights on the 128-row axis, BN tokens on the other.
 //
 // The one pass over the weights is what such a call costs, so the kernel keeps as much of it in flight as shared memory holds:
-// a ring of 16 KB weight tiles (gated: one of each projection) with their scales, and the tokens' BN rows beside them.
-// One CTA computes a tile of 128 channels over one part of K; the parts of a tile are a cluster, leave their sums in their own
-// shared memory, and after a cluster barrier each adds up some of the tokens over all parts, in the parts' order: the
-// same bits from call to call.  A warp finishes 32 channels of a token, a group of the next layer's codes.
+// a ring of 16 KB weight tiles with their scales, and the tokens' BN rows beside them.  A gated tile is 64 rows of the gate and
+// the 64 rows of the up projection beside it; a warp puts its block of scales together from the halves of the two that hold
+// them (a copy to tensor memory starts at a multiple of 4 columns, so halves cannot be laid side by side there).  One CTA computes a tile over one part of K; the parts of a tile are a
+// cluster, leave their sums in their own shared memory, and after a cluster barrier each adds up some of the tokens over all
+// parts, in the parts' order: the same bits from call to call.  A warp finishes 32 channels of a token, a group of the
+// next layer's codes.
 //
-// Warps: 0 TMA, 1 products, 2..9 read the accumulator, two to a quadrant of its lanes, and finish.
+// Two CTAs fit an SM, which evens out tiles that are not a multiple of the SMs, and lets a call's first loads be issued
+// while the call before is finishing.
+//
+// Warps: 0 TMA, 1 products, 2..9 read the accumulator, two to a quadrant of its lanes, and finish; 2 mixes scales before.
 // ---------------------------------------------------------------------------
 constexpr int kStreamThreads = 320;
 
 template <int GROUP, int BN, bool GATED>
 struct Stream {
-  static constexpr int kMats = GATED ? 2 : 1;
   static constexpr int kAtoms = kBlockK / GROUP / kAtomGroups;
   static constexpr int kScaleBytes = kAtoms * kAtomBytes;
   static constexpr int kTokenBytes = BN * kRowBytes;
-  static constexpr int kStageBytes = kMats * (kTileBytes + kScaleBytes) + kTokenBytes + kScaleBytes;
-  static constexpr int kStages = 200 * 1024 / kStageBytes;
-  static constexpr int kThreads = kStreamThreads;
-  static constexpr int kBarriers = 2 * kStages + 1;
+  static constexpr int kScales = GATED ? 3 : 2;                  // weights' (gate's and up's), tokens'
+  static constexpr int kStageBytes = kTileBytes + kTokenBytes + kScales * kScaleBytes;
+  static constexpr int kStages = 110 * 1024 / kStageBytes;
+  static constexpr int kTileRows = GATED ? kTile / 2 : kTile;    // output channels of a tile
+  static constexpr int kBarriers = (GATED ? 3 : 2) * kStages + 1;
   static constexpr int kRingBytes = kStages * kStageBytes;
-  static constexpr int kSumBytes = kMats * BN * kTile * 4;       // over the ring, once it has been used
+  static constexpr int kSumBytes = BN * kTile * 4;               // over the ring, once it has been used
   static constexpr int kSmemBytes = 1024 + kRingBytes + kBarriers * 8 + 16;
-  static constexpr int kScaleCol = kMats * BN;
-  static constexpr int kCols = kScaleCol + 4 * kAtoms * (kMats + 1);
-  static constexpr int kTmemCols = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static_assert(kCols <= 512, "tensor memory");
-  static_assert(kSumBytes <= kRingBytes && kSmemBytes <= 227 * 1024, "shared memory");
+  static constexpr int kScaleCol = BN;
+  static constexpr int kCols = kScaleCol + 8 * kAtoms;           // weights' scales, tokens' scales
+  static constexpr int kTmemCols = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
+  static_assert(kCols <= 256, "tensor memory of two CTAs");
+  static_assert(kSumBytes <= kRingBytes && 2 * (kSmemBytes + 1024) <= 228 * 1024, "shared memory of two CTAs");
   static_assert(kStageBytes % 1024 == 0, "swizzled tiles start on 1024 bytes");
 };
 
@@ -643,26 +649,37 @@ template <int GROUP, int BN, bool GATED, int STEPS>
 __device__ __forceinline__ void stream_block(uint32_t acc, uint32_t src, uint32_t sa, bool fresh) {
   using T = Stream<GROUP, BN, GATED>;
   constexpr int per = kStepsPerBlock / T::kAtoms;
-  const uint32_t tokens = src + T::kMats * kTileBytes / 16, sc = tokens + T::kTokenBytes / 16;
-  const uint32_t sb = sa + 4 * T::kAtoms * T::kMats;       // the tokens' scales follow the weights'
+  const uint32_t tokens = src + kTileBytes / 16, sc = tokens + T::kTokenBytes / 16;
+  const uint32_t sb = sa + 4 * T::kAtoms;
 #pragma unroll
   for (int j = 0; j < STEPS; ++j) {
     const int atom = j / per;
     if (j % per == 0) {
-#pragma unroll
-      for (int w = 0; w <= T::kMats; ++w)
-        copy_scales<1>(sa + 4 * (T::kAtoms * w + atom), sc + (w * T::kScaleBytes + atom * kAtomBytes) / 16);
+      copy_scales<1>(sa + 4 * atom, sc + atom * (kAtomBytes / 16));
+      copy_scales<1>(sb + 4 * atom, sc + ((T::kScales - 1) * T::kScaleBytes + atom * kAtomBytes) / 16);
     }
+    mma<GROUP, 1>(acc, src + 2 * j, tokens + 2 * j, instruction<GROUP>(128, BN, GROUP == 32 ? 2 * (j % 2) : 0), sa + 4 * atom,
+                  sb + 4 * atom, j > 0 || !fresh);
+  }
+}
+
+// A gated tile's scales: of every line of 16 bytes (4 words, 32 rows apart) the gate's two words of this half of 128 features
+// and then the up projection's two, in the gate's place.
+template <int BYTES>
+__device__ __forceinline__ void mix_scales(uint32_t gate, uint32_t up, bool upper, int lane) {
 #pragma unroll
-    for (int w = 0; w < T::kMats; ++w)
-      mma<GROUP, 1>(acc + w * BN, src + (w * kTileBytes) / 16 + 2 * j, tokens + 2 * j,
-                    instruction<GROUP>(128, BN, GROUP == 32 ? 2 * (j % 2) : 0), sa + 4 * (T::kAtoms * w + atom), sb + 4 * atom,
-                    j > 0 || !fresh);
+  for (int i = 0; i < BYTES; i += 512) {
+    const uint32_t half = uint32_t(i + lane * 16) + (upper ? 8u : 0u);
+    uint32_t g0, g1, u0, u1;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(g0), "=r"(g1) : "r"(gate + half) : "memory");
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(u0), "=r"(u1) : "r"(up + half) : "memory");
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(gate + uint32_t(i + lane * 16)), "r"(g0), "r"(g1), "r"(u0), "r"(u1)
+                 : "memory");
   }
 }
 
 template <int GROUP, int BN, int MODE>
-__global__ void __launch_bounds__(kStreamThreads, 1)
+__global__ void __launch_bounds__(kStreamThreads, 2)
 mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u,
                  const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_sw,
                  const __grid_constant__ CUtensorMap map_su, const __grid_constant__ CUtensorMap map_sx, const Args p,
@@ -676,14 +693,15 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   const uint32_t bar_base = base + T::kRingBytes;
   auto full = [&](int s) { return bar_base + 8u * s; };
   auto empty = [&](int s) { return bar_base + 8u * (T::kStages + s); };
-  const uint32_t done = bar_base + 8u * (2 * T::kStages);
+  auto mixed = [&](int s) { return bar_base + 8u * (2 * T::kStages + s); };      // gated tiles' scales
+  const uint32_t done = bar_base + 8u * (T::kBarriers - 1);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + T::kRingBytes + 8 * T::kBarriers);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = warp_number(), lane = threadIdx.x & 31;
   const int part = int(blockIdx.x) % parts;                 // rank in the cluster
   const int tile = int(blockIdx.x) / parts;
-  const int m0 = int(blockIdx.y) * BN, n0 = tile * kTile;
+  const int m0 = int(blockIdx.y) * BN, n0 = tile * T::kTileRows;
   const int k0 = int(int64_t(p.kblocks) * part / parts), k1 = int(int64_t(p.kblocks) * (part + 1) / parts);
   auto set_up = [] { asm volatile("bar.sync 1, %0;" ::"n"(kStreamThreads) : "memory"); };
   // Warp 0 sets up the barriers and has loads on their way before the others have their tensor memory.
@@ -693,6 +711,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       for (int s = 0; s < T::kStages; ++s) {
         bar_init(full(s), 1);
         bar_init(empty(s), 1);
+        if (GATED) bar_init(mixed(s), 1);
       }
       bar_init(done, 1);
       *abort_flag = 0;
@@ -700,6 +719,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       fence_async();
     }
     __syncwarp();
+    after_the_call_before();
     Ring<T::kStages> r;
     for (int kb = k0; kb < k1; ++kb, r.next()) {
       if (kb == k0 + T::kStages) set_up();       // the others may go on: the ring's first round is under way
@@ -707,34 +727,35 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       if (one) {
         const uint32_t bar = full(r.s);
         bar_expect(bar, uint32_t(T::kStageBytes));
-        const uint32_t dst = base + r.s * T::kStageBytes, sc = dst + T::kMats * kTileBytes + T::kTokenBytes;
+        const uint32_t dst = base + r.s * T::kStageBytes, sc = dst + kTileBytes + T::kTokenBytes;
         const int x = kb * (T::kScaleBytes / 8);
         tma_load(dst, &map_w, bar, kb * kRowBytes, n0);
-        if (GATED) tma_load(dst + kTileBytes, &map_u, bar, kb * kRowBytes, n0);
-        tma_load(dst + T::kMats * kTileBytes, &map_x, bar, kb * kRowBytes, m0);
-        tma_load(sc, &map_sw, bar, x, tile);
-        if (GATED) tma_load(sc + T::kScaleBytes, &map_su, bar, x, tile);
-        tma_load(sc + T::kMats * T::kScaleBytes, &map_sx, bar, x, m0 / kTile);
+        if (GATED) tma_load(dst + kTileBytes / 2, &map_u, bar, kb * kRowBytes, n0);
+        tma_load(dst + kTileBytes, &map_x, bar, kb * kRowBytes, m0);
+        tma_load(sc, &map_sw, bar, x, n0 / kTile);
+        if (GATED) tma_load(sc + T::kScaleBytes, &map_su, bar, x, n0 / kTile);
+        tma_load(sc + (T::kScales - 1) * T::kScaleBytes, &map_sx, bar, x, m0 / kTile);
       }
       __syncwarp();
     }
     if (k1 - k0 <= T::kStages) set_up();
   } else {
     if (warp == 1) tmem_alloc<1>(smem_u32(tmem_slot), T::kTmemCols);
+    after_the_call_before();
     fence_before();
     set_up();
     fence_after();
   }
   const uint32_t tmem = warp == 0 ? 0u : __shfl_sync(0xffffffffu, *tmem_slot, 0);
 
-  if (warp == 0) {
-  } else if (warp == 1) {
+  if (warp == 1) {
     const bool one = elected();
     const uint32_t sa = tmem + T::kScaleCol;
     Ring<T::kStages> r;
     bool ok = true;
     for (int kb = k0; kb < k1; ++kb, r.next()) {
       ok = bar_wait_warp(full(r.s), r.phase, abort_flag, kStreamFull);
+      if (GATED) ok = ok && bar_wait_warp(mixed(r.s), r.phase, abort_flag, kStreamMixed);
       if (!ok) break;
       fence_after();
       if (one) {
@@ -749,8 +770,19 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     }
     if (ok && one) commit(done);
     __syncwarp();
-  } else if (bar_wait_warp(done, 0, abort_flag, kStreamEpilogue)) {
-    // the ring has been read to its end: the sums take its place, [matrix][token][channel]
+  } else if (GATED && warp == 2) {
+    Ring<T::kStages> r;
+    for (int kb = k0; kb < k1; ++kb, r.next()) {
+      if (!bar_wait_warp(full(r.s), r.phase, abort_flag, kStreamMixed)) break;
+      const uint32_t sc = base + r.s * T::kStageBytes + kTileBytes + T::kTokenBytes;
+      mix_scales<T::kScaleBytes>(sc, sc + T::kScaleBytes, (tile & 1) != 0, lane);
+      fence_async();
+      __syncwarp();
+      if (lane == 0) bar_arrive_cluster(mixed(r.s));
+    }
+  }
+  if (warp >= 2 && bar_wait_warp(done, 0, abort_flag, kStreamEpilogue)) {
+    // the ring has been read to its end: the sums take its place, [token][row of the tile]
     fence_after();
     const int q = warp & 3, half = (warp - 2) >> 2;
     const uint32_t acc = tmem + (uint32_t(q * 32) << 16);
@@ -758,8 +790,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const int cols = min(BN, p.M - m0);
     constexpr int kRead = BN >= 32 ? 16 : 8;       // tokens at a time
 #pragma unroll 1
-    for (int c = half * kRead; c < T::kMats * BN; c += 2 * kRead) {
-      if ((c & (BN - 1)) >= cols) continue;
+    for (int c = half * kRead; c < cols; c += 2 * kRead) {
       float v[kRead];
       tmem_load(acc + c, v);
       tmem_wait_ld();
@@ -773,20 +804,22 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   if (parts > 1) cluster_sync();
   else __syncthreads();
   if (*abort_flag == 0 && warp >= 2) {
-    // this CTA's tokens are m0 + part, m0 + part + parts, ..; four of them at a time, a lane per channel
-    const int g = warp & 3, cols = min(BN, p.M - m0), n = n0 + g * 32 + lane;
+    // This CTA's tokens are m0 + part, m0 + part + parts, ..; four of them at a time, a lane per channel.  Eight warps share
+    // the tile's groups of 32 channels: 4, or 2 of a gated tile.
+    constexpr int kGroups = T::kTileRows / 32, kTeams = 8 / kGroups;
+    const int g = warp & (kGroups - 1), cols = min(BN, p.M - m0), n = n0 + g * 32 + lane;
     const bool on = n < p.N;
     if (n - lane < p.N) {
       const float ws = on && p.w_step != nullptr ? __ldg(p.w_step + n) : 1.0f;
       const float us = GATED && on && p.up_step != nullptr ? __ldg(p.up_step + n) : 1.0f;
       const uint32_t mine = base + uint32_t((g * 32 + lane) * 4);
       constexpr int U = 4;
-      for (int i0 = (warp - 2) >> 2; i0 * parts + part < cols; i0 += 2 * U) {
+      for (int i0 = (warp - 2) / kGroups; i0 * parts + part < cols; i0 += kTeams * U) {
         float a[U], b[U];
         int m[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          m[u] = (i0 + 2 * u) * parts + part;        // past the last token: its place, and nothing is written
+          m[u] = (i0 + kTeams * u) * parts + part;   // past the last token: that one's place, and nothing is written
           a[u] = 0.0f;
           b[u] = 0.0f;
         }
@@ -796,7 +829,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint32_t at = mine + uint32_t(min(m[u], cols - 1) * kTile * 4);
             const uint32_t src = parts > 1 ? map_to_cta(at, r) : at;
             a[u] += load_cluster(src);
-            if (GATED) b[u] += load_cluster(src + uint32_t(BN * kTile * 4));
+            if (GATED) b[u] += load_cluster(src + uint32_t(kTile / 2 * 4));
           }
         }
 #pragma unroll
@@ -925,47 +958,31 @@ int launch_pair(const Call& c) {
   auto kern = mx_pair_kernel<GROUP, MODE>;
   if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), T::kSmemBytes)) return SMOOTHROT_CUDA_ERROR;
   const int64_t tiles = int64_t(p.tiles_a) * p.tiles_b, pairs = device_sm_count() / 2;
-  kern<<<unsigned(2 * (tiles < pairs ? tiles : pairs)), T::kThreads, T::kSmemBytes, c.stream>>>(a, b, u, sa, sb, su, y, p);
-  count_launch();
-  return launch_status();
+  return launch(kern, dim3(unsigned(2 * (tiles < pairs ? tiles : pairs))), T::kThreads, T::kSmemBytes, 0, c.stream, a, b, u, sa, sb, su,
+                y, p);
 }
 
 template <int GROUP, int BN, int MODE>
 int launch_stream(const Call& c, int parts) {
   using T = Stream<GROUP, BN, MODE != kLinear>;
   CUtensorMap w, u, x, sw, su, sx;
-  if (!map_codes(&w, c.w, c.N, c.K, kTile) || !map_codes(&x, c.x, c.M, c.K, BN) ||
+  if (!map_codes(&w, c.w, c.N, c.K, T::kTileRows) || !map_codes(&x, c.x, c.M, c.K, BN) ||
       !map_scales(&sw, c.sw, c.N, c.K, GROUP) || !map_scales(&sx, c.sx, c.M, c.K, GROUP))
     return SMOOTHROT_CUDA_ERROR;
   u = w;
   su = sw;
-  if (MODE != kLinear && (!map_codes(&u, c.u, c.N, c.K, kTile) || !map_scales(&su, c.su, c.N, c.K, GROUP))) return SMOOTHROT_CUDA_ERROR;
+  if (MODE != kLinear && (!map_codes(&u, c.u, c.N, c.K, T::kTileRows) || !map_scales(&su, c.su, c.N, c.K, GROUP)))
+    return SMOOTHROT_CUDA_ERROR;
   auto kern = mx_stream_kernel<GROUP, BN, MODE>;
   if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), T::kSmemBytes)) return SMOOTHROT_CUDA_ERROR;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(unsigned((c.N + kTile - 1) / kTile * parts), unsigned((c.M + BN - 1) / BN), 1);
-  cfg.blockDim = dim3(T::kThreads, 1, 1);
-  cfg.dynamicSmemBytes = T::kSmemBytes;
-  cfg.stream = c.stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = unsigned(parts);
-  attr.val.clusterDim.y = 1;
-  attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kern, w, u, x, sw, su, sx, c.args, parts) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return SMOOTHROT_CUDA_ERROR;
-  }
-  count_launch();
-  return launch_status();
+  const dim3 grid(unsigned((c.N + T::kTileRows - 1) / T::kTileRows * parts), unsigned((c.M + BN - 1) / BN));
+  return launch(kern, grid, kStreamThreads, T::kSmemBytes, parts, c.stream, w, u, x, sw, su, sx, c.args, parts);
 }
 
 template <int GROUP, int MODE>
 int run(const Call& c) {
   if (c.M > 128) return launch_pair<GROUP, MODE>(c);
-  const int64_t tiles = (c.N + kTile - 1) / kTile;
+  const int64_t rows = MODE == kLinear ? kTile : kTile / 2, tiles = (c.N + rows - 1) / rows;
   int parts = 1;
   while (parts < 8 && 2 * parts * tiles <= device_sm_count() && c.args.kblocks >= 2 * parts) parts *= 2;
   if (c.M <= 16) return launch_stream<GROUP, 16, MODE>(c, parts);

@@ -24,6 +24,7 @@ mx_quant_kernel(const __half* __restrict__ x, int64_t ld, int rows, int K, const
   const int chunks = K >> 3, quads = K / (4 * GROUP);
   uint4 raw[CH];
   int m = blockIdx.x;
+  after_the_call_before();
   if (m < rows) {
     const uint4* src = reinterpret_cast<const uint4*>(x + int64_t(m) * ld);
 #pragma unroll
@@ -115,6 +116,7 @@ __global__ void __launch_bounds__(256)
 mx_dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scale, const float* __restrict__ step,
                   int64_t total, int chunks, __half* __restrict__ y, int64_t ldy) {
   const int quads = chunks / (GROUP / 2);
+  after_the_call_before();
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
     const int64_t m = i / chunks;
     const int chunk = int(i - m * chunks), group = chunk / (GROUP / 8);
@@ -166,14 +168,12 @@ int smoothrot_mx_quant(const void* X_f16, int64_t M, int64_t K, int64_t ldx, int
   const int64_t cap = sms * (1024 / T > 0 ? 1024 / T : 1);
   const int64_t grid = M < cap ? M : cap;
   const float norm = walsh != 0 ? float(1.0 / sqrt(double(walsh))) : 1.0f;
-  auto launch = [&](auto kern) {
-    kern<<<unsigned(grid), unsigned(T), 0, static_cast<cudaStream_t>(stream)>>>(
-        static_cast<const __half*>(X_f16), ldx, int(M), int(K), pre, walsh, norm, q_out, scale_out, step_out);
-    count_launch();
-    return launch_status();
+  auto go = [&](auto kern) {
+    return launch(kern, dim3(unsigned(grid)), T, 0, 0, static_cast<cudaStream_t>(stream), static_cast<const __half*>(X_f16), ldx,
+                  int(M), int(K), pre, walsh, norm, q_out, scale_out, step_out);
   };
-  if (group == 32) return ch == 1 ? launch(mx_quant_kernel<32, 1>) : launch(mx_quant_kernel<32, 4>);
-  return ch == 1 ? launch(mx_quant_kernel<16, 1>) : launch(mx_quant_kernel<16, 4>);
+  if (group == 32) return ch == 1 ? go(mx_quant_kernel<32, 1>) : go(mx_quant_kernel<32, 4>);
+  return ch == 1 ? go(mx_quant_kernel<16, 1>) : go(mx_quant_kernel<16, 4>);
 }
 
 int smoothrot_mx_dequant(const uint8_t* q, const uint8_t* scale, const float* step, int64_t M, int64_t K, int64_t group,
@@ -186,13 +186,11 @@ int smoothrot_mx_dequant(const uint8_t* q, const uint8_t* scale, const float* st
   if (q == nullptr || scale == nullptr || Y_f16 == nullptr || ldy < K || M > 0x7fffffffLL / 2) return SMOOTHROT_INVALID_ARG;
   if (!aligned16(q) || !aligned16(scale) || !aligned16(Y_f16) || ldy % 8 != 0) return SMOOTHROT_BAD_ALIGNMENT;
   const int64_t total = M * (K / 8), blocks = (total + 255) / 256, cap = int64_t(device_sm_count()) * 32;
-  auto launch = [&](auto kern) {
-    kern<<<unsigned(blocks < cap ? blocks : cap), 256, 0, static_cast<cudaStream_t>(stream)>>>(
-        q, scale, step, total, int(K / 8), static_cast<__half*>(Y_f16), ldy);
-    count_launch();
-    return launch_status();
+  auto go = [&](auto kern) {
+    return launch(kern, dim3(unsigned(blocks < cap ? blocks : cap)), 256, 0, 0, static_cast<cudaStream_t>(stream), q, scale, step,
+                  total, int(K / 8), static_cast<__half*>(Y_f16), ldy);
   };
-  return group == 32 ? launch(mx_dequant_kernel<32>) : launch(mx_dequant_kernel<16>);
+  return group == 32 ? go(mx_dequant_kernel<32>) : go(mx_dequant_kernel<16>);
 }
 
 }  // extern "C"
