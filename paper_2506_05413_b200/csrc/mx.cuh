@@ -60,6 +60,48 @@ __device__ __forceinline__ void after_the_call_before() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// ---- barriers of asynchronous copies ----
+
+constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s, of every wait
+constexpr unsigned long long kDrainNs = 50000ull;            // pause before leaving after a timeout
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+__device__ __forceinline__ void drain() {
+  const unsigned long long t0 = now_ns();
+  while (now_ns() - t0 < kDrainNs) __nanosleep(1000);
+}
+// Host: reads a status word and, where asked, clears it.
+inline int read_status_word(const int& symbol, int* out, int clear) {
+  if (cudaMemcpyFromSymbol(out, symbol, sizeof(int)) != cudaSuccess) return SMOOTHROT_CUDA_ERROR;
+  if (clear && *out != 0) {
+    const int zero = 0;
+    if (cudaMemcpyToSymbol(symbol, &zero, sizeof(int)) != cudaSuccess) return SMOOTHROT_CUDA_ERROR;
+  }
+  return SMOOTHROT_OK;
+}
+
 // Eight values to eight codes, round to nearest, ties to the even code, saturating at 6.
 __device__ __forceinline__ uint32_t to_codes(const float (&q)[8]) {
   uint32_t r;
@@ -116,89 +158,176 @@ __device__ __forceinline__ float quotient(float v, float d, float inv) {
   return __fmaf_rn(__fmaf_rn(-q, d, v), inv, q);
 }
 
-// A thread's eight neighbouring values of a row to a word of codes.  The lanes of a warp hold neighbouring
-// chunks of eight; all 32 take part, those past the row's end with zeros.
-// GROUP 32: returns the scale byte of the thread's group.
-__device__ __forceinline__ uint32_t encode_32(const float (&v)[8], uint32_t* byte) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[i]));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  *byte = scale_byte_32(top);
-  const float inv = inverse_scale_32(*byte);
-  float q[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = __fmul_rn(v[i], inv);
-  return to_codes(q);
+// ---- rows: a thread holds 16 neighbouring values, two neighbouring threads a group of 32 ----
+
+constexpr int kUnit = 16;
+
+// 32 bytes of fp16 values.  `wide`: the address is a multiple of 32, as one load; otherwise two of 16 bytes.
+struct Unit {
+  uint4 a, b;
+};
+__device__ __forceinline__ Unit load_unit(const __half* p, bool wide) {
+  Unit u;
+  if (wide) {
+    asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(u.a.x), "=r"(u.a.y), "=r"(u.a.z), "=r"(u.a.w), "=r"(u.b.x), "=r"(u.b.y), "=r"(u.b.z), "=r"(u.b.w)
+                 : "l"(p));
+  } else {
+    u.a = __ldcs(reinterpret_cast<const uint4*>(p));
+    u.b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+  }
+  return u;
 }
-// GROUP 16, `step` the row's (any positive number where the caller gives it).
-__device__ __forceinline__ uint32_t encode_16(const float (&v)[8], float step, uint32_t* byte) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[i]));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  *byte = to_e4m3(__fdiv_rn(__uint_as_float(top), __fmul_rn(6.0f, step)));
-  const float d = __fmul_rn(from_e4m3(*byte), step);
-  const float inv = d == 0.0f ? 0.0f : __frcp_rn(d);
-  float q[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = quotient(v[i], d, inv);
-  return to_codes(q);
+__device__ __forceinline__ void store_unit(__half* p, const Unit& u, bool wide) {
+  if (wide) {
+    asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u.a.x), "r"(u.a.y), "r"(u.a.z),
+                 "r"(u.a.w), "r"(u.b.x), "r"(u.b.y), "r"(u.b.z), "r"(u.b.w)
+                 : "memory");
+  } else {
+    __stcs(reinterpret_cast<uint4*>(p), u.a);
+    __stcs(reinterpret_cast<uint4*>(p) + 1, u.b);
+  }
+}
+__device__ __forceinline__ Unit zero_unit() { return Unit{make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)}; }
+inline bool wide_ok(const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0 && ld % 16 == 0; }
+
+__device__ __forceinline__ void widen(const Unit& u, f32x2 (&v)[8]) {
+  v[0] = half2_to_f32x2(u.a.x);
+  v[1] = half2_to_f32x2(u.a.y);
+  v[2] = half2_to_f32x2(u.a.z);
+  v[3] = half2_to_f32x2(u.a.w);
+  v[4] = half2_to_f32x2(u.b.x);
+  v[5] = half2_to_f32x2(u.b.y);
+  v[6] = half2_to_f32x2(u.b.z);
+  v[7] = half2_to_f32x2(u.b.w);
+}
+__device__ __forceinline__ uint32_t narrow2(f32x2 v) {
+  float lo, hi;
+  unpack2(v, lo, hi);
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ Unit narrow(const f32x2 (&v)[8]) {
+  return Unit{make_uint4(narrow2(v[0]), narrow2(v[1]), narrow2(v[2]), narrow2(v[3])),
+              make_uint4(narrow2(v[4]), narrow2(v[5]), narrow2(v[6]), narrow2(v[7]))};
 }
 
-// The scale bytes of 4 neighbouring groups as one word, in the first of their lanes (of every 16 lanes with groups
-// of 32, of every 8 with groups of 16).
+// Largest magnitude of a unit, as the bits of an fp32 value; a NaN wins over everything.
+__device__ __forceinline__ __half2 max_abs2(uint32_t a, uint32_t b) {
+  return __hmax2_nan(__habs2(*reinterpret_cast<const __half2*>(&a)), __habs2(*reinterpret_cast<const __half2*>(&b)));
+}
+__device__ __forceinline__ float top_of(const Unit& u) {
+  const __half2 m = __hmax2_nan(__hmax2_nan(max_abs2(u.a.x, u.a.y), max_abs2(u.a.z, u.a.w)),
+                                __hmax2_nan(max_abs2(u.b.x, u.b.y), max_abs2(u.b.z, u.b.w)));
+  return __half2float(__hmax_nan(__low2half(m), __high2half(m)));
+}
+__device__ __forceinline__ float max_abs(float a, float b) {
+  float r;
+  asm("{\n\t.reg .f32 x, y;\n\tabs.f32 x, %1;\n\tabs.f32 y, %2;\n\tmax.NaN.f32 %0, x, y;\n\t}" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float top_of(const f32x2 (&v)[8]) {
+  float m[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float a, b;
+    unpack2(v[i], a, b);
+    m[i] = max_abs(a, b);
+  }
+  return max_abs(max_abs(max_abs(m[0], m[1]), max_abs(m[2], m[3])), max_abs(max_abs(m[4], m[5]), max_abs(m[6], m[7])));
+}
+
+__device__ __forceinline__ uint2 codes_of(const f32x2 (&q)[8]) {
+  float a[8], b[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unpack2(q[i], a[2 * i], a[2 * i + 1]);
+    unpack2(q[4 + i], b[2 * i], b[2 * i + 1]);
+  }
+  return make_uint2(to_codes(a), to_codes(b));
+}
+// A thread's unit, with its largest magnitude, to codes and the scale byte of its group.  With groups of 32 the two threads of
+// a group take part together.
 template <int GROUP>
-__device__ __forceinline__ uint32_t scale_quad(uint32_t byte, int lane) {
-  constexpr int per = GROUP / 8;      // lanes of a group
-  uint32_t w = byte << (8 * ((lane / per) & 3));
-  w |= __shfl_xor_sync(0xffffffffu, w, per);
-  w |= __shfl_xor_sync(0xffffffffu, w, 2 * per);
-  return w;
+__device__ __forceinline__ uint2 encode(const f32x2 (&v)[8], float top, float step, uint32_t* byte) {
+  f32x2 q[8];
+  if constexpr (GROUP == 32) {
+    const uint32_t mine = __float_as_uint(top), other = __shfl_xor_sync(0xffffffffu, mine, 1);
+    *byte = scale_byte_32(max(mine, other));
+    const float inv = inverse_scale_32(*byte);
+    const f32x2 inv2 = pack2(inv, inv);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = mul2(v[i], inv2);
+  } else {
+    *byte = to_e4m3(__fdiv_rn(top, __fmul_rn(6.0f, step)));
+    const float d = __fmul_rn(from_e4m3(*byte), step);
+    const float inv = d == 0.0f ? 0.0f : __frcp_rn(d);
+    const f32x2 inv2 = pack2(inv, inv), neg2 = pack2(-d, -d);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {      // quotient()
+      const f32x2 r = mul2(v[i], inv2);
+      q[i] = fma2(fma2(r, neg2, v[i]), inv2, r);
+    }
+  }
+  return codes_of(q);
 }
+// Offset of a unit's scale byte within its row's scales, and whether the thread is the one of its group that writes it.
+template <int GROUP>
+__device__ __forceinline__ uint32_t scale_offset(int unit) {
+  const int group = unit / (GROUP / kUnit);
+  return uint32_t(group >> 2) * kAtomBytes + uint32_t(group & 3);
+}
+template <int GROUP>
+__device__ __forceinline__ bool writes_scale(int unit) { return GROUP == 16 || (unit & 1) == 0; }
 
-// Walsh rotation of blocks of n = 32, 64 or 128 neighbouring values, eight to a lane; strides 1, 2, 4, ... in turn, then
-// one product with 1 / sqrt(n).
-__device__ __forceinline__ void walsh_lanes(float (&v)[8], int n, float norm, int lane) {
+// Walsh rotation of blocks of W = 32, 64 or 128 values over 2, 4 or 8 neighbouring lanes; strides 1, 2, 4, ... in turn, then
+// one product with 1 / sqrt(W).
+template <int W>
+__device__ __forceinline__ void walsh_rows(f32x2 (&v)[8], float norm, int lane) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float a, b;
+    unpack2(v[i], a, b);
+    v[i] = pack2(__fadd_rn(a, b), __fsub_rn(a, b));
+  }
 #pragma unroll
   for (int s = 1; s < 8; s *= 2)
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if ((i & s) == 0) {
-        const float a = v[i], b = v[i + s];
-        v[i] = __fadd_rn(a, b);
-        v[i + s] = __fsub_rn(a, b);
+        const f32x2 a = v[i], b = v[i + s];
+        v[i] = add2(a, b);
+        v[i + s] = sub2(a, b);
       }
-  for (int x = 1; 8 * x < n; x *= 2) {
+#pragma unroll
+  for (int x = 1; x * kUnit < W; x *= 2) {
     const float sign = (lane & x) ? -1.0f : 1.0f;
+    const f32x2 sign2 = pack2(sign, sign);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __fmaf_rn(sign, v[i], __shfl_xor_sync(0xffffffffu, v[i], x));   // p + v or p - v
+    for (int i = 0; i < 8; ++i) {
+      const f32x2 p = __shfl_xor_sync(0xffffffffu, v[i], x);
+      v[i] = fma2(sign2, v[i], p);       // p + v or p - v
+    }
   }
+  const f32x2 norm2 = pack2(norm, norm);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], norm);
+  for (int i = 0; i < 8; ++i) v[i] = mul2(v[i], norm2);
 }
 
-// Sums of squares of fp16 values as a pair of floats (sum and what its roundings left), two lanes of each at a time: a square
-// of 11 bits is exact in fp32 and the error of every addition is kept, so the sum is good to some 2^-45.  The norm that
-// follows is then the same fp32 number whatever the order of the additions, and codes of its results do not hang on it.
-struct SquareSum {
-  f32x2 s, e;
-  __device__ __forceinline__ void clear() { s = pack2(0.0f, 0.0f); e = s; }
-  __device__ __forceinline__ void add(f32x2 x) {
-    const f32x2 p = mul2(x, x);
-    const f32x2 t = add2(s, p);
-    const f32x2 b = sub2(t, s);
-    e = add2(e, add2(sub2(p, b), sub2(s, sub2(t, b))));
-    s = t;
+// The sum of a unit's squares in 64 bits.  Statistics so good, rounded once, are the same fp32 number whatever the order of the
+// additions, and codes of what is computed from them do not hang on it.
+__device__ __forceinline__ double sum_of_squares(const Unit& u) {
+  const uint32_t w[8] = {u.a.x, u.a.y, u.a.z, u.a.w, u.b.x, u.b.y, u.b.z, u.b.w};
+  double s = 0.0, r = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    double lo, hi;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f64.f16 %0, l;\n\tcvt.f64.f16 %1, h;\n\t}" : "=d"(lo), "=d"(hi) : "r"(w[i]));
+    s = fma(lo, lo, s);
+    r = fma(hi, hi, r);
   }
-  __device__ __forceinline__ double total() const {
-    float a, b, c, d;
-    unpack2(s, a, b);
-    unpack2(e, c, d);
-    return (double(a) + double(b)) + (double(c) + double(d));
-  }
-};
+  return s + r;
+}
 
 }  // namespace mx
 }  // namespace smoothrot

@@ -17,11 +17,12 @@
 
 #include "mx.cuh"
 
+// defined with the norms: their timeout word and the limit of their waits
+extern "C" int smoothrot_norm_status_word(int* out, int clear);
+extern "C" int smoothrot_norm_set_wait_limit_ns(uint64_t ns);
+
 namespace smoothrot {
 namespace mx {
-
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s
-constexpr unsigned long long kDrainNs = 50000ull;            // pause before leaving after a timeout
 
 __device__ int g_mx_status = 0;
 __device__ unsigned long long g_mx_wait_limit_ns = kWaitLimitNs;
@@ -39,32 +40,9 @@ constexpr int kTileBytes = kTile * kRowBytes;
 
 // ---- PTX ----
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 // arrival on a barrier of this CTA or another of the cluster
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ unsigned long long now_ns() {
-  unsigned long long t;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-  return t;
 }
 // Waits for a phase; false if the limit has passed or another role of the CTA gave up.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int site) {
@@ -88,9 +66,7 @@ __device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, vol
 }
 // After a timeout copies and products that this CTA started may still be on their way: they land in microseconds.
 __device__ __forceinline__ void drain_after_abort(volatile int* abort_flag) {
-  if (*abort_flag == 0) return;
-  const unsigned long long t0 = now_ns();
-  while (now_ns() - t0 < kDrainNs) __nanosleep(1000);
+  if (*abort_flag != 0) drain();
 }
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -1017,20 +993,16 @@ int check_sizes(int64_t M, int64_t N, int64_t K, int64_t group) {
 extern "C" {
 
 int smoothrot_mx_status_word(int* out, int clear) {
-  int v = 0;
-  if (cudaMemcpyFromSymbol(&v, smoothrot::mx::g_mx_status, sizeof(int)) != cudaSuccess) return SMOOTHROT_CUDA_ERROR;
-  *out = v;
-  if (clear && v != 0) {
-    const int zero = 0;
-    if (cudaMemcpyToSymbol(smoothrot::mx::g_mx_status, &zero, sizeof(int)) != cudaSuccess) return SMOOTHROT_CUDA_ERROR;
-  }
-  return SMOOTHROT_OK;
+  int rc = smoothrot::mx::read_status_word(smoothrot::mx::g_mx_status, out, clear), norm = 0;
+  if (rc == SMOOTHROT_OK) rc = smoothrot_norm_status_word(&norm, clear);
+  if (*out == 0) *out = norm;
+  return rc;
 }
 
 int smoothrot_mx_set_wait_limit_ns(uint64_t ns) {
   const unsigned long long v = ns == 0 ? smoothrot::mx::kWaitLimitNs : static_cast<unsigned long long>(ns);
-  return cudaMemcpyToSymbol(smoothrot::mx::g_mx_wait_limit_ns, &v, sizeof(v)) == cudaSuccess ? SMOOTHROT_OK
-                                                                                               : SMOOTHROT_CUDA_ERROR;
+  if (cudaMemcpyToSymbol(smoothrot::mx::g_mx_wait_limit_ns, &v, sizeof(v)) != cudaSuccess) return SMOOTHROT_CUDA_ERROR;
+  return smoothrot_norm_set_wait_limit_ns(ns);
 }
 
 int smoothrot_debug_mx_wait_expiry(void* stream) {

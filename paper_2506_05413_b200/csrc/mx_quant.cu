@@ -1,11 +1,11 @@
 // Quantizer of microscaled 4-bit floating point, with the layer's diagonal and a Walsh rotation in blocks on the way,
 // and its inverse.  Formulas in mx.cuh and smoothrot.h.
 //
-// Streaming work: 2 bytes in, half a byte and a scale out per value.  A CTA takes a row at a time, a thread
-// up to 4 chunks of 8 neighbouring values (16-byte loads, chunk c of thread t is chunk t + c T of the row), whose 8 codes are one
-// aligned word of the output; groups, rotation blocks and the 4 scales that lie side by side are all made of the chunks
-// of neighbouring lanes, so everything but a row's maximum (groups of 16 have a step above them) stays inside a warp.
-// The next row's loads are in flight during the arithmetic.
+// Streaming work: 2 bytes in, half a byte and a scale out per value, and bound by the instructions it issues rather than by
+// memory unless they are few: a thread takes 16 neighbouring values at a time (one load of 32 bytes), so a group is one thread's or
+// two neighbours', and keeps to its place in the rows, so that its part of the diagonal stays in registers and every offset
+// but the row's is computed once.  Groups of 32 need nothing of the rest of their row: the rows are one long line of units,
+// shared out evenly.  Groups of 16 have a step above them: a CTA takes two rows at a time and meets once for their maxima.
 #include "mx.cuh"
 
 namespace smoothrot {
@@ -13,126 +13,188 @@ namespace mx {
 namespace {
 
 constexpr int kMaxThreads = 1024;
-constexpr int64_t kMaxWidth = 8 * 4 * kMaxThreads;
+constexpr int64_t kMaxWidth = 2 * kUnit * kMaxThreads;
+constexpr int kFlatThreads = 256;
 
-template <int GROUP, int CH>
-__global__ void __launch_bounds__(kMaxThreads)
-mx_quant_kernel(const __half* __restrict__ x, int64_t ld, int rows, int K, const float* __restrict__ pre, int walsh,
-                float norm, uint8_t* __restrict__ q_out, uint8_t* __restrict__ scale_out, float* __restrict__ step_out) {
-  __shared__ uint32_t red[2][kMaxThreads / 32];
-  const int t = threadIdx.x, T = blockDim.x, lane = t & 31;
-  const int chunks = K >> 3, quads = K / (4 * GROUP);
-  uint4 raw[CH];
-  int m = blockIdx.x;
-  after_the_call_before();
-  if (m < rows) {
-    const uint4* src = reinterpret_cast<const uint4*>(x + int64_t(m) * ld);
+struct QuantArgs {
+  const __half* x;
+  int64_t ld;
+  int rows, units;            // of a row
+  bool wide;
+  const float* pre;
+  float norm;
+  uint8_t *q_out, *scale_out;
+  float* step_out;
+};
+
+__device__ __forceinline__ void load_diagonal(const float* pre, int unit, f32x2 (&d)[8]) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) raw[c] = t + c * T < chunks ? __ldcs(src + t + c * T) : make_uint4(0u, 0u, 0u, 0u);
+  for (int i = 0; i < 4; ++i) {
+    const float4 w = __ldg(reinterpret_cast<const float4*>(pre + unit * kUnit) + i);
+    d[2 * i] = pack2(w.x, w.y);
+    d[2 * i + 1] = pack2(w.z, w.w);
   }
-  int parity = 0;
-  for (; m < rows; m += gridDim.x, parity ^= 1) {
-    float v[CH][8];
+}
+// A unit's values with the diagonal and the rotation, and their largest magnitude.
+template <int WALSH, bool PRE>
+__device__ __forceinline__ float transform(const Unit& raw, const f32x2 (&diagonal)[8], float norm, int lane, f32x2 (&v)[8]) {
+  widen(raw, v);
+  if constexpr (!PRE && WALSH == 0) return top_of(raw);
+  if constexpr (PRE) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      unpack2(half2_to_f32x2(raw[c].x), v[c][0], v[c][1]);
-      unpack2(half2_to_f32x2(raw[c].y), v[c][2], v[c][3]);
-      unpack2(half2_to_f32x2(raw[c].z), v[c][4], v[c][5]);
-      unpack2(half2_to_f32x2(raw[c].w), v[c][6], v[c][7]);
-    }
-    const int next = m + gridDim.x;
-    if (next < rows) {
-      const uint4* src = reinterpret_cast<const uint4*>(x + int64_t(next) * ld);
+    for (int i = 0; i < 8; ++i) v[i] = mul2(v[i], diagonal[i]);
+  }
+  if constexpr (WALSH != 0) walsh_rows<WALSH>(v, norm, lane);
+  return top_of(v);
+}
+template <int GROUP>
+__device__ __forceinline__ void put(const QuantArgs& a, int m, int unit, uint32_t offset, uint2 codes, uint32_t byte) {
+  __stcs(reinterpret_cast<uint2*>(a.q_out) + int64_t(m) * a.units + unit, codes);
+  if (writes_scale<GROUP>(unit)) a.scale_out[scale_word(m, 0, a.units / (GROUP / 4)) + offset] = uint8_t(byte);
+}
+
+// Groups of 32: `lines` rows side by side are under way, a thread takes its unit of every lines-th row.
+template <int WALSH, bool PRE>
+__global__ void __launch_bounds__(kFlatThreads, 4) mx_quant32_kernel(const QuantArgs a, const int lines) {
+  const int lane = threadIdx.x & 31;
+  const int64_t i = int64_t(blockIdx.x) * kFlatThreads + threadIdx.x;
+  const int line = int(i / a.units), unit = int(i - int64_t(line) * a.units);
+  const bool on = line < lines;         // lanes of a rotation block or a group are on or off together
+  const uint32_t offset = scale_offset<32>(unit);
+  f32x2 diagonal[8];
+  after_the_call_before();
+  if (PRE && on) load_diagonal(a.pre, unit, diagonal);
+  const __half* src = a.x + int64_t(line) * a.ld + unit * kUnit;
+  const int64_t stride = int64_t(lines) * a.ld;
+  constexpr int R = 2;
+  for (int m = line; m - line < a.rows; m += R * lines, src += R * stride) {
+    Unit raw[R];
 #pragma unroll
-      for (int c = 0; c < CH; ++c) raw[c] = t + c * T < chunks ? __ldcs(src + t + c * T) : make_uint4(0u, 0u, 0u, 0u);
-    }
-    if (pre != nullptr) {
-      const float4* p = reinterpret_cast<const float4*>(pre);
+    for (int r = 0; r < R; ++r) raw[r] = on && m + r * lines < a.rows ? load_unit(src + r * stride, a.wide) : zero_unit();
 #pragma unroll
-      for (int c = 0; c < CH; ++c)
-        if (t + c * T < chunks) {
-          const float4 a = __ldg(p + 2 * (t + c * T)), b = __ldg(p + 2 * (t + c * T) + 1);
-          const float d[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[c][i] = __fmul_rn(v[c][i], d[i]);
-        }
-    }
-    if (walsh != 0) {
-#pragma unroll
-      for (int c = 0; c < CH; ++c) walsh_lanes(v[c], walsh, norm, lane);
-    }
-    float step = 1.0f;
-    if constexpr (GROUP == 16) {
-      uint32_t top = 0;
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[c][i]));
-      top = __reduce_max_sync(0xffffffffu, top);
-      if (T > 32) {
-        // two sets of words in turn: a warp that is ahead writes the other one
-        if (lane == 0) red[parity][t >> 5] = top;
-        __syncthreads();
-        top = __reduce_max_sync(0xffffffffu, lane < (T >> 5) ? red[parity][lane] : 0u);
-      }
-      step = row_step_16(top);
-      if (t == 0) step_out[m] = step;
-      if (!(step > 0.0f)) step = 1.0f;      // NaN: whatever the codes are, the row's values are NaN
-    }
-    uint32_t* q_row = reinterpret_cast<uint32_t*>(q_out + int64_t(m) * (K >> 1));
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int chunk = t + c * T;
+    for (int r = 0; r < R; ++r) {
+      f32x2 v[8];
+      const float top = transform<WALSH, PRE>(raw[r], diagonal, a.norm, lane, v);
       uint32_t byte;
-      const uint32_t codes = GROUP == 32 ? encode_32(v[c], &byte) : encode_16(v[c], step, &byte);
-      const uint32_t word = scale_quad<GROUP>(byte, lane);
-      if (chunk < chunks) {
-        __stcs(q_row + chunk, codes);
-        if ((lane & (GROUP / 2 - 1)) == 0)
-          *reinterpret_cast<uint32_t*>(scale_out + scale_word(m, chunk / (GROUP / 2), quads)) = word;
+      const uint2 codes = encode<32>(v, top, 1.0f, &byte);
+      if (on && m + r * lines < a.rows) put<32>(a, m + r * lines, unit, offset, codes, byte);
+    }
+  }
+}
+
+// Groups of 16: U units a thread (the second one a row's length of threads further), R rows at a time.
+template <int WALSH, bool PRE, int U>
+__global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs a) {
+  constexpr int R = U == 1 ? 2 : 1;
+  __shared__ float red[2][R][kMaxThreads / 32];
+  const int t = threadIdx.x, T = blockDim.x, lane = t & 31, warps = T >> 5;
+  after_the_call_before();
+  for (int m = blockIdx.x * R, parity = 0; m < a.rows; m += gridDim.x * R, parity ^= 1) {
+    f32x2 v[R][U][8];
+    float top[R][U], most[R];
+    Unit raw[R][U];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int unit = t + u * T;
+        raw[r][u] = unit < a.units && m + r < a.rows ? load_unit(a.x + int64_t(m + r) * a.ld + unit * kUnit, a.wide) : zero_unit();
+      }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      most[r] = 0.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        f32x2 diagonal[8];
+        if (PRE && t + u * T < a.units) load_diagonal(a.pre, t + u * T, diagonal);
+        else if (PRE) widen(zero_unit(), diagonal);
+        top[r][u] = transform<WALSH, PRE>(raw[r][u], diagonal, a.norm, lane, v[r][u]);
+        most[r] = max_abs(most[r], top[r][u]);
+      }
+      most[r] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most[r])));
+      // two sets of words in turn: a warp that is ahead writes the other one
+      if (lane == 0 && warps > 1) red[parity][r][t >> 5] = most[r];
+    }
+    if (warps > 1) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (m + r >= a.rows) break;
+      uint32_t bits = __float_as_uint(most[r]);
+      if (warps > 1) bits = __reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(red[parity][r][lane]) : 0u);
+      float step = row_step_16(bits);
+      if (t == 0) a.step_out[m + r] = step;
+      if (!(step > 0.0f)) step = 1.0f;      // NaN: whatever the codes are, the row's values are NaN
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int unit = t + u * T;
+        uint32_t byte;
+        const uint2 codes = encode<16>(v[r][u], top[r][u], step, &byte);
+        if (unit < a.units) put<16>(a, m + r, unit, scale_offset<16>(unit), codes, byte);
       }
     }
   }
 }
 
-// Four codes' values (a 16-bit part of a word) as four floats.
-__device__ __forceinline__ void from_codes(uint32_t word, float (&v)[8]) {
-  uint32_t h[4];
+// A word's eight codes as four pairs of fp16 values, exact.
+__device__ __forceinline__ uint4 from_codes(uint32_t word) {
+  uint4 h;
   asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
       "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
       "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
       "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
       "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
       "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
-      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+      : "=r"(h.x), "=r"(h.y), "=r"(h.z), "=r"(h.w)
       : "r"(word));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) unpack2(half2_to_f32x2(h[i]), v[2 * i], v[2 * i + 1]);
+  return h;
 }
 
-// A thread per 8 values.
+// As mx_quant32_kernel: a thread keeps to its unit of every lines-th row.
 template <int GROUP>
-__global__ void __launch_bounds__(256)
-mx_dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scale, const float* __restrict__ step,
-                  int64_t total, int chunks, __half* __restrict__ y, int64_t ldy) {
-  const int quads = chunks / (GROUP / 2);
+__global__ void __launch_bounds__(kFlatThreads)
+mx_dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scale, const float* __restrict__ step, int rows,
+                  int units, int lines, __half* __restrict__ y, int64_t ldy, bool wide) {
+  const int64_t i = int64_t(blockIdx.x) * kFlatThreads + threadIdx.x;
+  const int line = int(i / units), unit = int(i - int64_t(line) * units);
+  if (line >= lines) return;
+  const uint32_t offset = scale_offset<GROUP>(unit);
   after_the_call_before();
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
-    const int64_t m = i / chunks;
-    const int chunk = int(i - m * chunks), group = chunk / (GROUP / 8);
-    const uint32_t word = __ldcs(reinterpret_cast<const uint32_t*>(q) + i);
-    const uint32_t byte = scale[scale_word(m, group >> 2, quads) + (group & 3)];
-    float d = GROUP == 16 ? from_e4m3(byte)
-                          : __uint_as_float(byte == 0u ? 0x00400000u : byte == 255u ? 0x7fffffffu : byte << 23);
-    if (step != nullptr) d = __fmul_rn(d, __ldg(step + m));
-    float v[8];
-    from_codes(word, v);
-    uint4 out;
-    __half2* h = reinterpret_cast<__half2*>(&out);
+  constexpr int R = 4;
+  for (int m = line; m < rows; m += R * lines) {
+    uint2 word[R];
+    uint32_t byte[R];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) h[k] = __floats2half2_rn(__fmul_rn(v[2 * k], d), __fmul_rn(v[2 * k + 1], d));
-    __stcs(reinterpret_cast<uint4*>(y + m * ldy) + chunk, out);
+    for (int r = 0; r < R; ++r) {
+      const int row = min(m + r * lines, rows - 1);
+      word[r] = __ldcs(reinterpret_cast<const uint2*>(q) + int64_t(row) * units + unit);
+      byte[r] = scale[scale_word(row, 0, units / (GROUP / 4)) + offset];
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int row = m + r * lines;
+      if (row >= rows) break;
+      float d = GROUP == 16 ? from_e4m3(byte[r])
+                            : __uint_as_float(byte[r] == 0u ? 0x00400000u : byte[r] == 255u ? 0x7fffffffu : byte[r] << 23);
+      if (step != nullptr) d = __fmul_rn(d, __ldg(step + row));
+      const Unit codes{from_codes(word[r].x), from_codes(word[r].y)};
+      f32x2 v[8];
+      widen(codes, v);
+      const f32x2 d2 = pack2(d, d);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = mul2(v[k], d2);
+      store_unit(y + int64_t(row) * ldy + unit * kUnit, narrow(v), wide);
+    }
   }
+}
+
+// Rows side by side for a kernel that shares out units: as many as give every SM `threads` threads, fewer where the last
+// round of rows would be thin.
+int lines_for(int64_t rows, int64_t units, int64_t threads) {
+  int64_t lines = device_sm_count() * threads / units;
+  if (lines < 1) lines = 1;
+  if (lines > rows) lines = rows;
+  const int64_t rounds = (rows + lines - 1) / lines;
+  return int((rows + rounds - 1) / rounds);
 }
 
 }  // namespace
@@ -160,20 +222,44 @@ int smoothrot_mx_quant(const void* X_f16, int64_t M, int64_t K, int64_t ldx, int
     return SMOOTHROT_INVALID_ARG;
   if (!aligned16(X_f16) || ldx % 8 != 0 || !aligned16(q_out) || !aligned16(scale_out) || (pre != nullptr && !aligned16(pre)))
     return SMOOTHROT_BAD_ALIGNMENT;
-  const int chunks = int(K / 8);
-  // one chunk a thread while the rows do not fill the machine (a row is then one load deep), four beyond
-  const int64_t sms = device_sm_count();
-  const int ch = (M <= sms && chunks <= kMaxThreads) ? 1 : 4;
-  const int T = ((chunks + ch - 1) / ch + 31) / 32 * 32;
-  const int64_t cap = sms * (1024 / T > 0 ? 1024 / T : 1);
-  const int64_t grid = M < cap ? M : cap;
-  const float norm = walsh != 0 ? float(1.0 / sqrt(double(walsh))) : 1.0f;
-  auto go = [&](auto kern) {
-    return launch(kern, dim3(unsigned(grid)), T, 0, 0, static_cast<cudaStream_t>(stream), static_cast<const __half*>(X_f16), ldx,
-                  int(M), int(K), pre, walsh, norm, q_out, scale_out, step_out);
-  };
-  if (group == 32) return ch == 1 ? go(mx_quant_kernel<32, 1>) : go(mx_quant_kernel<32, 4>);
-  return ch == 1 ? go(mx_quant_kernel<16, 1>) : go(mx_quant_kernel<16, 4>);
+  QuantArgs a{};
+  a.x = static_cast<const __half*>(X_f16);
+  a.ld = ldx;
+  a.rows = int(M);
+  a.units = int(K / kUnit);
+  a.wide = wide_ok(X_f16, ldx);
+  a.pre = pre;
+  a.norm = walsh != 0 ? float(1.0 / sqrt(double(walsh))) : 1.0f;
+  a.q_out = q_out;
+  a.scale_out = scale_out;
+  a.step_out = step_out;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (group == 32) {
+    const int lines = lines_for(M, a.units, 1024);
+    const dim3 grid(unsigned((int64_t(lines) * a.units + kFlatThreads - 1) / kFlatThreads));
+    auto go = [&](auto kern) { return launch(kern, grid, kFlatThreads, 0, 0, st, a, lines); };
+    switch (walsh) {
+      case 0: return pre ? go(mx_quant32_kernel<0, true>) : go(mx_quant32_kernel<0, false>);
+      case 32: return pre ? go(mx_quant32_kernel<32, true>) : go(mx_quant32_kernel<32, false>);
+      case 64: return pre ? go(mx_quant32_kernel<64, true>) : go(mx_quant32_kernel<64, false>);
+      default: return pre ? go(mx_quant32_kernel<128, true>) : go(mx_quant32_kernel<128, false>);
+    }
+  }
+  const int per = a.units <= kMaxThreads ? 1 : 2;
+  const int T = ((a.units + per - 1) / per + 31) / 32 * 32;
+  const int64_t rows_each = per == 1 ? 2 : 1, blocks = (M + rows_each - 1) / rows_each;
+  const int64_t cap = int64_t(device_sm_count()) * (1024 / T);
+  const dim3 grid(unsigned(blocks < cap ? blocks : cap));
+  auto go = [&](auto one, auto two) { return per == 1 ? launch(one, grid, T, 0, 0, st, a) : launch(two, grid, T, 0, 0, st, a); };
+#define SR_QUANT16(W) (pre ? go(mx_quant16_kernel<W, true, 1>, mx_quant16_kernel<W, true, 2>) \
+                           : go(mx_quant16_kernel<W, false, 1>, mx_quant16_kernel<W, false, 2>))
+  switch (walsh) {
+    case 0: return SR_QUANT16(0);
+    case 32: return SR_QUANT16(32);
+    case 64: return SR_QUANT16(64);
+    default: return SR_QUANT16(128);
+  }
+#undef SR_QUANT16
 }
 
 int smoothrot_mx_dequant(const uint8_t* q, const uint8_t* scale, const float* step, int64_t M, int64_t K, int64_t group,
@@ -185,10 +271,11 @@ int smoothrot_mx_dequant(const uint8_t* q, const uint8_t* scale, const float* st
   if (M == 0) return SMOOTHROT_OK;
   if (q == nullptr || scale == nullptr || Y_f16 == nullptr || ldy < K || M > 0x7fffffffLL / 2) return SMOOTHROT_INVALID_ARG;
   if (!aligned16(q) || !aligned16(scale) || !aligned16(Y_f16) || ldy % 8 != 0) return SMOOTHROT_BAD_ALIGNMENT;
-  const int64_t total = M * (K / 8), blocks = (total + 255) / 256, cap = int64_t(device_sm_count()) * 32;
+  const int units = int(K / kUnit), lines = lines_for(M, units, 2048);
+  const dim3 grid(unsigned((int64_t(lines) * units + kFlatThreads - 1) / kFlatThreads));
   auto go = [&](auto kern) {
-    return launch(kern, dim3(unsigned(blocks < cap ? blocks : cap)), 256, 0, 0, static_cast<cudaStream_t>(stream), q, scale, step,
-                  total, int(K / 8), static_cast<__half*>(Y_f16), ldy);
+    return launch(kern, grid, kFlatThreads, 0, 0, static_cast<cudaStream_t>(stream), q, scale, step, int(M), units, lines,
+                  static_cast<__half*>(Y_f16), ldy, wide_ok(Y_f16, ldy));
   };
   return group == 32 ? go(mx_dequant_kernel<32>) : go(mx_dequant_kernel<16>);
 }
