@@ -7,10 +7,13 @@
 //   x, and / or its codes: one step per row as in smoothrot_quant_act_plain, or microscaled as in smoothrot_mx_quant
 //
 // One pass: a row is read once (4 bytes a value), lives in registers as fp16 through both norms and leaves as h' and x
-// or codes.  A CTA takes two rows at a time, so that it meets and fetches the weights half as often, a thread 16 neighbouring
-// values of each.  Every product and sum of the formulas is rounded by itself and the norms' statistics are kept in 64
-// bits and rounded once to fp32, so the results do not hang on how a row is shared out, and the codes are those of the
-// quantizer run on x.
+// or codes, a thread holding 8 or 16 neighbouring values.  Every product and sum of the formulas is rounded by itself and the norms'
+// statistics are kept in 64 bits and rounded once to fp32, so the results do not hang on how a row is shared out, and the codes
+// are those of the quantizer run on x.
+//
+// With many rows it is bound by the instructions that takes and by the waits between them.  A CTA then takes two rows at a time, so that it
+// meets half as often and the rows' chains of instructions run beside one another; rows come through shared memory, ahead of
+// their use, and a thread keeps its part of the weights in registers over all its rows.
 #include "mx.cuh"
 
 namespace smoothrot {
@@ -23,15 +26,19 @@ constexpr int kNormRows = 51;      // code of a wait for rows that ran out
 namespace {
 
 constexpr int kMaxThreads = 1024;
-constexpr int64_t kMaxWidth = 2 * kUnit * kMaxThreads;
-constexpr int kRing = 3;           // pairs of rows that a CTA has in shared memory or on their way there
+constexpr int kChunk = 8;                            // values of a thread
+constexpr int kMostChunks = 4;                       // of a thread, in long rows
+constexpr int64_t kMaxWidth = kChunk * kMostChunks * kMaxThreads;
+constexpr int kPairThreads = 512;                   // at most, of a CTA that takes pairs of rows
+constexpr int kRing = 3;                             // pairs of rows that a CTA has in shared memory or on their way there
+typedef Part<kChunk / 2> Chunk;
 
 struct NormArgs {
   const __half *y, *h;
   int64_t ldy, ldh, ldho, ldxo;
   int rows, K;
-  int units, half_unit;       // of a row; the one with 8 values, or -1
-  bool wide;                  // every row starts on 32 bytes
+  int chunks;                 // of a row
+  bool wide;                  // rows of h_out and x_out start on 32 bytes
   const float *post_w, *gate, *pre_w;
   int post_norm;
   float block_scale, residual_scale;
@@ -51,33 +58,41 @@ __device__ __forceinline__ float rstd_of(double sum, double inv_k, double eps) {
   return float(r * (1.5 - 0.5 * a * r * r));
 }
 
-// The last unit of a row whose length is not a multiple of 16 has 8 values.
-__device__ __forceinline__ Unit load_part(const __half* p, bool wide, bool half) {
-  if (!half) return load_unit(p, wide);
-  return Unit{__ldcs(reinterpret_cast<const uint4*>(p)), make_uint4(0u, 0u, 0u, 0u)};
+__device__ __forceinline__ Chunk load_chunk(const __half* p) {
+  const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
+  return Chunk{{a.x, a.y, a.z, a.w}};
 }
-__device__ __forceinline__ void store_part(__half* p, const Unit& u, bool wide, bool half) {
-  if (!half) store_unit(p, u, wide);
-  else __stcs(reinterpret_cast<uint4*>(p), u.a);
-}
-// A unit's 16 weights.
-__device__ __forceinline__ void load_weights(const float* w, int unit, bool half, f32x2 (&v)[8]) {
+__device__ __forceinline__ Unit shared_unit(uint32_t addr) {
+  Unit u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (!half || i < 2) f = __ldg(reinterpret_cast<const float4*>(w + unit * kUnit) + i);
+  for (int i = 0; i < 8; i += 4)
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(u.w[i]), "=r"(u.w[i + 1]), "=r"(u.w[i + 2]), "=r"(u.w[i + 3]) : "r"(addr + 4u * i) : "memory");
+  return u;
+}
+__device__ __forceinline__ void store_chunk(__half* p, const Chunk& u) {
+  __stcs(reinterpret_cast<uint4*>(p), make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]));
+}
+// The weights of the part'th 2 W values; null: ones, which change nothing.
+template <int W>
+__device__ __forceinline__ void load_weights(const float* w, int part, f32x2 (&v)[W]) {
+#pragma unroll
+  for (int i = 0; i < W / 2; ++i) {
+    const float4 f = w != nullptr ? __ldg(reinterpret_cast<const float4*>(w + part * 2 * W) + i) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
     v[2 * i] = pack2(f.x, f.y);
     v[2 * i + 1] = pack2(f.z, f.w);
   }
 }
-__device__ __forceinline__ void times(f32x2 (&v)[8], const f32x2 (&w)[8]) {
+template <int W>
+__device__ __forceinline__ void times(f32x2 (&v)[W], const f32x2 (&w)[W]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = mul2(v[i], w[i]);
+  for (int i = 0; i < W; ++i) v[i] = mul2(v[i], w[i]);
 }
-__device__ __forceinline__ void times(f32x2 (&v)[8], float f) {
+template <int W>
+__device__ __forceinline__ void times(f32x2 (&v)[W], float f) {
   const f32x2 f2 = pack2(f, f);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = mul2(v[i], f2);
+  for (int i = 0; i < W; ++i) v[i] = mul2(v[i], f2);
 }
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -94,243 +109,291 @@ __device__ __forceinline__ bool wait_rows(uint32_t bar, uint32_t parity) {
     }
   return true;
 }
-__device__ __forceinline__ Unit shared_unit(uint32_t addr, bool half) {
-  Unit u = zero_unit();
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.a.x), "=r"(u.a.y), "=r"(u.a.z), "=r"(u.a.w) : "r"(addr) : "memory");
-  if (!half)
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(u.b.x), "=r"(u.b.y), "=r"(u.b.z), "=r"(u.b.w) : "r"(addr + 16u) : "memory");
-  return u;
+
+// v: a thread's part of the sum of squares of each of R rows; afterwards rstd of the rows.  `slot`: a place per row and warp.
+template <int R>
+__device__ __forceinline__ void statistics(const double (&v)[R], float (&rstd)[R], double (*slot)[kMaxThreads / 32], const NormArgs& a) {
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  // with two rows, even lanes go on with the first and odd lanes with the second
+  double mine = v[0];
+  if constexpr (R == 2) mine = (lane & 1 ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, lane & 1 ? v[0] : v[1], 1);
+#pragma unroll
+  for (int o = R; o < 32; o *= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  if (warps > 1) {
+    if (lane < R) slot[lane][wid] = mine;
+    __syncthreads();
+    mine = 0.0;
+    for (int w = lane / R; w < warps; w += 32 / R) mine += slot[lane % R][w];
+#pragma unroll
+    for (int o = R; o < 32; o *= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  }
+  const float f = rstd_of(mine, a.inv_k, a.eps);
+#pragma unroll
+  for (int r = 0; r < R; ++r) rstd[r] = __shfl_sync(0xffffffffu, f, r);
 }
 
-// CODES: 0 none, 4 one step per row, 16 and 32 microscaled groups.  U units a thread, R rows at a time.  Where R is 2 the
-// CTA comes back for more rows: they come through shared memory, two pairs ahead, and a thread keeps the weights of its unit in registers: read again for every row they took
-// three times what the rows themselves took of the path to the registers (8192 rows of 4096: 106 us).
-template <int CODES, int U, int R>
-__global__ void __launch_bounds__(R == 2 ? 512 : kMaxThreads) add_norm_kernel(const NormArgs a) {
-  __shared__ double sums[2][2][R][kMaxThreads / 32];
-  __shared__ float tops[2][R][kMaxThreads / 32];
-  const int t = threadIdx.x, T = blockDim.x, lane = t & 31, wid = t >> 5, warps = T >> 5;
-  after_the_call_before();
-  constexpr bool KEEP = R == 2;
-  f32x2 kept[KEEP ? 3 : 1][8];
-  if constexpr (KEEP) {
-    if (t < a.units) {
-      if (a.post_w != nullptr) load_weights(a.post_w, t, t == a.half_unit, kept[0]);
-      if (a.gate != nullptr) load_weights(a.gate, t, t == a.half_unit, kept[1]);
-      if (a.pre_w != nullptr) load_weights(a.pre_w, t, t == a.half_unit, kept[2]);
-    }
+// z (the block's output as it came) into the stream: fp16(residual_scale * h + block_scale * gate * z).
+template <bool POST, int W>
+__device__ __forceinline__ Part<W> add(const Part<W>& y, const Part<W>& h, float rstd, const f32x2 (&post)[W], const f32x2 (&gate)[W],
+                                       const NormArgs& a) {
+  f32x2 z[W], s[W];
+  widen(y, z);
+  if constexpr (POST) {
+    times(z, rstd);
+    times(z, post);
   }
-  auto weigh = [&](f32x2 (&v)[8], int which, const float* w, int unit, bool half) {
-    if (w == nullptr) return;
-    if constexpr (KEEP) {
-      times(v, kept[which]);
-    } else {
-      load_weights(w, unit, half, kept[0]);
-      times(v, kept[0]);
-    }
-  };
-  // KEEP: a ring of row pairs, each [row][y, h][K]
-  extern __shared__ __align__(128) uint8_t ring[];
-  __shared__ __align__(8) unsigned long long bars[kRing];
-  const uint32_t row_bytes = uint32_t(a.K) * 2u, ring_at = smem_u32(ring), bar_at = smem_u32(bars);
-  auto fetch = [&](int m, int s) {      // by one thread
-    const int rows = min(R, a.rows - m);
-    bar_expect(bar_at + 8u * s, uint32_t(rows) * row_bytes * uint32_t((a.y != nullptr) + (a.h != nullptr)));
-    for (int r = 0; r < rows; ++r) {
-      const uint32_t dst = ring_at + uint32_t(s * R + r) * 2u * row_bytes;
-      if (a.y != nullptr) bulk_load(dst, a.y + int64_t(m + r) * a.ldy, row_bytes, bar_at + 8u * s);
-      if (a.h != nullptr) bulk_load(dst + row_bytes, a.h + int64_t(m + r) * a.ldh, row_bytes, bar_at + 8u * s);
-    }
-  };
-  if (KEEP) {
-    if (t == 0) {
-      for (int s = 0; s < kRing; ++s) bar_init(bar_at + 8u * s, 1);
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      for (int s = 0; s < kRing; ++s)
-        if (int64_t(blockIdx.x + s * gridDim.x) * R < a.rows) fetch(int(blockIdx.x + s * gridDim.x) * R, s);
-    }
-    __syncthreads();
-  }
+  times(z, gate);
+  times(z, a.block_scale);
+  widen(h, s);
+  times(s, a.residual_scale);
   const f32x2 one = pack2(1.0f, 1.0f);
-  int stage = 0;
-  uint32_t phase = 0;
-  // what is kept for one pair of rows and the next are two sets in turn
-  for (int m = blockIdx.x * R, parity = 0; m < a.rows; m += gridDim.x * R, parity ^= 1) {
-    Unit y[R][U], h[R][U];
-    bool there = true;
-    if (KEEP) there = wait_rows(bar_at + 8u * stage, phase);
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+  for (int i = 0; i < W; ++i) s[i] = fma2(z[i], one, s[i]);      // a sum: a packed addition could take a product before it in
+  return narrow(s);
+}
+template <int W>
+__device__ __forceinline__ Part<W> norm(const Part<W>& h, float rstd, const f32x2 (&pre)[W]) {
+  f32x2 x[W];
+  widen(h, x);
+  times(x, rstd);
+  times(x, pre);
+  return narrow(x);
+}
+// Codes of a thread's values; every thread of the warp takes part, `on` ones write.
+template <int CODES, int W>
+__device__ __forceinline__ void put_codes(const Part<W>& x16, float top, float step, float inv, int m, int part, bool on, const NormArgs& a) {
+  f32x2 x[W];
+  widen(x16, x);
+  Part<W / 4> codes;
+  uint32_t byte = 0;
+  if constexpr (CODES == 4) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int unit = t + u * T;
-        const bool on = unit < a.units && m + r < a.rows, half = unit == a.half_unit;
-        if (KEEP) {
-          const uint32_t at = ring_at + uint32_t(stage * R + r) * 2u * row_bytes + uint32_t(unit) * 32u;
-          y[r][u] = on && a.y != nullptr ? shared_unit(at, half) : zero_unit();
-          h[r][u] = on && a.h != nullptr ? shared_unit(at + row_bytes, half) : zero_unit();
-        } else {
-          y[r][u] = on && a.y != nullptr ? load_part(a.y + int64_t(m + r) * a.ldy + unit * kUnit, a.wide, half) : zero_unit();
-          h[r][u] = on && a.h != nullptr ? load_part(a.h + int64_t(m + r) * a.ldh + unit * kUnit, a.wide, half) : zero_unit();
-        }
-      }
-    if (KEEP) {
-      if (__syncthreads_or(!there)) {       // a wait ran out: what is on its way lands before the memory is given back
-        drain();
-        return;
-      }
-      const int64_t next = int64_t(m) + int64_t(kRing) * gridDim.x * R;
-      if (t == 0 && next < a.rows) fetch(int(next), stage);
-      if (++stage == kRing) {
-        stage = 0;
-        phase ^= 1u;
+    for (int c = 0; c < W / 4; ++c) {
+      codes.w[c] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float lo, hi;
+        unpack2(x[4 * c + i / 2], lo, hi);
+        const float v = fmaxf(fminf(rintf(quotient(i % 2 ? hi : lo, step, inv)), 7.0f), -8.0f);
+        codes.w[c] |= (uint32_t(int(v)) & 15u) << (4 * i);
       }
     }
-    // v: a thread's part of each row's sum of squares; afterwards the rows' rstd
-    auto statistics = [&](double (&v)[R], float (&rstd)[R], double (*slot)[kMaxThreads / 32]) {
-      // with two rows, even lanes go on with the first and odd lanes with the second
-      double mine = v[0];
-      if (R == 2) mine = (lane & 1 ? v[R - 1] : v[0]) + __shfl_xor_sync(0xffffffffu, lane & 1 ? v[0] : v[R - 1], 1);
+  } else {
+    codes = encode<CODES>(x, top, step, &byte);
+  }
+  if (!on) return;
+  uint32_t* to = reinterpret_cast<uint32_t*>(a.q_out + int64_t(m) * (a.K >> 1)) + part * (W / 4);
+  if constexpr (W == 8) __stcs(reinterpret_cast<uint2*>(to), make_uint2(codes.w[0], codes.w[1]));
+  else __stcs(to, codes.w[0]);
+  if constexpr (CODES != 4)
+    if (writes_scale<CODES, W>(part))
+      a.scale_out[scale_word(m, 0, a.K / (4 * CODES)) + scale_offset<CODES, W>(part)] = uint8_t(byte);
+}
+// The step of a row from its largest magnitude, written by one thread; `inv` what codes of 4 bits per row are made with.
+template <int CODES>
+__device__ __forceinline__ float row_step(float most, int m, bool write, float* inv, const NormArgs& a) {
+  float step = CODES == 4 ? step_from_absmax(most, a.clip) : row_step_16(__float_as_uint(most));
+  if (write) a.step_out[m] = step;
+  if (CODES == 4) *inv = __frcp_rn(step);
+  else if (!(step > 0.0f)) step = 1.0f;       // NaN: whatever the codes are, the row's values are NaN
+  return step;
+}
+
+// CODES: 0 none, 4 one step per row, 16 and 32 microscaled groups.  POST: a norm after the block.
+
+// Many rows of up to 8192 values, whole units of 16, y and h both there: two rows at a time, a unit a thread.  Threads past a row's
+// end take its last unit again and an odd last row is taken twice, so that there is one course of instructions; they write nothing.
+template <int CODES, bool POST>
+__global__ void __launch_bounds__(kPairThreads) add_norm_pairs_kernel(const NormArgs a) {
+  constexpr int R = 2;
+  __shared__ double sums[2][2][R][kMaxThreads / 32];        // [pair in turn][norm]: a warp that is ahead writes the other pair's
+  __shared__ float tops[2][R][kMaxThreads / 32];
+  __shared__ __align__(8) unsigned long long bars[kRing];
+  extern __shared__ __align__(128) uint8_t ring[];          // [pair][row][y, h][K]
+  const int t = threadIdx.x, lane = t & 31, wid = t >> 5, warps = blockDim.x >> 5;
+  const int units = a.K / kUnit, unit = min(t, units - 1);
+  const bool on = t < units;
+  const uint32_t row_bytes = uint32_t(a.K) * 2u, ring_at = smem_u32(ring), bar_at = smem_u32(bars);
+  auto fetch = [&](int64_t m, int s) {      // by one thread
+    bar_expect(bar_at + 8u * s, 2u * R * row_bytes);
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = min(m + r, int64_t(a.rows) - 1);
+      const uint32_t dst = ring_at + uint32_t(s * R + r) * 2u * row_bytes;
+      bulk_load(dst, a.y + row * a.ldy, row_bytes, bar_at + 8u * s);
+      bulk_load(dst + row_bytes, a.h + row * a.ldh, row_bytes, bar_at + 8u * s);
+    }
+  };
+  const int64_t stride = int64_t(gridDim.x) * R;
+  after_the_call_before();
+  if (t == 0) {
+    for (int s = 0; s < kRing; ++s) bar_init(bar_at + 8u * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    for (int s = 0; s < kRing; ++s)
+      if (int64_t(blockIdx.x) * R + s * stride < a.rows) fetch(int64_t(blockIdx.x) * R + s * stride, s);
+  }
+  f32x2 post[8], gate[8], pre[8];
+  if constexpr (POST) load_weights(a.post_w, unit, post);
+  load_weights(a.gate, unit, gate);
+  load_weights(a.pre_w, unit, pre);
+  __syncthreads();
+  int stage = 0, parity = 0;
+  uint32_t phase = 0;
+  for (int64_t m = int64_t(blockIdx.x) * R; m < a.rows; m += stride, parity ^= 1) {
+    const int row[R] = {int(m), int(min(m + 1, int64_t(a.rows) - 1))};
+    const bool put[R] = {on, on && m + 1 < a.rows};
+    Unit y[R], h[R];
+    const bool there = wait_rows(bar_at + 8u * stage, phase);
 #pragma unroll
-      for (int o = R; o < 32; o *= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-      if (warps > 1) {
-        if (lane < R) slot[lane][wid] = mine;
-        __syncthreads();
-        mine = lane / R < warps ? slot[lane % R][lane / R] : 0.0;
-#pragma unroll
-        for (int o = R; o < 32; o *= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);      // R == 2: at most 16 warps
-      }
-      const float f = rstd_of(mine, a.inv_k, a.eps);
-#pragma unroll
-      for (int r = 0; r < R; ++r) rstd[r] = __shfl_sync(0xffffffffu, f, r);
-    };
+    for (int r = 0; r < R; ++r) {
+      const uint32_t at = ring_at + uint32_t(stage * R + r) * 2u * row_bytes + uint32_t(unit) * 32u;
+      y[r] = shared_unit(at);
+      h[r] = shared_unit(at + row_bytes);
+    }
+    if (__syncthreads_or(!there)) {       // a wait ran out: what is on its way lands before the memory is given back
+      drain();
+      return;
+    }
+    if (t == 0 && m + kRing * stride < a.rows) fetch(m + kRing * stride, stage);
+    if (++stage == kRing) {
+      stage = 0;
+      phase ^= 1u;
+    }
     double sum[R];
-    float rstd[R];
-    if (a.post_norm) {
+    float rstd[R] = {1.0f, 1.0f};
+    if constexpr (POST) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        sum[r] = 0.0;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          sum[r] += sum_of_squares(y[r][u]);
-        }
-      }
-      statistics(sum, rstd, sums[parity][0]);
+      for (int r = 0; r < R; ++r) sum[r] = on ? sum_of_squares(y[r]) : 0.0;
+      statistics(sum, rstd, sums[parity][0], a);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      sum[r] = 0.0;
+      h[r] = add<POST>(y[r], h[r], rstd[r], post, gate, a);
+      sum[r] = on ? sum_of_squares(h[r]) : 0.0;
+    }
+    if (a.h_out != nullptr) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int unit = t + u * T;
-        if (unit >= a.units || m + r >= a.rows) continue;
-        const bool half = unit == a.half_unit;
-        f32x2 z[8], s[8];
-        if (a.y != nullptr) {
-          widen(y[r][u], z);
-          if (a.post_norm) {
-            times(z, rstd[r]);
-            weigh(z, 0, a.post_w, unit, half);
-          }
-          weigh(z, 1, a.gate, unit, half);
-          times(z, a.block_scale);
-        }
-        if (a.h != nullptr) {
-          widen(h[r][u], s);
-          if (a.residual_scale != 1.0f) times(s, a.residual_scale);
-          if (a.y != nullptr) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] = fma2(z[i], one, s[i]);      // a sum: a packed addition could take z's last product in
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s[i] = z[i];
-        }
-        h[r][u] = narrow(s);
-        if (a.h_out != nullptr) store_part(a.h_out + int64_t(m + r) * a.ldho + unit * kUnit, h[r][u], a.wide, half);
-        sum[r] += sum_of_squares(h[r][u]);
-      }
+      for (int r = 0; r < R; ++r)
+        if (put[r]) store_unit(a.h_out + int64_t(row[r]) * a.ldho + unit * kUnit, h[r], a.wide);
     }
     if (CODES == 0 && a.x_out == nullptr) continue;
-    statistics(sum, rstd, sums[parity][1]);
-    float top[R][U], most[R];
+    statistics(sum, rstd, sums[parity][1], a);
+    float top[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      most[r] = 0.0f;
+    for (int r = 0; r < R; ++r) h[r] = norm(h[r], rstd[r], pre);
+    if (a.x_out != nullptr) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int unit = t + u * T;
-        const bool half = unit == a.half_unit;
-        top[r][u] = 0.0f;
-        if (unit >= a.units || m + r >= a.rows) continue;
-        f32x2 x[8];
-        widen(h[r][u], x);
-        times(x, rstd[r]);
-        weigh(x, 2, a.pre_w, unit, half);
-        h[r][u] = narrow(x);
-        if (a.x_out != nullptr) store_part(a.x_out + int64_t(m + r) * a.ldxo + unit * kUnit, h[r][u], a.wide, half);
-        if constexpr (CODES != 0) top[r][u] = top_of(h[r][u]);
-        most[r] = max_abs(most[r], top[r][u]);
-      }
+      for (int r = 0; r < R; ++r)
+        if (put[r]) store_unit(a.x_out + int64_t(row[r]) * a.ldxo + unit * kUnit, h[r], a.wide);
     }
     if constexpr (CODES != 0) {
-      if constexpr (CODES == 4 || CODES == 16) {
-  #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          most[r] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most[r])));
-          if (lane == 0) tops[parity][r][wid] = most[r];
-        }
+      float step[R] = {1.0f, 1.0f}, inv[R] = {0.0f, 0.0f};
+#pragma unroll
+      for (int r = 0; r < R; ++r) top[r] = top_of(h[r]);
+      if constexpr (CODES != 32) {
+        float most[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) most[r] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top[r])));
         if (warps > 1) {
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (lane == 0) tops[parity][r][wid] = most[r];
           __syncthreads();
-  #pragma unroll
+#pragma unroll
           for (int r = 0; r < R; ++r)
             most[r] = __uint_as_float(__reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(tops[parity][r][lane]) : 0u));
         }
+#pragma unroll
+        for (int r = 0; r < R; ++r) step[r] = row_step<CODES>(most[r], row[r], t == 0 && put[r], &inv[r], a);
       }
-  #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (m + r >= a.rows) break;
-        float step = 1.0f, inv = 0.0f;
-        if constexpr (CODES == 4) {
-          step = step_from_absmax(most[r], a.clip);
-          inv = __frcp_rn(step);
-          if (t == 0) a.step_out[m + r] = step;
-        } else if constexpr (CODES == 16) {
-          step = row_step_16(__float_as_uint(most[r]));
-          if (t == 0) a.step_out[m + r] = step;
-          if (!(step > 0.0f)) step = 1.0f;
-        }
-  #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int unit = t + u * T;
-          f32x2 x[8];
-          widen(h[r][u], x);
-          if constexpr (CODES == 4) {
-            uint32_t word[2] = {0u, 0u};
-  #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float lo, hi;
-              unpack2(x[i / 2], lo, hi);
-              const float c = fmaxf(fminf(rintf(quotient(i % 2 ? hi : lo, step, inv)), 7.0f), -8.0f);
-              word[i / 8] |= (uint32_t(int(c)) & 15u) << (4 * (i % 8));
-            }
-            uint32_t* to = reinterpret_cast<uint32_t*>(a.q_out + int64_t(m + r) * (a.K >> 1)) + 2 * unit;
-            if (unit < a.units) {
-              to[0] = word[0];
-              if (unit != a.half_unit) to[1] = word[1];
-            }
-          } else if constexpr (CODES >= 16) {
-            uint32_t byte;
-            const uint2 codes = encode<CODES>(x, top[r][u], step, &byte);
-            if (unit < a.units) {
-              __stcs(reinterpret_cast<uint2*>(a.q_out) + int64_t(m + r) * a.units + unit, codes);
-              if (writes_scale<CODES>(unit))
-                a.scale_out[scale_word(m + r, 0, a.units / (CODES / 4)) + scale_offset<CODES>(unit)] = uint8_t(byte);
-            }
+#pragma unroll
+      for (int r = 0; r < R; ++r) put_codes<CODES>(h[r], top[r], step[r], inv[r], row[r], unit, put[r], a);
+    }
+  }
+}
+
+// Few rows, long ones, or only one of y and h: a row at a time, U chunks a thread, straight from global memory.
+template <int CODES, int U>
+__global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a) {
+  __shared__ double sums[2][2][1][kMaxThreads / 32];
+  __shared__ float tops[2][kMaxThreads / 32];
+  const int t = threadIdx.x, T = blockDim.x, lane = t & 31, wid = t >> 5, warps = T >> 5;
+  after_the_call_before();
+  int parity = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, parity ^= 1) {
+    const int m = int(row);
+    Chunk y[U], h[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int chunk = t + u * T;
+      const bool on = chunk < a.chunks;
+      y[u] = on && a.y != nullptr ? load_chunk(a.y + row * a.ldy + chunk * kChunk) : no_values<4>();
+      h[u] = on && a.h != nullptr ? load_chunk(a.h + row * a.ldh + chunk * kChunk) : no_values<4>();
+    }
+    double sum[1] = {0.0};
+    float rstd[1] = {1.0f};
+    if (a.post_norm) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) sum[0] += sum_of_squares(y[u]);
+      statistics(sum, rstd, sums[parity][0], a);
+    }
+    sum[0] = 0.0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int chunk = t + u * T;
+      if (chunk >= a.chunks) continue;
+      if (a.y != nullptr) {
+        f32x2 post[4], gate[4];
+        load_weights(a.gate, chunk, gate);
+        if (a.post_norm) load_weights(a.post_w, chunk, post);
+        if (a.h == nullptr) {      // without the stream: nothing is added, a negative zero stays one
+          f32x2 z[4];
+          widen(y[u], z);
+          if (a.post_norm) {
+            times(z, rstd[0]);
+            times(z, post);
           }
+          times(z, gate);
+          times(z, a.block_scale);
+          h[u] = narrow(z);
+        } else {
+          h[u] = a.post_norm ? add<true>(y[u], h[u], rstd[0], post, gate, a) : add<false>(y[u], h[u], rstd[0], gate, gate, a);
         }
+      } else {
+        f32x2 s[4];
+        widen(h[u], s);
+        times(s, a.residual_scale);
+        h[u] = narrow(s);
       }
+      if (a.h_out != nullptr) store_chunk(a.h_out + row * a.ldho + chunk * kChunk, h[u]);
+      sum[0] += sum_of_squares(h[u]);
+    }
+    if (CODES == 0 && a.x_out == nullptr) continue;
+    statistics(sum, rstd, sums[parity][1], a);
+    float top[U], most = 0.0f, step = 1.0f, inv = 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int chunk = t + u * T;
+      top[u] = 0.0f;
+      if (chunk >= a.chunks) continue;
+      f32x2 pre[4];
+      load_weights(a.pre_w, chunk, pre);
+      h[u] = norm(h[u], rstd[0], pre);
+      if (a.x_out != nullptr) store_chunk(a.x_out + row * a.ldxo + chunk * kChunk, h[u]);
+      if constexpr (CODES != 0) top[u] = top_of(h[u]);
+      most = max_abs(most, top[u]);
+    }
+    if constexpr (CODES != 0) {
+      if constexpr (CODES != 32) {
+        most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+        if (warps > 1) {
+          if (lane == 0) tops[parity][wid] = most;
+          __syncthreads();
+          most = __uint_as_float(__reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(tops[parity][lane]) : 0u));
+        }
+        step = row_step<CODES>(most, m, t == 0, &inv, a);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) put_codes<CODES>(h[u], top[u], step, inv, m, t + u * T, t + u * T < a.chunks, a);
     }
   }
 }
@@ -393,25 +456,30 @@ int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_
   a.x_out = static_cast<__half*>(X_out_f16);
   a.clip = clip;
   a.q_out = q_out; a.scale_out = scale_out; a.step_out = step_out;
-  a.units = int((K + kUnit - 1) / kUnit);
-  a.half_unit = K % kUnit != 0 ? a.units - 1 : -1;
-  a.wide = true;
-  for (const auto& r : rows) a.wide = a.wide && (r.p == nullptr || wide_ok(r.p, r.ld));
-  const int per = a.units <= kMaxThreads ? 1 : 2;
-  const int T = ((a.units + per - 1) / per + 31) / 32 * 32;
+  a.chunks = int(K / kChunk);
   const int64_t sms = device_sm_count();
-  // two rows at a time where a row fits half the threads and there are rows for every place
-  const bool two = T <= 512 && M > sms * (1024 / T);
-  const int64_t blocks = two ? (M + 1) / 2 : M, places = two ? sms * (512 / T) : sms * (1024 / T);
-  const dim3 grid(unsigned(blocks < places ? blocks : places));
-  const int ring_bytes = int(kRing * 2 * 2 * K * 2);
-  auto go = [&](auto one_unit, auto two_units, auto two_rows) {
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (!two) return per == 1 ? launch(one_unit, grid, T, 0, 0, st, a) : launch(two_units, grid, T, 0, 0, st, a);
-    if (!allow_dynamic_smem(reinterpret_cast<const void*>(two_rows), ring_bytes)) return int(SMOOTHROT_CUDA_ERROR);
-    return launch(two_rows, grid, T, ring_bytes, 0, st, a);
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  // pairs of rows where there are more rows than places for one
+  const int T = int(K / kUnit + 31) / 32 * 32;
+  const bool pairs = T <= kPairThreads && K % kUnit == 0 && a.y != nullptr && a.h != nullptr && M > sms * (kMaxThreads / T);
+  a.wide = (H_out_f16 == nullptr || wide_ok(H_out_f16, ldho)) && (X_out_f16 == nullptr || wide_ok(X_out_f16, ldxo));
+  auto go_pairs = [&](auto kern) {
+    const int ring = int(kRing * 2 * 2 * K * 2);
+    const int64_t places = sms * (kPairThreads / T), blocks = (M + 1) / 2;
+    if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), ring)) return int(SMOOTHROT_CUDA_ERROR);
+    return launch(kern, dim3(unsigned(blocks < places ? blocks : places)), T, ring, 0, st, a);
   };
-#define SR_NORM(C) go(add_norm_kernel<C, 1, 1>, add_norm_kernel<C, 2, 1>, add_norm_kernel<C, 1, 2>)
+  const int per = a.chunks <= kMaxThreads ? 1 : a.chunks <= 2 * kMaxThreads ? 2 : kMostChunks;
+  auto go_rows = [&](auto one, auto two, auto most) {
+    const int threads = ((a.chunks + per - 1) / per + 31) / 32 * 32;
+    const int64_t places = sms * (kMaxThreads / threads);
+    const dim3 grid(unsigned(M < places ? M : places));
+    return per == 1 ? launch(one, grid, threads, 0, 0, st, a)
+                    : per == 2 ? launch(two, grid, threads, 0, 0, st, a) : launch(most, grid, threads, 0, 0, st, a);
+  };
+#define SR_NORM(C)                                                                                                     \
+  pairs ? (post_norm ? go_pairs(add_norm_pairs_kernel<C, true>) : go_pairs(add_norm_pairs_kernel<C, false>))            \
+        : go_rows(add_norm_kernel<C, 1>, add_norm_kernel<C, 2>, add_norm_kernel<C, kMostChunks>)
   switch (codes) {
     case 0: return SR_NORM(0);
     case 4: return SR_NORM(4);

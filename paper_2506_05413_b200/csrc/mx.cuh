@@ -158,127 +158,142 @@ __device__ __forceinline__ float quotient(float v, float d, float inv) {
   return __fmaf_rn(__fmaf_rn(-q, d, v), inv, q);
 }
 
-// ---- rows: a thread holds 16 neighbouring values, two neighbouring threads a group of 32 ----
+// ---- rows: a thread holds 2 W neighbouring values of one, as W words of two fp16 values ----
 
-constexpr int kUnit = 16;
-
-// 32 bytes of fp16 values.  `wide`: the address is a multiple of 32, as one load; otherwise two of 16 bytes.
-struct Unit {
-  uint4 a, b;
+template <int W>
+struct Part {
+  uint32_t w[W];
 };
+// The quantizer's: 32 bytes.  `wide`: the address is a multiple of 32, as one load; otherwise two of 16 bytes.
+constexpr int kUnit = 16;
+typedef Part<kUnit / 2> Unit;
+
 __device__ __forceinline__ Unit load_unit(const __half* p, bool wide) {
   Unit u;
   if (wide) {
     asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(u.a.x), "=r"(u.a.y), "=r"(u.a.z), "=r"(u.a.w), "=r"(u.b.x), "=r"(u.b.y), "=r"(u.b.z), "=r"(u.b.w)
+                 : "=r"(u.w[0]), "=r"(u.w[1]), "=r"(u.w[2]), "=r"(u.w[3]), "=r"(u.w[4]), "=r"(u.w[5]), "=r"(u.w[6]), "=r"(u.w[7])
                  : "l"(p));
   } else {
-    u.a = __ldcs(reinterpret_cast<const uint4*>(p));
-    u.b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p)), b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+    u = Unit{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
   }
   return u;
 }
 __device__ __forceinline__ void store_unit(__half* p, const Unit& u, bool wide) {
   if (wide) {
-    asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u.a.x), "r"(u.a.y), "r"(u.a.z),
-                 "r"(u.a.w), "r"(u.b.x), "r"(u.b.y), "r"(u.b.z), "r"(u.b.w)
+    asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u.w[0]), "r"(u.w[1]), "r"(u.w[2]),
+                 "r"(u.w[3]), "r"(u.w[4]), "r"(u.w[5]), "r"(u.w[6]), "r"(u.w[7])
                  : "memory");
   } else {
-    __stcs(reinterpret_cast<uint4*>(p), u.a);
-    __stcs(reinterpret_cast<uint4*>(p) + 1, u.b);
+    __stcs(reinterpret_cast<uint4*>(p), make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]));
+    __stcs(reinterpret_cast<uint4*>(p) + 1, make_uint4(u.w[4], u.w[5], u.w[6], u.w[7]));
   }
 }
-__device__ __forceinline__ Unit zero_unit() { return Unit{make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)}; }
 inline bool wide_ok(const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0 && ld % 16 == 0; }
 
-__device__ __forceinline__ void widen(const Unit& u, f32x2 (&v)[8]) {
-  v[0] = half2_to_f32x2(u.a.x);
-  v[1] = half2_to_f32x2(u.a.y);
-  v[2] = half2_to_f32x2(u.a.z);
-  v[3] = half2_to_f32x2(u.a.w);
-  v[4] = half2_to_f32x2(u.b.x);
-  v[5] = half2_to_f32x2(u.b.y);
-  v[6] = half2_to_f32x2(u.b.z);
-  v[7] = half2_to_f32x2(u.b.w);
+template <int W>
+__device__ __forceinline__ Part<W> no_values() {
+  Part<W> u;
+#pragma unroll
+  for (int i = 0; i < W; ++i) u.w[i] = 0u;
+  return u;
 }
-__device__ __forceinline__ uint32_t narrow2(f32x2 v) {
-  float lo, hi;
-  unpack2(v, lo, hi);
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
+template <int W>
+__device__ __forceinline__ void widen(const Part<W>& u, f32x2 (&v)[W]) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = half2_to_f32x2(u.w[i]);
 }
-__device__ __forceinline__ Unit narrow(const f32x2 (&v)[8]) {
-  return Unit{make_uint4(narrow2(v[0]), narrow2(v[1]), narrow2(v[2]), narrow2(v[3])),
-              make_uint4(narrow2(v[4]), narrow2(v[5]), narrow2(v[6]), narrow2(v[7]))};
+template <int W>
+__device__ __forceinline__ Part<W> narrow(const f32x2 (&v)[W]) {
+  Part<W> u;
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    float lo, hi;
+    unpack2(v[i], lo, hi);
+    const __half2 h = __floats2half2_rn(lo, hi);
+    u.w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return u;
 }
 
-// Largest magnitude of a unit, as the bits of an fp32 value; a NaN wins over everything.
-__device__ __forceinline__ __half2 max_abs2(uint32_t a, uint32_t b) {
-  return __hmax2_nan(__habs2(*reinterpret_cast<const __half2*>(&a)), __habs2(*reinterpret_cast<const __half2*>(&b)));
-}
-__device__ __forceinline__ float top_of(const Unit& u) {
-  const __half2 m = __hmax2_nan(__hmax2_nan(max_abs2(u.a.x, u.a.y), max_abs2(u.a.z, u.a.w)),
-                                __hmax2_nan(max_abs2(u.b.x, u.b.y), max_abs2(u.b.z, u.b.w)));
-  return __half2float(__hmax_nan(__low2half(m), __high2half(m)));
+// Largest magnitude, as an fp32 value; a NaN wins over everything.
+template <int W>
+__device__ __forceinline__ float top_of(const Part<W>& u) {
+  __half2 m[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) m[i] = __habs2(*reinterpret_cast<const __half2*>(&u.w[i]));
+#pragma unroll
+  for (int s = W / 2; s > 0; s /= 2)
+#pragma unroll
+    for (int i = 0; i < s; ++i) m[i] = __hmax2_nan(m[i], m[i + s]);
+  return __half2float(__hmax_nan(__low2half(m[0]), __high2half(m[0])));
 }
 __device__ __forceinline__ float max_abs(float a, float b) {
   float r;
   asm("{\n\t.reg .f32 x, y;\n\tabs.f32 x, %1;\n\tabs.f32 y, %2;\n\tmax.NaN.f32 %0, x, y;\n\t}" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-__device__ __forceinline__ float top_of(const f32x2 (&v)[8]) {
-  float m[8];
+template <int W>
+__device__ __forceinline__ float top_of(const f32x2 (&v)[W]) {
+  float m[W];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < W; ++i) {
     float a, b;
     unpack2(v[i], a, b);
     m[i] = max_abs(a, b);
   }
-  return max_abs(max_abs(max_abs(m[0], m[1]), max_abs(m[2], m[3])), max_abs(max_abs(m[4], m[5]), max_abs(m[6], m[7])));
+#pragma unroll
+  for (int s = W / 2; s > 0; s /= 2)
+#pragma unroll
+    for (int i = 0; i < s; ++i) m[i] = max_abs(m[i], m[i + s]);
+  return m[0];
 }
 
-__device__ __forceinline__ uint2 codes_of(const f32x2 (&q)[8]) {
-  float a[8], b[8];
+// A thread's values, with their largest magnitude, to codes (a word for every 8) and the scale byte of their group.  The threads
+// of a group, neighbouring lanes, take part together.
+template <int GROUP, int W>
+__device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, float step, uint32_t* byte) {
+  uint32_t most = __float_as_uint(top);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    unpack2(q[i], a[2 * i], a[2 * i + 1]);
-    unpack2(q[4 + i], b[2 * i], b[2 * i + 1]);
-  }
-  return make_uint2(to_codes(a), to_codes(b));
-}
-// A thread's unit, with its largest magnitude, to codes and the scale byte of its group.  With groups of 32 the two threads of
-// a group take part together.
-template <int GROUP>
-__device__ __forceinline__ uint2 encode(const f32x2 (&v)[8], float top, float step, uint32_t* byte) {
-  f32x2 q[8];
+  for (int x = 1; x < GROUP / (2 * W); x *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, x));
+  f32x2 q[W];
   if constexpr (GROUP == 32) {
-    const uint32_t mine = __float_as_uint(top), other = __shfl_xor_sync(0xffffffffu, mine, 1);
-    *byte = scale_byte_32(max(mine, other));
+    *byte = scale_byte_32(most);
     const float inv = inverse_scale_32(*byte);
     const f32x2 inv2 = pack2(inv, inv);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = mul2(v[i], inv2);
+    for (int i = 0; i < W; ++i) q[i] = mul2(v[i], inv2);
   } else {
-    *byte = to_e4m3(__fdiv_rn(top, __fmul_rn(6.0f, step)));
+    *byte = to_e4m3(__fdiv_rn(__uint_as_float(most), __fmul_rn(6.0f, step)));
     const float d = __fmul_rn(from_e4m3(*byte), step);
     const float inv = d == 0.0f ? 0.0f : __frcp_rn(d);
     const f32x2 inv2 = pack2(inv, inv), neg2 = pack2(-d, -d);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {      // quotient()
+    for (int i = 0; i < W; ++i) {      // quotient()
       const f32x2 r = mul2(v[i], inv2);
       q[i] = fma2(fma2(r, neg2, v[i]), inv2, r);
     }
   }
-  return codes_of(q);
+  Part<W / 4> codes;
+#pragma unroll
+  for (int c = 0; c < W / 4; ++c) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(q[4 * c + i], f[2 * i], f[2 * i + 1]);
+    codes.w[c] = to_codes(f);
+  }
+  return codes;
 }
-// Offset of a unit's scale byte within its row's scales, and whether the thread is the one of its group that writes it.
-template <int GROUP>
-__device__ __forceinline__ uint32_t scale_offset(int unit) {
-  const int group = unit / (GROUP / kUnit);
+// Offset within its row's scales of the scale byte of the part'th 2 W values, and whether their thread is the one of its group that
+// writes it.
+template <int GROUP, int W>
+__device__ __forceinline__ uint32_t scale_offset(int part) {
+  const int group = part / (GROUP / (2 * W));
   return uint32_t(group >> 2) * kAtomBytes + uint32_t(group & 3);
 }
-template <int GROUP>
-__device__ __forceinline__ bool writes_scale(int unit) { return GROUP == 16 || (unit & 1) == 0; }
+template <int GROUP, int W>
+__device__ __forceinline__ bool writes_scale(int part) { return part % (GROUP / (2 * W)) == 0; }
 
 // Walsh rotation of blocks of W = 32, 64 or 128 values over 2, 4 or 8 neighbouring lanes; strides 1, 2, 4, ... in turn, then
 // one product with 1 / sqrt(W).
@@ -314,15 +329,15 @@ __device__ __forceinline__ void walsh_rows(f32x2 (&v)[8], float norm, int lane) 
   for (int i = 0; i < 8; ++i) v[i] = mul2(v[i], norm2);
 }
 
-// The sum of a unit's squares in 64 bits.  Statistics so good, rounded once, are the same fp32 number whatever the order of the
+// The sum of squares in 64 bits.  Statistics so good, rounded once, are the same fp32 number whatever the order of the
 // additions, and codes of what is computed from them do not hang on it.
-__device__ __forceinline__ double sum_of_squares(const Unit& u) {
-  const uint32_t w[8] = {u.a.x, u.a.y, u.a.z, u.a.w, u.b.x, u.b.y, u.b.z, u.b.w};
+template <int W>
+__device__ __forceinline__ double sum_of_squares(const Part<W>& u) {
   double s = 0.0, r = 0.0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < W; ++i) {
     double lo, hi;
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f64.f16 %0, l;\n\tcvt.f64.f16 %1, h;\n\t}" : "=d"(lo), "=d"(hi) : "r"(w[i]));
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f64.f16 %0, l;\n\tcvt.f64.f16 %1, h;\n\t}" : "=d"(lo), "=d"(hi) : "r"(u.w[i]));
     s = fma(lo, lo, s);
     r = fma(hi, hi, r);
   }

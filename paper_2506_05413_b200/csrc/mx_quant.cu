@@ -48,9 +48,9 @@ __device__ __forceinline__ float transform(const Unit& raw, const f32x2 (&diagon
   return top_of(v);
 }
 template <int GROUP>
-__device__ __forceinline__ void put(const QuantArgs& a, int m, int unit, uint32_t offset, uint2 codes, uint32_t byte) {
-  __stcs(reinterpret_cast<uint2*>(a.q_out) + int64_t(m) * a.units + unit, codes);
-  if (writes_scale<GROUP>(unit)) a.scale_out[scale_word(m, 0, a.units / (GROUP / 4)) + offset] = uint8_t(byte);
+__device__ __forceinline__ void put(const QuantArgs& a, int m, int unit, uint32_t offset, const Part<2>& codes, uint32_t byte) {
+  __stcs(reinterpret_cast<uint2*>(a.q_out) + int64_t(m) * a.units + unit, make_uint2(codes.w[0], codes.w[1]));
+  if (writes_scale<GROUP, 8>(unit)) a.scale_out[scale_word(m, 0, a.units / (GROUP / 4)) + offset] = uint8_t(byte);
 }
 
 // Groups of 32: `lines` rows side by side are under way, a thread takes its unit of every lines-th row.
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kFlatThreads, 4) mx_quant32_kernel(const Quant
   const int64_t i = int64_t(blockIdx.x) * kFlatThreads + threadIdx.x;
   const int line = int(i / a.units), unit = int(i - int64_t(line) * a.units);
   const bool on = line < lines;         // lanes of a rotation block or a group are on or off together
-  const uint32_t offset = scale_offset<32>(unit);
+  const uint32_t offset = scale_offset<32, 8>(unit);
   f32x2 diagonal[8];
   after_the_call_before();
   if (PRE && on) load_diagonal(a.pre, unit, diagonal);
@@ -70,13 +70,13 @@ __global__ void __launch_bounds__(kFlatThreads, 4) mx_quant32_kernel(const Quant
   for (int m = line; m - line < a.rows; m += R * lines, src += R * stride) {
     Unit raw[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) raw[r] = on && m + r * lines < a.rows ? load_unit(src + r * stride, a.wide) : zero_unit();
+    for (int r = 0; r < R; ++r) raw[r] = on && m + r * lines < a.rows ? load_unit(src + r * stride, a.wide) : no_values<8>();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       f32x2 v[8];
       const float top = transform<WALSH, PRE>(raw[r], diagonal, a.norm, lane, v);
       uint32_t byte;
-      const uint2 codes = encode<32>(v, top, 1.0f, &byte);
+      const Part<2> codes = encode<32>(v, top, 1.0f, &byte);
       if (on && m + r * lines < a.rows) put<32>(a, m + r * lines, unit, offset, codes, byte);
     }
   }
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int unit = t + u * T;
-        raw[r][u] = unit < a.units && m + r < a.rows ? load_unit(a.x + int64_t(m + r) * a.ld + unit * kUnit, a.wide) : zero_unit();
+        raw[r][u] = unit < a.units && m + r < a.rows ? load_unit(a.x + int64_t(m + r) * a.ld + unit * kUnit, a.wide) : no_values<8>();
       }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs
       for (int u = 0; u < U; ++u) {
         f32x2 diagonal[8];
         if (PRE && t + u * T < a.units) load_diagonal(a.pre, t + u * T, diagonal);
-        else if (PRE) widen(zero_unit(), diagonal);
+        else if (PRE) widen(no_values<8>(), diagonal);
         top[r][u] = transform<WALSH, PRE>(raw[r][u], diagonal, a.norm, lane, v[r][u]);
         most[r] = max_abs(most[r], top[r][u]);
       }
@@ -128,8 +128,8 @@ __global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs
       for (int u = 0; u < U; ++u) {
         const int unit = t + u * T;
         uint32_t byte;
-        const uint2 codes = encode<16>(v[r][u], top[r][u], step, &byte);
-        if (unit < a.units) put<16>(a, m + r, unit, scale_offset<16>(unit), codes, byte);
+        const Part<2> codes = encode<16>(v[r][u], top[r][u], step, &byte);
+        if (unit < a.units) put<16>(a, m + r, unit, scale_offset<16, 8>(unit), codes, byte);
       }
     }
   }
@@ -157,7 +157,7 @@ mx_dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ sca
   const int64_t i = int64_t(blockIdx.x) * kFlatThreads + threadIdx.x;
   const int line = int(i / units), unit = int(i - int64_t(line) * units);
   if (line >= lines) return;
-  const uint32_t offset = scale_offset<GROUP>(unit);
+  const uint32_t offset = scale_offset<GROUP, 8>(unit);
   after_the_call_before();
   constexpr int R = 4;
   for (int m = line; m < rows; m += R * lines) {
@@ -176,7 +176,8 @@ mx_dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ sca
       float d = GROUP == 16 ? from_e4m3(byte[r])
                             : __uint_as_float(byte[r] == 0u ? 0x00400000u : byte[r] == 255u ? 0x7fffffffu : byte[r] << 23);
       if (step != nullptr) d = __fmul_rn(d, __ldg(step + row));
-      const Unit codes{from_codes(word[r].x), from_codes(word[r].y)};
+      const uint4 lo = from_codes(word[r].x), hi = from_codes(word[r].y);
+      const Unit codes{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}};
       f32x2 v[8];
       widen(codes, v);
       const f32x2 d2 = pack2(d, d);
