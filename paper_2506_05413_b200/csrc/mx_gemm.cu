@@ -583,8 +583,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // the 64 rows of the up projection beside it; a warp puts its block of scales together from the halves of the two that hold
 // them (a copy to tensor memory starts at a multiple of 4 columns, so halves cannot be laid side by side there).  One CTA computes a tile over one part of K; the parts of a tile are a
 // cluster, leave their sums in their own shared memory, and after a cluster barrier each adds up some of the tokens over all
-// parts, in the parts' order: the same bits from call to call.  A warp finishes 32 channels of a token, a group of the
-// next layer's codes.
+// parts, in the parts' order: the same bits from call to call.
 //
 // Two CTAs fit an SM, which evens out tiles that are not a multiple of the SMs, and lets a call's first loads be issued
 // while the call before is finishing.
@@ -614,10 +613,22 @@ struct Stream {
   static_assert(kStageBytes % 1024 == 0, "swizzled tiles start on 1024 bytes");
 };
 
-__device__ __forceinline__ float load_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
+// Eight neighbouring sums of a CTA of the cluster
+__device__ __forceinline__ void add_cluster(float (&v)[8], uint32_t addr) {
+  float4 a, b;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w) : "r"(addr) : "memory");
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(addr + 16u) : "memory");
+  v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+  v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+}
+__device__ __forceinline__ void eight_steps(const float* step, int n, float (&w)[8]) {
+  float4 a = make_float4(1.0f, 1.0f, 1.0f, 1.0f), b = a;
+  if (step != nullptr) {
+    a = __ldg(reinterpret_cast<const float4*>(step + n));
+    b = __ldg(reinterpret_cast<const float4*>(step + n) + 1);
+  }
+  w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+  w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
 }
 
 // A k-block's scale copies and products; `src` is the stage's low word, `sa` the first column of scales.
@@ -780,74 +791,68 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   if (parts > 1) cluster_sync();
   else __syncthreads();
   if (*abort_flag == 0 && warp >= 2) {
-    // This CTA's tokens are m0 + part, m0 + part + parts, ..; four of them at a time, a lane per channel.  Eight warps share
-    // the tile's groups of 32 channels: 4, or 2 of a gated tile.
-    constexpr int kGroups = T::kTileRows / 32, kTeams = 8 / kGroups;
-    const int g = warp & (kGroups - 1), cols = min(BN, p.M - m0), n = n0 + g * 32 + lane;
+    // This CTA's tokens are m0 + part, m0 + part + parts, ..; a thread finishes 8 neighbouring channels of one, so that 4 lanes hold
+    // a group or rotation block of 32.  All lanes of a warp take part; those past the last token repeat it and write nothing.
+    constexpr int kChunks = T::kTileRows / 8, kTeams = 256 / kChunks;
+    const int f = int(threadIdx.x) - 64, chunk = f % kChunks, n = n0 + chunk * 8;
+    const int cols = min(BN, p.M - m0), mine = (cols - part + parts - 1) / parts;
     const bool on = n < p.N;
-    if (n - lane < p.N) {
-      const float ws = on && p.w_step != nullptr ? __ldg(p.w_step + n) : 1.0f;
-      const float us = GATED && on && p.up_step != nullptr ? __ldg(p.up_step + n) : 1.0f;
-      const uint32_t mine = base + uint32_t((g * 32 + lane) * 4);
-      constexpr int U = 4;
-      for (int i0 = (warp - 2) / kGroups; i0 * parts + part < cols; i0 += kTeams * U) {
-        float a[U], b[U];
-        int m[U];
+    float ws[8], us[8];
+    eight_steps(on ? p.w_step : nullptr, n, ws);
+    if (GATED) eight_steps(on ? p.up_step : nullptr, n, us);
+    for (int i0 = warp_number() * 32 - 64; i0 / kChunks < mine; i0 += 256) {
+      const int i = (i0 + lane) / kChunks;
+      const bool there = i < mine && on;
+      const int c = min(i, mine - 1) * parts + part, m = m0 + c;
+      float a[8], b[8];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          m[u] = (i0 + kTeams * u) * parts + part;   // past the last token: that one's place, and nothing is written
-          a[u] = 0.0f;
-          b[u] = 0.0f;
+      for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0f;
+      const uint32_t at = base + uint32_t((c * kTile + chunk * 8) * 4);
+      for (int r = 0; r < parts; ++r) {
+        const uint32_t src = parts > 1 ? map_to_cta(at, r) : at;
+        add_cluster(a, src);
+        if (GATED) add_cluster(b, src + uint32_t(kTile / 2 * 4));
+      }
+      const float xs = p.x_step != nullptr ? __ldg(p.x_step + m) : 1.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a[j] *= xs * ws[j];
+      if constexpr (GATED) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) a[j] = silu_times(a[j], b[j] * (xs * us[j]));
+        if (p.walsh) {
+#pragma unroll
+          for (int x = 1; x < 8; x *= 2)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if ((j & x) == 0) {
+                const float lo = a[j], hi = a[j + x];
+                a[j] = __fadd_rn(lo, hi);
+                a[j + x] = __fsub_rn(lo, hi);
+              }
+#pragma unroll
+          for (int x = 1; x < 4; x *= 2)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              a[j] = __fmaf_rn((lane & x) ? -1.0f : 1.0f, a[j], __shfl_xor_sync(0xffffffffu, a[j], x));
+#pragma unroll
+          for (int j = 0; j < 8; ++j) a[j] = __fmul_rn(a[j], p.norm);
         }
-        for (int r = 0; r < parts; ++r) {
+      }
+      f32x2 v[4];
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const uint32_t at = mine + uint32_t(min(m[u], cols - 1) * kTile * 4);
-            const uint32_t src = parts > 1 ? map_to_cta(at, r) : at;
-            a[u] += load_cluster(src);
-            if (GATED) b[u] += load_cluster(src + uint32_t(kTile / 2 * 4));
-          }
+      for (int j = 0; j < 4; ++j) v[j] = pack2(a[2 * j], a[2 * j + 1]);
+      if constexpr (MODE == kGatedCodes) {
+        uint32_t byte;
+        const float hs = GROUP == 16 ? __ldg(p.h_step + m) : 1.0f;
+        const Part<1> codes = encode<GROUP>(v, top_of(v), hs, &byte);
+        if (there) {
+          *reinterpret_cast<uint32_t*>(p.q_out + int64_t(m) * (p.N / 2) + n / 2) = codes.w[0];
+          if (writes_scale<GROUP, 4>(chunk))
+            p.scale_out[scale_word(m, 0, p.N / (4 * GROUP)) + scale_offset<GROUP, 4>(n / 8)] = uint8_t(byte);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const bool there = m[u] < cols;
-          m[u] = m0 + min(m[u], cols - 1);
-          const float xs = p.x_step != nullptr ? __ldg(p.x_step + m[u]) : 1.0f;
-          float h = a[u] * (xs * ws);
-          if constexpr (GATED) {
-            h = silu_times(h, b[u] * (xs * us));
-            if (p.walsh) {
-#pragma unroll
-              for (int x = 1; x < 32; x *= 2) h = __fmaf_rn((lane & x) ? -1.0f : 1.0f, h, __shfl_xor_sync(0xffffffffu, h, x));
-              h = __fmul_rn(h, p.norm);
-            }
-          }
-          if constexpr (MODE == kGatedCodes) {
-            uint32_t top = abs_bits(h), byte;
-#pragma unroll
-            for (int x = 1; x < GROUP; x *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
-            float v;
-            if constexpr (GROUP == 32) {
-              byte = scale_byte_32(top);
-              v = __fmul_rn(h, inverse_scale_32(byte));
-            } else {
-              const float hs = __ldg(p.h_step + m[u]);
-              byte = to_e4m3(__fdiv_rn(__uint_as_float(top), __fmul_rn(6.0f, hs)));
-              const float d = __fmul_rn(from_e4m3(byte), hs);
-              v = quotient(h, d, d == 0.0f ? 0.0f : __frcp_rn(d));
-            }
-            float c8[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) c8[i] = __shfl_sync(0xffffffffu, v, (lane & 3) * 8 + i);
-            const uint32_t word = to_codes(c8);
-            if (there && lane < 4)
-              *reinterpret_cast<uint32_t*>(p.q_out + int64_t(m[u]) * (p.N / 2) + (n - lane) / 2 + lane * 4) = word;
-            if (there && (lane & (GROUP - 1)) == 0)
-              p.scale_out[scale_word(m[u], n / (4 * GROUP), p.N / (4 * GROUP)) + (n / GROUP & 3)] = uint8_t(byte);
-          } else {
-            if (there && on) p.y[int64_t(m[u]) * p.ldy + n] = __float2half_rn(h);
-          }
-        }
+      } else {
+        const Part<4> h = narrow(v);
+        if (there) *reinterpret_cast<uint4*>(p.y + int64_t(m) * p.ldy + n) = make_uint4(h.w[0], h.w[1], h.w[2], h.w[3]);
       }
     }
   }
