@@ -582,8 +582,8 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // a ring of 16 KB weight tiles with their scales, and the tokens' BN rows beside them.  A gated tile is 64 rows of the gate and
 // the 64 rows of the up projection beside it; a warp puts its block of scales together from the halves of the two that hold
 // them (a copy to tensor memory starts at a multiple of 4 columns, so halves cannot be laid side by side there).  One CTA computes a tile over one part of K; the parts of a tile are a
-// cluster, leave their sums in their own shared memory, and after a cluster barrier each adds up some of the tokens over all
-// parts, in the parts' order: the same bits from call to call.
+// cluster, send each other the sums of the tokens that the other finishes, and each adds up its own over all parts, in the
+// parts' order: the same bits from call to call.
 //
 // Two CTAs fit an SM, which evens out tiles that are not a multiple of the SMs, and lets a call's first loads be issued
 // while the call before is finishing.
@@ -603,8 +603,9 @@ struct Stream {
   static constexpr int kTileRows = GATED ? kTile / 2 : kTile;    // output channels of a tile
   static constexpr int kBarriers = (GATED ? 3 : 2) * kStages + 1;
   static constexpr int kRingBytes = kStages * kStageBytes;
-  static constexpr int kSumBytes = BN * kTile * 4;               // over the ring, once it has been used
-  static constexpr int kSmemBytes = 1024 + kRingBytes + kBarriers * 8 + 16;
+  static constexpr int kSumBytes = BN * kTile * 4;               // of one part: over the ring, once it has been used; of more: behind it
+  static constexpr int kHeadBytes = (kBarriers * 8 + 16 + 127) / 128 * 128;
+  static constexpr int kSmemBytes = 1024 + kRingBytes + kHeadBytes;
   static constexpr int kScaleCol = BN;
   static constexpr int kCols = kScaleCol + 8 * kAtoms;           // weights' scales, tokens' scales
   static constexpr int kTmemCols = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
@@ -613,11 +614,11 @@ struct Stream {
   static_assert(kStageBytes % 1024 == 0, "swizzled tiles start on 1024 bytes");
 };
 
-// Eight neighbouring sums of a CTA of the cluster
-__device__ __forceinline__ void add_cluster(float (&v)[8], uint32_t addr) {
+// Eight neighbouring sums of a part
+__device__ __forceinline__ void add_shared(float (&v)[8], uint32_t addr) {
   float4 a, b;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w) : "r"(addr) : "memory");
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(addr + 16u) : "memory");
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w) : "r"(addr) : "memory");
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(addr + 16u) : "memory");
   v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
   v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
 }
@@ -690,6 +691,8 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   const int tile = int(blockIdx.x) / parts;
   const int m0 = int(blockIdx.y) * BN, n0 = tile * T::kTileRows;
   const int k0 = int(int64_t(p.kblocks) * part / parts), k1 = int(int64_t(p.kblocks) * (part + 1) / parts);
+  if (parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");     // this CTA runs: its memory may be written
+  const uint32_t sums_at = parts > 1 ? base + uint32_t(T::kRingBytes + T::kHeadBytes) : base;
   auto set_up = [] { asm volatile("bar.sync 1, %0;" ::"n"(kStreamThreads) : "memory"); };
   // Warp 0 sets up the barriers and has loads on their way before the others have their tensor memory.
   if (warp == 0) {
@@ -768,13 +771,15 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       if (lane == 0) bar_arrive_cluster(mixed(r.s));
     }
   }
+  __syncwarp();
+  if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (warp >= 2 && bar_wait_warp(done, 0, abort_flag, kStreamEpilogue)) {
-    // the ring has been read to its end: the sums take its place, [token][row of the tile]
+    // [part][token][row of the tile] of the tokens that a CTA finishes: token c is the c / parts th of CTA c % parts
     fence_after();
     const int q = warp & 3, half = (warp - 2) >> 2;
     const uint32_t acc = tmem + (uint32_t(q * 32) << 16);
-    float* sums = reinterpret_cast<float*>(smem) + q * 32 + lane;
-    const int cols = min(BN, p.M - m0);
+    const uint32_t to = sums_at + uint32_t((part * (BN / parts) * kTile + q * 32 + lane) * 4);
+    const int cols = min(BN, p.M - m0), shift = 31 - __clz(parts);
     constexpr int kRead = BN >= 32 ? 16 : 8;       // tokens at a time
 #pragma unroll 1
     for (int c = half * kRead; c < cols; c += 2 * kRead) {
@@ -782,7 +787,13 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       tmem_load(acc + c, v);
       tmem_wait_ld();
 #pragma unroll
-      for (int i = 0; i < kRead; ++i) sums[(c + i) * kTile] = v[i];
+      for (int i = 0; i < kRead; ++i) {
+        const uint32_t at = to + uint32_t(((c + i) >> shift) * kTile * 4);
+        if (parts > 1)
+          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(at, uint32_t((c + i) & (parts - 1)))), "f"(v[i]) : "memory");
+        else
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v[i]) : "memory");
+      }
     }
   }
   drain_after_abort(abort_flag);
@@ -793,7 +804,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   if (*abort_flag == 0 && warp >= 2) {
     // This CTA's tokens are m0 + part, m0 + part + parts, ..; a thread finishes 8 neighbouring channels of one, so that 4 lanes hold
     // a group or rotation block of 32.  All lanes of a warp take part; those past the last token repeat it and write nothing.
-    constexpr int kChunks = T::kTileRows / 8, kTeams = 256 / kChunks;
+    constexpr int kChunks = T::kTileRows / 8;
     const int f = int(threadIdx.x) - 64, chunk = f % kChunks, n = n0 + chunk * 8;
     const int cols = min(BN, p.M - m0), mine = (cols - part + parts - 1) / parts;
     const bool on = n < p.N;
@@ -807,11 +818,10 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       float a[8], b[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0f;
-      const uint32_t at = base + uint32_t((c * kTile + chunk * 8) * 4);
-      for (int r = 0; r < parts; ++r) {
-        const uint32_t src = parts > 1 ? map_to_cta(at, r) : at;
-        add_cluster(a, src);
-        if (GATED) add_cluster(b, src + uint32_t(kTile / 2 * 4));
+      uint32_t at = sums_at + uint32_t((min(i, mine - 1) * kTile + chunk * 8) * 4);
+      for (int r = 0; r < parts; ++r, at += uint32_t(BN / parts * kTile * 4)) {
+        add_shared(a, at);
+        if (GATED) add_shared(b, at + uint32_t(kTile / 2 * 4));
       }
       const float xs = p.x_step != nullptr ? __ldg(p.x_step + m) : 1.0f;
 #pragma unroll
@@ -856,9 +866,6 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       }
     }
   }
-  __syncwarp();
-  if (parts > 1) cluster_sync();        // nobody leaves while its sums may still be read
-  else __syncthreads();
   if (warp == 1) {
     __syncwarp();
     fence_after();
@@ -955,9 +962,43 @@ int launch_stream(const Call& c, int parts) {
   if (MODE != kLinear && (!map_codes(&u, c.u, c.N, c.K, T::kTileRows) || !map_scales(&su, c.su, c.N, c.K, GROUP)))
     return SMOOTHROT_CUDA_ERROR;
   auto kern = mx_stream_kernel<GROUP, BN, MODE>;
-  if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), T::kSmemBytes)) return SMOOTHROT_CUDA_ERROR;
+  if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), T::kSmemBytes + T::kSumBytes)) return SMOOTHROT_CUDA_ERROR;
   const dim3 grid(unsigned((c.N + T::kTileRows - 1) / T::kTileRows * parts), unsigned((c.M + BN - 1) / BN));
-  return launch(kern, grid, kStreamThreads, T::kSmemBytes, parts, c.stream, w, u, x, sw, su, sx, c.args, parts);
+  return launch(kern, grid, kStreamThreads, T::kSmemBytes + (parts > 1 ? T::kSumBytes : 0), parts, c.stream, w, u, x, sw, su, sx, c.args, parts);
+}
+
+// Clusters of `size` CTAs, one to an SM, that the device runs at once: a cluster stays inside a part of the chip, so large ones
+// leave SMs over (148, 74, 33, 15 of 1, 2, 4, 8 on B200).  Asked of the runtime once per device.
+int clusters_at_once(int size) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices][4];
+  const int which = size >= 8 ? 3 : size >= 4 ? 2 : size >= 2 ? 1 : 0;
+  int dev = 0;
+  if (size <= 1 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return device_sm_count() / (size * 2);
+  int n = known[dev][which].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  typedef Stream<32, 128, false> T;
+  auto kern = mx_stream_kernel<32, 128, kLinear>;
+  const int bytes = T::kSmemBytes + T::kSumBytes;
+  if (allow_dynamic_smem(reinterpret_cast<const void*>(kern), bytes)) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(size * 32), 1, 1);
+    cfg.blockDim = dim3(kStreamThreads, 1, 1);
+    cfg.dynamicSmemBytes = size_t(bytes);
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(size);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) n = 0;
+  }
+  if (n <= 0) {
+    (void)cudaGetLastError();
+    return device_sm_count() / (size * 2);
+  }
+  known[dev][which].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 template <int GROUP, int MODE>
@@ -965,7 +1006,7 @@ int run(const Call& c) {
   if (c.M > 128) return launch_pair<GROUP, MODE>(c);
   const int64_t rows = MODE == kLinear ? kTile : kTile / 2, tiles = (c.N + rows - 1) / rows;
   int parts = 1;
-  while (parts < 8 && 2 * parts * tiles <= device_sm_count() && c.args.kblocks >= 2 * parts) parts *= 2;
+  while (parts < 8 && tiles <= clusters_at_once(2 * parts) && c.args.kblocks >= 2 * parts) parts *= 2;
   if (c.M <= 16) return launch_stream<GROUP, 16, MODE>(c, parts);
   if (c.M <= 32) return launch_stream<GROUP, 32, MODE>(c, parts);
   if (c.M <= 64) return launch_stream<GROUP, 64, MODE>(c, parts);
