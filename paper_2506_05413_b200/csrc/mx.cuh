@@ -164,7 +164,7 @@ template <int W>
 struct Part {
   uint32_t w[W];
 };
-// The quantizer's: 32 bytes.  `wide`: the address is a multiple of 32, as one load; otherwise two of 16 bytes.
+// The quantizers': 32 bytes.  `wide`: the address is a multiple of 32, as one load; otherwise two of 16 bytes.
 constexpr int kUnit = 16;
 typedef Part<kUnit / 2> Unit;
 
@@ -295,38 +295,38 @@ __device__ __forceinline__ uint32_t scale_offset(int part) {
 template <int GROUP, int W>
 __device__ __forceinline__ bool writes_scale(int part) { return part % (GROUP / (2 * W)) == 0; }
 
-// Walsh rotation of blocks of W = 32, 64 or 128 values over 2, 4 or 8 neighbouring lanes; strides 1, 2, 4, ... in turn, then
-// one product with 1 / sqrt(W).
-template <int W>
-__device__ __forceinline__ void walsh_rows(f32x2 (&v)[8], float norm, int lane) {
+// Walsh rotation of blocks of N = 32, 64 or 128 values over the lanes that hold them, 2 W values each; strides 1, 2, 4, ... in turn,
+// then one product with 1 / sqrt(N).
+template <int N, int W>
+__device__ __forceinline__ void walsh_rows(f32x2 (&v)[W], float norm, int lane) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < W; ++i) {
     float a, b;
     unpack2(v[i], a, b);
     v[i] = pack2(__fadd_rn(a, b), __fsub_rn(a, b));
   }
 #pragma unroll
-  for (int s = 1; s < 8; s *= 2)
+  for (int s = 1; s < W; s *= 2)
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < W; ++i)
       if ((i & s) == 0) {
         const f32x2 a = v[i], b = v[i + s];
         v[i] = add2(a, b);
         v[i + s] = sub2(a, b);
       }
 #pragma unroll
-  for (int x = 1; x * kUnit < W; x *= 2) {
+  for (int x = 1; x * 2 * W < N; x *= 2) {
     const float sign = (lane & x) ? -1.0f : 1.0f;
     const f32x2 sign2 = pack2(sign, sign);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < W; ++i) {
       const f32x2 p = __shfl_xor_sync(0xffffffffu, v[i], x);
       v[i] = fma2(sign2, v[i], p);       // p + v or p - v
     }
   }
   const f32x2 norm2 = pack2(norm, norm);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = mul2(v[i], norm2);
+  for (int i = 0; i < W; ++i) v[i] = mul2(v[i], norm2);
 }
 
 // The sum of squares in 64 bits.  Statistics so good, rounded once, are the same fp32 number whatever the order of the

@@ -1001,12 +1001,24 @@ int clusters_at_once(int size) {
   return n;
 }
 
+// Which kernel.  Up to 128 tokens the few-token one was the faster at every size tried (1 x 4096 x 4096: 3.8 us against 8.5; 128 x
+// 6144 x 4096: 8.4 against 9.9; gated 14336 x 4096: 13.8 against 22.6 with one token, 19.1 against 18.6 with 128).
+// Beyond, gated calls go to the pair kernel (129 x 5632 x 2048: 8.4 us, 10.8 with few-token tiles) and for the others the estimate
+// decides, in us: a fixed part, then a time per k-block and wave of tiles (256 x 4096 x 14336: 16.3 with few-token tiles, K in 2
+// parts, against 21.9; 512 x 4096 x 14336: 25.7 against 22.0).
 template <int GROUP, int MODE>
 int run(const Call& c) {
-  if (c.M > 128) return launch_pair<GROUP, MODE>(c);
-  const int64_t rows = MODE == kLinear ? kTile : kTile / 2, tiles = (c.N + rows - 1) / rows;
+  const int64_t rows = MODE == kLinear ? kTile : kTile / 2, tiles = (c.N + rows - 1) / rows * ((c.M + 127) / 128);
   int parts = 1;
   while (parts < 8 && tiles <= clusters_at_once(2 * parts) && c.args.kblocks >= 2 * parts) parts *= 2;
+  if (c.M > 128) {
+    if (MODE != kLinear) return launch_pair<GROUP, MODE>(c);
+    const int64_t sms = device_sm_count(), pairs = sms / 2, pair_tiles = (c.M + 255) / 256 * ((c.N + 255) / 256);
+    const double pair_us = 4.6 + 0.30 * double(c.args.kblocks) * double((pair_tiles + pairs - 1) / pairs);
+    const double blocks = double((c.args.kblocks + parts - 1) / parts), ctas = double(tiles * parts);
+    const double stream_us = 4.6 + 0.38 * blocks * (ctas > double(sms) ? ctas / double(sms) : 1.0);
+    return stream_us < pair_us ? launch_stream<GROUP, 128, kLinear>(c, parts) : launch_pair<GROUP, MODE>(c);
+  }
   if (c.M <= 16) return launch_stream<GROUP, 16, MODE>(c, parts);
   if (c.M <= 32) return launch_stream<GROUP, 32, MODE>(c, parts);
   if (c.M <= 64) return launch_stream<GROUP, 64, MODE>(c, parts);

@@ -5,7 +5,8 @@
 // memory unless they are few: a thread takes 16 neighbouring values at a time (one load of 32 bytes), so a group is one thread's or
 // two neighbours', and keeps to its place in the rows, so that its part of the diagonal stays in registers and every offset
 // but the row's is computed once.  Groups of 32 need nothing of the rest of their row: the rows are one long line of units,
-// shared out evenly.  Groups of 16 have a step above them: a CTA takes two rows at a time and meets once for their maxima.
+// shared out evenly, and where they are rotated a thread takes 32 values, so that a block of 32 is its own and larger ones
+// cross fewer lanes.  Groups of 16 have a step above them: a CTA takes two rows at a time and meets once for their maxima.
 #include "mx.cuh"
 
 namespace smoothrot {
@@ -19,7 +20,7 @@ constexpr int kFlatThreads = 256;
 struct QuantArgs {
   const __half* x;
   int64_t ld;
-  int rows, units;            // of a row
+  int rows, K;
   bool wide;
   const float* pre;
   float norm;
@@ -27,57 +28,75 @@ struct QuantArgs {
   float* step_out;
 };
 
-__device__ __forceinline__ void load_diagonal(const float* pre, int unit, f32x2 (&d)[8]) {
+// The part'th 2 W values of a row, or of the diagonal
+template <int W>
+__device__ __forceinline__ Part<W> load_part(const __half* p, bool wide) {
+  Part<W> u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 w = __ldg(reinterpret_cast<const float4*>(pre + unit * kUnit) + i);
+  for (int i = 0; i < W; i += 8) {
+    const Unit h = load_unit(p + 2 * i, wide);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u.w[i + j] = h.w[j];
+  }
+  return u;
+}
+template <int W>
+__device__ __forceinline__ void load_diagonal(const float* pre, int part, f32x2 (&d)[W]) {
+#pragma unroll
+  for (int i = 0; i < W / 2; ++i) {
+    const float4 w = __ldg(reinterpret_cast<const float4*>(pre + part * 2 * W) + i);
     d[2 * i] = pack2(w.x, w.y);
     d[2 * i + 1] = pack2(w.z, w.w);
   }
 }
-// A unit's values with the diagonal and the rotation, and their largest magnitude.
-template <int WALSH, bool PRE>
-__device__ __forceinline__ float transform(const Unit& raw, const f32x2 (&diagonal)[8], float norm, int lane, f32x2 (&v)[8]) {
+// Values with the diagonal and the rotation, and their largest magnitude.
+template <int WALSH, bool PRE, int W>
+__device__ __forceinline__ float transform(const Part<W>& raw, const f32x2 (&diagonal)[W], float norm, int lane, f32x2 (&v)[W]) {
   widen(raw, v);
   if constexpr (!PRE && WALSH == 0) return top_of(raw);
   if constexpr (PRE) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = mul2(v[i], diagonal[i]);
+    for (int i = 0; i < W; ++i) v[i] = mul2(v[i], diagonal[i]);
   }
   if constexpr (WALSH != 0) walsh_rows<WALSH>(v, norm, lane);
   return top_of(v);
 }
-template <int GROUP>
-__device__ __forceinline__ void put(const QuantArgs& a, int m, int unit, uint32_t offset, const Part<2>& codes, uint32_t byte) {
-  __stcs(reinterpret_cast<uint2*>(a.q_out) + int64_t(m) * a.units + unit, make_uint2(codes.w[0], codes.w[1]));
-  if (writes_scale<GROUP, 8>(unit)) a.scale_out[scale_word(m, 0, a.units / (GROUP / 4)) + offset] = uint8_t(byte);
+template <int GROUP, int W>
+__device__ __forceinline__ void put(const QuantArgs& a, int m, int part, uint32_t offset, const Part<W / 4>& codes, uint32_t byte) {
+  uint8_t* to = a.q_out + int64_t(m) * (a.K / 2) + part * W;
+  if constexpr (W == 16) __stcs(reinterpret_cast<uint4*>(to), make_uint4(codes.w[0], codes.w[1], codes.w[2], codes.w[3]));
+  else __stcs(reinterpret_cast<uint2*>(to), make_uint2(codes.w[0], codes.w[1]));
+  if (writes_scale<GROUP, W>(part)) a.scale_out[scale_word(m, 0, a.K / (4 * GROUP)) + offset] = uint8_t(byte);
 }
 
-// Groups of 32: `lines` rows side by side are under way, a thread takes its unit of every lines-th row.
+// Groups of 32: `lines` rows side by side are under way, a thread takes its 2 W values of every lines-th row.
+__host__ __device__ constexpr int flat_words(int walsh) { return walsh != 0 ? 16 : 8; }
+
 template <int WALSH, bool PRE>
-__global__ void __launch_bounds__(kFlatThreads, 4) mx_quant32_kernel(const QuantArgs a, const int lines) {
-  const int lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(kFlatThreads, WALSH != 0 && PRE ? 2 : WALSH != 0 ? 3 : 4) mx_quant32_kernel(const QuantArgs a, const int lines) {
+  constexpr int W = flat_words(WALSH);
+  const int lane = threadIdx.x & 31, parts = a.K / (2 * W);
   const int64_t i = int64_t(blockIdx.x) * kFlatThreads + threadIdx.x;
-  const int line = int(i / a.units), unit = int(i - int64_t(line) * a.units);
+  const int line = int(i / parts), part = int(i - int64_t(line) * parts);
   const bool on = line < lines;         // lanes of a rotation block or a group are on or off together
-  const uint32_t offset = scale_offset<32, 8>(unit);
-  f32x2 diagonal[8];
+  const uint32_t offset = scale_offset<32, W>(part);
+  f32x2 diagonal[W];
   after_the_call_before();
-  if (PRE && on) load_diagonal(a.pre, unit, diagonal);
-  const __half* src = a.x + int64_t(line) * a.ld + unit * kUnit;
+  if (PRE && on) load_diagonal(a.pre, part, diagonal);
+  const __half* src = a.x + int64_t(line) * a.ld + part * 2 * W;
   const int64_t stride = int64_t(lines) * a.ld;
   constexpr int R = 2;
   for (int m = line; m - line < a.rows; m += R * lines, src += R * stride) {
-    Unit raw[R];
+    Part<W> raw[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) raw[r] = on && m + r * lines < a.rows ? load_unit(src + r * stride, a.wide) : no_values<8>();
+    for (int r = 0; r < R; ++r) raw[r] = on && m + r * lines < a.rows ? load_part<W>(src + r * stride, a.wide) : no_values<W>();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      f32x2 v[8];
+      f32x2 v[W];
       const float top = transform<WALSH, PRE>(raw[r], diagonal, a.norm, lane, v);
       uint32_t byte;
-      const Part<2> codes = encode<32>(v, top, 1.0f, &byte);
-      if (on && m + r * lines < a.rows) put<32>(a, m + r * lines, unit, offset, codes, byte);
+      const Part<W / 4> codes = encode<32>(v, top, 1.0f, &byte);
+      if (on && m + r * lines < a.rows) put<32, W>(a, m + r * lines, part, offset, codes, byte);
     }
   }
 }
@@ -87,7 +106,7 @@ template <int WALSH, bool PRE, int U>
 __global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs a) {
   constexpr int R = U == 1 ? 2 : 1;
   __shared__ float red[2][R][kMaxThreads / 32];
-  const int t = threadIdx.x, T = blockDim.x, lane = t & 31, warps = T >> 5;
+  const int t = threadIdx.x, T = blockDim.x, lane = t & 31, warps = T >> 5, units = a.K / kUnit;
   after_the_call_before();
   for (int m = blockIdx.x * R, parity = 0; m < a.rows; m += gridDim.x * R, parity ^= 1) {
     f32x2 v[R][U][8];
@@ -98,7 +117,7 @@ __global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int unit = t + u * T;
-        raw[r][u] = unit < a.units && m + r < a.rows ? load_unit(a.x + int64_t(m + r) * a.ld + unit * kUnit, a.wide) : no_values<8>();
+        raw[r][u] = unit < units && m + r < a.rows ? load_unit(a.x + int64_t(m + r) * a.ld + unit * kUnit, a.wide) : no_values<8>();
       }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -106,7 +125,7 @@ __global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         f32x2 diagonal[8];
-        if (PRE && t + u * T < a.units) load_diagonal(a.pre, t + u * T, diagonal);
+        if (PRE && t + u * T < units) load_diagonal(a.pre, t + u * T, diagonal);
         else if (PRE) widen(no_values<8>(), diagonal);
         top[r][u] = transform<WALSH, PRE>(raw[r][u], diagonal, a.norm, lane, v[r][u]);
         most[r] = max_abs(most[r], top[r][u]);
@@ -129,7 +148,7 @@ __global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs
         const int unit = t + u * T;
         uint32_t byte;
         const Part<2> codes = encode<16>(v[r][u], top[r][u], step, &byte);
-        if (unit < a.units) put<16>(a, m + r, unit, scale_offset<16, 8>(unit), codes, byte);
+        if (unit < units) put<16, 8>(a, m + r, unit, scale_offset<16, 8>(unit), codes, byte);
       }
     }
   }
@@ -190,8 +209,8 @@ mx_dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ sca
 
 // Rows side by side for a kernel that shares out units: as many as give every SM `threads` threads, fewer where the last
 // round of rows would be thin.
-int lines_for(int64_t rows, int64_t units, int64_t threads) {
-  int64_t lines = device_sm_count() * threads / units;
+int lines_for(int64_t rows, int64_t parts, int64_t threads) {
+  int64_t lines = device_sm_count() * threads / parts;
   if (lines < 1) lines = 1;
   if (lines > rows) lines = rows;
   const int64_t rounds = (rows + lines - 1) / lines;
@@ -227,7 +246,7 @@ int smoothrot_mx_quant(const void* X_f16, int64_t M, int64_t K, int64_t ldx, int
   a.x = static_cast<const __half*>(X_f16);
   a.ld = ldx;
   a.rows = int(M);
-  a.units = int(K / kUnit);
+  a.K = int(K);
   a.wide = wide_ok(X_f16, ldx);
   a.pre = pre;
   a.norm = walsh != 0 ? float(1.0 / sqrt(double(walsh))) : 1.0f;
@@ -236,8 +255,9 @@ int smoothrot_mx_quant(const void* X_f16, int64_t M, int64_t K, int64_t ldx, int
   a.step_out = step_out;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (group == 32) {
-    const int lines = lines_for(M, a.units, 1024);
-    const dim3 grid(unsigned((int64_t(lines) * a.units + kFlatThreads - 1) / kFlatThreads));
+    const int64_t parts = K / (2 * flat_words(walsh));
+    const int lines = lines_for(M, parts, walsh == 0 ? 1024 : pre == nullptr ? 768 : 512);
+    const dim3 grid(unsigned((lines * parts + kFlatThreads - 1) / kFlatThreads));
     auto go = [&](auto kern) { return launch(kern, grid, kFlatThreads, 0, 0, st, a, lines); };
     switch (walsh) {
       case 0: return pre ? go(mx_quant32_kernel<0, true>) : go(mx_quant32_kernel<0, false>);
@@ -246,8 +266,8 @@ int smoothrot_mx_quant(const void* X_f16, int64_t M, int64_t K, int64_t ldx, int
       default: return pre ? go(mx_quant32_kernel<128, true>) : go(mx_quant32_kernel<128, false>);
     }
   }
-  const int per = a.units <= kMaxThreads ? 1 : 2;
-  const int T = ((a.units + per - 1) / per + 31) / 32 * 32;
+  const int units = int(K / kUnit), per = units <= kMaxThreads ? 1 : 2;
+  const int T = ((units + per - 1) / per + 31) / 32 * 32;
   const int64_t rows_each = per == 1 ? 2 : 1, blocks = (M + rows_each - 1) / rows_each;
   const int64_t cap = int64_t(device_sm_count()) * (1024 / T);
   const dim3 grid(unsigned(blocks < cap ? blocks : cap));
