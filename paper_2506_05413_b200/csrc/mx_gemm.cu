@@ -354,8 +354,8 @@ struct Args {
 // type's, so the pair moves 16 KB through shared memory per CTA and 128-clock instruction: the layout with the least.
 //
 // Tensor memory: two accumulators of 256 columns and the scales of a k-block (24 or 48 columns) are more than 512, so the
-// second accumulator starts 224 (208) columns after the first and they share 32 (48).  The epilogue's
-// warps take all of an accumulator into registers at once and hand it over before they work on it.
+// second accumulator starts 224 (208) columns after the first and they share 32 (48).  The epilogue's warps take a whole accumulator
+// into registers at once, and the next tile's products wait only for those that hold shared columns.
 //
 // Warps: 0 TMA, 1 products (of the first CTA), 2..17 epilogue, four to a quadrant of tensor-memory lanes, a chunk of columns
 // each: with two to a quadrant a gated tile's activation and encoding took longer than its products.
@@ -369,7 +369,7 @@ struct Pair {
   static constexpr int kEpiWarps = 16, kThreads = 32 * (2 + kEpiWarps);
   static constexpr int kBoxBytes = 32 * 64;                         // 32 rows x 32 fp16
   static constexpr int kOutBytes = kEpiWarps * kBoxBytes;
-  static constexpr int kBarriers = 2 * kStages + 4;
+  static constexpr int kBarriers = 2 * kStages + 5;
   static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kOutBytes + kBarriers * 8 + 16;
   static constexpr int kSecond = GROUP == 32 ? 224 : 208;           // first column of the second accumulator
   static constexpr int kScaleCol = kSecond + 256;                   // scales of A, then of B
@@ -412,7 +412,9 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   auto full = [&](int s) { return bar_base + 8u * s; };                       // in the first CTA, for both
   auto empty = [&](int s) { return bar_base + 8u * (T::kStages + s); };       // in each
   const uint32_t acc_full = bar_base + 8u * (2 * T::kStages);                 // one per accumulator, in each
-  const uint32_t acc_empty = acc_full + 16u;                                  // in the first CTA
+  const uint32_t acc_empty = acc_full + 16u;                                  // one per accumulator, in the first CTA
+  const uint32_t acc_shared = acc_empty + 16u;                                // the columns that both hold, in the first CTA
+  constexpr int kHolders = MODE != kLinear && GROUP == 16 ? 2 : 1;            // chunks with shared columns
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + (bar_base - base) + 8 * T::kBarriers);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -426,6 +428,8 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     bar_init(acc_full, 1);
     bar_init(acc_full + 8u, 1);
     bar_init(acc_empty, 2 * T::kEpiWarps);
+    bar_init(acc_empty + 8u, 2 * T::kEpiWarps);
+    bar_init(acc_shared, 2 * 4 * kHolders);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
@@ -484,8 +488,9 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       uint32_t n = 0;
       bool ok = true;
       for (int tile = first; tile < tiles && ok; tile += step, ++n) {
-        // the tile before has left the columns that this one's accumulator shares with it
-        if (!bar_wait_warp(acc_empty, (n & 1u) ^ 1u, abort_flag, kPairAcc)) break;
+        // the tile before the last has left this accumulator, and the last one the columns that it shares with it
+        if (!bar_wait_warp(acc_empty + 8u * (n & 1u), ((n >> 1) & 1u) ^ 1u, abort_flag, kPairAcc)) break;
+        if (!bar_wait_warp(acc_shared, (n & 1u) ^ 1u, abort_flag, kPairAcc)) break;
         fence_after();
         const uint32_t acc = tmem + ((n & 1u) ? T::kSecond : 0);
         for (int kb = 0; kb < p.kblocks; ++kb, r.next()) {
@@ -510,7 +515,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   } else {
     const int q = warp & 3;                    // quadrant of tensor-memory lanes
     const uint32_t box = out_base + uint32_t(warp - 2) * T::kBoxBytes;
-    const uint32_t acc_free = map_to_cta(acc_empty, 0);
+    const uint32_t acc_free = map_to_cta(acc_empty, 0), shared_free = map_to_cta(acc_shared, 0);
     const bool steps = p.x_step != nullptr || p.w_step != nullptr || p.up_step != nullptr;
     uint32_t n = 0;
     for (int tile = first; tile < tiles; tile += step, ++n) {
@@ -530,7 +535,11 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       tmem_wait_ld();
       fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive_cluster(acc_free);
+      if (lane == 0) {
+        // the shared columns are the last of the first accumulator and the first of the second
+        if ((n & 1u) ? chunk < kHolders : chunk >= 4 - kHolders) bar_arrive_cluster(shared_free);
+        bar_arrive_cluster(acc_free + 8u * (n & 1u));
+      }
       if (steps) {
         times_steps(a, xs, p.w_step, n0, p.N);
         times_steps(b, xs, MODE == kLinear ? p.w_step : p.up_step, MODE == kLinear ? n0 + 32 : n0, p.N);

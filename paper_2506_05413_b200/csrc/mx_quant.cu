@@ -101,39 +101,47 @@ __global__ void __launch_bounds__(kFlatThreads, WALSH != 0 && PRE ? 2 : WALSH !=
   }
 }
 
-// Groups of 16: U units a thread (the second one a row's length of threads further), R rows at a time.
+// Groups of 16: U times 2 W values a thread (the second ones a row's length of threads further), R rows at a time.
+__host__ __device__ constexpr int row_threads(int walsh) { return walsh != 0 ? 512 : 1024; }
+
 template <int WALSH, bool PRE, int U>
-__global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs a) {
-  constexpr int R = U == 1 ? 2 : 1;
+__global__ void __launch_bounds__(row_threads(WALSH)) mx_quant16_kernel(const QuantArgs a) {
+  constexpr int W = flat_words(WALSH), R = U == 1 && WALSH == 0 ? 2 : 1;
   __shared__ float red[2][R][kMaxThreads / 32];
-  const int t = threadIdx.x, T = blockDim.x, lane = t & 31, warps = T >> 5, units = a.K / kUnit;
+  const int t = threadIdx.x, T = blockDim.x, lane = t & 31, warps = T >> 5, parts = a.K / (2 * W);
+  f32x2 diagonal[W];
   after_the_call_before();
-  for (int m = blockIdx.x * R, parity = 0; m < a.rows; m += gridDim.x * R, parity ^= 1) {
-    f32x2 v[R][U][8];
-    float top[R][U], most[R];
-    Unit raw[R][U];
+  if (PRE && U == 1 && t < parts) load_diagonal(a.pre, t, diagonal);
+  Part<W> raw[R][U];
+  auto fetch = [&](int m) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int unit = t + u * T;
-        raw[r][u] = unit < units && m + r < a.rows ? load_unit(a.x + int64_t(m + r) * a.ld + unit * kUnit, a.wide) : no_values<8>();
+        const int part = t + u * T;
+        raw[r][u] = part < parts && m + r < a.rows ? load_part<W>(a.x + int64_t(m + r) * a.ld + part * 2 * W, a.wide) : no_values<W>();
       }
+  };
+  if (U == 1) fetch(blockIdx.x * R);
+  for (int m = blockIdx.x * R, parity = 0; m < a.rows; m += gridDim.x * R, parity ^= 1) {
+    if (U > 1) fetch(m);
+    f32x2 v[R][U][W];
+    float top[R][U], most[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       most[r] = 0.0f;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        f32x2 diagonal[8];
-        if (PRE && t + u * T < units) load_diagonal(a.pre, t + u * T, diagonal);
-        else if (PRE) widen(no_values<8>(), diagonal);
+        if (PRE && U > 1 && t + u * T < parts) load_diagonal(a.pre, t + u * T, diagonal);
         top[r][u] = transform<WALSH, PRE>(raw[r][u], diagonal, a.norm, lane, v[r][u]);
+        if (t + u * T >= parts) top[r][u] = 0.0f;
         most[r] = max_abs(most[r], top[r][u]);
       }
       most[r] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most[r])));
       // two sets of words in turn: a warp that is ahead writes the other one
       if (lane == 0 && warps > 1) red[parity][r][t >> 5] = most[r];
     }
+    if (U == 1) fetch(m + gridDim.x * R);      // on its way while these are coded
     if (warps > 1) __syncthreads();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -145,10 +153,23 @@ __global__ void __launch_bounds__(kMaxThreads) mx_quant16_kernel(const QuantArgs
       if (!(step > 0.0f)) step = 1.0f;      // NaN: whatever the codes are, the row's values are NaN
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int unit = t + u * T;
-        uint32_t byte;
-        const Part<2> codes = encode<16>(v[r][u], top[r][u], step, &byte);
-        if (unit < units) put<16, 8>(a, m + r, unit, scale_offset<16, 8>(unit), codes, byte);
+        const int part = t + u * T;
+        if constexpr (W == 8) {
+          uint32_t byte;
+          const Part<2> codes = encode<16>(v[r][u], top[r][u], step, &byte);
+          if (part < parts) put<16, 8>(a, m + r, part, scale_offset<16, 8>(part), codes, byte);
+        } else {
+          // two groups of 16, each as the other kind of thread would have it
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            f32x2 half[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) half[i] = v[r][u][8 * g + i];
+            uint32_t byte;
+            const Part<2> codes = encode<16>(half, top_of(half), step, &byte);
+            if (part < parts) put<16, 8>(a, m + r, 2 * part + g, scale_offset<16, 8>(2 * part + g), codes, byte);
+          }
+        }
       }
     }
   }
@@ -266,10 +287,10 @@ int smoothrot_mx_quant(const void* X_f16, int64_t M, int64_t K, int64_t ldx, int
       default: return pre ? go(mx_quant32_kernel<128, true>) : go(mx_quant32_kernel<128, false>);
     }
   }
-  const int units = int(K / kUnit), per = units <= kMaxThreads ? 1 : 2;
-  const int T = ((units + per - 1) / per + 31) / 32 * 32;
-  const int64_t rows_each = per == 1 ? 2 : 1, blocks = (M + rows_each - 1) / rows_each;
-  const int64_t cap = int64_t(device_sm_count()) * (1024 / T);
+  const int parts = int(K / (2 * flat_words(walsh))), most = row_threads(walsh), per = parts <= most ? 1 : 2;
+  const int T = ((parts + per - 1) / per + 31) / 32 * 32;
+  const int64_t rows_each = per == 1 && walsh == 0 ? 2 : 1, blocks = (M + rows_each - 1) / rows_each;
+  const int64_t cap = int64_t(device_sm_count()) * (most / T);
   const dim3 grid(unsigned(blocks < cap ? blocks : cap));
   auto go = [&](auto one, auto two) { return per == 1 ? launch(one, grid, T, 0, 0, st, a) : launch(two, grid, T, 0, 0, st, a); };
 #define SR_QUANT16(W) (pre ? go(mx_quant16_kernel<W, true, 1>, mx_quant16_kernel<W, true, 2>) \
