@@ -106,7 +106,6 @@ __device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, 
 __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int LEFT>
 __device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
-__device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // Matrix descriptors: only the low word, the address in 16 bytes, differs from one to the next.
 // K-major operand, 128-byte swizzle: rows of 128 bytes, groups of 8 rows 1024 bytes apart.
@@ -420,27 +419,34 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
   const int warp = warp_number(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < T::kStages; ++s) {
-      bar_init(full(s), 1);
-      bar_init(empty(s), 1);
+  // Set-up: barriers, which both CTAs have to have before a load of either is issued, and tensor memory meanwhile.
+  if (warp == 0) {
+    if (elected()) {
+      for (int s = 0; s < T::kStages; ++s) {
+        bar_init(full(s), 1);
+        bar_init(empty(s), 1);
+      }
+      bar_init(acc_full, 1);
+      bar_init(acc_full + 8u, 1);
+      bar_init(acc_empty, 2 * T::kEpiWarps);
+      bar_init(acc_empty + 8u, 2 * T::kEpiWarps);
+      bar_init(acc_shared, 2 * 4 * kHolders);
+      *abort_flag = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      fence_async();
     }
-    bar_init(acc_full, 1);
-    bar_init(acc_full + 8u, 1);
-    bar_init(acc_empty, 2 * T::kEpiWarps);
-    bar_init(acc_empty + 8u, 2 * T::kEpiWarps);
-    bar_init(acc_shared, 2 * 4 * kHolders);
-    *abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    fence_async();
+    __syncwarp();
   }
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   if (warp == 1) tmem_alloc<2>(smem_u32(tmem_slot), 512);
   after_the_call_before();
-  fence_before();
-  __syncthreads();
-  cluster_sync();
-  fence_after();
-  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (warp != 0) {
+    fence_before();
+    asm volatile("bar.sync 1, %0;" ::"n"(T::kThreads - 32) : "memory");
+    fence_after();
+  }
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);       // in warp 0, which has no use for it, anything
   const int tiles = p.tiles_a * p.tiles_b;
   const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
 
@@ -566,7 +572,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
       }
     }
-    if (MODE != kGatedCodes && lane == 0) store_wait_all();
+    if (MODE != kGatedCodes && lane == 0) store_wait_read<0>();      // the box may go; what was stored arrives before the grid ends
   }
 
   // a CTA that gave up tells the other, which waits for it before it leaves
@@ -745,7 +751,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     set_up();
     fence_after();
   }
-  const uint32_t tmem = warp == 0 ? 0u : __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);       // in warp 0, which has no use for it, anything
 
   if (warp == 1) {
     const bool one = elected();
