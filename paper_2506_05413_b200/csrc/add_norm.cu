@@ -11,9 +11,10 @@
 // statistics are kept in 64 bits and rounded once to fp32, so the results do not hang on how a row is shared out, and the codes
 // are those of the quantizer run on x.
 //
-// With many rows it is bound by the instructions that takes and by the waits between them.  A CTA then takes two rows at a time, so that it
-// meets half as often and the rows' chains of instructions run beside one another; rows come through shared memory, ahead of
-// their use, and a thread keeps its part of the weights in registers over all its rows.
+// With many rows it is bound by the instructions that takes and, more, by the exchanges between a row's threads that the statistics
+// need (with 256 threads to a row of 4096 values those took 18 of 60 us).  So a row is one team's of few threads, up to 64 values each,
+// which meet cheaply and have several chains of instructions side by side; teams fill an SM independently of one another and share the
+// weights in its shared memory; rows come through shared memory too, the next one while the last is worked on.
 #include "mx.cuh"
 
 namespace smoothrot {
@@ -29,8 +30,8 @@ constexpr int kMaxThreads = 1024;
 constexpr int kChunk = 8;                            // values of a thread
 constexpr int kMostChunks = 4;                       // of a thread, in long rows
 constexpr int64_t kMaxWidth = kChunk * kMostChunks * kMaxThreads;
-constexpr int kPairThreads = 512;                   // at most, of a CTA that takes pairs of rows
-constexpr int kRing = 3;                             // pairs of rows that a CTA has in shared memory or on their way there
+constexpr int kTeamThreads = 512;                    // of a CTA of teams: 128 registers each
+constexpr int kMaxTeams = 15;                        // a barrier each
 typedef Part<kChunk / 2> Chunk;
 
 struct NormArgs {
@@ -62,13 +63,9 @@ __device__ __forceinline__ Chunk load_chunk(const __half* p) {
   const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
   return Chunk{{a.x, a.y, a.z, a.w}};
 }
-__device__ __forceinline__ Unit shared_unit(uint32_t addr) {
-  Unit u;
-#pragma unroll
-  for (int i = 0; i < 8; i += 4)
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(u.w[i]), "=r"(u.w[i + 1]), "=r"(u.w[i + 2]), "=r"(u.w[i + 3]) : "r"(addr + 4u * i) : "memory");
-  return u;
+__device__ __forceinline__ Unit shared_unit(const uint8_t* p) {
+  const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + 16);
+  return Unit{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
 }
 __device__ __forceinline__ void store_chunk(__half* p, const Chunk& u) {
   __stcs(reinterpret_cast<uint4*>(p), make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]));
@@ -110,26 +107,42 @@ __device__ __forceinline__ bool wait_rows(uint32_t bar, uint32_t parity) {
   return true;
 }
 
-// v: a thread's part of the sum of squares of each of R rows; afterwards rstd of the rows.  `slot`: a place per row and warp.
-template <int R>
-__device__ __forceinline__ void statistics(const double (&v)[R], float (&rstd)[R], double (*slot)[kMaxThreads / 32], const NormArgs& a) {
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  // with two rows, even lanes go on with the first and odd lanes with the second
-  double mine = v[0];
-  if constexpr (R == 2) mine = (lane & 1 ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, lane & 1 ? v[0] : v[1], 1);
+// The threads that share a row: `warps` warps, which meet at barrier `id`; `slot` is their first place of those for a value per warp.
+struct Team {
+  int id, warps, slot;
+  __device__ __forceinline__ void meet() const { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(warps * 32) : "memory"); }
+};
+
+// rstd of a row from its threads' parts of the sum of squares.
+__device__ __forceinline__ float statistics(double mine, double* slots, const Team& team, int wid, const NormArgs& a) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int o = R; o < 32; o *= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-  if (warps > 1) {
-    if (lane < R) slot[lane][wid] = mine;
-    __syncthreads();
-    mine = 0.0;
-    for (int w = lane / R; w < warps; w += 32 / R) mine += slot[lane % R][w];
+  for (int o = 16; o > 0; o /= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  if (team.warps > 1) {
+    double* slot = slots + team.slot;
+    if (lane == 0) slot[wid] = mine;
+    team.meet();
+    if (team.warps <= 4) {
+      mine = slot[0] + slot[1];
+      if (team.warps > 2) mine += slot[2] + (team.warps > 3 ? slot[3] : 0.0);
+    } else {
+      mine = lane < team.warps ? slot[lane] : 0.0;
 #pragma unroll
-    for (int o = R; o < 32; o *= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+      for (int o = 16; o > 0; o /= 2) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    }
   }
-  const float f = rstd_of(mine, a.inv_k, a.eps);
-#pragma unroll
-  for (int r = 0; r < R; ++r) rstd[r] = __shfl_sync(0xffffffffu, f, r);
+  return rstd_of(mine, a.inv_k, a.eps);
+}
+// The largest of a row's threads' values.
+__device__ __forceinline__ float largest(float mine, float* slots, const Team& team, int wid) {
+  const int lane = threadIdx.x & 31;
+  uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(mine));
+  if (team.warps > 1) {
+    if (lane == 0) slots[team.slot + wid] = __uint_as_float(m);
+    team.meet();
+    m = __reduce_max_sync(0xffffffffu, lane < team.warps ? __float_as_uint(slots[team.slot + lane]) : 0u);
+  }
+  return __uint_as_float(m);
 }
 
 // z (the block's output as it came) into the stream: fp16(residual_scale * h + block_scale * gate * z).
@@ -201,112 +214,116 @@ __device__ __forceinline__ float row_step(float most, int m, bool write, float* 
 
 // CODES: 0 none, 4 one step per row, 16 and 32 microscaled groups.  POST: a norm after the block.
 
-// Many rows of up to 8192 values, whole units of 16, y and h both there: two rows at a time, a unit a thread.  Threads past a row's
-// end take its last unit again and an odd last row is taken twice, so that there is one course of instructions; they write nothing.
-template <int CODES, bool POST>
-__global__ void __launch_bounds__(kPairThreads) add_norm_pairs_kernel(const NormArgs a) {
-  constexpr int R = 2;
-  __shared__ double sums[2][2][R][kMaxThreads / 32];        // [pair in turn][norm]: a warp that is ahead writes the other pair's
-  __shared__ float tops[2][R][kMaxThreads / 32];
-  __shared__ __align__(8) unsigned long long bars[kRing];
-  extern __shared__ __align__(128) uint8_t ring[];          // [pair][row][y, h][K]
-  const int t = threadIdx.x, lane = t & 31, wid = t >> 5, warps = blockDim.x >> 5;
-  const int units = a.K / kUnit, unit = min(t, units - 1);
-  const bool on = t < units;
-  const uint32_t row_bytes = uint32_t(a.K) * 2u, ring_at = smem_u32(ring), bar_at = smem_u32(bars);
-  auto fetch = [&](int64_t m, int s) {      // by one thread
-    bar_expect(bar_at + 8u * s, 2u * R * row_bytes);
-    for (int r = 0; r < R; ++r) {
-      const int64_t row = min(m + r, int64_t(a.rows) - 1);
-      const uint32_t dst = ring_at + uint32_t(s * R + r) * 2u * row_bytes;
-      bulk_load(dst, a.y + row * a.ldy, row_bytes, bar_at + 8u * s);
-      bulk_load(dst + row_bytes, a.h + row * a.ldh, row_bytes, bar_at + 8u * s);
-    }
+// Weights in shared memory: values 4 i .. 4 i + 3 of unit u are float4 number i * units + u, so that a warp reads them without conflicts.
+__device__ __forceinline__ void shared_weights(const float4* w, int unit, int units, f32x2 (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 f = w[i * units + unit];
+    v[2 * i] = pack2(f.x, f.y);
+    v[2 * i + 1] = pack2(f.z, f.w);
+  }
+}
+
+// Many rows of up to 8192 values, whole units of 16, y and h both there: a team of `threads` threads takes a row, U units a
+// thread.  Threads past a row's end take its last unit again, so that there is one course of instructions; they write nothing.
+template <int CODES, bool POST, int U>
+__global__ void __launch_bounds__(kTeamThreads) add_norm_teams_kernel(const NormArgs a, const int threads) {
+  __shared__ double sums[2][2][kTeamThreads / 32];          // [row in turn][norm]: a warp that is ahead writes the other row's
+  __shared__ float tops[2][kTeamThreads / 32];
+  __shared__ __align__(8) unsigned long long bars[kMaxTeams];
+  extern __shared__ __align__(128) uint8_t dynamic[];       // three arrays of weights, then each team's row [y, h][K]
+  const int which = int(threadIdx.x) / threads, teams = int(blockDim.x) / threads;
+  const Team team{1 + which, threads >> 5, which * (threads >> 5)};
+  const int t = int(threadIdx.x) - which * threads, wid = t >> 5, units = a.K / kUnit;
+  const uint32_t row_bytes = uint32_t(a.K) * 2u;
+  float4* weights = reinterpret_cast<float4*>(dynamic);     // three times K / 4
+  const uint8_t* rows = dynamic + size_t(a.K) * 12u + size_t(which) * 2u * row_bytes;
+  const uint32_t row_at = smem_u32(rows), bar = smem_u32(bars) + 8u * which;
+  auto fetch = [&](int64_t m) {      // by one thread
+    bar_expect(bar, 2u * row_bytes);
+    bulk_load(row_at, a.y + m * a.ldy, row_bytes, bar);
+    bulk_load(row_at + row_bytes, a.h + m * a.ldh, row_bytes, bar);
   };
-  const int64_t stride = int64_t(gridDim.x) * R;
+  int unit[U];
+  bool on[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    unit[u] = min(t + u * threads, units - 1);
+    on[u] = t + u * threads < units;
+  }
+  const int64_t first = int64_t(blockIdx.x) * teams + which, stride = int64_t(gridDim.x) * teams;
   after_the_call_before();
   if (t == 0) {
-    for (int s = 0; s < kRing; ++s) bar_init(bar_at + 8u * s, 1);
+    bar_init(bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    for (int s = 0; s < kRing; ++s)
-      if (int64_t(blockIdx.x) * R + s * stride < a.rows) fetch(int64_t(blockIdx.x) * R + s * stride, s);
+    if (first < a.rows) fetch(first);
   }
-  f32x2 post[8], gate[8], pre[8];
-  if constexpr (POST) load_weights(a.post_w, unit, post);
-  load_weights(a.gate, unit, gate);
-  load_weights(a.pre_w, unit, pre);
-  __syncthreads();
-  int stage = 0, parity = 0;
-  uint32_t phase = 0;
-  for (int64_t m = int64_t(blockIdx.x) * R; m < a.rows; m += stride, parity ^= 1) {
-    const int row[R] = {int(m), int(min(m + 1, int64_t(a.rows) - 1))};
-    const bool put[R] = {on, on && m + 1 < a.rows};
-    Unit y[R], h[R];
-    const bool there = wait_rows(bar_at + 8u * stage, phase);
+  const float* arrays[3] = {a.post_w, a.gate, a.pre_w};
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const uint32_t at = ring_at + uint32_t(stage * R + r) * 2u * row_bytes + uint32_t(unit) * 32u;
-      y[r] = shared_unit(at);
-      h[r] = shared_unit(at + row_bytes);
+  for (int w = POST ? 0 : 1; w < 3; ++w)
+    for (int i = threadIdx.x; i < a.K / 4; i += blockDim.x) {
+      // none: ones, which change nothing
+      const float4 f = arrays[w] != nullptr ? __ldg(reinterpret_cast<const float4*>(arrays[w]) + i) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+      weights[w * (a.K / 4) + (i & 3) * units + (i >> 2)] = f;
     }
-    if (__syncthreads_or(!there)) {       // a wait ran out: what is on its way lands before the memory is given back
+  __syncthreads();
+  int parity = 0;
+  for (int64_t row = first; row < a.rows; row += stride, parity ^= 1) {
+    const int m = int(row);
+    Unit y[U], h[U];
+    const bool there = wait_rows(bar, uint32_t(parity));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      y[u] = shared_unit(rows + unit[u] * 32);
+      h[u] = shared_unit(rows + row_bytes + unit[u] * 32);
+    }
+    uint32_t late;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(late) : "r"(uint32_t(!there)), "r"(team.id), "r"(threads) : "memory");
+    if (late != 0) {       // a wait ran out: what is on its way lands before the memory is given back
       drain();
       return;
     }
-    if (t == 0 && m + kRing * stride < a.rows) fetch(m + kRing * stride, stage);
-    if (++stage == kRing) {
-      stage = 0;
-      phase ^= 1u;
-    }
-    double sum[R];
-    float rstd[R] = {1.0f, 1.0f};
+    if (t == 0 && row + stride < a.rows) fetch(row + stride);
+    double sum = 0.0;
+    float rstd = 1.0f;
     if constexpr (POST) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) sum[r] = on ? sum_of_squares(y[r]) : 0.0;
-      statistics(sum, rstd, sums[parity][0], a);
+      for (int u = 0; u < U; ++u) {
+        const double s = sum_of_squares(y[u]);
+        sum += on[u] ? s : 0.0;
+      }
+      rstd = statistics(sum, sums[parity][0], team, wid, a);
+      sum = 0.0;
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      h[r] = add<POST>(y[r], h[r], rstd[r], post, gate, a);
-      sum[r] = on ? sum_of_squares(h[r]) : 0.0;
-    }
-    if (a.h_out != nullptr) {
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-        if (put[r]) store_unit(a.h_out + int64_t(row[r]) * a.ldho + unit * kUnit, h[r], a.wide);
+    for (int u = 0; u < U; ++u) {
+      f32x2 post[8], gate[8];
+      if constexpr (POST) shared_weights(weights, unit[u], units, post);
+      shared_weights(weights + a.K / 4, unit[u], units, gate);
+      h[u] = add<POST>(y[u], h[u], rstd, post, gate, a);
+      const double s = sum_of_squares(h[u]);
+      sum += on[u] ? s : 0.0;
+      if (a.h_out != nullptr && on[u]) store_unit(a.h_out + row * a.ldho + unit[u] * kUnit, h[u], a.wide);
     }
     if (CODES == 0 && a.x_out == nullptr) continue;
-    statistics(sum, rstd, sums[parity][1], a);
-    float top[R];
+    rstd = statistics(sum, sums[parity][1], team, wid, a);
+    float top[U], most = 0.0f, step = 1.0f, inv = 0.0f;
 #pragma unroll
-    for (int r = 0; r < R; ++r) h[r] = norm(h[r], rstd[r], pre);
-    if (a.x_out != nullptr) {
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-        if (put[r]) store_unit(a.x_out + int64_t(row[r]) * a.ldxo + unit * kUnit, h[r], a.wide);
+    for (int u = 0; u < U; ++u) {
+      f32x2 pre[8];
+      shared_weights(weights + a.K / 2, unit[u], units, pre);
+      h[u] = norm(h[u], rstd, pre);
+      if (a.x_out != nullptr && on[u]) store_unit(a.x_out + row * a.ldxo + unit[u] * kUnit, h[u], a.wide);
+      if constexpr (CODES != 0) {
+        top[u] = top_of(h[u]);
+        most = max_abs(most, top[u]);
+      }
     }
     if constexpr (CODES != 0) {
-      float step[R] = {1.0f, 1.0f}, inv[R] = {0.0f, 0.0f};
+      if constexpr (CODES != 32) step = row_step<CODES>(largest(most, tops[parity], team, wid), m, t == 0, &inv, a);
 #pragma unroll
-      for (int r = 0; r < R; ++r) top[r] = top_of(h[r]);
-      if constexpr (CODES != 32) {
-        float most[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) most[r] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top[r])));
-        if (warps > 1) {
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-            if (lane == 0) tops[parity][r][wid] = most[r];
-          __syncthreads();
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-            most[r] = __uint_as_float(__reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(tops[parity][r][lane]) : 0u));
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) step[r] = row_step<CODES>(most[r], row[r], t == 0 && put[r], &inv[r], a);
-      }
-#pragma unroll
-      for (int r = 0; r < R; ++r) put_codes<CODES>(h[r], top[r], step[r], inv[r], row[r], unit, put[r], a);
+      for (int u = 0; u < U; ++u) put_codes<CODES>(h[u], top[u], step, inv, m, unit[u], on[u], a);
     }
   }
 }
@@ -314,9 +331,10 @@ __global__ void __launch_bounds__(kPairThreads) add_norm_pairs_kernel(const Norm
 // Few rows, long ones, or only one of y and h: a row at a time, U chunks a thread, straight from global memory.
 template <int CODES, int U>
 __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a) {
-  __shared__ double sums[2][2][1][kMaxThreads / 32];
+  __shared__ double sums[2][2][kMaxThreads / 32];
   __shared__ float tops[2][kMaxThreads / 32];
-  const int t = threadIdx.x, T = blockDim.x, lane = t & 31, wid = t >> 5, warps = T >> 5;
+  const int t = threadIdx.x, T = blockDim.x, wid = t >> 5;
+  const Team team{1, T >> 5, 0};
   after_the_call_before();
   int parity = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, parity ^= 1) {
@@ -329,14 +347,14 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a)
       y[u] = on && a.y != nullptr ? load_chunk(a.y + row * a.ldy + chunk * kChunk) : no_values<4>();
       h[u] = on && a.h != nullptr ? load_chunk(a.h + row * a.ldh + chunk * kChunk) : no_values<4>();
     }
-    double sum[1] = {0.0};
-    float rstd[1] = {1.0f};
+    double sum = 0.0;
+    float rstd = 1.0f;
     if (a.post_norm) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) sum[0] += sum_of_squares(y[u]);
-      statistics(sum, rstd, sums[parity][0], a);
+      for (int u = 0; u < U; ++u) sum += sum_of_squares(y[u]);
+      rstd = statistics(sum, sums[parity][0], team, wid, a);
     }
-    sum[0] = 0.0;
+    sum = 0.0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int chunk = t + u * T;
@@ -349,14 +367,14 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a)
           f32x2 z[4];
           widen(y[u], z);
           if (a.post_norm) {
-            times(z, rstd[0]);
+            times(z, rstd);
             times(z, post);
           }
           times(z, gate);
           times(z, a.block_scale);
           h[u] = narrow(z);
         } else {
-          h[u] = a.post_norm ? add<true>(y[u], h[u], rstd[0], post, gate, a) : add<false>(y[u], h[u], rstd[0], gate, gate, a);
+          h[u] = a.post_norm ? add<true>(y[u], h[u], rstd, post, gate, a) : add<false>(y[u], h[u], rstd, gate, gate, a);
         }
       } else {
         f32x2 s[4];
@@ -365,10 +383,10 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a)
         h[u] = narrow(s);
       }
       if (a.h_out != nullptr) store_chunk(a.h_out + row * a.ldho + chunk * kChunk, h[u]);
-      sum[0] += sum_of_squares(h[u]);
+      sum += sum_of_squares(h[u]);
     }
     if (CODES == 0 && a.x_out == nullptr) continue;
-    statistics(sum, rstd, sums[parity][1], a);
+    rstd = statistics(sum, sums[parity][1], team, wid, a);
     float top[U], most = 0.0f, step = 1.0f, inv = 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -377,21 +395,13 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a)
       if (chunk >= a.chunks) continue;
       f32x2 pre[4];
       load_weights(a.pre_w, chunk, pre);
-      h[u] = norm(h[u], rstd[0], pre);
+      h[u] = norm(h[u], rstd, pre);
       if (a.x_out != nullptr) store_chunk(a.x_out + row * a.ldxo + chunk * kChunk, h[u]);
       if constexpr (CODES != 0) top[u] = top_of(h[u]);
       most = max_abs(most, top[u]);
     }
     if constexpr (CODES != 0) {
-      if constexpr (CODES != 32) {
-        most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
-        if (warps > 1) {
-          if (lane == 0) tops[parity][wid] = most;
-          __syncthreads();
-          most = __uint_as_float(__reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(tops[parity][lane]) : 0u));
-        }
-        step = row_step<CODES>(most, m, t == 0, &inv, a);
-      }
+      if constexpr (CODES != 32) step = row_step<CODES>(largest(most, tops[parity], team, wid), m, t == 0, &inv, a);
 #pragma unroll
       for (int u = 0; u < U; ++u) put_codes<CODES>(h[u], top[u], step, inv, m, t + u * T, t + u * T < a.chunks, a);
     }
@@ -459,15 +469,18 @@ int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_
   a.chunks = int(K / kChunk);
   const int64_t sms = device_sm_count();
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // pairs of rows where there are more rows than places for one
-  const int T = int(K / kUnit + 31) / 32 * 32;
-  const bool pairs = T <= kPairThreads && K % kUnit == 0 && a.y != nullptr && a.h != nullptr && M > sms * (kMaxThreads / T);
+  // Teams where there are more rows than places for one of them each: a thread of a team takes 1, 2 or 4 units.
+  const int units = int(K / kUnit), each = units <= 32 ? 1 : units <= 64 ? 2 : 4;
+  const int T = ((units + each - 1) / each + 31) / 32 * 32, most = T > 0 ? kTeamThreads / T : 0, teams = most < kMaxTeams ? most : kMaxTeams;
+  const bool in_teams = K % kUnit == 0 && K <= 8192 && a.y != nullptr && a.h != nullptr && M > sms * teams;
   a.wide = (H_out_f16 == nullptr || wide_ok(H_out_f16, ldho)) && (X_out_f16 == nullptr || wide_ok(X_out_f16, ldxo));
-  auto go_pairs = [&](auto kern) {
-    const int ring = int(kRing * 2 * 2 * K * 2);
-    const int64_t places = sms * (kPairThreads / T), blocks = (M + 1) / 2;
-    if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), ring)) return int(SMOOTHROT_CUDA_ERROR);
-    return launch(kern, dim3(unsigned(blocks < places ? blocks : places)), T, ring, 0, st, a);
+  auto go_teams = [&](auto one, auto two, auto four) {
+    const int bytes = int(3 * 4 * K + int64_t(teams) * 2 * 2 * K);
+    const int64_t blocks = (M + teams - 1) / teams;
+    const dim3 grid(unsigned(blocks < sms ? blocks : sms));
+    auto kern = each == 1 ? one : each == 2 ? two : four;
+    if (!allow_dynamic_smem(reinterpret_cast<const void*>(kern), bytes)) return int(SMOOTHROT_CUDA_ERROR);
+    return launch(kern, grid, teams * T, bytes, 0, st, a, T);
   };
   const int per = a.chunks <= kMaxThreads ? 1 : a.chunks <= 2 * kMaxThreads ? 2 : kMostChunks;
   auto go_rows = [&](auto one, auto two, auto most) {
@@ -477,9 +490,10 @@ int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_
     return per == 1 ? launch(one, grid, threads, 0, 0, st, a)
                     : per == 2 ? launch(two, grid, threads, 0, 0, st, a) : launch(most, grid, threads, 0, 0, st, a);
   };
-#define SR_NORM(C)                                                                                                     \
-  pairs ? (post_norm ? go_pairs(add_norm_pairs_kernel<C, true>) : go_pairs(add_norm_pairs_kernel<C, false>))            \
-        : go_rows(add_norm_kernel<C, 1>, add_norm_kernel<C, 2>, add_norm_kernel<C, kMostChunks>)
+#define SR_TEAMS(C, P) go_teams(add_norm_teams_kernel<C, P, 1>, add_norm_teams_kernel<C, P, 2>, add_norm_teams_kernel<C, P, 4>)
+#define SR_NORM(C)                                                                                                      \
+  in_teams ? (post_norm ? SR_TEAMS(C, true) : SR_TEAMS(C, false))                                                       \
+           : go_rows(add_norm_kernel<C, 1>, add_norm_kernel<C, 2>, add_norm_kernel<C, kMostChunks>)
   switch (codes) {
     case 0: return SR_NORM(0);
     case 4: return SR_NORM(4);
@@ -487,6 +501,7 @@ int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_
     default: return SR_NORM(32);
   }
 #undef SR_NORM
+#undef SR_TEAMS
 }
 
 }  // extern "C"

@@ -183,8 +183,7 @@ __device__ __forceinline__ Unit load_unit(const __half* p, bool wide) {
 __device__ __forceinline__ void store_unit(__half* p, const Unit& u, bool wide) {
   if (wide) {
     asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u.w[0]), "r"(u.w[1]), "r"(u.w[2]),
-                 "r"(u.w[3]), "r"(u.w[4]), "r"(u.w[5]), "r"(u.w[6]), "r"(u.w[7])
-                 : "memory");
+                 "r"(u.w[3]), "r"(u.w[4]), "r"(u.w[5]), "r"(u.w[6]), "r"(u.w[7]));
   } else {
     __stcs(reinterpret_cast<uint4*>(p), make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]));
     __stcs(reinterpret_cast<uint4*>(p) + 1, make_uint4(u.w[4], u.w[5], u.w[6], u.w[7]));
