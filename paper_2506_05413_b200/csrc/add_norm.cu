@@ -469,10 +469,22 @@ int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_
   a.chunks = int(K / kChunk);
   const int64_t sms = device_sm_count();
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // Teams where there are more rows than places for one of them each: a thread of a team takes 1, 2 or 4 units.
-  const int units = int(K / kUnit), each = units <= 32 ? 1 : units <= 64 ? 2 : 4;
-  const int T = ((units + each - 1) / each + 31) / 32 * 32, most = T > 0 ? kTeamThreads / T : 0, teams = most < kMaxTeams ? most : kMaxTeams;
-  const bool in_teams = K % kUnit == 0 && K <= 8192 && a.y != nullptr && a.h != nullptr && M > sms * teams;
+  // A row at a time while there is a place for each; teams beyond, whose threads take 1, 2 or 4 units: more of them let more rows
+  // be under way and cost a round of rows more.  The estimate, in us (a fixed part and a time per round; 1200 rows of 4096 take 17.2,
+  // 16.8 and 20.2, 4096 rows 39.1, 31.9 and 32.3), decides.
+  const int row_threads = (a.chunks + 31) / 32 * 32, units = int(K / kUnit);
+  const bool in_teams = K % kUnit == 0 && K <= 8192 && a.y != nullptr && a.h != nullptr && M > sms * (kMaxThreads / row_threads);
+  int each = 0, T = 0, teams = 0;
+  double least = 0.0;
+  for (int e = 1; in_teams && e <= 4; e *= 2) {
+    const int threads = ((units + e - 1) / e + 31) / 32 * 32, most = kTeamThreads / threads, n = most < kMaxTeams ? most : kMaxTeams;
+    const double rounds = double((M + sms * n - 1) / (sms * n)), us = e == 1 ? 4.0 + 2.5 * rounds : e == 2 ? 5.5 + 3.9 * rounds : 6.5 + 6.5 * rounds;
+    if (each != 0 && us >= least) continue;
+    least = us;
+    each = e;
+    T = threads;
+    teams = n;
+  }
   a.wide = (H_out_f16 == nullptr || wide_ok(H_out_f16, ldho)) && (X_out_f16 == nullptr || wide_ok(X_out_f16, ldxo));
   auto go_teams = [&](auto one, auto two, auto four) {
     const int bytes = int(3 * 4 * K + int64_t(teams) * 2 * 2 * K);
