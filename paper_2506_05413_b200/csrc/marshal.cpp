@@ -269,8 +269,9 @@ PyObject* attn_prefill(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ---- microscaled codes and norms ----
 
 // The work goes to the current device's current stream: its tensors have to be there too.
+thread_local int g_device = 0;        // asked for once a call
 void here(const at::Tensor& t, const char* name) {
-  if (t.device().index() != c10::cuda::current_device())
+  if (t.device().index() != g_device)
     throw BadValue(std::string(name) + " is not on the current CUDA device");
 }
 float* step_of(PyObject* o, int64_t n, const char* name) {
@@ -328,6 +329,7 @@ Coded coded(PyObject* q, PyObject* scale, int64_t group, const char* q_name, con
 // X, q_out, scale_out, step_out, group, pre, walsh
 PyObject* mx_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> int {
+    g_device = c10::cuda::current_device();
     const Rows x = half_rows(a[0], "X");
     const int64_t group = whole(a[4], "group");
     uint8_t* q = codes_of(a[1], x.rows, x.cols / 2, "q_out");
@@ -340,6 +342,7 @@ PyObject* mx_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // q, scale, step, Y, group
 PyObject* mx_dequant(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 5, [&]() -> int {
+    g_device = c10::cuda::current_device();
     const int64_t group = whole(a[4], "group");
     const Coded c = coded(a[0], a[1], group, "q", "scale");
     const Rows y = half_rows(a[3], c.rows, c.K, "Y");
@@ -350,6 +353,7 @@ PyObject* mx_dequant(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // Xq, x_scale, x_step, Wq, w_scale, w_step, Y, group
 PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 8, [&]() -> int {
+    g_device = c10::cuda::current_device();
     const int64_t group = whole(a[7], "group");
     const Coded x = coded(a[0], a[1], group, "Xq", "x_scale"), w = coded(a[3], a[4], group, "Wq", "w_scale");
     if (x.K != w.K) throw BadValue("Xq and Wq disagree on K");
@@ -362,6 +366,7 @@ PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // Xq, x_scale, x_step, gate_q, gate_scale, gate_step, up_q, up_scale, up_step, h_out, q_out, scale_out, h_step, group, walsh
 PyObject* mx_glu(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 15, [&]() -> int {
+    g_device = c10::cuda::current_device();
     const int64_t group = whole(a[13], "group");
     const Coded x = coded(a[0], a[1], group, "Xq", "x_scale");
     const Coded g = coded(a[3], a[4], group, "gate_q", "gate_scale"), u = coded(a[6], a[7], group, "up_q", "up_scale");
@@ -389,6 +394,7 @@ PyObject* mx_glu(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // residual_scale, eps, clip
 PyObject* add_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 16, [&]() -> int {
+    g_device = c10::cuda::current_device();
     if (a[0] == Py_None && a[1] == Py_None) throw BadValue("one of y and h is required");
     Rows y, h, ho, xo;
     if (a[0] != Py_None) y = half_rows(a[0], "y");
