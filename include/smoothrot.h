@@ -429,8 +429,10 @@ int smoothrot_mx_glu(const uint8_t* Xq, const uint8_t* x_scale, const float* x_s
  *     products from the left, each and the sum rounded to fp32 by itself
  * Y NULL: H' = fp16(residual_scale * H), H NULL: H' = fp16(block_scale * (gate * z)).  Written are, of H_out [M x ldho], X_out [M x ldxo]
  * (fp16) and the codes of x, those that are asked for: `codes` 0 none; 4 what smoothrot_quant_act_plain makes of X_out
- * with ratio `clip` (step_out: dx_out); 16 or 32 what smoothrot_mx_quant makes of X_out in groups of that size.
- * H_out may be H or Y and X_out may be H or Y, with the same leading dimension, but not one and the same.
+ * with ratio `clip` (step_out: dx_out), except that a NaN in a row makes its step NaN; 16 or 32 what smoothrot_mx_quant makes of
+ * X_out in groups of that size.
+ * H_out may be H or Y and X_out may be H or Y, with the same leading dimension, but not one and the same.  q_out and step_out go with
+ * codes, scale_out with codes 16 and 32; where they are not asked for they are NULL.
  * K a multiple of 8, of 128 with codes 16 and 32; K <= 32768.  eps > 0.
  */
 int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_t ldh, int64_t M, int64_t K, int post_norm,

@@ -60,7 +60,7 @@ __device__ __forceinline__ float rstd_of(double sum, double inv_k, double eps) {
 }
 
 __device__ __forceinline__ Chunk load_chunk(const __half* p) {
-  const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
+  const uint4 a = load_once(reinterpret_cast<const uint4*>(p));
   return Chunk{{a.x, a.y, a.z, a.w}};
 }
 __device__ __forceinline__ Unit shared_unit(const uint8_t* p) {
@@ -75,7 +75,7 @@ template <int W>
 __device__ __forceinline__ void load_weights(const float* w, int part, f32x2 (&v)[W]) {
 #pragma unroll
   for (int i = 0; i < W / 2; ++i) {
-    const float4 f = w != nullptr ? __ldg(reinterpret_cast<const float4*>(w + part * 2 * W) + i) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+    const float4 f = w != nullptr ? load(reinterpret_cast<const float4*>(w + part * 2 * W) + i) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
     v[2 * i] = pack2(f.x, f.y);
     v[2 * i + 1] = pack2(f.z, f.w);
   }
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kTeamThreads) add_norm_teams_kernel(const Norm
   for (int w = POST ? 0 : 1; w < 3; ++w)
     for (int i = threadIdx.x; i < a.K / 4; i += blockDim.x) {
       // none: ones, which change nothing
-      const float4 f = arrays[w] != nullptr ? __ldg(reinterpret_cast<const float4*>(arrays[w]) + i) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+      const float4 f = arrays[w] != nullptr ? load(reinterpret_cast<const float4*>(arrays[w]) + i) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
       weights[w * (a.K / 4) + (i & 3) * units + (i >> 2)] = f;
     }
   __syncthreads();
@@ -442,6 +442,7 @@ int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_
   if (H_out_f16 == nullptr && X_out_f16 == nullptr && codes == 0) return SMOOTHROT_INVALID_ARG;
   if (codes != 0 && (q_out == nullptr || (codes != 32) != (step_out != nullptr) || (codes >= 16 && scale_out == nullptr)))
     return SMOOTHROT_INVALID_ARG;
+  if ((codes == 0 && (q_out != nullptr || step_out != nullptr)) || (codes < 16 && scale_out != nullptr)) return SMOOTHROT_INVALID_ARG;
   if (H_out_f16 != nullptr && H_out_f16 == X_out_f16) return SMOOTHROT_INVALID_ARG;
   const struct { const void* p; int64_t ld; } rows[] = {{Y_f16, ldy}, {H_f16, ldh}, {H_out_f16, ldho}, {X_out_f16, ldxo}};
   for (const auto& r : rows)
@@ -451,6 +452,10 @@ int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_
   for (const float* p : {post_w, gate, pre_w})
     if (p != nullptr && !aligned16(p)) return SMOOTHROT_BAD_ALIGNMENT;
   if (codes != 0 && (!aligned16(q_out) || (codes >= 16 && !aligned16(scale_out)))) return SMOOTHROT_BAD_ALIGNMENT;
+  // written over an input: row for row, or one row's output would be another's input
+  for (int i = 0; i < 2; ++i)
+    for (int o = 2; o < 4; ++o)
+      if (M > 1 && rows[i].p != nullptr && rows[i].p == rows[o].p && rows[i].ld != rows[o].ld) return SMOOTHROT_INVALID_ARG;
   NormArgs a{};
   a.y = static_cast<const __half*>(Y_f16);
   a.h = static_cast<const __half*>(H_f16);

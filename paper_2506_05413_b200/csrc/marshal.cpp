@@ -269,8 +269,9 @@ PyObject* attn_prefill(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ---- microscaled codes and norms ----
 
 // The work goes to the current device's current stream: its tensors have to be there too.
-thread_local int g_device = 0;        // asked for once a call
+thread_local int g_device = -1;        // asked for once a call, when a CUDA tensor has been seen
 void here(const at::Tensor& t, const char* name) {
+  if (g_device < 0) g_device = c10::cuda::current_device();
   if (t.device().index() != g_device)
     throw BadValue(std::string(name) + " is not on the current CUDA device");
 }
@@ -293,6 +294,7 @@ Rows half_rows(PyObject* o, int64_t rows, int64_t cols, const char* name) {
 int64_t whole(PyObject* o, const char* name) {
   const int64_t x = PyLong_AsLongLong(o);
   if (x == -1 && PyErr_Occurred()) throw TypeMismatch(std::string(name) + " must be a whole number");
+  if (x != int(x)) throw BadValue(std::string(name) + " is out of range");
   return x;
 }
 
@@ -329,7 +331,7 @@ Coded coded(PyObject* q, PyObject* scale, int64_t group, const char* q_name, con
 // X, q_out, scale_out, step_out, group, pre, walsh
 PyObject* mx_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> int {
-    g_device = c10::cuda::current_device();
+    g_device = -1;
     const Rows x = half_rows(a[0], "X");
     const int64_t group = whole(a[4], "group");
     uint8_t* q = codes_of(a[1], x.rows, x.cols / 2, "q_out");
@@ -342,7 +344,7 @@ PyObject* mx_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // q, scale, step, Y, group
 PyObject* mx_dequant(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 5, [&]() -> int {
-    g_device = c10::cuda::current_device();
+    g_device = -1;
     const int64_t group = whole(a[4], "group");
     const Coded c = coded(a[0], a[1], group, "q", "scale");
     const Rows y = half_rows(a[3], c.rows, c.K, "Y");
@@ -353,7 +355,7 @@ PyObject* mx_dequant(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // Xq, x_scale, x_step, Wq, w_scale, w_step, Y, group
 PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 8, [&]() -> int {
-    g_device = c10::cuda::current_device();
+    g_device = -1;
     const int64_t group = whole(a[7], "group");
     const Coded x = coded(a[0], a[1], group, "Xq", "x_scale"), w = coded(a[3], a[4], group, "Wq", "w_scale");
     if (x.K != w.K) throw BadValue("Xq and Wq disagree on K");
@@ -366,7 +368,7 @@ PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // Xq, x_scale, x_step, gate_q, gate_scale, gate_step, up_q, up_scale, up_step, h_out, q_out, scale_out, h_step, group, walsh
 PyObject* mx_glu(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 15, [&]() -> int {
-    g_device = c10::cuda::current_device();
+    g_device = -1;
     const int64_t group = whole(a[13], "group");
     const Coded x = coded(a[0], a[1], group, "Xq", "x_scale");
     const Coded g = coded(a[3], a[4], group, "gate_q", "gate_scale"), u = coded(a[6], a[7], group, "up_q", "up_scale");
@@ -394,7 +396,7 @@ PyObject* mx_glu(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // residual_scale, eps, clip
 PyObject* add_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 16, [&]() -> int {
-    g_device = c10::cuda::current_device();
+    g_device = -1;
     if (a[0] == Py_None && a[1] == Py_None) throw BadValue("one of y and h is required");
     Rows y, h, ho, xo;
     if (a[0] != Py_None) y = half_rows(a[0], "y");
@@ -405,6 +407,8 @@ PyObject* add_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t codes = whole(a[8], "codes");
     uint8_t *q = nullptr, *scale = nullptr;
     float* step = nullptr;
+    if ((codes == 0 && (a[5] != Py_None || a[7] != Py_None)) || (codes < 16 && a[6] != Py_None))
+      throw BadValue("q_out and step_out go with codes, scale_out with microscaled ones");
     if (codes != 0) {
       if (a[5] == Py_None || (codes >= 16 && a[6] == Py_None)) throw BadValue("codes need q_out, and scale_out where they are microscaled");
       q = codes_of(a[5], rows, K / 2, "q_out");

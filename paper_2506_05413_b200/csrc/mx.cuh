@@ -60,6 +60,33 @@ __device__ __forceinline__ void after_the_call_before() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// Loads of what a call before may have written: volatile, so that none is moved to before that wait.  _once: data that is not read again.
+__device__ __forceinline__ float load(const float* p) {
+  float v;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ float4 load(const float4* p) {
+  float4 v;
+  asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t load(const uint8_t* p) {
+  uint32_t v;
+  asm volatile("ld.global.u8 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint2 load_once(const uint2* p) {
+  uint2 v;
+  asm volatile("ld.global.cs.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
 // ---- barriers of asynchronous copies ----
 
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s, of every wait
@@ -164,7 +191,7 @@ template <int W>
 struct Part {
   uint32_t w[W];
 };
-// The quantizers': 32 bytes.  `wide`: the address is a multiple of 32, as one load; otherwise two of 16 bytes.
+// A unit is 32 bytes.  `wide`: the address is a multiple of 32, as one load; otherwise two of 16 bytes.
 constexpr int kUnit = 16;
 typedef Part<kUnit / 2> Unit;
 
@@ -175,7 +202,7 @@ __device__ __forceinline__ Unit load_unit(const __half* p, bool wide) {
                  : "=r"(u.w[0]), "=r"(u.w[1]), "=r"(u.w[2]), "=r"(u.w[3]), "=r"(u.w[4]), "=r"(u.w[5]), "=r"(u.w[6]), "=r"(u.w[7])
                  : "l"(p));
   } else {
-    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p)), b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+    const uint4 a = load_once(reinterpret_cast<const uint4*>(p)), b = load_once(reinterpret_cast<const uint4*>(p) + 1);
     u = Unit{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
   }
   return u;

@@ -93,7 +93,7 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, u
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
-// the same with a barrier that may be the other CTA's of the pair
+// a load with a barrier that may be the other CTA's of the pair
 __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
   asm volatile(
       "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
@@ -295,7 +295,7 @@ __device__ __forceinline__ void times_steps(float (&v)[32], float row, const flo
 #pragma unroll
   for (int j = 0; j < 32; j += 4) {
     float4 w = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-    if (step != nullptr && n0 + j < n) w = __ldg(reinterpret_cast<const float4*>(step + n0 + j));
+    if (step != nullptr && n0 + j < n) w = load(reinterpret_cast<const float4*>(step + n0 + j));
     v[j] *= row * w.x;
     v[j + 1] *= row * w.y;
     v[j + 2] *= row * w.z;
@@ -527,7 +527,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     for (int tile = first; tile < tiles; tile += step, ++n) {
       const int ta = tile % p.tiles_a, tb = tile / p.tiles_a;
       const int row0 = ta * 256 + int(rank) * kTile + q * 32, m = row0 + lane;
-      const float xs = p.x_step != nullptr && m < p.M ? __ldg(p.x_step + m) : 1.0f;
+      const float xs = p.x_step != nullptr && m < p.M ? load(p.x_step + m) : 1.0f;
       const int chunk = (warp - 2) >> 2;
       // the chunk's first column of the output, and where its two parts of 32 columns lie in the accumulator
       const int n0 = MODE == kLinear ? tb * 256 + 64 * chunk : tb * kTile + 32 * chunk;
@@ -561,7 +561,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           store_box(&map_y, box, a, n0, row0, p.N, p.M, lane);
         } else {
           uint4 codes;
-          const float hs = GROUP == 16 && m < p.M ? __ldg(p.h_step + m) : 1.0f;
+          const float hs = GROUP == 16 && m < p.M ? load(p.h_step + m) : 1.0f;
           const uint32_t bytes = encode_values<GROUP>(a, hs, &codes);
           if (m < p.M && n0 < p.N) {
             __stcs(reinterpret_cast<uint4*>(p.q_out + int64_t(m) * (p.N / 2) + n0 / 2), codes);
@@ -640,8 +640,8 @@ __device__ __forceinline__ void add_shared(float (&v)[8], uint32_t addr) {
 __device__ __forceinline__ void eight_steps(const float* step, int n, float (&w)[8]) {
   float4 a = make_float4(1.0f, 1.0f, 1.0f, 1.0f), b = a;
   if (step != nullptr) {
-    a = __ldg(reinterpret_cast<const float4*>(step + n));
-    b = __ldg(reinterpret_cast<const float4*>(step + n) + 1);
+    a = load(reinterpret_cast<const float4*>(step + n));
+    b = load(reinterpret_cast<const float4*>(step + n) + 1);
   }
   w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
   w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
@@ -838,7 +838,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         add_shared(a, at);
         if (GATED) add_shared(b, at + uint32_t(kTile / 2 * 4));
       }
-      const float xs = p.x_step != nullptr ? __ldg(p.x_step + m) : 1.0f;
+      const float xs = p.x_step != nullptr ? load(p.x_step + m) : 1.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) a[j] *= xs * ws[j];
       if constexpr (GATED) {
@@ -868,7 +868,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       for (int j = 0; j < 4; ++j) v[j] = pack2(a[2 * j], a[2 * j + 1]);
       if constexpr (MODE == kGatedCodes) {
         uint32_t byte;
-        const float hs = GROUP == 16 ? __ldg(p.h_step + m) : 1.0f;
+        const float hs = GROUP == 16 ? load(p.h_step + m) : 1.0f;
         const Part<1> codes = encode<GROUP>(v, top_of(v), hs, &byte);
         if (there) {
           *reinterpret_cast<uint32_t*>(p.q_out + int64_t(m) * (p.N / 2) + n / 2) = codes.w[0];

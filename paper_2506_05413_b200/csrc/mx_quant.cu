@@ -44,7 +44,7 @@ template <int W>
 __device__ __forceinline__ void load_diagonal(const float* pre, int part, f32x2 (&d)[W]) {
 #pragma unroll
   for (int i = 0; i < W / 2; ++i) {
-    const float4 w = __ldg(reinterpret_cast<const float4*>(pre + part * 2 * W) + i);
+    const float4 w = load(reinterpret_cast<const float4*>(pre + part * 2 * W) + i);
     d[2 * i] = pack2(w.x, w.y);
     d[2 * i + 1] = pack2(w.z, w.w);
   }
@@ -192,8 +192,8 @@ __device__ __forceinline__ uint4 from_codes(uint32_t word) {
 // As mx_quant32_kernel: a thread keeps to its unit of every lines-th row.
 template <int GROUP>
 __global__ void __launch_bounds__(kFlatThreads)
-mx_dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scale, const float* __restrict__ step, int rows,
-                  int units, int lines, __half* __restrict__ y, int64_t ldy, bool wide) {
+mx_dequant_kernel(const uint8_t* q, const uint8_t* scale, const float* step, int rows, int units, int lines, __half* y, int64_t ldy,
+                  bool wide) {
   const int64_t i = int64_t(blockIdx.x) * kFlatThreads + threadIdx.x;
   const int line = int(i / units), unit = int(i - int64_t(line) * units);
   if (line >= lines) return;
@@ -206,8 +206,8 @@ mx_dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ sca
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int row = min(m + r * lines, rows - 1);
-      word[r] = __ldcs(reinterpret_cast<const uint2*>(q) + int64_t(row) * units + unit);
-      byte[r] = scale[scale_word(row, 0, units / (GROUP / 4)) + offset];
+      word[r] = load_once(reinterpret_cast<const uint2*>(q) + int64_t(row) * units + unit);
+      byte[r] = load(scale + scale_word(row, 0, units / (GROUP / 4)) + offset);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -215,7 +215,7 @@ mx_dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ sca
       if (row >= rows) break;
       float d = GROUP == 16 ? from_e4m3(byte[r])
                             : __uint_as_float(byte[r] == 0u ? 0x00400000u : byte[r] == 255u ? 0x7fffffffu : byte[r] << 23);
-      if (step != nullptr) d = __fmul_rn(d, __ldg(step + row));
+      if (step != nullptr) d = __fmul_rn(d, load(step + row));
       const uint4 lo = from_codes(word[r].x), hi = from_codes(word[r].y);
       const Unit codes{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}};
       f32x2 v[8];

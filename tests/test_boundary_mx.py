@@ -115,3 +115,11 @@ def test_the_binding_asks_for_cuda_tensors():
             call()
     with pytest.raises(ValueError):
         sr.add_norm(x, x, codes="mx8")
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(q=P), -1), (dict(step=P), -1), (dict(s=P), -1), (dict(codes=4, q=P, step=P, s=P), -1), (dict(ldho=512), -1), (dict(Xo=P, Ho=None, ldxo=264), -1),
+    (dict(M=0, ldho=512), 0),
+])
+def test_norm_arguments_that_do_not_go_together(lib, change, status):
+    assert _norm(lib, **change) == status
