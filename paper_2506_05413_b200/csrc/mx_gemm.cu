@@ -93,6 +93,10 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, u
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
+// into L2 alone, where what is written later still counts
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap* map, int x, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
+}
 // a load with a barrier that may be the other CTA's of the pair
 __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
   asm volatile(
@@ -618,7 +622,8 @@ struct Stream {
   static constexpr int kTileRows = GATED ? kTile / 2 : kTile;    // output channels of a tile
   static constexpr int kBarriers = (GATED ? 3 : 2) * kStages + 1;
   static constexpr int kRingBytes = kStages * kStageBytes;
-  static constexpr int kSumBytes = BN * kTile * 4;               // of one part: over the ring, once it has been used; of more: behind it
+  // of one part: over the ring, once it has been used; of more: behind it, rounded up to whole rows of tokens (3 parts: BN + 2)
+  static constexpr int kSumBytes = (BN + 2) * kTile * 4;
   static constexpr int kHeadBytes = (kBarriers * 8 + 16 + 127) / 128 * 128;
   static constexpr int kSmemBytes = 1024 + kRingBytes + kHeadBytes;
   static constexpr int kScaleCol = BN;
@@ -629,13 +634,15 @@ struct Stream {
   static_assert(kStageBytes % 1024 == 0, "swizzled tiles start on 1024 bytes");
 };
 
-// Eight neighbouring sums of a part
+// Eight neighbouring sums of a part; every other four lanes take the halves in the other order, and no two meet in a bank.
 __device__ __forceinline__ void add_shared(float (&v)[8], uint32_t addr) {
+  const bool other = (threadIdx.x & 4) != 0;
+  const uint32_t flip = other ? 16u : 0u;
   float4 a, b;
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w) : "r"(addr) : "memory");
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(addr + 16u) : "memory");
-  v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-  v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w) : "r"(addr + flip) : "memory");
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(addr + (16u - flip)) : "memory");
+  v[0] += other ? b.x : a.x; v[1] += other ? b.y : a.y; v[2] += other ? b.z : a.z; v[3] += other ? b.w : a.w;
+  v[4] += other ? a.x : b.x; v[5] += other ? a.y : b.y; v[6] += other ? a.z : b.z; v[7] += other ? a.w : b.w;
 }
 __device__ __forceinline__ void eight_steps(const float* step, int n, float (&w)[8]) {
   float4 a = make_float4(1.0f, 1.0f, 1.0f, 1.0f), b = a;
@@ -707,6 +714,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   const int m0 = int(blockIdx.y) * BN, n0 = tile * T::kTileRows;
   const int k0 = int(int64_t(p.kblocks) * part / parts), k1 = int(int64_t(p.kblocks) * (part + 1) / parts);
   if (parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");     // this CTA runs: its memory may be written
+  const int slots = (BN + parts - 1) / parts;               // tokens that a CTA finishes, at the most
   const uint32_t sums_at = parts > 1 ? base + uint32_t(T::kRingBytes + T::kHeadBytes) : base;
   auto set_up = [] { asm volatile("bar.sync 1, %0;" ::"n"(kStreamThreads) : "memory"); };
   // Warp 0 sets up the barriers and has loads on their way before the others have their tensor memory.
@@ -746,6 +754,18 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     if (k1 - k0 <= T::kStages) set_up();
   } else {
     if (warp == 1) tmem_alloc<1>(smem_u32(tmem_slot), T::kTmemCols);
+    if (warp == 3 && blockIdx.y == 0 && elected()) {
+      // While the call before finishes, the first weights are asked into L2 (no further: that one may be asking for its own; two
+      // k-blocks were 3 % faster than none over 40 calls with weights from memory, four 2.6 %).
+      for (int kb = k0; kb < min(k1, k0 + 2); ++kb) {
+        const int x = kb * (T::kScaleBytes / 8);
+        tma_prefetch(&map_w, kb * kRowBytes, n0);
+        tma_prefetch(&map_sw, x, n0 / kTile);
+        if (GATED) tma_prefetch(&map_u, kb * kRowBytes, n0);
+        if (GATED) tma_prefetch(&map_su, x, n0 / kTile);
+      }
+    }
+    __syncwarp();
     after_the_call_before();
     fence_before();
     set_up();
@@ -793,7 +813,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     fence_after();
     const int q = warp & 3, half = (warp - 2) >> 2;
     const uint32_t acc = tmem + (uint32_t(q * 32) << 16);
-    const uint32_t to = sums_at + uint32_t((part * (BN / parts) * kTile + q * 32 + lane) * 4);
+    const uint32_t to = sums_at + uint32_t((part * slots * kTile + q * 32 + lane) * 4);
     const int cols = min(BN, p.M - m0), shift = 31 - __clz(parts);
     constexpr int kRead = BN >= 32 ? 16 : 8;       // tokens at a time
 #pragma unroll 1
@@ -801,13 +821,19 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       float v[kRead];
       tmem_load(acc + c, v);
       tmem_wait_ld();
+      auto send = [&](auto quotient_of, auto rest_of) {
 #pragma unroll
-      for (int i = 0; i < kRead; ++i) {
-        const uint32_t at = to + uint32_t(((c + i) >> shift) * kTile * 4);
-        if (parts > 1)
-          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(at, uint32_t((c + i) & (parts - 1)))), "f"(v[i]) : "memory");
-        else
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v[i]) : "memory");
+        for (int i = 0; i < kRead; ++i)
+          asm volatile("st.shared::cluster.f32 [%0], %1;"
+                       ::"r"(map_to_cta(to + uint32_t(quotient_of(c + i) * kTile * 4), uint32_t(rest_of(c + i)))), "f"(v[i]) : "memory");
+      };
+      if (parts == 1) {
+#pragma unroll
+        for (int i = 0; i < kRead; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + uint32_t((c + i) * kTile * 4)), "f"(v[i]) : "memory");
+      } else if (parts == 3) {
+        send([](int t) { return (t * 342) >> 10; }, [](int t) { return t - ((t * 342) >> 10) * 3; });      // t / 3, t % 3 for t < 512
+      } else {
+        send([&](int t) { return t >> shift; }, [&](int t) { return t & (parts - 1); });
       }
     }
   }
@@ -834,7 +860,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 #pragma unroll
       for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.0f;
       uint32_t at = sums_at + uint32_t((min(i, mine - 1) * kTile + chunk * 8) * 4);
-      for (int r = 0; r < parts; ++r, at += uint32_t(BN / parts * kTile * 4)) {
+      for (int r = 0; r < parts; ++r, at += uint32_t(slots * kTile * 4)) {
         add_shared(a, at);
         if (GATED) add_shared(b, at + uint32_t(kTile / 2 * 4));
       }
@@ -985,12 +1011,11 @@ int launch_stream(const Call& c, int parts) {
 // Clusters of `size` CTAs, one to an SM, that the device runs at once: a cluster stays inside a part of the chip, so large ones
 // leave SMs over (148, 74, 33, 15 of 1, 2, 4, 8 on B200).  Asked of the runtime once per device.
 int clusters_at_once(int size) {
-  constexpr int kDevices = 64;
-  static std::atomic<int> known[kDevices][4];
-  const int which = size >= 8 ? 3 : size >= 4 ? 2 : size >= 2 ? 1 : 0;
+  constexpr int kDevices = 64, kMostParts = 8;
+  static std::atomic<int> known[kDevices][kMostParts + 1];
   int dev = 0;
-  if (size <= 1 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return device_sm_count() / (size * 2);
-  int n = known[dev][which].load(std::memory_order_relaxed);
+  if (size > kMostParts || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return device_sm_count() / (size * 2);
+  int n = known[dev][size].load(std::memory_order_relaxed);
   if (n > 0) return n;
   typedef Stream<32, 128, false> T;
   auto kern = mx_stream_kernel<32, 128, kLinear>;
@@ -1012,27 +1037,40 @@ int clusters_at_once(int size) {
     (void)cudaGetLastError();
     return device_sm_count() / (size * 2);
   }
-  known[dev][which].store(n, std::memory_order_relaxed);
+  known[dev][size].store(n, std::memory_order_relaxed);
   return n;
 }
 
-// Which kernel.  Up to 128 tokens the few-token one was the faster at every size tried (1 x 4096 x 4096: 3.8 us against 8.5; 128 x
-// 6144 x 4096: 8.4 against 9.9; gated 14336 x 4096: 13.8 against 22.6 with one token, 19.1 against 18.6 with 128).
-// Beyond, gated calls go to the pair kernel (129 x 5632 x 2048: 8.4 us, 10.8 with few-token tiles) and for the others the estimate
-// decides, in us: a fixed part, then a time per k-block and wave of tiles (256 x 4096 x 14336: 16.3 with few-token tiles, K in 2
-// parts, against 21.9; 512 x 4096 x 14336: 25.7 against 22.0).
+// Which kernel.  Up to 128 tokens the few-token one was the faster at every size tried (1 x 4096 x 4096: 4.1 us against 8.5; 128 x
+// 6144 x 4096: 8.2 against 9.9; gated 14336 x 4096: 13.4 against 22.6 with one token, 17.0 against 18.6 with 128).  K is split over
+// as many CTAs as leave every tile's cluster a place at once (61 x 5120 x 4096 in 3 parts 6.2 us, in 2 6.5; 4096 x 14336 in 4
+// 9.3, in 2 12.5, in 8, not all at once, 18.7).
+// Beyond 128 tokens an estimate decides, in us: a fixed part, then a time per k-block and wave of tiles.  Linear, stream | pair: 256 x 4096
+// x 14336 15.9 | 21.5, 200 x 2048 x 5632 7.1 | 11.0, 512 x 4096 x 4096 10.3 | 9.7.  Gated: 200 x 1408 x 2048 6.7 | 7.5, 333 x 5632 x 2048
+// 10.2 | 10.7, 200 x 5632 x 2048 10.3 | 8.6, 300 x 14336 x 4096 37 | 27.
 template <int GROUP, int MODE>
 int run(const Call& c) {
-  const int64_t rows = MODE == kLinear ? kTile : kTile / 2, tiles = (c.N + rows - 1) / rows * ((c.M + 127) / 128);
+  constexpr bool gated = MODE != kLinear;
+  const int64_t rows = gated ? kTile / 2 : kTile, tiles = (c.N + rows - 1) / rows * ((c.M + 127) / 128);
   int parts = 1;
-  while (parts < 8 && tiles <= clusters_at_once(2 * parts) && c.args.kblocks >= 2 * parts) parts *= 2;
+  for (int more : {2, 3, 4, 8}) {
+    if (c.args.kblocks < more || tiles > clusters_at_once(more)) break;
+    parts = more;
+  }
   if (c.M > 128) {
-    if (MODE != kLinear) return launch_pair<GROUP, MODE>(c);
-    const int64_t sms = device_sm_count(), pairs = sms / 2, pair_tiles = (c.M + 255) / 256 * ((c.N + 255) / 256);
-    const double pair_us = 4.6 + 0.30 * double(c.args.kblocks) * double((pair_tiles + pairs - 1) / pairs);
-    const double blocks = double((c.args.kblocks + parts - 1) / parts), ctas = double(tiles * parts);
-    const double stream_us = 4.6 + 0.38 * blocks * (ctas > double(sms) ? ctas / double(sms) : 1.0);
-    return stream_us < pair_us ? launch_stream<GROUP, 128, kLinear>(c, parts) : launch_pair<GROUP, MODE>(c);
+    const int width = gated ? kTile : 256;
+    const int64_t sms = device_sm_count(), pairs = sms / 2, ctas = tiles * parts;
+    const double waves = double(((c.M + 255) / 256 * ((c.N + width - 1) / width) + pairs - 1) / pairs);
+    const double blocks = double((c.args.kblocks + parts - 1) / parts);
+    double pair_us, stream_us;
+    if (gated) {
+      pair_us = 5.4 + 0.33 * double(c.args.kblocks) * waves;
+      stream_us = 5.0 + blocks * (ctas <= sms ? 0.5 : 0.67 * double((ctas + 2 * sms - 1) / (2 * sms)));
+    } else {
+      pair_us = 4.6 + 0.30 * double(c.args.kblocks) * waves;
+      stream_us = 4.6 + blocks * 0.38 * (ctas > sms ? double(ctas) / double(sms) : 1.0);
+    }
+    return stream_us < pair_us ? launch_stream<GROUP, 128, MODE>(c, parts) : launch_pair<GROUP, MODE>(c);
   }
   if (c.M <= 16) return launch_stream<GROUP, 16, MODE>(c, parts);
   if (c.M <= 32) return launch_stream<GROUP, 32, MODE>(c, parts);

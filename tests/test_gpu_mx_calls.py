@@ -96,6 +96,35 @@ def test_the_first_call_of_a_process_may_be_captured(sr):
     assert done.returncode == 0 and "same" in done.stdout, done.stderr[-2000:]
 
 
+@pytest.mark.parametrize("group", [32, 16])
+@pytest.mark.parametrize("m,n,k", [(1, 5000, 1024), (2, 4360, 768), (16, 4360, 896), (31, 5120, 2048), (61, 5120, 640), (64, 5000, 896), (127, 4488, 768), (128, 5120, 1024),
+                                   (150, 2600, 896)])
+def test_k_in_three_parts(sr, mu, m, n, k, group):
+    """Sizes whose tiles leave room for three parts of K, which divide neither the tokens of a tile nor the k-blocks."""
+    import torch
+    g = mu.gen(m + n)
+    x, w = mu.random_coded(g, m, k, group), mu.random_coded(g, n, k, group)
+    y = torch.full((m, n + 8), 9.0, dtype=torch.float16, device=mu.DEV)
+    again = torch.empty(m, n, dtype=torch.float16, device=mu.DEV)
+    for out in (y[:, :n], again):
+        sr.mx_linear(x.q, x.s, w.q, w.s, out, group=group, x_step=x.step, w_step=w.step)
+    want, extra = mu.product(x.values(), w.values(), k)
+    assert bool(((again.double() - want).abs() <= mu.half_bound(want, extra)).all())
+    assert torch.equal(y[:, :n], again) and bool((y[:, n:] == 9).all()) and sr.device_status() == 0
+
+
+@pytest.mark.parametrize("m", [1, 15, 40, 100])
+def test_gated_tiles_in_three_parts(sr, mu, m):
+    import torch
+    g = mu.gen(m)
+    x, a, b = (mu.random_coded(g, r, 896, 32) for r in (m, 2536, 2536))
+    step = torch.full((2536,), 2.0 / 30, device=mu.DEV)
+    h = torch.full((m, 2536), 9.0, dtype=torch.float16, device=mu.DEV)
+    sr.mx_glu(x.q, x.s, a.q, a.s, b.q, b.s, h_out=h, gate_step=step, up_step=step)
+    want, extra = mu.gated(x.values(), a.values() * step.double()[:, None], b.values() * step.double()[:, None], 896)
+    assert bool(((h.double() - want).abs() <= mu.half_bound(want, extra)).all()) and sr.device_status() == 0
+
+
 def test_two_threads_with_a_stream_each(sr, mu):
     """Calls of both product kernels, the quantizer and the norm side by side."""
     import torch
