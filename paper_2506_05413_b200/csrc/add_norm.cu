@@ -174,7 +174,7 @@ __device__ __forceinline__ Part<W> norm(const Part<W>& h, float rstd, const f32x
 }
 // Codes of a thread's values; every thread of the warp takes part, `on` ones write.
 template <int CODES, int W>
-__device__ __forceinline__ void put_codes(const Part<W>& x16, float top, float step, float inv, int m, int part, bool on, const NormArgs& a) {
+__device__ __forceinline__ void put_codes(const Part<W>& x16, float top, const RowStep& row, int m, int part, bool on, const NormArgs& a) {
   f32x2 x[W];
   widen(x16, x);
   Part<W / 4> codes;
@@ -187,12 +187,12 @@ __device__ __forceinline__ void put_codes(const Part<W>& x16, float top, float s
       for (int i = 0; i < 8; ++i) {
         float lo, hi;
         unpack2(x[4 * c + i / 2], lo, hi);
-        const float v = fmaxf(fminf(rintf(quotient(i % 2 ? hi : lo, step, inv)), 7.0f), -8.0f);
+        const float v = fmaxf(fminf(rintf(quotient(i % 2 ? hi : lo, row.step, row.inverse)), 7.0f), -8.0f);
         codes.w[c] |= (uint32_t(int(v)) & 15u) << (4 * i);
       }
     }
   } else {
-    codes = encode<CODES>(x, top, step, &byte);
+    codes = encode<CODES>(x, top, row, &byte);
   }
   if (!on) return;
   uint32_t* to = reinterpret_cast<uint32_t*>(a.q_out + int64_t(m) * (a.K >> 1)) + part * (W / 4);
@@ -202,14 +202,13 @@ __device__ __forceinline__ void put_codes(const Part<W>& x16, float top, float s
     if (writes_scale<CODES, W>(part))
       a.scale_out[scale_word(m, 0, a.K / (4 * CODES)) + scale_offset<CODES, W>(part)] = uint8_t(byte);
 }
-// The step of a row from its largest magnitude, written by one thread; `inv` what codes of 4 bits per row are made with.
+// The step of a row from its largest magnitude, written by one thread.
 template <int CODES>
-__device__ __forceinline__ float row_step(float most, int m, bool write, float* inv, const NormArgs& a) {
-  float step = CODES == 4 ? step_from_absmax(most, a.clip) : row_step_16(__float_as_uint(most));
+__device__ __forceinline__ RowStep step_of(float most, int m, bool write, const NormArgs& a) {
+  const float step = CODES == 4 ? step_from_absmax(most, a.clip) : row_step_16(__float_as_uint(most));
   if (write) a.step_out[m] = step;
-  if (CODES == 4) *inv = __frcp_rn(step);
-  else if (!(step > 0.0f)) step = 1.0f;       // NaN: whatever the codes are, the row's values are NaN
-  return step;
+  if (CODES == 4) return RowStep{step, 0.0f, __frcp_rn(step)};
+  return row_step(step > 0.0f ? step : 1.0f);       // NaN: whatever the codes are, the row's values are NaN
 }
 
 // CODES: 0 none, 4 one step per row, 16 and 32 microscaled groups.  POST: a norm after the block.
@@ -308,7 +307,8 @@ __global__ void __launch_bounds__(kTeamThreads) add_norm_teams_kernel(const Norm
     }
     if (CODES == 0 && a.x_out == nullptr) continue;
     rstd = statistics(sum, sums[parity][1], team, wid, a);
-    float top[U], most = 0.0f, step = 1.0f, inv = 0.0f;
+    float top[U], most = 0.0f;
+    RowStep step{};
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       f32x2 pre[8];
@@ -321,9 +321,9 @@ __global__ void __launch_bounds__(kTeamThreads) add_norm_teams_kernel(const Norm
       }
     }
     if constexpr (CODES != 0) {
-      if constexpr (CODES != 32) step = row_step<CODES>(largest(most, tops[parity], team, wid), m, t == 0, &inv, a);
+      if constexpr (CODES != 32) step = step_of<CODES>(largest(most, tops[parity], team, wid), m, t == 0, a);
 #pragma unroll
-      for (int u = 0; u < U; ++u) put_codes<CODES>(h[u], top[u], step, inv, m, unit[u], on[u], a);
+      for (int u = 0; u < U; ++u) put_codes<CODES>(h[u], top[u], step, m, unit[u], on[u], a);
     }
   }
 }
@@ -387,7 +387,8 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a)
     }
     if (CODES == 0 && a.x_out == nullptr) continue;
     rstd = statistics(sum, sums[parity][1], team, wid, a);
-    float top[U], most = 0.0f, step = 1.0f, inv = 0.0f;
+    float top[U], most = 0.0f;
+    RowStep step{};
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int chunk = t + u * T;
@@ -401,9 +402,9 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a)
       most = max_abs(most, top[u]);
     }
     if constexpr (CODES != 0) {
-      if constexpr (CODES != 32) step = row_step<CODES>(largest(most, tops[parity], team, wid), m, t == 0, &inv, a);
+      if constexpr (CODES != 32) step = step_of<CODES>(largest(most, tops[parity], team, wid), m, t == 0, a);
 #pragma unroll
-      for (int u = 0; u < U; ++u) put_codes<CODES>(h[u], top[u], step, inv, m, t + u * T, t + u * T < a.chunks, a);
+      for (int u = 0; u < U; ++u) put_codes<CODES>(h[u], top[u], step, m, t + u * T, t + u * T < a.chunks, a);
     }
   }
 }

@@ -50,8 +50,6 @@ inline int launch(void (*kern)(Params...), dim3 grid, int threads, int smem, int
   return launch_status();
 }
 
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-
 // Kernels of this kind are launched so that one may be set up while the one before it in the stream finishes; each
 // waits here, before it reads or writes what others may use.
 // The wait comes first: a call that follows and waits for the end of this one has then waited for all before it too.
@@ -276,10 +274,18 @@ __device__ __forceinline__ float top_of(const f32x2 (&v)[W]) {
   return m[0];
 }
 
+// A row's step as groups of 16 need it.
+struct RowStep {
+  float step, six, inverse;      // 6 step and its reciprocal
+};
+__device__ __forceinline__ RowStep row_step(float step) {
+  const float six = __fmul_rn(6.0f, step);
+  return RowStep{step, six, __frcp_rn(six)};
+}
 // A thread's values, with their largest magnitude, to codes (a word for every 8) and the scale byte of their group.  The threads
 // of a group, neighbouring lanes, take part together.
 template <int GROUP, int W>
-__device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, float step, uint32_t* byte) {
+__device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, const RowStep& row, uint32_t* byte) {
   uint32_t most = __float_as_uint(top);
 #pragma unroll
   for (int x = 1; x < GROUP / (2 * W); x *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, x));
@@ -291,8 +297,9 @@ __device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, fl
 #pragma unroll
     for (int i = 0; i < W; ++i) q[i] = mul2(v[i], inv2);
   } else {
-    *byte = to_e4m3(__fdiv_rn(__uint_as_float(most), __fmul_rn(6.0f, step)));
-    const float d = __fmul_rn(from_e4m3(*byte), step);
+    const float t = __uint_as_float(most);
+    *byte = to_e4m3(t >= 448.0f * row.six ? 448.0f : quotient(t, row.six, row.inverse));
+    const float d = __fmul_rn(from_e4m3(*byte), row.step);
     const float inv = d == 0.0f ? 0.0f : __frcp_rn(d);
     const f32x2 inv2 = pack2(inv, inv), neg2 = pack2(-d, -d);
 #pragma unroll

@@ -199,8 +199,7 @@ __device__ __forceinline__ void tmem_free(uint32_t base, uint32_t cols) {
   else
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&v)[32]) {
-  uint32_t r[32];
+__device__ __forceinline__ void tmem_load32(uint32_t taddr, uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -211,8 +210,6 @@ __device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&v)[32]) {
         "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr)
       : "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[16]) {
   uint32_t r[16];
@@ -239,91 +236,70 @@ __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.
 
 // ---- what the epilogues share ----
 
-// g / (1 + exp(-g)) * u; an exponential beyond the range gives 0 or g
-__device__ __forceinline__ float silu_times(float g, float u) {
-  return __fdividef(g, 1.0f + __expf(-g)) * u;
-}
-
-// Walsh rotation of a thread's 32 values: strides 1, 2, 4, ..., then 1 / sqrt(32).
-__device__ __forceinline__ void walsh_32(float (&v)[32], float norm) {
+// g / (1 + 2^(-g log2 e)) * u, two at a time; a power beyond the range gives 0 or g
+__device__ __forceinline__ f32x2 silu_times(f32x2 g, f32x2 u) {
+  const float minus = -1.44269504f;      // log2 e
+  float t[2], e[2], r[2];
+  unpack2(mul2(g, pack2(minus, minus)), t[0], t[1]);
 #pragma unroll
-  for (int s = 1; s < 32; s *= 2)
+  for (int i = 0; i < 2; ++i) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[i]) : "f"(t[i]));
+  unpack2(add2(pack2(e[0], e[1]), pack2(1.0f, 1.0f)), t[0], t[1]);
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if ((i & s) == 0) {
-        const float a = v[i], b = v[i + s];
-        v[i] = __fadd_rn(a, b);
-        v[i + s] = __fsub_rn(a, b);
-      }
-#pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __fmul_rn(v[i], norm);
+  for (int i = 0; i < 2; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r[i]) : "f"(t[i]));
+  return mul2(mul2(g, pack2(r[0], r[1])), u);
 }
 
 // A thread's 32 neighbouring values to codes; the scale bytes of their one or two groups in the low bits of the result.
 template <int GROUP>
-__device__ __forceinline__ uint32_t encode_values(const float (&v)[32], float step, uint4* codes) {
+__device__ __forceinline__ uint32_t encode_values(const f32x2 (&v)[16], float step, uint4* codes) {
+  const RowStep row = GROUP == 16 ? row_step(step) : RowStep{};
   uint32_t bytes = 0;
   uint32_t* out = reinterpret_cast<uint32_t*>(codes);
 #pragma unroll
   for (int g = 0; g < 32 / GROUP; ++g) {
-    uint32_t top = 0;
+    constexpr int W = GROUP / 2;
+    f32x2 part[W];
 #pragma unroll
-    for (int i = 0; i < GROUP; ++i) top = max(top, abs_bits(v[g * GROUP + i]));
-    float d = 1.0f, inv;
+    for (int i = 0; i < W; ++i) part[i] = v[g * W + i];
     uint32_t byte;
-    if constexpr (GROUP == 32) {
-      byte = scale_byte_32(top);
-      inv = inverse_scale_32(byte);
-    } else {
-      byte = to_e4m3(__fdiv_rn(__uint_as_float(top), __fmul_rn(6.0f, step)));
-      d = __fmul_rn(from_e4m3(byte), step);
-      inv = d == 0.0f ? 0.0f : __frcp_rn(d);
-    }
+    const Part<W / 4> c = encode<GROUP>(part, top_of(part), row, &byte);
     bytes |= byte << (8 * g);
 #pragma unroll
-    for (int c = 0; c < GROUP / 8; ++c) {
-      float q[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = v[g * GROUP + 8 * c + i];
-        q[i] = GROUP == 32 ? __fmul_rn(x, inv) : quotient(x, d, inv);
-      }
-      out[g * (GROUP / 8) + c] = to_codes(q);
-    }
+    for (int i = 0; i < W / 4; ++i) out[g * (W / 4) + i] = c.w[i];
   }
   return bytes;
 }
 
-// 32 columns of a row times its step and the columns' (null: 1).
-__device__ __forceinline__ void times_steps(float (&v)[32], float row, const float* step, int n0, int n) {
+// 32 columns of a row times its step and the columns', which lie at `at` in shared memory (0: none).
+__device__ __forceinline__ void times_steps(f32x2 (&v)[16], float row, uint32_t at) {
+  const f32x2 row2 = pack2(row, row);
+  if (at == 0u) {
 #pragma unroll
-  for (int j = 0; j < 32; j += 4) {
-    float4 w = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-    if (step != nullptr && n0 + j < n) w = load(reinterpret_cast<const float4*>(step + n0 + j));
-    v[j] *= row * w.x;
-    v[j + 1] *= row * w.y;
-    v[j + 2] *= row * w.z;
-    v[j + 3] *= row * w.w;
+    for (int j = 0; j < 16; ++j) v[j] = mul2(v[j], row2);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 16; j += 2) {
+    float4 w;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(w.x), "=f"(w.y), "=f"(w.z), "=f"(w.w) : "r"(at + 8u * j) : "memory");
+    v[j] = mul2(v[j], mul2(row2, pack2(w.x, w.y)));
+    v[j + 1] = mul2(v[j + 1], mul2(row2, pack2(w.z, w.w)));
   }
 }
 
 // A warp's 32 rows x 32 columns to fp16 through its box in shared memory (64-byte swizzle) and TMA, which clips at the matrix's
 // edges: rows of 64 bytes leave whole.
-__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t box, const float (&v)[32], int x, int y, int n, int m,
+__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t box, const f32x2 (&v)[16], int x, int y, int n, int m,
                                           int lane) {
   if (lane == 0) store_wait_read<0>();
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    uint32_t o[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const __half2 h = __floats2half2_rn(v[8 * j + 2 * e], v[8 * j + 2 * e + 1]);
-      o[e] = *reinterpret_cast<const uint32_t*>(&h);
-    }
+    const f32x2 part[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+    const Part<4> h = narrow(part);
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                 ::"r"(box + uint32_t(lane) * 64u + ((uint32_t(j) ^ uint32_t((lane >> 1) & 3)) << 4)), "r"(o[0]), "r"(o[1]),
-                   "r"(o[2]), "r"(o[3]) : "memory");
+                 ::"r"(box + uint32_t(lane) * 64u + ((uint32_t(j) ^ uint32_t((lane >> 1) & 3)) << 4)), "r"(h.w[0]), "r"(h.w[1]),
+                   "r"(h.w[2]), "r"(h.w[3]) : "memory");
   }
   fence_async();
   __syncwarp();
@@ -526,22 +502,39 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int q = warp & 3;                    // quadrant of tensor-memory lanes
     const uint32_t box = out_base + uint32_t(warp - 2) * T::kBoxBytes;
     const uint32_t acc_free = map_to_cta(acc_empty, 0), shared_free = map_to_cta(acc_shared, 0);
-    const bool steps = p.x_step != nullptr || p.w_step != nullptr || p.up_step != nullptr;
+    const bool steps = p.x_step != nullptr || p.w_step != nullptr || p.up_step != nullptr || (MODE == kGatedCodes && GROUP == 16);
+    const int chunk = (warp - 2) >> 2;
+    // the tile's place and the next one's, without a division for each
+    int ta = first % p.tiles_a, tb = first / p.tiles_a;
+    const int step_a = step % p.tiles_a, step_b = step / p.tiles_a;
+    // A tile's steps are asked for while the one before is finished, each lane those of its row and of a column of either part; the
+    // columns' then go round through the warp's box (512 x 5632 x 2048 gated with all steps 12.8 us where each lane loaded all columns', of
+    // which 2 were those loads).
+    const float* second = MODE == kLinear ? p.w_step : p.up_step;
+    const bool column_steps = p.w_step != nullptr || second != nullptr;
+    float xs_next = 1.0f, hs_next = 1.0f, w_next = 1.0f, w2_next = 1.0f;
+    auto row_of = [&] { return ta * 256 + int(rank) * kTile + q * 32; };
+    auto column_of = [&] { return MODE == kLinear ? tb * 256 + 64 * chunk : tb * kTile + 32 * chunk; };
+    auto ask = [&] {
+      const int m = row_of() + lane, n = column_of() + lane, n2 = MODE == kLinear ? n + 32 : n;
+      if (p.x_step != nullptr && m < p.M) xs_next = load(p.x_step + m);
+      if (MODE == kGatedCodes && GROUP == 16 && m < p.M) hs_next = load(p.h_step + m);
+      if (p.w_step != nullptr && n < p.N) w_next = load(p.w_step + n);
+      if (second != nullptr && n2 < p.N) w2_next = load(second + n2);
+    };
+    if (first < tiles) ask();
     uint32_t n = 0;
     for (int tile = first; tile < tiles; tile += step, ++n) {
-      const int ta = tile % p.tiles_a, tb = tile / p.tiles_a;
-      const int row0 = ta * 256 + int(rank) * kTile + q * 32, m = row0 + lane;
-      const float xs = p.x_step != nullptr && m < p.M ? load(p.x_step + m) : 1.0f;
-      const int chunk = (warp - 2) >> 2;
-      // the chunk's first column of the output, and where its two parts of 32 columns lie in the accumulator
-      const int n0 = MODE == kLinear ? tb * 256 + 64 * chunk : tb * kTile + 32 * chunk;
+      const int row0 = row_of(), m = row0 + lane, n0 = column_of();
+      const float xs = xs_next, hs = hs_next, w = w_next, w2 = w2_next;
+      // where the chunk's two parts of 32 columns lie in the accumulator
       const int col_a = MODE == kLinear ? 64 * chunk : 32 * chunk, col_b = MODE == kLinear ? col_a + 32 : 128 + col_a;
       if (!bar_wait_warp(acc_full + 8u * (n & 1u), (n >> 1) & 1u, abort_flag, kPairEpilogue)) break;
       fence_after();
       const uint32_t acc = tmem + (uint32_t(q * 32) << 16) + ((n & 1u) ? T::kSecond : 0);
-      float a[32], b[32];
-      tmem_load32(acc + col_a, a);
-      tmem_load32(acc + col_b, b);
+      uint32_t raw_a[32], raw_b[32];
+      tmem_load32(acc + col_a, raw_a);
+      tmem_load32(acc + col_b, raw_b);
       tmem_wait_ld();
       fence_before();
       __syncwarp();
@@ -550,22 +543,41 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         if ((n & 1u) ? chunk < kHolders : chunk >= 4 - kHolders) bar_arrive_cluster(shared_free);
         bar_arrive_cluster(acc_free + 8u * (n & 1u));
       }
+      ta += step_a;
+      tb += step_b;
+      if (ta >= p.tiles_a) {
+        ta -= p.tiles_a;
+        ++tb;
+      }
+      if (steps && tile + step < tiles) ask();
+      f32x2 a[16], b[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        a[j] = pack2(__uint_as_float(raw_a[2 * j]), __uint_as_float(raw_a[2 * j + 1]));
+        b[j] = pack2(__uint_as_float(raw_b[2 * j]), __uint_as_float(raw_b[2 * j + 1]));
+      }
       if (steps) {
-        times_steps(a, xs, p.w_step, n0, p.N);
-        times_steps(b, xs, MODE == kLinear ? p.w_step : p.up_step, MODE == kLinear ? n0 + 32 : n0, p.N);
+        if (column_steps) {
+          if (MODE != kGatedCodes && lane == 0) store_wait_read<0>();
+          __syncwarp();
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(box + 4u * lane), "f"(w) : "memory");
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(box + 128u + 4u * lane), "f"(w2) : "memory");
+          __syncwarp();
+        }
+        times_steps(a, xs, column_steps ? box : 0u);
+        times_steps(b, xs, column_steps ? box + 128u : 0u);
       }
       if constexpr (MODE == kLinear) {
         store_box(&map_y, box, a, n0, row0, p.N, p.M, lane);
         store_box(&map_y, box, b, n0 + 32, row0, p.N, p.M, lane);
       } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) a[j] = silu_times(a[j], b[j]);
-        if (p.walsh) walsh_32(a, p.norm);
+        for (int j = 0; j < 16; ++j) a[j] = silu_times(a[j], b[j]);
+        if (p.walsh) walsh_rows<32>(a, p.norm, lane);
         if constexpr (MODE == kGatedHalf) {
           store_box(&map_y, box, a, n0, row0, p.N, p.M, lane);
         } else {
           uint4 codes;
-          const float hs = GROUP == 16 && m < p.M ? load(p.h_step + m) : 1.0f;
           const uint32_t bytes = encode_values<GROUP>(a, hs, &codes);
           if (m < p.M && n0 < p.N) {
             __stcs(reinterpret_cast<uint4*>(p.q_out + int64_t(m) * (p.N / 2) + n0 / 2), codes);
@@ -807,6 +819,20 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     }
   }
   __syncwarp();
+  // What the end needs of the steps is asked for meanwhile: a thread finishes 8 neighbouring channels of tokens, so that 4 lanes hold a
+  // group or rotation block of 32.  The tokens' steps as far as the SM's cache.
+  constexpr int kChunks = T::kTileRows / 8;
+  const int f = int(threadIdx.x) - 64, chunk = f % kChunks, n = n0 + chunk * 8;
+  const bool on = n < p.N;
+  float ws[8], us[8];
+  if (warp >= 2) {
+    eight_steps(on ? p.w_step : nullptr, n, ws);
+    if (GATED) eight_steps(on ? p.up_step : nullptr, n, us);
+    if (f < BN && m0 + f < p.M) {
+      if (p.x_step != nullptr) (void)load(p.x_step + m0 + f);
+      if (MODE == kGatedCodes && GROUP == 16) (void)load(p.h_step + m0 + f);
+    }
+  }
   if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (warp >= 2 && bar_wait_warp(done, 0, abort_flag, kStreamEpilogue)) {
     // [part][token][row of the tile] of the tokens that a CTA finishes: token c is the c / parts th of CTA c % parts
@@ -843,15 +869,9 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   if (parts > 1) cluster_sync();
   else __syncthreads();
   if (*abort_flag == 0 && warp >= 2) {
-    // This CTA's tokens are m0 + part, m0 + part + parts, ..; a thread finishes 8 neighbouring channels of one, so that 4 lanes hold
-    // a group or rotation block of 32.  All lanes of a warp take part; those past the last token repeat it and write nothing.
-    constexpr int kChunks = T::kTileRows / 8;
-    const int f = int(threadIdx.x) - 64, chunk = f % kChunks, n = n0 + chunk * 8;
+    // This CTA's tokens are m0 + part, m0 + part + parts, ..  All lanes of a warp take part; those past the last token repeat it and
+    // write nothing.
     const int cols = min(BN, p.M - m0), mine = (cols - part + parts - 1) / parts;
-    const bool on = n < p.N;
-    float ws[8], us[8];
-    eight_steps(on ? p.w_step : nullptr, n, ws);
-    if (GATED) eight_steps(on ? p.up_step : nullptr, n, us);
     for (int i0 = warp_number() * 32 - 64; i0 / kChunks < mine; i0 += 256) {
       const int i = (i0 + lane) / kChunks;
       const bool there = i < mine && on;
@@ -865,37 +885,18 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         if (GATED) add_shared(b, at + uint32_t(kTile / 2 * 4));
       }
       const float xs = p.x_step != nullptr ? load(p.x_step + m) : 1.0f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) a[j] *= xs * ws[j];
-      if constexpr (GATED) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) a[j] = silu_times(a[j], b[j] * (xs * us[j]));
-        if (p.walsh) {
-#pragma unroll
-          for (int x = 1; x < 8; x *= 2)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if ((j & x) == 0) {
-                const float lo = a[j], hi = a[j + x];
-                a[j] = __fadd_rn(lo, hi);
-                a[j + x] = __fsub_rn(lo, hi);
-              }
-#pragma unroll
-          for (int x = 1; x < 4; x *= 2)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              a[j] = __fmaf_rn((lane & x) ? -1.0f : 1.0f, a[j], __shfl_xor_sync(0xffffffffu, a[j], x));
-#pragma unroll
-          for (int j = 0; j < 8; ++j) a[j] = __fmul_rn(a[j], p.norm);
-        }
-      }
+      const f32x2 xs2 = pack2(xs, xs);
       f32x2 v[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = pack2(a[2 * j], a[2 * j + 1]);
+      for (int j = 0; j < 4; ++j) {
+        v[j] = mul2(pack2(a[2 * j], a[2 * j + 1]), mul2(xs2, pack2(ws[2 * j], ws[2 * j + 1])));
+        if constexpr (GATED) v[j] = silu_times(v[j], mul2(pack2(b[2 * j], b[2 * j + 1]), mul2(xs2, pack2(us[2 * j], us[2 * j + 1]))));
+      }
+      if (GATED && p.walsh) walsh_rows<32>(v, p.norm, lane);
       if constexpr (MODE == kGatedCodes) {
         uint32_t byte;
-        const float hs = GROUP == 16 ? load(p.h_step + m) : 1.0f;
-        const Part<1> codes = encode<GROUP>(v, top_of(v), hs, &byte);
+        const RowStep row = GROUP == 16 ? row_step(load(p.h_step + m)) : RowStep{};
+        const Part<1> codes = encode<GROUP>(v, top_of(v), row, &byte);
         if (there) {
           *reinterpret_cast<uint32_t*>(p.q_out + int64_t(m) * (p.N / 2) + n / 2) = codes.w[0];
           if (writes_scale<GROUP, 4>(chunk))

@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kFlatThreads, WALSH != 0 && PRE ? 2 : WALSH !=
       f32x2 v[W];
       const float top = transform<WALSH, PRE>(raw[r], diagonal, a.norm, lane, v);
       uint32_t byte;
-      const Part<W / 4> codes = encode<32>(v, top, 1.0f, &byte);
+      const Part<W / 4> codes = encode<32>(v, top, RowStep{}, &byte);
       if (on && m + r * lines < a.rows) put<32, W>(a, m + r * lines, part, offset, codes, byte);
     }
   }
@@ -151,12 +151,13 @@ __global__ void __launch_bounds__(row_threads(WALSH)) mx_quant16_kernel(const Qu
       float step = row_step_16(bits);
       if (t == 0) a.step_out[m + r] = step;
       if (!(step > 0.0f)) step = 1.0f;      // NaN: whatever the codes are, the row's values are NaN
+      const RowStep row = row_step(step);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int part = t + u * T;
         if constexpr (W == 8) {
           uint32_t byte;
-          const Part<2> codes = encode<16>(v[r][u], top[r][u], step, &byte);
+          const Part<2> codes = encode<16>(v[r][u], top[r][u], row, &byte);
           if (part < parts) put<16, 8>(a, m + r, part, scale_offset<16, 8>(part), codes, byte);
         } else {
           // two groups of 16, each as the other kind of thread would have it
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(row_threads(WALSH)) mx_quant16_kernel(const Qu
 #pragma unroll
             for (int i = 0; i < 8; ++i) half[i] = v[r][u][8 * g + i];
             uint32_t byte;
-            const Part<2> codes = encode<16>(half, top_of(half), step, &byte);
+            const Part<2> codes = encode<16>(half, top_of(half), row, &byte);
             if (part < parts) put<16, 8>(a, m + r, 2 * part + g, scale_offset<16, 8>(2 * part + g), codes, byte);
           }
         }
