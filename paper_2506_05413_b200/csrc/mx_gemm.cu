@@ -1043,12 +1043,13 @@ int clusters_at_once(int size) {
 }
 
 // Which kernel.  Up to 128 tokens the few-token one was the faster at every size tried (1 x 4096 x 4096: 4.1 us against 8.5; 128 x
-// 6144 x 4096: 8.2 against 9.9; gated 14336 x 4096: 13.4 against 22.6 with one token, 17.0 against 18.6 with 128).  K is split over
+// 6144 x 4096: 8.3 against 9.9; gated 14336 x 4096: 13.2 against 22.6 with one token, 16.6 against 18.4 with 128).  K is split over
 // as many CTAs as leave every tile's cluster a place at once (61 x 5120 x 4096 in 3 parts 6.2 us, in 2 6.5; 4096 x 14336 in 4
 // 9.3, in 2 12.5, in 8, not all at once, 18.7).
-// Beyond 128 tokens an estimate decides, in us: a fixed part, then a time per k-block and wave of tiles.  Linear, stream | pair: 256 x 4096
-// x 14336 15.9 | 21.5, 200 x 2048 x 5632 7.1 | 11.0, 512 x 4096 x 4096 10.3 | 9.7.  Gated: 200 x 1408 x 2048 6.7 | 7.5, 333 x 5632 x 2048
-// 10.2 | 10.7, 200 x 5632 x 2048 10.3 | 8.6, 300 x 14336 x 4096 37 | 27.
+// Beyond 128 tokens an estimate decides, in us: a fixed part, then a time per k-block and wave of tiles; scales of groups of 16, twice as
+// many, weigh on the few-token kernel.  Measured, few-token | pair: 256 x 4096 x 14336 15.9 | 21.5, 200 x 2048 x 5632 7.0 | 11.1, 512 x
+// 4096 x 4096 10.3 | 9.9.  Gated: 200 x 1408 x 2048 6.5 | 7.3, 300 x 5632 x 2048 10.1 | 10.8, in groups of 16 13.1 | 11.4, 200 x 5632 x
+// 2048 9.8 | 8.4.
 template <int GROUP, int MODE>
 int run(const Call& c) {
   constexpr bool gated = MODE != kLinear;
@@ -1065,8 +1066,9 @@ int run(const Call& c) {
     const double blocks = double((c.args.kblocks + parts - 1) / parts);
     double pair_us, stream_us;
     if (gated) {
+      const double each = (ctas <= sms ? 0.5 : 0.67 * double((ctas + 2 * sms - 1) / (2 * sms))) * (GROUP == 16 ? 1.45 : 1.0);
       pair_us = 5.4 + 0.33 * double(c.args.kblocks) * waves;
-      stream_us = 5.0 + blocks * (ctas <= sms ? 0.5 : 0.67 * double((ctas + 2 * sms - 1) / (2 * sms)));
+      stream_us = 5.0 + blocks * each;
     } else {
       pair_us = 4.6 + 0.30 * double(c.args.kblocks) * waves;
       stream_us = 4.6 + blocks * 0.38 * (ctas > sms ? double(ctas) / double(sms) : 1.0);
