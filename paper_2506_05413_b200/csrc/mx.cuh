@@ -298,7 +298,8 @@ __device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, co
     for (int i = 0; i < W; ++i) q[i] = mul2(v[i], inv2);
   } else {
     const float t = __uint_as_float(most);
-    *byte = to_e4m3(t >= 448.0f * row.six ? 448.0f : quotient(t, row.six, row.inverse));
+    // beyond the largest scale: that one, but the quotient of an infinity is NaN
+    *byte = to_e4m3(t >= 448.0f * row.six && most < 0x7f800000u ? 448.0f : quotient(t, row.six, row.inverse));
     const float d = __fmul_rn(from_e4m3(*byte), row.step);
     const float inv = d == 0.0f ? 0.0f : __frcp_rn(d);
     const f32x2 inv2 = pack2(inv, inv), neg2 = pack2(-d, -d);

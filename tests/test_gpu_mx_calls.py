@@ -216,6 +216,34 @@ def test_integer_codes_of_rows_with_infinities_and_nan(sr, mu, m):
     assert torch.equal(q[whole], want[whole]) and torch.equal(step[whole], ws[whole]) and bool(step[~whole].isnan().all())
 
 
+@pytest.mark.parametrize("group", [32, 16])
+@pytest.mark.parametrize("m", [3, 40, 300])
+def test_gated_values_that_leave_the_range(sr, mu, m, group):
+    """Through a weight step: feature 5's sums are infinite, feature 70's NaN, feature 200's large, the rest ordinary.  Infinities and
+    NaN make their group NaN; what is only too large for the row's step saturates."""
+    import torch
+    g = mu.gen(m)
+    x, a, b = (mu.random_coded(g, r, 512, group) for r in (m, 256, 256))
+    a.step = torch.full((256,), 2.0 ** -4, device=mu.DEV)
+    b.step = a.step.clone()
+    a.q[5], b.q[5], x.q[:] = 0x22, 0x22, x.q & 0x77        # sums of positive products
+    a.step[5] = b.step[5] = 2.0 ** 100
+    a.step[70] = float("nan")
+    b.step[200] = 2.0 ** 60
+    a.q[200], b.q[200] = 0x22, 0x22
+    a.step[200] = 1.0
+    c, h = mu.Coded(m, 256, group), torch.full((m,), 2.0 ** -6, device=mu.DEV)
+    sr.mx_glu(x.q, x.s, a.q, a.s, b.q, b.s, group=group, x_step=x.step, gate_step=a.step, up_step=b.step, q_out=c.q, scale_out=c.s,
+              h_step=h if group == 16 else None)
+    c.step = h if group == 16 else None
+    nan = c.units().isnan()
+    want = torch.zeros(256 // group, dtype=torch.bool, device=mu.DEV)
+    want[5 // group] = want[70 // group] = True
+    assert bool((nan == want).all())
+    far = c.values()[:, 200]
+    assert bool((far == (2688.0 * 2.0 ** -6)).all()) if group == 16 else bool((far > 2.0 ** 55).all())
+
+
 def test_arguments_that_do_not_go_together(sr, mu):
     import torch
     x = torch.zeros(4, 256, dtype=torch.float16, device=mu.DEV)
