@@ -244,6 +244,28 @@ def test_gated_values_that_leave_the_range(sr, mu, m, group):
     assert bool((far == (2688.0 * 2.0 ** -6)).all()) if group == 16 else bool((far > 2.0 ** 55).all())
 
 
+@pytest.mark.parametrize("which", ["x", "gate", "up", "x and up"])
+@pytest.mark.parametrize("m", [20, 150, 600])
+def test_steps_one_at_a_time(sr, mu, m, which):
+    """The linear layer and the gated pair with some of their steps only, channels that end inside a tile, several tiles to a CTA."""
+    import torch
+    g = mu.gen(m)
+    f, k = 2824 if m == 600 else 392, 384
+    x, a, b = (mu.random_coded(g, r, k, 32) for r in (m, f, f))
+    steps = {name: torch.rand(n, generator=g, device=mu.DEV) * 0.1 + 0.01 for name, n in (("x", m), ("gate", f), ("up", f))}
+    given = {name: s if name in which else None for name, s in steps.items()}
+    xs, gs, us = (x.values(), a.values(), b.values())
+    xs, gs, us = (v if given[n] is None else v * given[n].double()[:, None] for n, v in (("x", xs), ("gate", gs), ("up", us)))
+    y, h = (torch.empty(m, f, dtype=torch.float16, device=mu.DEV) for _ in range(2))
+    sr.mx_linear(x.q, x.s, a.q, a.s, y, x_step=given["x"], w_step=given["gate"])
+    want, extra = mu.product(xs, gs, k)
+    assert bool(((y.double() - want).abs() <= mu.half_bound(want, extra)).all())
+    sr.mx_glu(x.q, x.s, a.q, a.s, b.q, b.s, h_out=h, x_step=given["x"], gate_step=given["gate"], up_step=given["up"])
+    want, extra = mu.gated(xs, gs, us, k)
+    fine = (want.abs() + extra) < 65504          # beyond, fp16 is infinite
+    assert bool((((h.double() - want).abs() <= mu.half_bound(want, extra)) | ~fine).all())
+
+
 def test_arguments_that_do_not_go_together(sr, mu):
     import torch
     x = torch.zeros(4, 256, dtype=torch.float16, device=mu.DEV)
