@@ -274,13 +274,22 @@ __device__ __forceinline__ float top_of(const f32x2 (&v)[W]) {
   return m[0];
 }
 
+// 1 / d by one step of Newton's iteration on the hardware's approximation.  Where d is a scale or 6 over a power of two (8 mantissas)
+// it gives the codes that the correctly rounded reciprocal gives; over other steps it is off by a unit in the last place at the most, which
+// quotient() makes good wherever the quotient is a border between codes.  8192 x 4096 18.4 -> 17.5 us.
+__device__ __forceinline__ float reciprocal(float d) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+  return __fmaf_rn(r, __fmaf_rn(-d, r, 1.0f), r);
+}
+
 // A row's step as groups of 16 need it.
 struct RowStep {
   float step, six, inverse;      // 6 step and its reciprocal
 };
 __device__ __forceinline__ RowStep row_step(float step) {
   const float six = __fmul_rn(6.0f, step);
-  return RowStep{step, six, __frcp_rn(six)};
+  return RowStep{step, six, reciprocal(six)};
 }
 // A thread's values, with their largest magnitude, to codes (a word for every 8) and the scale byte of their group.  The threads
 // of a group, neighbouring lanes, take part together.
@@ -301,7 +310,7 @@ __device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, co
     // beyond the largest scale: that one, but the quotient of an infinity is NaN
     *byte = to_e4m3(t >= 448.0f * row.six && most < 0x7f800000u ? 448.0f : quotient(t, row.six, row.inverse));
     const float d = __fmul_rn(from_e4m3(*byte), row.step);
-    const float inv = d == 0.0f ? 0.0f : __frcp_rn(d);
+    const float inv = d == 0.0f ? 0.0f : reciprocal(d);
     const f32x2 inv2 = pack2(inv, inv), neg2 = pack2(-d, -d);
 #pragma unroll
     for (int i = 0; i < W; ++i) {      // quotient()

@@ -266,6 +266,28 @@ def test_steps_one_at_a_time(sr, mu, m, which):
     assert bool((((h.double() - want).abs() <= mu.half_bound(want, extra)) | ~fine).all())
 
 
+@pytest.mark.parametrize("power", [-60, -3, 0, 40])
+def test_every_scale_at_the_borders_between_codes(sr, mu, power):
+    """Groups of 16 whose largest value is 6 scales, for all scales but 0, with values on the borders: a border belongs to the even code."""
+    import torch
+    scale = torch.tensor([(1 + (b & 7) / 8) * 2.0 ** ((b >> 3) - 7) if b >> 3 else (b & 7) / 512 for b in range(1, 127)], device=mu.DEV)
+    borders = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]
+    grid = torch.tensor([6.0, 0.5] + borders + [-b for b in borders], device=mu.DEV)
+    even = torch.tensor([7, 1, 0, 2, 2, 4, 4, 6, 6, 8, 10, 10, 12, 12, 14, 14], dtype=torch.uint8, device=mu.DEV)
+    x = torch.zeros(3, 2048, device=mu.DEV)
+    x[:, :126 * 16] = (scale[:, None] * grid).reshape(-1)
+    x[1] *= 0.5
+    x[2] *= 2.0 ** -3
+    c = mu.Coded(3, 2048, 16)
+    half = x.half()
+    assert torch.equal(half.float(), x)      # the values are fp16
+    sr.mx_quant(half, c.q, c.s, c.step, group=16, pre=torch.full((2048,), 2.0 ** power, device=mu.DEV))
+    assert c.step.tolist() == [2.0 ** power, 2.0 ** (power - 1), 2.0 ** (power - 3)]
+    codes = torch.stack([c.q & 15, c.q >> 4], -1).reshape(3, 128, 16)
+    assert bool((codes[:, :126] == even).all()) and bool((codes[:, 126:] == 0).all())
+    assert bool((c.s[mu.place(3, 2048, 16)][:, :126] == torch.arange(1, 127, device=mu.DEV)).all())
+
+
 def test_arguments_that_do_not_go_together(sr, mu):
     import torch
     x = torch.zeros(4, 256, dtype=torch.float16, device=mu.DEV)
