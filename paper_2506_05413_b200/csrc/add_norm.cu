@@ -180,15 +180,22 @@ __device__ __forceinline__ void put_codes(const Part<W>& x16, float top, const R
   Part<W / 4> codes;
   uint32_t byte = 0;
   if constexpr (CODES == 4) {
+    // quotient(), two at a time; added to 1.5 * 2^23 it is rounded to the integer, ties to even, whose low bits are the code
+    const float magic = 12582912.0f;
+    const f32x2 inv2 = pack2(row.inverse, row.inverse), neg2 = pack2(-row.step, -row.step), magic2 = pack2(magic, magic);
 #pragma unroll
     for (int c = 0; c < W / 4; ++c) {
       codes.w[c] = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 4; ++i) {
+        const f32x2 r = mul2(x[4 * c + i], inv2);
+        const f32x2 q = fma2(fma2(r, neg2, x[4 * c + i]), inv2, r);
         float lo, hi;
-        unpack2(x[4 * c + i / 2], lo, hi);
-        const float v = fmaxf(fminf(rintf(quotient(i % 2 ? hi : lo, row.step, row.inverse)), 7.0f), -8.0f);
-        codes.w[c] |= (uint32_t(int(v)) & 15u) << (4 * i);
+        unpack2(add2(q, magic2), lo, hi);
+        lo = fmaxf(fminf(lo, magic + 7.0f), magic - 8.0f);
+        hi = fmaxf(fminf(hi, magic + 7.0f), magic - 8.0f);
+        const uint32_t pair = (__float_as_uint(lo) & 15u) | ((__float_as_uint(hi) & 15u) << 4);
+        codes.w[c] |= pair << (8 * i);
       }
     }
   } else {
