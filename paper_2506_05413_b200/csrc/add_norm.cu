@@ -482,21 +482,34 @@ int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_
   a.chunks = int(K / kChunk);
   const int64_t sms = device_sm_count();
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // A row at a time while there is a place for each; teams beyond, whose threads take 1, 2 or 4 units: more of them let more rows
-  // be under way and cost a round of rows more.  The estimate, in us (a fixed part and a time per round; 1200 rows of 4096 take 17.2,
-  // 16.8 and 20.2, 4096 rows 39.1, 31.9 and 32.3), decides.
+  // A row at a time while there is a place for each.  Beyond, teams whose threads take 1, 2 or 4 units: more of them let more rows be under
+  // way and cost a round of rows more.  An estimate in us decides: a fixed part, which grows with the weights, and a time per round of rows,
+  // less where a round leaves threads over.  Measured, a row at a time | 1 | 2 | 4 units, with a norm after the block: 600 x 4096 11.7 |
+  // 12.2 | 12.9 | 12.5, 2048 x 4096 32.0 | 22.6 | 21.3 | 21.1, 8192 x 4096 97 | 72 | 56 | 49; without: 7.9 | 8.4 | 9.2 | 10.0,
+  // 22.1 | 15.8 | 15.1 | 17.7, 82 | 51 | 41 | 45.
   const int row_threads = (a.chunks + 31) / 32 * 32, units = int(K / kUnit);
-  const bool in_teams = K % kUnit == 0 && K <= 8192 && a.y != nullptr && a.h != nullptr && M > sms * (kMaxThreads / row_threads);
+  const bool may_team = K % kUnit == 0 && K <= 8192 && a.y != nullptr && a.h != nullptr;
+  const int64_t at_once = may_team ? sms * (kMaxThreads / row_threads) : 0;
+  const double thousands = double(K) / 1024.0;
+  auto share = [](double used) { return 0.4 + 0.6 * used; };      // of a full round's time
+  bool in_teams = false;
   int each = 0, T = 0, teams = 0;
-  double least = 0.0;
-  for (int e = 1; in_teams && e <= 4; e *= 2) {
-    const int threads = ((units + e - 1) / e + 31) / 32 * 32, most = kTeamThreads / threads, n = most < kMaxTeams ? most : kMaxTeams;
-    const double rounds = double((M + sms * n - 1) / (sms * n)), us = e == 1 ? 4.0 + 2.5 * rounds : e == 2 ? 5.5 + 3.9 * rounds : 6.5 + 6.5 * rounds;
-    if (each != 0 && us >= least) continue;
-    least = us;
-    each = e;
-    T = threads;
-    teams = n;
+  if (may_team && M > at_once) {
+    const double f = share(double(kMaxThreads / row_threads * row_threads) / kMaxThreads), x = double(M) / double(at_once);
+    double least = post_norm ? 4.0 + 4.0 * f * x : 2.0 + 2.9 * f * x;
+    for (int e = 1, i = 0; e <= 4; e *= 2, ++i) {
+      const int threads = ((units + e - 1) / e + 31) / 32 * 32, most = kTeamThreads / threads, n = most < kMaxTeams ? most : kMaxTeams;
+      const double rounds = double((M + sms * n - 1) / (sms * n)), used = double(n * units) / double(kTeamThreads * e);
+      const double fixed[2][3] = {{3.0, 3.0, 3.5}, {3.5, 4.3, 6.0}}, weights[2][3] = {{0.2, 0.2, 0.7}, {0.35, 0.35, 0.8}};
+      const double round[2][3] = {{1.65, 2.7, 5.6}, {2.1 + 0.06 * thousands, 3.1 + 0.12 * thousands, 5.8}};
+      const double us = fixed[post_norm][i] + weights[post_norm][i] * thousands + round[post_norm][i] * share(used) * rounds;
+      if (us >= least) continue;
+      least = us;
+      in_teams = true;
+      each = e;
+      T = threads;
+      teams = n;
+    }
   }
   a.wide = (H_out_f16 == nullptr || wide_ok(H_out_f16, ldho)) && (X_out_f16 == nullptr || wide_ok(X_out_f16, ldxo));
   auto go_teams = [&](auto one, auto two, auto four) {
