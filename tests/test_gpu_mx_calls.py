@@ -288,6 +288,36 @@ def test_every_scale_at_the_borders_between_codes(sr, mu, power):
     assert bool((c.s[mu.place(3, 2048, 16)][:, :126] == torch.arange(1, 127, device=mu.DEV)).all())
 
 
+@pytest.mark.parametrize("codes", [None, "int4", "mx16", "mx32"])
+@pytest.mark.parametrize("m,k,post", [(777, 4096, False), (2049, 4096, False), (3001, 4096, True), (1201, 2048, True), (1100, 896, True), (2300, 8192, True), (4099, 1152, False),
+                                      (3700, 5120, True), (900, 384, True), (9001, 5632, False)])
+def test_many_rows_are_normed_as_few(sr, mu, m, k, post, codes):
+    """Calls of many rows, shared out in several ways, against calls of 70 rows of them: the same bits."""
+    import torch
+    g = mu.gen(m + k)
+    y, h = mu.rows(g, m, k, pad=8), mu.rows(g, m, k)
+    w = [torch.rand(k, generator=g, device=mu.DEV) + 0.5 for _ in range(3)]
+    group = {"mx16": 16, "mx32": 32}.get(codes)
+
+    def call(rows):
+        n = rows.stop - rows.start
+        out = dict(h_out=torch.empty(n, k, dtype=torch.float16, device=mu.DEV), x_out=torch.empty(n, k, dtype=torch.float16, device=mu.DEV))
+        if codes is not None:
+            c = mu.Coded(n, k, group or 16)
+            out.update(q_out=c.q, scale_out=c.s if group else None, step_out=c.step if codes != "mx32" else None)
+        sr.add_norm(y[rows], h[rows], w[0], codes=codes, post_weight=w[1] if post else None, gate=w[2], block_scale=0.5, **out)
+        return out
+
+    many = call(slice(0, m))
+    for at in (0, 128 * (m // 256), m - 70):
+        few = call(slice(at, at + 70))
+        for name in ("h_out", "x_out", "q_out", "step_out"):
+            if few.get(name) is not None:
+                assert torch.equal(many[name][at:at + 70], few[name]), name
+        if group:
+            assert torch.equal(many["scale_out"][mu.place(m, k, group)[at:at + 70]], few["scale_out"][mu.place(70, k, group)])
+
+
 def test_arguments_that_do_not_go_together(sr, mu):
     import torch
     x = torch.zeros(4, 256, dtype=torch.float16, device=mu.DEV)
