@@ -69,7 +69,8 @@ __device__ __forceinline__ void put(const QuantArgs& a, int m, int part, uint32_
   if (writes_scale<GROUP, W>(part)) a.scale_out[scale_word(m, 0, a.K / (4 * GROUP)) + offset] = uint8_t(byte);
 }
 
-// Groups of 32: `lines` rows side by side are under way, a thread takes its 2 W values of every lines-th row.
+// Groups of 32: `lines` rows side by side are under way, a thread takes its 2 W values of every lines-th row.  8192 x 4096: 14.9 us
+// (5.7 TB/s, 0.87 of the copy rate), rotated in blocks of 32 16.9, of 64 19.5, of 128 with a diagonal 23.8 (3.6 TB/s): issue, and shuffles.
 __host__ __device__ constexpr int flat_words(int walsh) { return walsh != 0 ? 16 : 8; }
 
 template <int WALSH, bool PRE>
@@ -101,7 +102,8 @@ __global__ void __launch_bounds__(kFlatThreads, WALSH != 0 && PRE ? 2 : WALSH !=
   }
 }
 
-// Groups of 16: U times 2 W values a thread (the second ones a row's length of threads further), R rows at a time.
+// Groups of 16: U times 2 W values a thread (the second ones a row's length of threads further), R rows at a time.  8192 x 4096: 17.2 us
+// (4.9 TB/s), with a diagonal and blocks of 128 29.0: issue (two thirds of the slots).  32 values a thread without a rotation: 19.5 to 21.
 __host__ __device__ constexpr int row_threads(int walsh) { return walsh != 0 ? 512 : 1024; }
 
 template <int WALSH, bool PRE, int U>
@@ -190,7 +192,7 @@ __device__ __forceinline__ uint4 from_codes(uint32_t word) {
   return h;
 }
 
-// As mx_quant32_kernel: a thread keeps to its unit of every lines-th row.
+// As mx_quant32_kernel: a thread keeps to its unit of every lines-th row.  8192 x 4096: 15.3 us in groups of 32, 16.4 of 16 (5.5, 5.2 TB/s).
 template <int GROUP>
 __global__ void __launch_bounds__(kFlatThreads)
 mx_dequant_kernel(const uint8_t* q, const uint8_t* scale, const float* step, int rows, int units, int lines, __half* y, int64_t ldy,
