@@ -370,7 +370,8 @@ int smoothrot_attn_prefill(const void* Q_f16, int64_t ldq, int64_t total_q, cons
  * the row first: row r and group g are at
  *     ((r / 128) * (K / group / 4) + g / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + g % 4
  * of smoothrot_mx_scale_bytes(rows, K, group) bytes.  Bytes of rows past the last are not written, and their contents do
- * not matter to the calls that read the rest.  Codes and scales are 16-byte aligned, K is a multiple of 128.
+ * not matter to the calls that read the rest.  Codes, scales and fp32 vectors along channels (pre, steps of weights, weights
+ * of norms) are 16-byte aligned, K is a multiple of 128.
  */
 
 /* Host. Bytes of the scales of `rows` rows of K values; 0 for a group or K that is not supported. */
@@ -529,7 +530,7 @@ int smoothrot_base_matrix(int order, int8_t* out_host);
 /*
  * Host, synchronous.  Kernels never spin without bound: a wait that runs out
  * records a non-zero code in a device-side status word and the kernel
- * returns (42 to 49 in the microscaled products); the cache and attention calls record 32 to 35 for a slot, position, page or
+ * returns (42 to 49 in the microscaled products, 51 in smoothrot_add_norm); the cache and attention calls record 32 to 35 for a slot, position, page or
  * length out of range.  This call copies that word for the current device into
  * *status_host (0 = none so far) and clears it when `clear` is non-zero.
  */
