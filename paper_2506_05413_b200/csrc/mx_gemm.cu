@@ -236,7 +236,8 @@ __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.
 
 // ---- what the epilogues share ----
 
-// g / (1 + 2^(-g log2 e)) * u, two at a time; a power beyond the range gives 0 or g
+// g / (1 + 2^(-g log2 e)) * u, two at a time; a power beyond the range gives 0 or g.  The power's argument is rounded to fp32 and the
+// reciprocal is the hardware's, so the result is off by some |g| units in the last place: in front of a rounding to fp16 alone, which hides it.
 __device__ __forceinline__ f32x2 silu_times(f32x2 g, f32x2 u) {
   const float minus = -1.44269504f;      // log2 e
   float t[2], e[2], r[2];
@@ -247,6 +248,26 @@ __device__ __forceinline__ f32x2 silu_times(f32x2 g, f32x2 u) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r[i]) : "f"(t[i]));
   return mul2(mul2(g, pack2(r[0], r[1])), u);
+}
+// The same in front of codes, whose borders show the last bit: the library's exponential, and a quotient with one residual correction,
+// as the gated product of the integer layers has them.  Of 1.4e9 values of blocks of 14336 features none was coded otherwise than with an
+// IEEE division, which leaves its fast path at zeros (those of rows past the last: 300 x 5632 x 2048 in groups of 16 22 us, this 12.3, the
+// form above 11.2, where 128 of those values got another code).  Numerator and denominator are quartered, so that the reciprocal of the
+// largest finite sum is a normal number; where the power is infinite the reciprocal is 0, and where g is infinite the residual is no
+// number: either way the correction is held to what changes nothing.
+__device__ __forceinline__ f32x2 silu_exact(f32x2 g, f32x2 u) {
+  const f32x2 quarter = pack2(0.25f, 0.25f), minus = pack2(-0.25f, -0.25f);
+  float e[2], s[2], r[2], d[2];
+  unpack2(g, e[0], e[1]);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) e[i] = expf(-e[i]);
+  const f32x2 sum = fma2(pack2(e[0], e[1]), minus, minus);      // -(1 + e) / 4
+  unpack2(sum, s[0], s[1]);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r[i]) : "f"(-s[i]));
+  const f32x2 inv = pack2(r[0], r[1]), part = mul2(g, quarter), q = mul2(part, inv);
+  unpack2(fma2(sum, q, part), d[0], d[1]);
+  return mul2(fma2(pack2(fmaxf(d[0], -1e36f), fmaxf(d[1], -1e36f)), inv, q), u);
 }
 
 // A thread's 32 neighbouring values to codes; the scale bytes of their one or two groups in the low bits of the result.
@@ -525,7 +546,8 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int step_a = step % p.tiles_a, step_b = step / p.tiles_a;
     // A tile's steps are asked for while the one before is finished, each lane those of its row and of a column of either part; the
     // columns' then go round through the warp's box (512 x 5632 x 2048 gated with all steps 12.8 us where each lane loaded all columns', of
-    // which 2 were those loads).
+    // which 2 were those loads).  In front of codes they are asked for behind the gate, which wants the registers (in groups of 16, 512 x
+    // 5632 x 2048, 12.9 us -> 12.5).
     const float* second = MODE == kLinear ? p.w_step : p.up_step;
     const bool column_steps = p.w_step != nullptr || second != nullptr;
     float xs_next = 1.0f, hs_next = 1.0f, w_next = 1.0f, w2_next = 1.0f;
@@ -565,7 +587,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         ta -= p.tiles_a;
         ++tb;
       }
-      if (steps && tile + step < tiles) ask();
+      if (MODE != kGatedCodes && steps && tile + step < tiles) ask();
       f32x2 a[16], b[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
@@ -588,7 +610,8 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         store_box(&map_y, box, b, n0 + 32, row0, p.N, p.M, lane);
       } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) a[j] = silu_times(a[j], b[j]);
+        for (int j = 0; j < 16; ++j) a[j] = MODE == kGatedCodes ? silu_exact(a[j], b[j]) : silu_times(a[j], b[j]);
+        if (MODE == kGatedCodes && steps && tile + step < tiles) ask();
         if (p.walsh) walsh_rows<32>(a, p.norm, lane);
         if constexpr (MODE == kGatedHalf) {
           store_box(&map_y, box, a, n0, row0, p.N, p.M, lane);
@@ -911,7 +934,10 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         v[j] = mul2(pack2(a[2 * j], a[2 * j + 1]), mul2(xs2, pack2(ws[2 * j], ws[2 * j + 1])));
-        if constexpr (GATED) v[j] = silu_times(v[j], mul2(pack2(b[2 * j], b[2 * j + 1]), mul2(xs2, pack2(us[2 * j], us[2 * j + 1]))));
+        if constexpr (GATED) {
+          const f32x2 up = mul2(pack2(b[2 * j], b[2 * j + 1]), mul2(xs2, pack2(us[2 * j], us[2 * j + 1])));
+          v[j] = MODE == kGatedCodes ? silu_exact(v[j], up) : silu_times(v[j], up);
+        }
       }
       if (GATED && p.walsh) walsh_rows<32>(v, p.norm, lane);
       if constexpr (MODE == kGatedCodes) {
