@@ -413,8 +413,8 @@ int smoothrot_mx_linear(const uint8_t* Xq, const uint8_t* x_scale, const float* 
  *                 weights went through smoothrot_mx_quant with walsh = 32;  0: none
  * and either H [M x ldh] = fp16(h), or, with q_out and scale_out in place of H, h in codes for the down projection, as
  * smoothrot_mx_quant makes them except that with group 16 the steps h_step [M] are the caller's (calibrated: a row's
- * maximum is not known while its first features leave), positive; where a row's values exceed 2688 steps they saturate,
- * but an infinity or NaN makes its group's scale NaN.  h_step is NULL with group 32.  F a multiple of 8, of 32 with walsh, of 128 with codes.
+ * maximum is not known while its first features leave), from 2^-100 to 2^117 as the quantizer's own are; where a row's values
+ * exceed 2688 steps they saturate with their sign, but an infinity or NaN makes its group's scale NaN.  h_step is NULL with group 32.  F a multiple of 8, of 32 with walsh, of 128 with codes.
  */
 int smoothrot_mx_glu(const uint8_t* Xq, const uint8_t* x_scale, const float* x_step, int64_t M, const uint8_t* gate_q,
                      const uint8_t* gate_scale, const float* gate_step, const uint8_t* up_q, const uint8_t* up_scale,

@@ -291,8 +291,9 @@ __device__ __forceinline__ RowStep row_step(float step) {
   return RowStep{step, six, reciprocal(six)};
 }
 // A thread's values, with their largest magnitude, to codes (a word for every 8) and the scale byte of their group.  The threads
-// of a group, neighbouring lanes, take part together.
-template <int GROUP, int W>
+// of a group, neighbouring lanes, take part together.  ANY_STEP: the step is not the row's own, and values may be so far beyond it that
+// no fp32 number holds the quotient.
+template <int GROUP, bool ANY_STEP = false, int W>
 __device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, const RowStep& row, uint32_t* byte) {
   uint32_t most = __float_as_uint(top);
 #pragma unroll
@@ -307,7 +308,8 @@ __device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, co
   } else {
     const float t = __uint_as_float(most);
     // beyond the largest scale: that one, but the quotient of an infinity is NaN
-    *byte = to_e4m3(t >= 448.0f * row.six && most < 0x7f800000u ? 448.0f : quotient(t, row.six, row.inverse));
+    const bool beyond = t >= 448.0f * row.six;
+    *byte = to_e4m3(beyond && most < 0x7f800000u ? 448.0f : quotient(t, row.six, row.inverse));
     const float d = __fmul_rn(from_e4m3(*byte), row.step);
     const float inv = d == 0.0f ? 0.0f : reciprocal(d);
     const f32x2 inv2 = pack2(inv, inv), neg2 = pack2(-d, -d);
@@ -315,6 +317,15 @@ __device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, co
     for (int i = 0; i < W; ++i) {      // quotient()
       const f32x2 r = mul2(v[i], inv2);
       q[i] = fma2(fma2(r, neg2, v[i]), inv2, r);
+    }
+    if (ANY_STEP && beyond) {      // rare: what is beyond 8 units is 6 of them as well
+      const float far = 8.0f * d;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        float lo, hi;
+        unpack2(v[i], lo, hi);
+        q[i] = pack2(fabsf(lo) > far ? copysignf(8.0f, lo) : quotient(lo, d, inv), fabsf(hi) > far ? copysignf(8.0f, hi) : quotient(hi, d, inv));
+      }
     }
   }
   Part<W / 4> codes;

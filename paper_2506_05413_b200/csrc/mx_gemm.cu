@@ -283,7 +283,7 @@ __device__ __forceinline__ uint32_t encode_values(const f32x2 (&v)[16], float st
 #pragma unroll
     for (int i = 0; i < W; ++i) part[i] = v[g * W + i];
     uint32_t byte;
-    const Part<W / 4> c = encode<GROUP>(part, top_of(part), row, &byte);
+    const Part<W / 4> c = encode<GROUP, true>(part, top_of(part), row, &byte);
     bytes |= byte << (8 * g);
 #pragma unroll
     for (int i = 0; i < W / 4; ++i) out[g * (W / 4) + i] = c.w[i];
@@ -943,7 +943,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       if constexpr (MODE == kGatedCodes) {
         uint32_t byte;
         const RowStep row = GROUP == 16 ? row_step(load(p.h_step + m)) : RowStep{};
-        const Part<1> codes = encode<GROUP>(v, top_of(v), row, &byte);
+        const Part<1> codes = encode<GROUP, true>(v, top_of(v), row, &byte);
         if (there) {
           *reinterpret_cast<uint32_t*>(p.q_out + int64_t(m) * (p.N / 2) + n / 2) = codes.w[0];
           if (writes_scale<GROUP, 4>(chunk))

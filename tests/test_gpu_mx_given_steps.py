@@ -1,4 +1,4 @@
-"""The gated block's codes in groups of 16 under steps of the caller's of no particular form."""
+"""The gated block's codes in groups of 16 under steps of the caller's: of no particular form, and far too small for the values."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -62,3 +62,23 @@ def test_borders_under_steps_of_no_particular_form(sr, mu, m):
         q = torch.where(d[:, None] == 0, torch.zeros_like(v), v / d[:, None]).double()
         assert bool((c.codes().reshape(m, 640, 16) == mu.nearest(q, torch.ones_like(q))).all()), float(step)
     assert sr.device_status() == 0
+
+
+@pytest.mark.parametrize("m", [1, 40, 300])
+@pytest.mark.parametrize("step", [2.0 ** -100, 1e-30, 3e-20])
+def test_values_far_beyond_the_steps_saturate_with_their_sign(sr, mu, m, step):
+    """Quotients that no fp32 number holds among ordinary ones: a value beyond 2688 steps is 6 scales of its sign, the others are coded as ever."""
+    import torch
+    s = torch.tensor([step], device=mu.DEV)
+    d = 448 * s
+    far = torch.tensor([1e12, -1e12, 3e38, -3e38, 1e25, -1e25], device=mu.DEV)
+    ordinary = torch.tensor([0.0, 0.6, -1.4, 2.2, -3.2, 4.4, -5.6, 0.1, 6.0, -6.0], device=mu.DEV) * d
+    h = torch.cat([far, ordinary, far.flip(0), ordinary, ordinary, far * 1e-3]).repeat(8)
+    h = h[:h.numel() // 128 * 128]
+    c = _codes(sr, mu, m, h, s)
+    v = h.double().reshape(-1, 16)
+    scale = torch.full((v.shape[0], 1), 448.0, dtype=torch.float64, device=mu.DEV) * s.double()
+    want = mu.nearest(v / scale, torch.ones_like(v)).reshape(-1)
+    over = v.abs().amax(1) >= 2688 * s.double()
+    assert bool(over.all()) and bool((c.s[mu.place(m, h.numel(), 16)] == 126).all())
+    assert bool((c.codes() == want).all()) and sr.device_status() == 0
