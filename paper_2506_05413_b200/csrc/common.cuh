@@ -84,8 +84,9 @@ inline TensorMapEncodeFn tensor_map_encoder() {
 }
 #endif
 
-// Raises a kernel's dynamic shared-memory limit: one runtime call per kernel, device and size, then a
-// table look-up (the runtime call costs a microsecond or so on every eager launch otherwise).
+// Raises a kernel's dynamic shared-memory limit: one runtime call per kernel, device and size beyond the largest so far, then a
+// table look-up (the runtime call costs a microsecond or so on every eager launch otherwise).  The runtime's call sets the limit, to a smaller
+// one too, so it is made under the table's lock: of two threads' first calls the one with fewer bytes could come last otherwise.
 inline bool allow_dynamic_smem(const void* kern, int bytes) {
   struct Entry {
     const void* kern;
@@ -96,14 +97,14 @@ inline bool allow_dynamic_smem(const void* kern, int bytes) {
   static std::vector<Entry> done;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return false;
-  {
-    std::lock_guard<std::mutex> lock(mu);
-    for (const Entry& e : done)
-      if (e.kern == kern && e.dev == dev && e.bytes >= bytes) return true;
-  }
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
   std::lock_guard<std::mutex> lock(mu);
-  done.push_back(Entry{kern, dev, bytes});
+  Entry* known = nullptr;
+  for (Entry& e : done)
+    if (e.kern == kern && e.dev == dev) known = &e;
+  if (known != nullptr && known->bytes >= bytes) return true;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  if (known != nullptr) known->bytes = bytes;
+  else done.push_back(Entry{kern, dev, bytes});
   return true;
 }
 
