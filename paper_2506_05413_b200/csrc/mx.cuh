@@ -339,11 +339,11 @@ __device__ __forceinline__ Part<W / 4> encode(const f32x2 (&v)[W], float top, co
   return codes;
 }
 // Offset within its row's scales of the scale byte of the part'th 2 W values, and whether their thread is the one of its group that
-// writes it.
+// writes it.  64 bits: beyond 2^29 values of a row in groups of 16 the offset passes 2^32.
 template <int GROUP, int W>
-__device__ __forceinline__ uint32_t scale_offset(int part) {
+__device__ __forceinline__ int64_t scale_offset(int part) {
   const int group = part / (GROUP / (2 * W));
-  return uint32_t(group >> 2) * kAtomBytes + uint32_t(group & 3);
+  return int64_t(group >> 2) * kAtomBytes + (group & 3);
 }
 template <int GROUP, int W>
 __device__ __forceinline__ bool writes_scale(int part) { return part % (GROUP / (2 * W)) == 0; }

@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(kFlatThreads, WALSH != 0 && PRE ? 2 : WALSH !=
   const int64_t i = int64_t(blockIdx.x) * kFlatThreads + threadIdx.x;
   const int line = int(i / parts), part = int(i - int64_t(line) * parts);
   const bool on = line < lines;         // lanes of a rotation block or a group are on or off together
-  const uint32_t offset = scale_offset<32, W>(part);
+  const uint32_t offset = uint32_t(scale_offset<32, W>(part));      // rows end at kMaxWidth
   f32x2 diagonal[W];
   after_the_call_before();
   if (PRE && on) load_diagonal(a.pre, part, diagonal);
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(row_threads(WALSH)) mx_quant16_kernel(const Qu
         if constexpr (W == 8) {
           uint32_t byte;
           const Part<2> codes = encode<16>(v[r][u], top[r][u], row, &byte);
-          if (part < parts) put<16, 8>(a, m + r, part, scale_offset<16, 8>(part), codes, byte);
+          if (part < parts) put<16, 8>(a, m + r, part, uint32_t(scale_offset<16, 8>(part)), codes, byte);
         } else {
           // two groups of 16, each as the other kind of thread would have it
 #pragma unroll
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(row_threads(WALSH)) mx_quant16_kernel(const Qu
             for (int i = 0; i < 8; ++i) half[i] = v[r][u][8 * g + i];
             uint32_t byte;
             const Part<2> codes = encode<16>(half, top_of(half), row, &byte);
-            if (part < parts) put<16, 8>(a, m + r, 2 * part + g, scale_offset<16, 8>(2 * part + g), codes, byte);
+            if (part < parts) put<16, 8>(a, m + r, 2 * part + g, uint32_t(scale_offset<16, 8>(2 * part + g)), codes, byte);
           }
         }
       }
@@ -200,7 +200,7 @@ mx_dequant_kernel(const uint8_t* q, const uint8_t* scale, const float* step, int
   const int64_t i = int64_t(blockIdx.x) * kFlatThreads + threadIdx.x;
   const int line = int(i / units), unit = int(i - int64_t(line) * units);
   if (line >= lines) return;
-  const uint32_t offset = scale_offset<GROUP, 8>(unit);
+  const int64_t offset = scale_offset<GROUP, 8>(unit);
   after_the_call_before();
   constexpr int R = 4;
   for (int m = line; m < rows; m += R * lines) {
