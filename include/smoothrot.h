@@ -512,11 +512,13 @@ int smoothrot_debug_gemm_i32(const uint8_t* Xq, int64_t M, const uint8_t* Wq, in
  *   smoothrot_debug_attn_wait_expiry: the same through the waits of the attention kernels; `code` is the one to record,
  *     36 to 40 for smoothrot_attn_prefill's and 41 for smoothrot_attn_decode's.
  *   smoothrot_debug_mx_wait_expiry: the same through the waits of the microscaled products, code 50.
+ *   smoothrot_debug_norm_wait_expiry: the same through smoothrot_add_norm's wait for rows, code 51.
  */
 int smoothrot_debug_set_wait_limit_ns(uint64_t ns);
 int smoothrot_debug_wait_expiry(void* stream);
 int smoothrot_debug_attn_wait_expiry(int code, void* stream);
 int smoothrot_debug_mx_wait_expiry(void* stream);
+int smoothrot_debug_norm_wait_expiry(void* stream);
 
 /* Host. Writes the library's own order-28 Paley matrix, row-major, entries
  * +1 / -1, into out[784] (a host buffer). */

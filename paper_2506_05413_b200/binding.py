@@ -63,6 +63,7 @@ SIGNATURES = {
     "smoothrot_debug_wait_expiry": (_int, [_vp]),
     "smoothrot_debug_attn_wait_expiry": (_int, [_int, _vp]),
     "smoothrot_debug_mx_wait_expiry": (_int, [_vp]),
+    "smoothrot_debug_norm_wait_expiry": (_int, [_vp]),
     "smoothrot_paley28": (_int, [_vp]),
     "smoothrot_base_matrix": (_int, [_int, _vp]),
     "smoothrot_device_status": (_int, [ctypes.POINTER(_int), _int]),
@@ -527,6 +528,11 @@ def debug_attn_wait_expiry(code: int) -> None:
 def debug_mx_wait_expiry() -> None:
     """The same through the waits of the microscaled products (code 50)."""
     _check(load().smoothrot_debug_mx_wait_expiry(_stream()))
+
+
+def debug_norm_wait_expiry() -> None:
+    """The same through add_norm's wait for rows (code 51)."""
+    _check(load().smoothrot_debug_norm_wait_expiry(_stream()))
 
 
 def device_status(clear: bool = True) -> int:

@@ -22,7 +22,7 @@ namespace mx {
 
 __device__ int g_norm_status = 0;
 __device__ unsigned long long g_norm_wait_limit_ns = kWaitLimitNs;
-constexpr int kNormRows = 51;      // code of a wait for rows that ran out
+constexpr int kNormRows = 51;      // code of a wait for rows that ran out, in the test probe too
 
 namespace {
 
@@ -112,6 +112,16 @@ struct Team {
   int id, warps, slot;
   __device__ __forceinline__ void meet() const { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(warps * 32) : "memory"); }
 };
+
+// Whether a wait of one of the team's threads ran out: one answer for all.  They leave then, once what is on its way has landed and the
+// memory may be given back.
+__device__ __forceinline__ bool team_gives_up(bool there, const Team& team) {
+  uint32_t late;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(late) : "r"(uint32_t(!there)), "r"(team.id), "r"(team.warps * 32) : "memory");
+  if (late != 0) drain();
+  return late != 0;
+}
 
 // rstd of a row from its threads' parts of the sum of squares.
 __device__ __forceinline__ float statistics(double mine, double* slots, const Team& team, int wid, const NormArgs& a) {
@@ -284,13 +294,7 @@ __global__ void __launch_bounds__(kTeamThreads) add_norm_teams_kernel(const Norm
       y[u] = shared_unit(rows + unit[u] * 32);
       h[u] = shared_unit(rows + row_bytes + unit[u] * 32);
     }
-    uint32_t late;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(late) : "r"(uint32_t(!there)), "r"(team.id), "r"(threads) : "memory");
-    if (late != 0) {       // a wait ran out: what is on its way lands before the memory is given back
-      drain();
-      return;
-    }
+    if (team_gives_up(there, team)) return;
     if (t == 0 && row + stride < a.rows) fetch(row + stride);
     double sum = 0.0;
     float rstd = 1.0f;
@@ -417,6 +421,19 @@ __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a)
   }
 }
 
+// Test probe: a team waits for rows that nobody sends, and leaves as the kernel's teams do.
+constexpr int kProbeThreads = 64;
+__global__ void norm_wait_probe_kernel() {
+  __shared__ __align__(8) unsigned long long storage;
+  const uint32_t bar = smem_u32(&storage);
+  if (threadIdx.x == 0) {
+    bar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  (void)team_gives_up(wait_rows(bar, 0u), Team{1, kProbeThreads / 32, 0});
+}
+
 }  // namespace
 }  // namespace mx
 }  // namespace smoothrot
@@ -431,6 +448,12 @@ int smoothrot_norm_set_wait_limit_ns(uint64_t ns) {
   const unsigned long long v = ns == 0 ? smoothrot::mx::kWaitLimitNs : static_cast<unsigned long long>(ns);
   return cudaMemcpyToSymbol(smoothrot::mx::g_norm_wait_limit_ns, &v, sizeof(v)) == cudaSuccess ? SMOOTHROT_OK
                                                                                                  : SMOOTHROT_CUDA_ERROR;
+}
+
+int smoothrot_debug_norm_wait_expiry(void* stream) {
+  smoothrot::mx::norm_wait_probe_kernel<<<1, smoothrot::mx::kProbeThreads, 0, static_cast<cudaStream_t>(stream)>>>();
+  smoothrot::count_launch();
+  return smoothrot::launch_status();
 }
 
 int smoothrot_add_norm(const void* Y_f16, int64_t ldy, const void* H_f16, int64_t ldh, int64_t M, int64_t K, int post_norm,
