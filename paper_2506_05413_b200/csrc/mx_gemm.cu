@@ -655,8 +655,9 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // cluster, send each other the sums of the tokens that the other finishes, and each adds up its own over all parts, in the
 // parts' order: the same bits from call to call.
 //
-// Two CTAs fit an SM, which evens out tiles that are not a multiple of the SMs, and lets a call's first loads be issued
-// while the call before is finishing.
+// Where K is not split, two CTAs fit an SM, which evens out tiles that are not a multiple of the SMs, and lets a call's first loads be
+// issued while the call before is finishing.  Where it is split, the places of the sums lie behind the ring and one CTA fits, two in
+// three forms (16 tokens and groups of 32; gated: 32 tokens and groups of 32, 16 and groups of 16).
 //
 // Warps: 0 TMA, 1 products, 2..9 read the accumulator, two to a quadrant of its lanes, and finish; 2 mixes scales before.
 //
@@ -684,7 +685,8 @@ struct Stream {
   static constexpr int kCols = kScaleCol + 8 * kAtoms;           // weights' scales, tokens' scales
   static constexpr int kTmemCols = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
   static_assert(kCols <= 256, "tensor memory of two CTAs");
-  static_assert(kSumBytes <= kRingBytes && 2 * (kSmemBytes + 1024) <= 228 * 1024, "shared memory of two CTAs");
+  static_assert(kSumBytes <= kRingBytes && 2 * (kSmemBytes + 1024) <= 228 * 1024, "shared memory of two CTAs of one part");
+  static_assert(kSmemBytes + kSumBytes <= 227 * 1024, "shared memory of a CTA of more parts");
   static_assert(kStageBytes % 1024 == 0, "swizzled tiles start on 1024 bytes");
 };
 
@@ -1057,7 +1059,8 @@ int launch_stream(const Call& c, int parts) {
 }
 
 // Clusters of `size` CTAs, one to an SM, that the device runs at once: a cluster stays inside a part of the chip, so large ones
-// leave SMs over (148, 74, 33, 15 of 1, 2, 4, 8 on B200).  Asked of the runtime once per device.
+// leave SMs over (148, 74, 33, 15 of 1, 2, 4, 8 on B200).  Asked of the runtime once per device, for the form with the most tokens, of which
+// one CTA fits an SM as of nearly all that are split.
 int clusters_at_once(int size) {
   constexpr int kDevices = 64, kMostParts = 8;
   static std::atomic<int> known[kDevices][kMostParts + 1];
