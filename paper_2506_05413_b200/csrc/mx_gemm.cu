@@ -237,24 +237,25 @@ __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.
 // ---- what the epilogues share ----
 
 // g / (1 + 2^(-g log2 e)) * u, two at a time; a power beyond the range gives 0 or g.  The power's argument is rounded to fp32 and the
-// reciprocal is the hardware's, so the result is off by some |g| units in the last place: in front of a rounding to fp16 alone, which hides it.
+// reciprocal is the hardware's, so the result is off by some |g| units in the last place: in front of a rounding to fp16 alone, which hides
+// it.  Numerator and denominator are quartered, so that the reciprocal of the largest finite sum is a normal number.
 __device__ __forceinline__ f32x2 silu_times(f32x2 g, f32x2 u) {
+  const f32x2 quarter = pack2(0.25f, 0.25f);
   const float minus = -1.44269504f;      // log2 e
   float t[2], e[2], r[2];
   unpack2(mul2(g, pack2(minus, minus)), t[0], t[1]);
 #pragma unroll
   for (int i = 0; i < 2; ++i) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[i]) : "f"(t[i]));
-  unpack2(add2(pack2(e[0], e[1]), pack2(1.0f, 1.0f)), t[0], t[1]);
+  unpack2(fma2(pack2(e[0], e[1]), quarter, quarter), t[0], t[1]);
 #pragma unroll
   for (int i = 0; i < 2; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r[i]) : "f"(t[i]));
-  return mul2(mul2(g, pack2(r[0], r[1])), u);
+  return mul2(mul2(mul2(g, quarter), pack2(r[0], r[1])), u);
 }
 // The same in front of codes, whose borders show the last bit: the library's exponential, and a quotient with one residual correction,
 // as the gated product of the integer layers has them.  Of 1.4e9 values of blocks of 14336 features none was coded otherwise than with an
 // IEEE division, which leaves its fast path at zeros (those of rows past the last: 300 x 5632 x 2048 in groups of 16 22 us, this 12.3, the
-// form above 11.2, where 128 of those values got another code).  Numerator and denominator are quartered, so that the reciprocal of the
-// largest finite sum is a normal number; where the power is infinite the reciprocal is 0, and where g is infinite the residual is no
-// number: either way the correction is held to what changes nothing.
+// form above 11.2, where 128 of those values got another code).  Where the power is infinite the reciprocal is 0, and where g is
+// infinite the residual is no number: either way the correction is held to what changes nothing.
 __device__ __forceinline__ f32x2 silu_exact(f32x2 g, f32x2 u) {
   const f32x2 quarter = pack2(0.25f, 0.25f), minus = pack2(-0.25f, -0.25f);
   float e[2], s[2], r[2], d[2];
