@@ -115,10 +115,10 @@ struct Team {
 
 // Whether a wait of one of the team's threads ran out: one answer for all.  They leave then, once what is on its way has landed and the
 // memory may be given back.
-__device__ __forceinline__ bool team_gives_up(bool there, const Team& team) {
+__device__ __forceinline__ bool team_gives_up(bool there, const Team& team, int threads) {
   uint32_t late;
   asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(late) : "r"(uint32_t(!there)), "r"(team.id), "r"(team.warps * 32) : "memory");
+               : "=r"(late) : "r"(uint32_t(!there)), "r"(team.id), "r"(threads) : "memory");
   if (late != 0) drain();
   return late != 0;
 }
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kTeamThreads) add_norm_teams_kernel(const Norm
       y[u] = shared_unit(rows + unit[u] * 32);
       h[u] = shared_unit(rows + row_bytes + unit[u] * 32);
     }
-    if (team_gives_up(there, team)) return;
+    if (team_gives_up(there, team, threads)) return;
     if (t == 0 && row + stride < a.rows) fetch(row + stride);
     double sum = 0.0;
     float rstd = 1.0f;
@@ -431,7 +431,7 @@ __global__ void norm_wait_probe_kernel() {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  (void)team_gives_up(wait_rows(bar, 0u), Team{1, kProbeThreads / 32, 0});
+  (void)team_gives_up(wait_rows(bar, 0u), Team{1, kProbeThreads / 32, 0}, kProbeThreads);
 }
 
 }  // namespace
