@@ -415,6 +415,7 @@ int smoothrot_mx_linear(const uint8_t* Xq, const uint8_t* x_scale, const float* 
  * smoothrot_mx_quant makes them except that with group 16 the steps h_step [M] are the caller's (calibrated: a row's
  * maximum is not known while its first features leave), from 2^-100 to 2^117 as the quantizer's own are; where a row's values
  * exceed 2688 steps they saturate with their sign, but an infinity or NaN makes its group's scale NaN.  h_step is NULL with group 32.  F a multiple of 8, of 32 with walsh, of 128 with codes.
+ * A diagonal on h, in front of the rotation, goes into up_step.
  */
 int smoothrot_mx_glu(const uint8_t* Xq, const uint8_t* x_scale, const float* x_step, int64_t M, const uint8_t* gate_q,
                      const uint8_t* gate_scale, const float* gate_step, const uint8_t* up_q, const uint8_t* up_scale,

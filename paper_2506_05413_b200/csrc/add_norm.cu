@@ -242,7 +242,9 @@ __device__ __forceinline__ void shared_weights(const float4* w, int unit, int un
 
 // Many rows of up to 8192 values, whole units of 16, y and h both there: a team of `threads` threads takes a row, U units a
 // thread.  Threads past a row's end take its last unit again, so that there is one course of instructions; they write nothing.
-// 8192 x 4096 into codes: 41 us (5.3 TB/s), with a norm after the block 49 (4.5), fp16 47 (5.7); issue and the statistics in 64 bits.
+// 8192 x 4096 into codes: 41 us (5.3 TB/s), of groups of 16 45, integer ones 45, with a norm after the block 49 (4.5), 51 and 51, fp16 47
+// (5.7).  Two exchanges of a row stand in line with its arithmetic at 16 warps an SM; issue (53 %) and the statistics in 64 bits (34 % of
+// their pipe) alone do not bound it.
 template <int CODES, bool POST, int U>
 __global__ void __launch_bounds__(kTeamThreads) add_norm_teams_kernel(const NormArgs a, const int threads) {
   __shared__ double sums[2][2][kTeamThreads / 32];          // [row in turn][norm]: a warp that is ahead writes the other row's
@@ -340,7 +342,9 @@ __global__ void __launch_bounds__(kTeamThreads) add_norm_teams_kernel(const Norm
   }
 }
 
-// Few rows, long ones, or only one of y and h: a row at a time, U chunks a thread, straight from global memory.  1 x 4096: 2.5 us.
+// Few rows, long ones, or only one of y and h: a row at a time, U chunks a thread, straight from global memory.  1 x 4096: 2.5 us.  Many
+// rows come to it where they are long or one-sided, and it is far from their bytes then: 4096 x 16384 into codes 105 us, with a norm after
+// the block 157 (67 at the copy rate), 8192 x 4096 of the stream alone 70 (13).
 template <int CODES, int U>
 __global__ void __launch_bounds__(kMaxThreads) add_norm_kernel(const NormArgs a) {
   __shared__ double sums[2][2][kMaxThreads / 32];

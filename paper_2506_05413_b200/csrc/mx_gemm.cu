@@ -253,7 +253,7 @@ __device__ __forceinline__ f32x2 silu_times(f32x2 g, f32x2 u) {
 }
 // The same in front of codes, whose borders show the last bit: the library's exponential, and a quotient with one residual correction,
 // as the gated product of the integer layers has them.  Of 1.4e9 values of blocks of 14336 features none was coded otherwise than with an
-// IEEE division, which leaves its fast path at zeros (those of rows past the last: 300 x 5632 x 2048 in groups of 16 22 us, this 12.3, the
+// IEEE division, which leaves its fast path at zeros (those of rows past the last: 300 x 5632 x 2048 in groups of 16 22 us, this 12.5, the
 // form above 11.2, where 128 of those values got another code).  Where the power is infinite the reciprocal is 0, and where g is
 // infinite the residual is no number: either way the correction is held to what changes nothing.
 __device__ __forceinline__ f32x2 silu_exact(f32x2 g, f32x2 u) {
@@ -1099,8 +1099,8 @@ int clusters_at_once(int size) {
 // 9.3, in 2 12.5, in 8, not all at once, 18.7).
 // Beyond 128 tokens an estimate decides, in us: a fixed part, then a time per k-block and wave of tiles; scales of groups of 16, twice as
 // many, weigh on the few-token kernel.  Measured, few-token | pair: 256 x 4096 x 14336 15.9 | 21.5, 200 x 2048 x 5632 7.0 | 11.1, 512 x
-// 4096 x 4096 10.3 | 9.9.  Gated: 200 x 1408 x 2048 6.5 | 7.3, 300 x 5632 x 2048 10.1 | 10.8, in groups of 16 13.1 | 11.4, 200 x 5632 x
-// 2048 9.8 | 8.4.
+// 4096 x 4096 10.3 | 9.9.  Gated into codes: 200 x 1408 x 2048 6.3 | 7.1, 300 x 5632 x 2048 10.6 | 10.7, in groups of 16 13.1 | 12.5,
+// 200 x 5632 x 2048 10.2 | 8.1.
 template <int GROUP, int MODE>
 int run(const Call& c) {
   constexpr bool gated = MODE != kLinear;

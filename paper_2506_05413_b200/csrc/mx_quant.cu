@@ -103,7 +103,9 @@ __global__ void __launch_bounds__(kFlatThreads, WALSH != 0 && PRE ? 2 : WALSH !=
 }
 
 // Groups of 16: U times 2 W values a thread (the second ones a row's length of threads further), R rows at a time.  8192 x 4096: 17.2 us
-// (4.9 TB/s), with a diagonal and blocks of 128 29.0: issue (two thirds of the slots).  32 values a thread without a rotation: 19.5 to 21.
+// (4.9 TB/s), with a diagonal 22.8 (it spills 18 registers), with that and blocks of 128 29.0: issue (two thirds of the slots).  32 values
+// a thread without a rotation: 19.5 to 21; with a diagonal 21.9, 1 to 14 % faster at seven of ten sizes, but 300 x 4096 3.3 -> 4.5 and 1000 x
+// 2048 3.5 -> 4.8.
 __host__ __device__ constexpr int row_threads(int walsh) { return walsh != 0 ? 512 : 1024; }
 
 template <int WALSH, bool PRE, int U>
