@@ -398,7 +398,7 @@ int smoothrot_mx_dequant(const uint8_t* q, const uint8_t* scale, const float* st
 
 /*
  * The layer on microscaled codes:
- *     Y[m][n] = fp16( (sum over groups of x_scale w_scale (sum of x w)) * x_step[m] * w_step[n] )       fp32 sums
+ *     Y[m][n] = fp16( (sum over groups of x_scale w_scale (sum of x w)) * (x_step[m] * w_step[n]) )     fp32 sums
  * Xq, x_scale [M rows], Wq, w_scale [N rows], both of K values in groups of `group`; x_step [M], w_step [N] or NULL (1).
  * Y [M x ldy] fp16.  Any M >= 0, N a multiple of 8, K <= 2^20.  A call repeated gives the same bits.  No workspace.
  */
